@@ -1,0 +1,166 @@
+// Rotary positions of queries and keys (jpi_rope, include/jpi_prefix.h).
+//
+// Every element is read and written once and each pair's sine and cosine serve
+// all heads of its token, so the call is bound by memory: a workgroup takes a
+// few tokens, forms their table of (cos, sin) in LDS once, and then streams the
+// heads of both tensors through it in 16-byte pieces.
+//
+// Angles.  A position times f_i in fp32 is off by 2^-24 of the angle itself,
+// which for position 10^5 is 6e-3 radians; here the angle is formed in turns in
+// fp64 (position exact, f_i / 2 pi to 2^-52), reduced to [-1/2, 1/2] turns there,
+// and only then rounded to fp32 for sincospi.
+#include "jpi_device.h"
+#include "jpi_prefix_internal.h"
+
+namespace jpi {
+namespace {
+
+constexpr int ROPE_THREADS = 256;
+constexpr int ROPE_MAX_PAIRS = 256;
+constexpr int ROPE_TOKENS = 4;  // tokens per workgroup at most
+
+// f_i / 2 pi: turns per position of pair i
+__device__ __forceinline__ double rope_turns(const RopeLaunch& l, int i) {
+  constexpr double inv_2pi = 0.15915494309189533577;
+  const double f = exp2(-(double)i * l.log2_step);
+  double g = f;
+  if (l.scaling == JPI_ROPE_LINEAR) {
+    g = f / l.factor;
+  } else if (l.scaling == JPI_ROPE_PARTS) {
+    const double r = l.trained * f * inv_2pi;
+    const double keep = fmin(1.0, fmax(0.0, (r - l.beta_slow) / (l.beta_fast - l.beta_slow)));
+    g = f * (keep + (1.0 - keep) / l.factor);
+  }
+  return g * inv_2pi;
+}
+
+// N consecutive elements: one piece where they are aligned to their size, else one by one
+template <typename T, int N, bool VEC>
+struct Piece {
+  typedef T vec __attribute__((ext_vector_type(N)));
+  T v[N];
+  __device__ __forceinline__ void load(const T* p) {
+    if constexpr (VEC) {
+      const vec x = *reinterpret_cast<const vec*>(p);
+#pragma unroll
+      for (int e = 0; e < N; ++e) v[e] = x[e];
+    } else {
+#pragma unroll
+      for (int e = 0; e < N; ++e) v[e] = p[e];
+    }
+  }
+  __device__ __forceinline__ void store(T* p) const {
+    if constexpr (VEC) {
+      vec x;
+#pragma unroll
+      for (int e = 0; e < N; ++e) x[e] = v[e];
+      *reinterpret_cast<vec*>(p) = x;
+    } else {
+#pragma unroll
+      for (int e = 0; e < N; ++e) p[e] = v[e];
+    }
+  }
+};
+
+// A unit is N elements of a head, with JPI_ROPE_HALF and their N partners half a rotation further on.
+template <typename T, int N, bool VEC, bool INTER>
+__global__ __launch_bounds__(ROPE_THREADS) void k_rope(RopeLaunch l, int n_tok, int tile) {
+  __shared__ float2 table[ROPE_TOKENS * ROPE_MAX_PAIRS];
+  const int pairs = l.rot_dim >> 1;
+  const int tok0 = (int)blockIdx.x * tile, here = min(tile, n_tok - tok0);
+
+  int have = -1;
+  double f = 0.0;
+  for (int e = threadIdx.x; e < here * pairs; e += ROPE_THREADS) {
+    const int tt = e / pairs, i = e - tt * pairs, n = tok0 + tt;
+    if (i != have) f = rope_turns(l, i), have = i;
+    const int b = n / l.tokens, t = n - b * l.tokens;
+    const double turns = (double)(l.pos ? l.pos[b * l.pos_stride + t] : t) * f;
+    float sn, cs;
+    sincospif(2.f * (float)(turns - rint(turns)), &sn, &cs);
+    table[e] = float2{l.amplitude * cs, l.inverse ? -l.amplitude * sn : l.amplitude * sn};
+  }
+  __syncthreads();
+
+  const unsigned rot_units = (INTER ? l.rot_dim : pairs) / N, per_head = rot_units + (l.head_dim - l.rot_dim) / N;
+  const unsigned q_units = l.t[0].heads * per_head, per_tok = q_units + l.t[1].heads * per_head;
+  for (unsigned u = threadIdx.x; u < here * per_tok; u += ROPE_THREADS) {
+    const unsigned tt = u / per_tok, r = u - tt * per_tok;
+    const bool key = r >= q_units;
+    const RopeTensor& x = l.t[key];
+    const unsigned w = key ? r - q_units : r, h = w / per_head, c = w - h * per_head;
+    const unsigned n = tok0 + tt, b = n / (unsigned)l.tokens, t = n - b * l.tokens;
+    const T* src = reinterpret_cast<const T*>(x.src) + b * x.so + t * x.sr + h * x.sh;
+    T* dst = reinterpret_cast<T*>(x.dst) + b * x.d_o + t * x.dr + h * x.dh;
+    if (c >= rot_units) {
+      const int d = l.rot_dim + (int)(c - rot_units) * N;
+      Piece<T, N, VEC> p;
+      p.load(src + d);
+      p.store(dst + d);
+    } else if constexpr (INTER) {
+      const int d = (int)c * N;
+      Piece<T, N, VEC> p;
+      p.load(src + d);
+#pragma unroll
+      for (int e = 0; e < N; e += 2) {
+        const float2 cs = table[tt * pairs + (d + e) / 2];
+        const float a = (float)p.v[e], z = (float)p.v[e + 1];
+        p.v[e] = from_f32<T>(a * cs.x - z * cs.y);
+        p.v[e + 1] = from_f32<T>(a * cs.y + z * cs.x);
+      }
+      p.store(dst + d);
+    } else {
+      const int d = (int)c * N;
+      Piece<T, N, VEC> lo, hi;
+      lo.load(src + d);
+      hi.load(src + pairs + d);
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        const float2 cs = table[tt * pairs + d + e];
+        const float a = (float)lo.v[e], z = (float)hi.v[e];
+        lo.v[e] = from_f32<T>(a * cs.x - z * cs.y);
+        hi.v[e] = from_f32<T>(a * cs.y + z * cs.x);
+      }
+      lo.store(dst + d);
+      hi.store(dst + pairs + d);
+    }
+  }
+}
+
+template <typename T>
+bool rope_aligned(const RopeLaunch& l) {
+  constexpr int N = 16 / sizeof(T);
+  const int unit = l.interleaved ? l.rot_dim : l.rot_dim / 2;
+  int64_t any = unit % N | (l.head_dim - l.rot_dim) % N;
+  for (const RopeTensor& t : l.t)
+    if (t.heads) {
+      any |= (t.so | t.sr | t.sh | t.d_o | t.dr | t.dh) % N;
+      any |= (int64_t)(((uintptr_t)t.src | (uintptr_t)t.dst) & 15);
+    }
+  return any == 0;
+}
+
+template <typename T>
+hipError_t rope_typed(const RopeLaunch& l, hipStream_t s) {
+  constexpr int N = 16 / sizeof(T);
+  const int n = l.batch * l.tokens;
+  const int tile = n < 1024 ? 1 : ROPE_TOKENS;
+  const dim3 grid((unsigned)((n + (int64_t)tile - 1) / tile));
+  if (rope_aligned<T>(l)) {
+    if (l.interleaved) k_rope<T, N, true, true><<<grid, ROPE_THREADS, 0, s>>>(l, n, tile);
+    else k_rope<T, N, true, false><<<grid, ROPE_THREADS, 0, s>>>(l, n, tile);
+  } else if (l.interleaved) {
+    k_rope<T, 2, false, true><<<grid, ROPE_THREADS, 0, s>>>(l, n, tile);
+  } else {
+    k_rope<T, 1, false, false><<<grid, ROPE_THREADS, 0, s>>>(l, n, tile);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_rope(jpi_dtype dt, const RopeLaunch& l, hipStream_t s) {
+  return dt == JPI_BF16 ? rope_typed<bf16>(l, s) : rope_typed<float>(l, s);
+}
+
+}  // namespace jpi

@@ -30,7 +30,11 @@ EXPORTED = ["jpi_abi_version", "jpi_status_str", "jpi_last_error", "jpi_create",
             "jpi_sched_run", "jpi_sched_sim_hooks", "jpi_vlm_create", "jpi_vlm_destroy", "jpi_vlm_set_weight",
             "jpi_vlm_finalize_weights", "jpi_vlm_prefill", "jpi_vlm_last_error", "jpi_set_committed_t0", "jpi_bind_robot_state", "jpi_corr_create",
             "jpi_corr_destroy", "jpi_corr_set_weight", "jpi_corr_finalize_weights", "jpi_corr_compress",
-            "jpi_corr_predict", "jpi_corr_last_error"]
+            "jpi_corr_predict", "jpi_corr_last_error", "jpi_prefix_last_error", "jpi_rope",
+            "jpi_shared_attention_workspace", "jpi_prefix_weight_workspace", "jpi_shared_attention", "jpi_prefix_weight",
+            "jpi_evict"]
+JPI_ROPE_HALF, JPI_ROPE_INTERLEAVED = 0, 1
+JPI_ROPE_PLAIN, JPI_ROPE_LINEAR, JPI_ROPE_BASE, JPI_ROPE_PARTS = range(4)
 JPI_KERNEL_NONE, JPI_KERNEL_QKV, JPI_KERNEL_ATTENTION, JPI_KERNEL_OPROJ, JPI_KERNEL_GATEUP, JPI_KERNEL_DOWN, \
     JPI_KERNEL_PERSISTENT = range(-1, 6)
 
@@ -59,6 +63,36 @@ class jpi_corr_config(ctypes.Structure):
                 ("vlm_width", ctypes.c_int), ("n_query", ctypes.c_int), ("max_batch", ctypes.c_int),
                 ("max_actions", ctypes.c_int), ("max_vlm_tokens", ctypes.c_int), ("dtype", ctypes.c_int),
                 ("rms_eps", ctypes.c_float), ("rope_base", ctypes.c_float)]
+
+
+# include/jpi_prefix.h
+class jpi_view(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("outer", ctypes.c_int64), ("row", ctypes.c_int64), ("head", ctypes.c_int64)]
+
+
+class jpi_rope_config(ctypes.Structure):
+    _fields_ = [("head_dim", ctypes.c_int), ("rot_dim", ctypes.c_int), ("layout", ctypes.c_int), ("scaling", ctypes.c_int),
+                ("inverse", ctypes.c_int), ("base", ctypes.c_double), ("factor", ctypes.c_double),
+                ("trained", ctypes.c_double), ("beta_fast", ctypes.c_double), ("beta_slow", ctypes.c_double),
+                ("amplitude", ctypes.c_double)]
+
+
+class jpi_shared_attn(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int), ("n_groups", ctypes.c_int), ("group", ctypes.c_int), ("q_rows", ctypes.c_int),
+                ("n_heads", ctypes.c_int), ("n_kv_heads", ctypes.c_int), ("head_dim", ctypes.c_int),
+                ("prefix", ctypes.c_int), ("suffix", ctypes.c_int), ("causal", ctypes.c_int), ("scale", ctypes.c_float),
+                ("q", jpi_view), ("k_prefix", jpi_view), ("v_prefix", jpi_view), ("k_suffix", jpi_view),
+                ("v_suffix", jpi_view), ("prefix_len", ctypes.c_void_p), ("suffix_len", ctypes.c_void_p),
+                ("out", jpi_view), ("lse", ctypes.c_void_p)]
+
+
+class jpi_evict_args(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int), ("n_outer", ctypes.c_int), ("n_heads", ctypes.c_int), ("head_dim", ctypes.c_int),
+                ("slots", ctypes.c_int), ("keep", ctypes.c_int), ("n_first", ctypes.c_int), ("n_last", ctypes.c_int),
+                ("weight", ctypes.c_void_p), ("weight_stride", ctypes.c_int64), ("len", ctypes.c_void_p),
+                ("k", jpi_view), ("v", jpi_view), ("k_out", jpi_view), ("v_out", jpi_view),
+                ("weight_out", ctypes.c_void_p), ("weight_out_stride", ctypes.c_int64), ("index", ctypes.c_void_p),
+                ("len_out", ctypes.c_void_p)]
 
 
 # include/jpi_sched.h
@@ -152,6 +186,14 @@ _sig = {
     "jpi_corr_compress": (_i, [_vp, _vp, _i, _i, _vp, _vp]),
     "jpi_corr_predict": (_i, [_vp, _vp, _vp, _i, _i, _vp, _vp, _vp]),
     "jpi_corr_last_error": (ctypes.c_char_p, [_vp]),
+    "jpi_prefix_last_error": (ctypes.c_char_p, []),
+    "jpi_rope": (_i, [ctypes.POINTER(jpi_rope_config), _i, _i, _i, _vp, _i64, ctypes.POINTER(jpi_view),
+                      ctypes.POINTER(jpi_view), _i, ctypes.POINTER(jpi_view), ctypes.POINTER(jpi_view), _i, _vp]),
+    "jpi_shared_attention_workspace": (_i, [ctypes.POINTER(jpi_shared_attn), ctypes.POINTER(ctypes.c_size_t)]),
+    "jpi_prefix_weight_workspace": (_i, [ctypes.POINTER(jpi_shared_attn), ctypes.POINTER(ctypes.c_size_t)]),
+    "jpi_shared_attention": (_i, [ctypes.POINTER(jpi_shared_attn), _vp, ctypes.c_size_t, _vp]),
+    "jpi_prefix_weight": (_i, [ctypes.POINTER(jpi_shared_attn), _vp, _f, _vp, _vp, ctypes.c_size_t, _vp]),
+    "jpi_evict": (_i, [ctypes.POINTER(jpi_evict_args), _vp]),
 }
 for _name, (_res, _args) in _sig.items():
     _fn = getattr(_lib, _name)
@@ -381,6 +423,43 @@ def jpi_corr_predict(m, state, actions, batch: int, n_actions: int, item_out, co
 
 def jpi_corr_last_error(m) -> str:
     return _lib.jpi_corr_last_error(m).decode()
+
+
+def jpi_prefix_last_error() -> str:
+    return (_lib.jpi_prefix_last_error() or b"").decode()
+
+
+def jpi_rope(cfg, dtype: int, batch: int, tokens: int, positions, pos_stride: int, q, q_out, q_heads: int, k=None, k_out=None,
+             k_heads: int = 0, stream=None) -> int:
+    """cfg a jpi_rope_config; q, q_out, k, k_out jpi_view structures (or references to them)."""
+    return _lib.jpi_rope(cfg, dtype, batch, tokens, addr(positions), pos_stride, q, q_out, q_heads, k, k_out, k_heads,
+                         stream_handle(stream))
+
+
+def jpi_shared_attention_workspace(args: jpi_shared_attn):
+    n = ctypes.c_size_t()
+    st = _lib.jpi_shared_attention_workspace(args, n)
+    return st, n.value
+
+
+def jpi_prefix_weight_workspace(args: jpi_shared_attn):
+    n = ctypes.c_size_t()
+    st = _lib.jpi_prefix_weight_workspace(args, n)
+    return st, n.value
+
+
+def jpi_shared_attention(args: jpi_shared_attn, workspace=None, workspace_bytes: int = 0, stream=None) -> int:
+    return _lib.jpi_shared_attention(args, addr(workspace), workspace_bytes, stream_handle(stream))
+
+
+def jpi_prefix_weight(args: jpi_shared_attn, weight_in, decay: float, weight_out, workspace=None, workspace_bytes: int = 0,
+                      stream=None) -> int:
+    return _lib.jpi_prefix_weight(args, addr(weight_in), decay, addr(weight_out), addr(workspace), workspace_bytes,
+                                  stream_handle(stream))
+
+
+def jpi_evict(args: jpi_evict_args, stream=None) -> int:
+    return _lib.jpi_evict(args, stream_handle(stream))
 
 
 class JpiError(RuntimeError):

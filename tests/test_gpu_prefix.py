@@ -1,0 +1,594 @@
+"""The prefix-cache operators (include/jpi_prefix.h) against plain implementations in 64 bits on the CPU.
+
+Tolerances come from the formats: h is half a step of the output type relative to the value (bf16 2^-8, fp32 2^-24),
+u = 2^-24 a rounding in fp32.
+"""
+import math
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+H = {torch.bfloat16: 2.0 ** -8, torch.float32: U}
+TYPES = [torch.bfloat16, torch.float32]
+INF = float("inf")
+
+
+@pytest.fixture(scope="module")
+def ops():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2607_12659_amd import prefix_ops
+    return prefix_ops
+
+
+def rand(seed, *shape, dtype=torch.float32):
+    g = torch.Generator().manual_seed(seed)
+    return torch.randn(shape, generator=g).to(dtype)
+
+
+def dev(t):
+    return None if t is None else t.cuda()
+
+
+def within(got, ref, tol):
+    """Every element within its own tolerance; non-finite ones equal."""
+    got, ref = got.double().cpu(), ref.double()
+    fin = torch.isfinite(ref)
+    assert torch.equal(torch.isfinite(got), fin)
+    assert torch.equal(got[~fin & ~torch.isnan(ref)], ref[~fin & ~torch.isnan(ref)])
+    tol = tol if torch.is_tensor(tol) else torch.full_like(ref, tol)
+    over = ((got - ref).abs() - tol)[fin]
+    assert over.numel() == 0 or over.max() <= 0, "off by %g past the tolerance" % over.max()
+
+
+# ---------------------------------------------------------------------------
+# rotary positions
+# ---------------------------------------------------------------------------
+def rope64(x, pos, rot, layout="half", base=1e4, scaling="none", factor=1.0, trained=0, beta_fast=32.0, beta_slow=1.0,
+           amplitude=1.0, inverse=False):
+    x = x.double()
+    if scaling == "base":
+        base = base * factor ** (rot / (rot - 2))
+    f = torch.tensor([base ** (-2 * i / rot) for i in range(rot // 2)], dtype=torch.float64)
+    if scaling == "linear":
+        f = f / factor
+    if scaling == "parts":
+        keep = ((trained * f / (2 * math.pi) - beta_slow) / (beta_fast - beta_slow)).clamp(0, 1)
+        f = f * keep + f / factor * (1 - keep)
+    ang = pos.double()[..., None, None] * f * (-1 if inverse else 1)
+    c, s = amplitude * torch.cos(ang), amplitude * torch.sin(ang)
+    y = x.clone()
+    lo, hi = (slice(0, rot // 2), slice(rot // 2, rot)) if layout == "half" else (slice(0, rot, 2), slice(1, rot, 2))
+    a, b = x[..., lo], x[..., hi]
+    y[..., lo], y[..., hi] = a * c - b * s, a * s + b * c
+    # size of a pair, the scale of the errors of its sine and cosine
+    size = torch.zeros_like(x)
+    size[..., lo] = size[..., hi] = amplitude * (a.abs() + b.abs())
+    return y, size
+
+
+def rope_close(got, x, pos, rot, **kw):
+    """Angle to fp32 turns and sine and cosine to an ulp or two (8 u of the pair's size), then the output's rounding."""
+    ref, size = rope64(x, pos, rot, **kw)
+    within(got, ref, H[x.dtype] * ref.abs() + 8 * U * size)
+
+
+ROPE = [
+    # batch, tokens, heads, kv heads, head dim, rot, what else
+    (1, 1, 8, 1, 256, 256, {}),
+    (2, 7, 3, 2, 64, 32, dict(layout="interleaved")),
+    (3, 1030, 2, 0, 128, 128, dict(scaling="linear", factor=4.0)),
+    (2, 513, 4, 1, 64, 64, dict(layout="interleaved", scaling="base", factor=8.0)),
+    (1, 90, 2, 1, 128, 64, dict(scaling="parts", factor=5.5, trained=4096, amplitude=1.125)),
+    (2, 5, 3, 1, 10, 6, {}),                           # pieces of single elements
+    (2, 5, 3, 1, 10, 6, dict(layout="interleaved")),
+    (1, 3, 1, 1, 512, 512, dict(inverse=True, amplitude=0.5)),
+    (1, 3, 2, 1, 2, 2, dict(base=500.0)),
+]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("case", ROPE, ids=lambda c: "b%d-n%d-h%d+%d-d%d-r%d" % c[:6])
+def test_rope(ops, case, dtype):
+    b, n, heads, kv, dh, rot, kw = case
+    q, k = rand(1, b, n, heads, dh, dtype=dtype), rand(2, b, n, kv, dh, dtype=dtype) if kv else None
+    pos = torch.randint(0, 1 << 20, (b, n), generator=torch.Generator().manual_seed(3)).int()
+    qo, ko = ops.rope(dev(q), dev(k), dev(pos), rot_dim=rot, **kw)
+    rope_close(qo, q, pos, rot, **kw)
+    assert torch.equal(qo[..., rot:].cpu(), q[..., rot:])
+    if kv:
+        rope_close(ko, k, pos, rot, **kw)
+    else:
+        assert ko is None
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_rope_positions_strides_and_in_place(ops, dtype):
+    # q and k as slices of one projection whose rows start off 16-byte boundaries, k_out a cache's middle
+    b, n, dh = 2, 9, 64
+    both = rand(5, b, n, 6, dh + 3, dtype=dtype)
+    d = dev(both)
+    q, k = d[:, :, :4, :dh], d[:, :, 4:, :dh]
+    cache = torch.full((b, 20, 2, dh), 7.0, dtype=dtype, device="cuda")
+    pos = torch.tensor([3, -5, 0, 100000, 2, 2, 1 << 24, -(1 << 24), 8]).int()
+    qo, ko = ops.rope(q, k, dev(pos), q_out=q, k_out=cache[:, 5:14])
+    assert qo is q
+    for got, x in ((qo, both[:, :, :4, :dh]), (ko, both[:, :, 4:, :dh])):
+        rope_close(got, x, pos.expand(b, n), dh)
+    assert torch.equal(d[:, :, 4:].cpu(), both[:, :, 4:]) and torch.equal(d[..., dh:].cpu(), both[..., dh:])
+    assert (cache[:, :5] == 7).all() and (cache[:, 14:] == 7).all()
+    # consecutive positions by default
+    x = rand(6, 2, 5, 1, dh, dtype=dtype)
+    rope_close(ops.rope(dev(x))[0], x, torch.arange(5).expand(2, 5), dh)
+    # one head read by all (stride 0)
+    one = rand(7, 2, 5, 1, dh, dtype=dtype)
+    rope_close(ops.rope(dev(one).expand(2, 5, 3, dh))[0], one.expand(2, 5, 3, dh), torch.arange(5).expand(2, 5), dh)
+
+
+def test_rope_inverse_is_the_gradient_and_moves_keys(ops):
+    x, w = rand(8, 1, 6, 2, 64), rand(9, 1, 6, 2, 64)
+    pos = torch.arange(40, 46).int()
+    kw = dict(rot_dim=32, scaling="linear", factor=3.0, amplitude=1.25)
+    # d (w . rope(x)) / dx by autograd of the formula
+    x64 = x.double().requires_grad_()
+    ang = pos.double()[:, None, None] * torch.tensor([1e4 ** (-2 * i / 32) / 3.0 for i in range(16)], dtype=torch.float64)
+    c, s = 1.25 * ang.cos(), 1.25 * ang.sin()
+    a, b = x64[..., :16], x64[..., 16:32]
+    y = torch.cat([a * c - b * s, a * s + b * c, x64[..., 32:]], -1)
+    (y * w.double()).sum().backward()
+    got = ops.rope(dev(w), positions=dev(pos), inverse=True, **kw)[0]
+    within(got, x64.grad, (8 * 1.25 * 2 + 1) * U * w.double().abs().max())
+    # differences: the map is linear, so (f(x + h w) - f(x - h w)) / 2h is f(w) but for roundings of values below 16
+    h = 0.5
+    plus, minus = (ops.rope(dev(x + z * h * w), positions=dev(pos), **kw)[0] for z in (1, -1))
+    within((plus - minus).cpu() / (2 * h), ops.rope(dev(w), positions=dev(pos), **kw)[0].cpu(), 16 * 32 * U)
+    # keys rotated at 10 .. 15 and moved by differences to 40 .. 45
+    kk = ops.rope(dev(x), positions=dev(torch.arange(10, 16).int()))[0]
+    kk = ops.rope(kk, positions=torch.full((6,), 30, dtype=torch.int32, device="cuda"), q_out=kk)[0]
+    ref, size = rope64(x, pos[None], 64)
+    within(kk, ref, 32 * U * (1 + size))
+
+
+# ---------------------------------------------------------------------------
+# shared attention and slot weights
+# ---------------------------------------------------------------------------
+def attn64(q, kp, vp, ks, vs, plen, slen, causal, scale):
+    """out, lse, and per element the sum of p |v|, per row the scale of its scores' rounding errors."""
+    B, Hq, nh, D = q.shape
+    G, _, kv, _ = kp.shape
+    q, kp, vp = q.double(), kp.double(), vp.double()
+    out, mag = torch.zeros(B, Hq, nh, D, dtype=torch.float64), torch.zeros(B, Hq, nh, D, dtype=torch.float64)
+    lse = torch.full((B, Hq, nh), -INF, dtype=torch.float64)
+    err = torch.zeros(B, Hq, nh, dtype=torch.float64)
+    for b in range(B):
+        g, n = b // (B // G), 0 if ks is None else slen[b]
+        for h in range(nh):
+            hk = h // (nh // kv)
+            K, V = kp[g, :plen[g], hk], vp[g, :plen[g], hk]
+            if n:
+                K, V = torch.cat([K, ks[b, :n, hk].double()]), torch.cat([V, vs[b, :n, hk].double()])
+            if not len(K):
+                continue
+            s = scale * (q[b, :, h] @ K.T)
+            if causal:
+                at = torch.arange(len(K)) - plen[g]
+                hide = (at >= 0) & (at > n - Hq + torch.arange(Hq)[:, None])
+                s = s.masked_fill(hide, -INF)
+            lse[b, :, h] = torch.logsumexp(s, -1)
+            p = torch.nan_to_num(torch.exp(s - lse[b, :, h, None]), nan=0.0)
+            out[b, :, h], mag[b, :, h] = p @ V, p @ V.abs()
+            err[b, :, h] = scale * (q[b, :, h].abs() @ K.abs().T).amax(-1)
+    return out, lse, mag, err
+
+
+def attn_tolerance(dtype, ref, lse, mag, err, keys, D):
+    """Scores: products summed in fp32, (D + 3) u of the sum of magnitudes each; exp2, sums and joins (keys + 40) u; in
+    bf16 the probability's rounding, and the output's."""
+    ds = (D + 3) * U * err + 8 * U * (lse.abs() + 1).nan_to_num(posinf=0)
+    soft = 2 * ds + (keys + 40) * U
+    p = H[dtype] if dtype == torch.bfloat16 else 0.0
+    return H[dtype] * ref.abs() + mag * (soft[..., None] + p) * 1.01 + 1e-30, (soft + 1e-30).masked_fill(lse == -INF, 0)
+
+
+ATTN = [
+    # groups, rollouts, rows, heads, kv heads, dim, prefix lengths (of slots), tail slots, tail lengths (None: all), causal
+    (1, 1, 1, 1, 1, 64, [1], 1, 0, None, False),
+    (1, 4, 1, 8, 1, 256, [816], 816, 51, [51, 1, 0, 32], False),
+    (2, 3, 50, 8, 1, 256, [130, 96], 130, 50, None, True),
+    (3, 5, 7, 4, 2, 64, [333, 0, 17], 333, 13, [13, 7, 0, 3, 12, 1, 0, 13, 6, 7, 8, 2, 13, 0, 5], True),
+    (1, 70, 1, 8, 8, 64, [40], 47, 33, [(i * 11) % 34 for i in range(70)], False),
+    (2, 20, 3, 6, 2, 128, [0, 0], 0, 65, [(i * 13) % 66 for i in range(40)], True),
+    (1, 2, 5, 16, 4, 128, [1500], 1501, 0, None, False),
+    (1, 64, 1, 8, 1, 128, [1057], 1057, 40, [40 - i % 41 for i in range(64)], False),
+    (2, 1, 33, 2, 2, 256, [64, 31], 64, 33, None, True),
+    (1, 9, 1, 5, 1, 64, [4100], 4100, 3, None, False),
+]
+
+
+def attn_inputs(case, dtype, seed=11):
+    G, R, Hq, nh, kv, D, plen, P, S, slen, causal = case
+    q = rand(seed, G * R, Hq, nh, D, dtype=dtype)
+    kp, vp = (rand(seed + i, G, P, kv, D, dtype=dtype) for i in (1, 2))
+    ks, vs = (rand(seed + i, G * R, S, kv, D, dtype=dtype) for i in (3, 4)) if S else (None, None)
+    slen = [S] * (G * R) if slen is None else slen
+    # what lies past the lengths is never read
+    for g in range(G):
+        kp[g, plen[g]:], vp[g, plen[g]:] = math.nan, math.nan
+    if S:
+        for b in range(G * R):
+            ks[b, slen[b]:], vs[b, slen[b]:] = math.nan, INF
+    return q, kp, vp, ks, vs, plen, slen, causal
+
+
+def i32(v):
+    return torch.tensor(v, dtype=torch.int32, device="cuda")
+
+
+def run_attn(ops, q, kp, vp, ks, vs, plen, slen, causal, **kw):
+    return ops.shared_attention(dev(q), dev(kp), dev(vp), dev(ks), dev(vs), prefix_len=i32(plen),
+                                suffix_len=None if ks is None else i32(slen), causal=causal, **kw)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("case", ATTN, ids=lambda c: "g%dx%d-q%d-h%d/%d-d%d-p%d-s%d" % (*c[:6], c[7], c[8]))
+def test_shared_attention(ops, case, dtype):
+    x = attn_inputs(case, dtype)
+    D, scale = case[5], case[5] ** -0.5
+    ref, lse, mag, err = attn64(*x, scale)
+    out, got_lse = run_attn(ops, *x)
+    tol, lse_tol = attn_tolerance(dtype, ref, lse, mag, err, case[7] + case[8], D)
+    within(out, ref, tol)
+    within(got_lse, lse, lse_tol)
+    # all together: two independent roundings (probabilities, output), each at most h of what it rounds
+    n = ref.norm()
+    if n > 0:
+        assert (out.double().cpu() - ref).norm() <= 1.5 * H[dtype] * n + (mag * tol.new_tensor(64 * U)).norm()
+    assert (out.cpu()[lse == -INF] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_shared_attention_strides_lengths_and_buffers(ops, dtype):
+    G, R, Hq, nh, kv, D, P, S = 2, 3, 4, 4, 2, 64, 70, 9
+    x = attn_inputs((G, R, Hq, nh, kv, D, [70, 70], P, S, None, False), dtype, 31)
+    q, kp, vp, ks, vs = x[:5]
+    ref, lse = run_attn(ops, *x)
+    # queries, tail keys and values in one projection; caches with the heads outermost; an output between other data
+    fused = dev(torch.cat([q, rand(1, G * R, Hq, 3, D, dtype=dtype)], 2))
+    heads_first = [dev(t).transpose(1, 2).contiguous().transpose(1, 2) for t in (kp, vp, ks, vs)]
+    buf = torch.full((G * R, Hq, 2 * nh, D), 5.0, dtype=dtype, device="cuda")
+    out, lse2 = ops.shared_attention(fused[:, :, :nh], *heads_first, out=buf[:, :, 1:nh + 1])
+    assert torch.equal(out, ref) and torch.equal(lse, lse2)
+    assert (buf[:, :, 0] == 5).all() and (buf[:, :, nh + 1:] == 5).all()
+    # lengths outside the slots count as the nearer end
+    a = run_attn(ops, *x[:5], [P, 0], [S, 0, S, S, 0, S], False)
+    b = run_attn(ops, *x[:5], [P + 100, -3], [S + 1, -1, 2 ** 31 - 1, S, -2 ** 31, S], False)
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+    # an explicit scale
+    c = ops.shared_attention(*(dev(t) for t in x[:5]), scale=0.5)
+    r, l, mag, err = attn64(*x, 0.5)
+    within(c[0], r, attn_tolerance(dtype, r, l, mag, err, P + S, D)[0])
+    # misaligned rows are refused
+    from paper_2607_12659_amd.jpi import JpiError
+    with pytest.raises(JpiError, match="aligned"):
+        ops.shared_attention(dev(torch.zeros(G * R, Hq, nh, D + 1, dtype=dtype))[..., 1:], *(dev(t) for t in x[1:5]))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_shared_attention_keeps_rollouts_apart(ops, dtype):
+    """NaN and infinity of one rollout reach its rows only, wherever rollouts share a row tile."""
+    G, R, Hq, nh, kv, D, P, S = 1, 9, 3, 2, 1, 64, 50, 40
+    x = attn_inputs((G, R, Hq, nh, kv, D, [P], P, S, None, False), dtype, 41)
+    ref, _ = run_attn(ops, *x)
+    q, ks, vs = x[0].clone(), x[3].clone(), x[4].clone()
+    q[1, 0, 0, 5] = math.nan
+    ks[3, 7] = math.nan
+    vs[4, 35] = INF
+    vs[6, 2] = math.nan
+    out, _ = run_attn(ops, q, x[1], x[2], ks, vs, *x[5:])
+    sick = [1, 3, 4, 6]
+    well = [b for b in range(R) if b not in sick]
+    assert torch.equal(out[well], ref[well])
+    assert torch.isnan(out[3]).all() and torch.isnan(out[6]).all() and (out[4] == INF).all()
+    assert torch.isnan(out[1, 0, 0]).all() and torch.equal(out[1, 1:], ref[1, 1:]) and torch.equal(out[1, 0, 1], ref[1, 0, 1])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_shared_attention_of_extreme_scores(ops, dtype):
+    """Scores that grow along the sequence by far more than fp32's exponent range, and -inf among them."""
+    D, P = 64, 200
+    q = torch.zeros(1, 1, 1, D, dtype=dtype)
+    q[..., 0] = 8.0
+    k, v = torch.zeros(1, P, 1, D, dtype=dtype), rand(3, 1, P, 1, D, dtype=dtype)
+    k[0, :, 0, 0] = torch.arange(P).to(dtype) * 8  # score = 8 j: one key takes nearly all
+    k[0, 100, 0, 0] = -INF                         # visible, of weight 0
+    out, lse = ops.shared_attention(dev(q), dev(k), dev(v))
+    s = (8.0 * k[0, :, 0, 0].double()) / 8.0
+    p = torch.softmax(s, 0)
+    ref = p @ v[0, :, 0].double()
+    within(out[0, 0, 0], ref, 2 * H[dtype] * v[0, :, 0].double().abs().amax(0) + 64 * U)
+    within(lse[0, 0, 0], torch.logsumexp(s, 0), 64 * U * 1600)
+    k[0, :, 0, 0] = -INF
+    out, lse = ops.shared_attention(dev(q), dev(k), dev(v))
+    assert (out == 0).all() and (lse == -INF).all()
+
+
+def weight64(q, kp, lse, plen, scale):
+    B, _, nh, D = q.shape
+    G, P, kv, _ = kp.shape
+    w, err = torch.zeros(G, kv, P, dtype=torch.float64), torch.zeros(G, kv, P, dtype=torch.float64)
+    for g in range(G):
+        rows = slice(g * (B // G), (g + 1) * (B // G))
+        for h in range(kv):
+            heads = slice(h * (nh // kv), (h + 1) * (nh // kv))
+            K = kp[g, :plen[g], h].double()
+            qq = q[rows, :, heads].double().reshape(-1, D)
+            l = lse[rows, :, heads].double().reshape(-1, 1)
+            on = (l > -INF).double()
+            p = torch.exp(scale * qq @ K.T - l.nan_to_num(neginf=0)) * on
+            ds = (D + 3) * U * scale * (qq.abs() @ K.abs().T) + 8 * U * (l.nan_to_num(neginf=0).abs() + 1)
+            w[g, h, :plen[g]] = p.sum(0)
+            err[g, h, :plen[g]] = (p * (2 * ds + 8 * U)).sum(0) + (len(qq) + 8) * U * p.sum(0)
+    return w, err
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("case", [c for c in ATTN if c[7]], ids=lambda c: "g%dx%d-q%d-h%d/%d-d%d-p%d" % (*c[:6], c[7]))
+def test_prefix_weight(ops, case, dtype):
+    q, kp, vp, ks, vs, plen, slen, causal = x = attn_inputs(case, dtype)
+    G, kv, P, scale = case[0], case[4], case[7], case[5] ** -0.5
+    _, lse, _, _ = attn64(*x, scale)
+    lse = lse.float()
+    ref, err = weight64(q, kp, lse, plen, scale)
+    args = (dev(q), dev(kp), dev(lse))
+    got = ops.prefix_weight(*args, prefix_len=i32(plen))
+    within(got, ref, err + 1e-30)  # slots past the lengths: 0
+    # accumulated with decay, in place: slots past the lengths stay as they were
+    w0 = rand(77, G, kv, P).abs()
+    w = dev(w0)
+    assert ops.prefix_weight(*args, w, prefix_len=i32(plen), decay=0.75, out=w) is w
+    inside = torch.arange(P) < torch.tensor(plen)[:, None, None]
+    acc = torch.where(inside, 0.75 * w0.double() + ref, w0.double())
+    within(w, acc, err + 4 * U * acc)
+    assert torch.equal(w.cpu()[~inside.expand_as(w0)], w0[~inside.expand_as(w0)])
+    # the same bits again
+    assert torch.equal(ops.prefix_weight(*args, prefix_len=i32(plen)), got)
+
+
+# ---------------------------------------------------------------------------
+# eviction
+# ---------------------------------------------------------------------------
+def kept_slots(w, n, keep, first, last):
+    if n <= keep:
+        return list(range(n))
+    w = torch.nan_to_num(w.double(), nan=-INF, posinf=INF, neginf=-INF).tolist()
+    mid = sorted(range(first, n - last), key=lambda j: (-w[j], j))[:keep - first - last]
+    return list(range(first)) + sorted(mid) + list(range(n - last, n))
+
+
+def weights(kind, seed, *shape):
+    w = rand(seed, *shape)
+    if kind == "equal":
+        return torch.full(shape, 0.25)
+    if kind == "ties":
+        return torch.round(w * 2) / 2  # many equal, zeros of both signs
+    if kind == "odd":
+        w = w * 1e-3
+        w[..., ::7], w[..., 1::11], w[..., 2::13], w[..., 3::5] = math.nan, INF, -INF, -0.0
+        return w
+    return w
+
+
+EVICT = [
+    # outer, heads, dim, slots, keep, first, last, lengths, weights
+    (1, 1, 64, 1, 1, 0, 0, None, "plain"),
+    (3, 1, 256, 816, 408, 4, 48, None, "plain"),
+    (2, 2, 64, 1000, 999, 0, 1, None, "ties"),
+    (4, 1, 128, 1025, 100, 50, 50, [1025, 100, 101, 0], "ties"),
+    (2, 1, 64, 5000, 1234, 0, 0, [5000, 4097], "equal"),
+    (1, 2, 64, 17000, 16999, 1, 1, None, "odd"),
+    (1, 1, 64, 40000, 321, 0, 5, None, "odd"),
+    (2, 3, 5, 77, 20, 3, 2, [77, 19], "odd"),       # rows that are no multiple of 16 bytes
+    (1, 1, 64, 30, 64, 2, 2, None, "plain"),        # room for more than there is
+    (2, 1, 512, 600, 1, 0, 0, None, "equal"),
+]
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("case", EVICT, ids=lambda c: "n%dx%d-d%d-p%d-k%d-%s" % (*c[:5], c[8]))
+def test_evict(ops, case, dtype, in_place):
+    n, heads, dh, slots, keep, first, last, lens, kind = case
+    k, v = rand(1, n, slots, heads, dh, dtype=dtype), rand(2, n, slots, heads, dh, dtype=dtype)
+    w = weights(kind, 3, n, heads, slots)
+    lengths = [slots] * n if lens is None else lens
+    most = min(keep, slots)
+    dk, dv, dw = dev(k), dev(v), dev(w)
+    dlen = None if lens is None else i32(lens)
+    if in_place:
+        ko, vo, wo = dk, dv, dw
+        before = k, v, w
+        index, out_len = ops.evict(dk, dv, dw, keep, lens=dlen, n_first=first, n_last=last, lens_out=dlen)
+        assert dlen is None or out_len is dlen
+    else:
+        before = tuple(torch.full(s, 9.0, dtype=t) for s, t in (((n, most + 2, heads, dh), dtype),) * 2 +
+                       (((n, heads, most + 3), torch.float32),))
+        ko, vo, wo = (dev(t) for t in before)
+        index, out_len = ops.evict(dk, dv, dw, keep, lens=dlen, n_first=first, n_last=last, k_out=ko, v_out=vo, weight_out=wo)
+        assert torch.equal(dk.cpu(), k) and torch.equal(dv.cpu(), v)
+        assert torch.equal(dw.cpu().nan_to_num(), w.nan_to_num())
+    assert out_len.tolist() == [min(x, keep) for x in lengths]
+    ko, vo, wo, index = ko.cpu(), vo.cpu(), wo.cpu(), index.cpu()
+    for o in range(n):
+        for h in range(heads):
+            kept = kept_slots(w[o, h], lengths[o], keep, first, last)
+            m = len(kept)
+            assert index[o, h].tolist() == kept + [-1] * (keep - m)
+            for got, src, was in ((ko, k, before[0]), (vo, v, before[1])):
+                assert torch.equal(got[o, :m, h], src[o, kept, h])
+                assert torch.equal(got[o, m:, h], was[o, m:, h])
+            assert torch.equal(wo[o, h, :m].nan_to_num(nan=-1), w[o, h, kept].nan_to_num(nan=-1))
+            assert torch.equal(wo[o, h, m:].nan_to_num(nan=-1), before[2][o, h, m:].nan_to_num(nan=-1))
+
+
+def test_evict_layouts(ops):
+    """Heads outermost in memory, K in place and V elsewhere, rows off 16-byte boundaries, no slots at all."""
+    n, heads, dh, slots, keep = 2, 2, 64, 200, 60
+    k, v, w = rand(1, n, slots, heads, dh), rand(2, n, slots, heads, dh), rand(3, n, heads, slots)
+    dk = dev(k).transpose(1, 2).contiguous().transpose(1, 2)
+    wide = torch.zeros(n, slots, heads, dh + 1, device="cuda")
+    wide[..., 1:] = dev(v)
+    vo = torch.zeros(n, keep, heads, dh, device="cuda")
+    ops.evict(dk, wide[..., 1:], dev(w), keep, k_out=dk, v_out=vo, weight_out=torch.empty(n, heads, keep, device="cuda"))
+    for o in range(n):
+        for h in range(heads):
+            kept = kept_slots(w[o, h], slots, keep, 0, 0)
+            assert torch.equal(dk[o, :keep, h].cpu(), k[o, kept, h]) and torch.equal(dk[o, keep:, h].cpu(), k[o, keep:, h])
+            assert torch.equal(vo[o, :, h].cpu(), v[o, kept, h])
+    e = torch.empty(n, 0, heads, dh, device="cuda")
+    index, lens = ops.evict(e, e.clone(), torch.empty(n, heads, 0, device="cuda"), 4)
+    assert lens.tolist() == [0, 0] and (index == -1).all()
+
+
+# ---------------------------------------------------------------------------
+# together
+# ---------------------------------------------------------------------------
+def serve(ops, s, keep):
+    """One observation's prefix: rotate into the cache, attend, weigh, evict, attend to what is left."""
+    q, k = ops.rope(s["q"], positions=s["qpos"], q_out=s["q_rot"])[0], ops.rope(s["k"], q_out=s["cache_k"])[0]
+    out, lse = ops.shared_attention(q, k, s["v"], s["ks"], s["vs"], out=s["out"], lse=s["lse"])
+    w = ops.prefix_weight(q, k, lse, out=s["w"])
+    _, lens = ops.evict(k, s["v"], w, keep, n_first=2, k_out=s["k2"], v_out=s["v2"], weight_out=s["w2"], index=s["index"],
+                        lens_out=s["lens"])
+    ops.shared_attention(q, s["k2"], s["v2"], s["ks"], s["vs"], prefix_len=lens, out=s["out2"], lse=s["lse2"])
+    return [s[n] for n in ("out", "lse", "w", "k2", "v2", "w2", "index", "lens", "out2", "lse2")]
+
+
+def serving_state(seed, dtype=torch.bfloat16, P=300, keep=100, R=6, Hq=5, S=5):
+    d = lambda i, *sh: dev(rand(seed * 100 + i, *sh, dtype=dtype))  # noqa: E731
+    z = lambda *sh, t=dtype: torch.zeros(sh, dtype=t, device="cuda")  # noqa: E731
+    return {"q": d(1, R, Hq, 8, 64), "k": d(2, 1, P, 1, 64), "v": d(3, 1, P, 1, 64), "ks": d(4, R, S, 1, 64),
+            "vs": d(5, R, S, 1, 64), "qpos": torch.arange(P, P + Hq, dtype=torch.int32, device="cuda"),
+            "q_rot": z(R, Hq, 8, 64), "cache_k": z(1, P, 1, 64), "out": z(R, Hq, 8, 64), "lse": z(R, Hq, 8, t=torch.float32),
+            "w": z(1, 1, P, t=torch.float32), "k2": z(1, keep, 1, 64), "v2": z(1, keep, 1, 64),
+            "w2": z(1, 1, keep, t=torch.float32), "index": z(1, 1, keep, t=torch.int32), "lens": z(1, t=torch.int32),
+            "out2": z(R, Hq, 8, 64), "lse2": z(R, Hq, 8, t=torch.float32)}
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_a_prefix_from_rotation_to_eviction(ops, dtype):
+    P, keep = 300, 100
+    s = serving_state(1, dtype)
+    serve(ops, s, keep)
+    q, k = s["q_rot"].cpu(), s["cache_k"].cpu()
+    rope_close(s["q_rot"], s["q"].cpu(), s["qpos"].cpu()[None], 64)
+    rope_close(s["cache_k"], s["k"].cpu(), torch.arange(P)[None], 64)
+    cpu = [s[n].cpu() for n in ("v", "ks", "vs")]
+    ref, lse, mag, err = attn64(q, k, *cpu, [P], [5] * 6, False, 0.125)
+    within(s["out"], ref, attn_tolerance(dtype, ref, lse, mag, err, P + 5, 64)[0])
+    wref, werr = weight64(q, k, s["lse"].cpu(), [P], 0.125)
+    within(s["w"], wref, werr)
+    kept = kept_slots(s["w"][0, 0].cpu(), P, keep, 2, 0)
+    assert s["index"][0, 0].tolist() == kept and s["lens"].tolist() == [keep]
+    ref, lse, mag, err = attn64(q, k[:, kept], cpu[0][:, kept], *cpu[1:], [keep], [5] * 6, False, 0.125)
+    within(s["out2"], ref, attn_tolerance(dtype, ref, lse, mag, err, keep + 5, 64)[0])
+    within(s["lse2"], lse, attn_tolerance(dtype, ref, lse, mag, err, keep + 5, 64)[1])
+
+
+def test_captured_runs_replay(ops):
+    """Two captured runs and eager ones of other inputs in turn, each replay against its eager result."""
+    keep = 100
+    states = [serving_state(i) for i in (1, 2)]
+    want = [[t.clone() for t in serve(ops, s, keep)] for s in states]
+    other = serving_state(3, P=700)
+    torch.cuda.synchronize()
+    graphs = []
+    for s in states:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            outs = serve(ops, s, keep)
+        graphs.append((g, outs))
+    for turn in range(3):
+        for (g, outs), w in zip(graphs, want):
+            for t in outs:
+                t.zero_()
+            serve(ops, other, keep)
+            g.replay()
+            serve(ops, other, keep)
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(outs, w)), turn
+    # both at once, on streams of their own
+    a, b = torch.cuda.Stream(), torch.cuda.Stream()
+    for (g, outs), st in zip(graphs, (a, b)):
+        with torch.cuda.stream(st):
+            g.replay()
+    torch.cuda.synchronize()
+    for (g, outs), w in zip(graphs, want):
+        assert all(torch.equal(x, y) for x, y in zip(outs, w))
+
+
+def test_calls_on_several_streams(ops):
+    states = [serving_state(10 + i) for i in range(3)]
+    want = [[t.clone() for t in serve(ops, s, 100)] for s in states]
+    for s in states:
+        for n in ("out", "w", "k2", "out2", "index"):
+            s[n].zero_()
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in states]
+    for _ in range(5):
+        for s, st in zip(states, streams):
+            with torch.cuda.stream(st):
+                serve(ops, s, 100)
+    torch.cuda.synchronize()
+    for s, w in zip(states, want):
+        assert all(torch.equal(a, b) for a, b in zip(serve(ops, s, 100), w))
+
+
+def test_evicted_prefix_in_the_denoiser(ops):
+    """A bound prefix compacted in the context's own buffers denoises as the same prefix cut on the host does."""
+    import numpy as np
+
+    import synth
+    from paper_2607_12659_amd import jpi
+    from paper_2607_12659_amd.expert import ActionExpert, to_device
+    wl = synth.WORKLOADS["tiny-fp32"]
+    d, P, keep = wl.dims, wl.prefix, 24
+    K, V = synth.make_prefix(wl)
+    noise = to_device(synth.make_noise(wl))
+    w = rand(4, d.n_layers, wl.batch, P).abs()  # one weight per layer, rollout and slot
+    acts = []
+    for on_device in (False, True):
+        ae = ActionExpert(d, wl.dtype, wl.batch, P)
+        try:
+            ae.load_weights(synth.make_weights(wl))
+            if on_device:
+                ae.bind_prefix(to_device(K), to_device(V))
+                st, kp, vp = jpi.jpi_prefix_buffers(ae.ctx)
+                assert st == jpi.JPI_OK
+                n = d.n_layers * wl.batch
+                index = torch.empty(n, keep, dtype=torch.int32, device="cuda")
+                dw = dev(w)
+                a = jpi.jpi_evict_args(jpi.JPI_F32, n, 1, d.head_dim, P, keep, 1, 3, dw.data_ptr(), P)
+                row = P * d.head_dim
+                a.k = a.k_out = jpi.jpi_view(kp, row, d.head_dim, 0)
+                a.v = a.v_out = jpi.jpi_view(vp, row, d.head_dim, 0)
+                a.index = index.data_ptr()
+                assert jpi.jpi_evict(a) == jpi.JPI_OK
+                ae._chk(jpi.jpi_bind_prefix(ae.ctx, kp, vp, [keep] * wl.batch, wl.batch, P))
+            else:
+                k2, v2 = (np.empty((d.n_layers, wl.batch, keep, d.head_dim), K.dtype) for _ in range(2))
+                for l in range(d.n_layers):
+                    for b in range(wl.batch):
+                        kept = kept_slots(w[l, b], P, keep, 1, 3)
+                        k2[l, b], v2[l, b] = K[l, b, kept], V[l, b, kept]
+                ae.bind_prefix(to_device(k2), to_device(v2))
+            # actions follow the prefix at position prefix_len in both
+            acts.append(ae.denoise(noise, wl.n_steps).clone())
+            ae.sync()
+        finally:
+            ae.close()
+    # the same keys in the same order, but ranges of the key axis follow the buffer's size: fp32 sums in another order
+    within(acts[1], acts[0].cpu(), 1e-5)
