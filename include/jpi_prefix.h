@@ -113,7 +113,7 @@ jpi_status jpi_rope(const jpi_rope_config* cfg, jpi_dtype dt, int batch, int tok
  * (already rotated); in bf16 the probabilities are rounded to bf16 for the
  * product with V, while the row sum and lse take them in fp32.  Rollouts do not
  * affect each other: NaN or infinity in one rollout's queries or tail stays in
- * its rows. */
+ * the rows that see it (of which it may reach every element). */
 typedef struct {
   jpi_dtype dtype;                     /* JPI_BF16 or JPI_F32: q, keys, values and out */
   int n_groups, group, q_rows;         /* each >= 1 */

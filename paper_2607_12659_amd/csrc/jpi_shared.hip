@@ -33,23 +33,40 @@ constexpr int KEYS = 32;          // keys per tile
 constexpr float LOG2E = 1.44269504088896341f, LN2 = 0.693147180559945309f;
 constexpr float HEADROOM = 16.f;  // log2 of the most that a probability may exceed its row's reference by
 
-// A tile of 32 rows (keys, or queries) of DH elements in LDS, in 16-byte chunks.  Chunk c of row r lies at
-// chunk place(r, c) of the row: the permutations keep the lanes of one LDS read in different banks.
+// A tile of 32 rows (keys, or queries) of DH elements in LDS, in 1 KB pieces of 8 rows x 128 bytes.  A load instruction
+// fills a piece lane after lane, and it is fast only where neighbouring lanes ask for neighbouring memory, so rows stay
+// whole in a piece and their eight 16-byte chunks are permuted, row by row, such that the lanes of one LDS read share
+// out the 64 banks evenly.  A read's address is one of a few bases of its lane plus a constant.
 template <typename T, int DH>
 struct Tile {
   static constexpr int CE = 16 / sizeof(T);      // elements of a chunk
   static constexpr int CPR = DH / CE;            // chunks of a row
-  static constexpr int KS = CPR / 2;             // chunk pairs (the two lane halves) of a row
+  static constexpr int KS = CPR / 2;             // k-steps: a chunk for each lane half
   static constexpr int NT = DH / 32;             // 32-wide output tiles
   static constexpr int BYTES = KEYS * DH * (int)sizeof(T);
+  static constexpr int PIECES = BYTES / 1024;    // piece f: chunks 8 (f / 4) .. + 7 of rows 8 (f % 4) .. + 7
   typedef T chunk __attribute__((ext_vector_type(CE)));
-  // 32 rows at one chunk: 16 rows fill the 64 banks
-  static __device__ __forceinline__ int place(int r, int c) { return c ^ (CPR >= 16 ? r & 15 : (r >> 1) & 7); }
-  // V as the transposed operand.  bf16: four consecutive keys at 64 bytes; fp32: keys r and r + 4 at 128 bytes
-  static __device__ __forceinline__ int place_v(int r, int c) {
-    if constexpr (sizeof(T) == 4) return c ^ ((r >> 2) & 1) * 8;
-    return c ^ (CPR >= 16 ? (r & 3) << 2 : ((r >> 1) & 1) << 2);
+  // Rows of a product over DH (K, or queries) are read 32 at a time at one chunk: chunk c of row r lies at c ^ swz(r).
+  static __device__ __forceinline__ int swz(int r) { return (r & 7) ^ (r >> 3 & 1); }
+  // V in bf16 is read transposed, 16 lanes addressing 4 keys x 16 dims: keys 4 .. 7, 2 keys apart, change 64-byte halves.
+  static __device__ __forceinline__ int swz_v(int r) { return sizeof(T) == 2 ? (r & 2) << 1 : 0; }
+  // what chunk `at` of a piece holds: a row of its eight, and a chunk of the row's eight
+  static __device__ __forceinline__ int row(int at) { return at >> 3; }
+  static __device__ __forceinline__ int col(int f, int at) { return (at & 7) ^ swz(8 * (f & 3) + (at >> 3)); }
+  static __device__ __forceinline__ int col_v(int at) { return (at & 7) ^ swz_v(at >> 3); }
+  // the chunk of k-step k that a lane (row lane % 32, half lane / 32) reads: base(lane, k % 4) + step(k)
+  static __device__ __forceinline__ int base(int lane, int j) {
+    const int r = lane & 31, h = lane >> 5;
+    return r * 128 + ((2 * j + h) ^ swz(r)) * 16;
   }
+  static constexpr int step(int k) { return (k >> 2) * 4096; }
+  // V, bf16: the 8 bytes that a lane addresses for 16-key step u, output tile t and keys 8 z .. of it:
+  // base_v(lane, t % 2) + step_v(t, u, z)
+  static __device__ __forceinline__ int base_v(int lane, int tp) {
+    const int key = 4 * (lane >> 5) + (lane >> 2 & 3);
+    return key * 128 + ((tp ^ (key >> 1 & 1)) * 64) + (lane >> 4 & 1) * 32 + (lane & 3) * 8;
+  }
+  static constexpr int step_v(int t, int u, int z) { return (t >> 1) * 4096 + (2 * u + z) * 1024; }
 };
 
 template <typename T>
@@ -113,104 +130,312 @@ __device__ __forceinline__ int clamp_len(const int32_t* len, int i, int most) {
   return len ? max(0, min(len[i], most)) : most;
 }
 
-// One 32-key tile for this wave's 32 rows.  `lim`: keys of the tile below it are visible to the lane's row.  `mixed`:
-// only lanes with `mine` take the result (rows of other rollouts keep theirs, whatever this tile's V holds).
-// The row's reference is the maximum of the first tile with a visible key; it moves up, and the row's sums are
-// rescaled, only when a later score exceeds it by more than 2^HEADROOM.
-template <typename T, int DH>
-__device__ __forceinline__ void tile_step(const char* kt, const char* vt, const typename Tile<T, DH>::chunk (&q)[Tile<T, DH>::KS],
-                                          f32x16 (&o)[Tile<T, DH>::NT], float& m_ref, float& l_run, float qscale, int lim,
-                                          bool mixed, bool mine) {
+// Rows that do not see a key have probability 0 for it, and 0 * V of the matrix product would carry NaN or infinity of
+// its V into them.  In a tile of a tail that not all rows see, such values are therefore taken out of LDS, by each wave in
+// the pieces that it loaded, and their keys noted; the rows that see one add its kind to all their elements at the end.
+// kinds[0 .. 2]: keys with +inf, -inf, NaN.
+template <typename T, int DH, int NW>
+__device__ __forceinline__ void take_out(char* vt, u32* kinds) {
   using TL = Tile<T, DH>;
-  const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
-  f32x16 s;
+  constexpr u32 ones = sizeof(T) == 2 ? 0x7f807f80u : 0x7f800000u, step = sizeof(T) == 2 ? 0x00800080u : 0x00800000u;
+  constexpr u32 carry = sizeof(T) == 2 ? 0x80008000u : 0x80000000u;
+  u32x4 x[TL::PIECES / NW];
+  u32 hit = 0;
 #pragma unroll
-  for (int r = 0; r < 16; ++r) s[r] = 0.f;
+  for (int i = 0; i < TL::PIECES / NW; ++i) x[i] = *reinterpret_cast<const u32x4*>(vt + i * NW * 1024);
 #pragma unroll
-  for (int k = 0; k < TL::KS; ++k) {
-    const auto a = *reinterpret_cast<const typename TL::chunk*>(kt + (col * TL::CPR + TL::place(col, 2 * k + half)) * 16);
-    s = mfma_chunk<T>(a, q[k], s);
-  }
-  if (__any(lim < KEYS)) {
+  for (int i = 0; i < TL::PIECES / NW; ++i)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) s[r] = 8 * (r >> 2) + 4 * half + (r & 3) < lim ? s[r] : -INFINITY;
-  }
-  float m = -INFINITY;
-#pragma unroll
-  for (int r = 0; r < 16; ++r) m = fmaxf(m, s[r]);
-  m = halves_max(m) * qscale;
-  const bool over = m > m_ref + HEADROOM || (m_ref == -INFINITY && m > -INFINITY);
-  if (__any(over)) {
-    const float f = over ? __builtin_amdgcn_exp2f(m_ref - m) : 1.f;
-    l_run *= f;
-#pragma unroll
-    for (int t = 0; t < TL::NT; ++t) o[t] *= f;
-    m_ref = over ? m : m_ref;
-  }
-  const float ref = m_ref == -INFINITY ? 0.f : m_ref;  // nothing seen yet: every probability is 2^-inf
-  float sum = 0.f;
-#pragma unroll
-  for (int r = 0; r < 16; ++r) {
-    s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], qscale, -ref));
-    sum += s[r];
-  }
-  l_run += sum;
-  if constexpr (sizeof(T) == 2) {
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {  // 16 keys: registers 8u .. 8u + 7
-      bf16x8 p;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) p[e] = static_cast<bf16>(s[8 * u + e]);
-      // transposed reads: the 16 lanes of a group address 4 keys x 16 dims and get 4 keys of one dim each
-      const int grp = lane >> 4, at = lane & 15;
-      const int key0 = 16 * u + 4 * half + (at >> 2), dim = 16 * (grp & 1) + 4 * (at & 3);
-#pragma unroll
-      for (int t = 0; t < TL::NT; ++t) {
-        const int c = 4 * t + (dim >> 3), sub = (dim & 4) * 2;
-        typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
-        const i16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-            (lds_i16x4*)(vt + (key0 * TL::CPR + TL::place_v(key0, c)) * 16 + sub));
-        const i16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-            (lds_i16x4*)(vt + ((key0 + 8) * TL::CPR + TL::place_v(key0 + 8, c)) * 16 + sub));
-        typedef short i16x8 __attribute__((ext_vector_type(8)));
-        const bf16x8 v = __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
-        const f32x16 n = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, p, o[t], 0, 0, 0);
-        if (mixed) {
-#pragma unroll
-          for (int r = 0; r < 16; ++r) o[t][r] = mine ? n[r] : o[t][r];
-        } else {
-          o[t] = n;
-        }
-      }
-    }
-  } else {
-#pragma unroll
-    for (int t = 0; t < TL::NT; ++t) {
-      f32x16 n = o[t];
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int key = 8 * (r >> 2) + 4 * half + (r & 3), d = 32 * t + col;
-        const float v = *reinterpret_cast<const float*>(vt + (key * TL::CPR + TL::place_v(key, d >> 2)) * 16 + (d & 3) * 4);
-        n = __builtin_amdgcn_mfma_f32_32x32x2f32(v, s[r], n, 0, 0, 0);
-      }
-      if (mixed) {
-#pragma unroll
-        for (int r = 0; r < 16; ++r) o[t][r] = mine ? n[r] : o[t][r];
-      } else {
-        o[t] = n;
-      }
+    for (int e = 0; e < 4; ++e) hit |= (x[i][e] & ones) + step;
+  if (__all((hit & carry) == 0)) return;
+#pragma unroll 1
+  for (int i = 0; i < TL::PIECES / NW; ++i) {
+    T* v = reinterpret_cast<T*>(vt + i * NW * 1024);
+    const int f = (threadIdx.x >> 6) + i * NW, key = 8 * (f & 3) + TL::row(threadIdx.x & 63);
+#pragma unroll 1
+    for (int e = 0; e < TL::CE; ++e) {
+      const float y = (float)v[e];
+      if (__builtin_isfinite(y)) continue;
+      atomicOr(&kinds[y == INFINITY ? 0 : y == -INFINITY ? 1 : 2], 1u << key);
+      v[e] = (T)0.f;
     }
   }
 }
 
-template <typename T, int DH, int NW>
-__global__ __launch_bounds__(64 * NW) void k_shared(SharedLaunch l) {
+// what the keys below `lim` among those add to a row
+__device__ __forceinline__ float taint_of(const u32* kinds, int lim) {
+  const u32 seen = lim >= KEYS ? ~0u : (1u << max(lim, 0)) - 1;
+  const bool pos = (kinds[0] & seen) != 0, neg = (kinds[1] & seen) != 0, nan = (kinds[2] & seen) != 0;
+  return nan || (pos && neg) ? __builtin_nanf("") : pos ? INFINITY : neg ? -INFINITY : 0.f;
+}
+
+constexpr int SCHED_MFMA = 0x008, SCHED_DS_READ = 0x100;
+
+// V^T operands of one 16-key step and output tile (bf16)
+typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
+__device__ __forceinline__ bf16x8 read_vt(const char* p) {
+  typedef short i16x8 __attribute__((ext_vector_type(8)));
+  const i16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)p);
+  const i16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(p + 1024));
+  return __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+
+// S^T = K q^T of one tile.  LDS reads run AHEAD operands before the products, each of which takes less time than a read.
+template <typename T, int DH>
+struct Steps {
   using TL = Tile<T, DH>;
-  constexpr int ROWS = 32 * NW;
-  __shared__ __attribute__((aligned(1024))) char lds[2 * TL::BYTES];
-  __shared__ int cum[ROWS + 1];  // tail tiles of the rollouts that this row tile touches, summed up
-  char* const kt = lds;
-  char* const vt = lds + TL::BYTES;
+  typedef typename TL::chunk chunk;
+  static constexpr bool HALF = sizeof(T) == 2;
+  static constexpr int KS = TL::KS, NT = TL::NT;
+  static constexpr int AHEAD = KS < 8 ? KS : 8, VA = 4;  // operands of K, of V (bf16), that are read ahead
+
+  struct State {  // of this wave's 32 rows: a row in each lane, its keys and dims shared by the lane halves
+    f32x16 o[NT];   // sum of p v
+    float m_ref;    // reference of the row's probabilities: 2^(s - m_ref)
+    float l_run;    // sum of p over this half's keys
+  };
+
+  static __device__ __forceinline__ void k_bases(const char* kt, const char* (&kl)[4]) {
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) kl[j] = kt + TL::base(lane, j);
+  }
+  static __device__ __forceinline__ f32x16 scores(const char* kt, const chunk (&q)[KS]) {
+    const char* kl[4];
+    k_bases(kt, kl);
+    f32x16 s;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[r] = 0.f;
+#pragma unroll
+    for (int k = 0; k < KS; ++k) s = mfma_chunk<T>(*reinterpret_cast<const chunk*>(kl[k & 3] + TL::step(k)), q[k], s);
+    if constexpr (HALF) {
+      __builtin_amdgcn_sched_group_barrier(SCHED_DS_READ, AHEAD, 0);
+#pragma unroll
+      for (int k = 0; k < KS; ++k) {
+        __builtin_amdgcn_sched_group_barrier(SCHED_MFMA, 1, 0);
+        if (k < KS - AHEAD) __builtin_amdgcn_sched_group_barrier(SCHED_DS_READ, 1, 0);
+      }
+    }
+    return s;
+  }
+  // Keys from `lim` on are not visible to the row.  Returns the row's largest score in powers of two.
+  static __device__ __forceinline__ float mask_max(f32x16& s, int lim, float qscale) {
+    const int rest = lim - 4 * ((threadIdx.x & 63) >> 5);
+    float m = -INFINITY;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      s[r] = 8 * (r >> 2) + (r & 3) < rest ? s[r] : -INFINITY;
+      m = fmaxf(m, s[r]);
+    }
+    return halves_max(m) * qscale;
+  }
+  // The row's reference is the maximum of its first tile with a visible key; it moves up, and the row's sums are
+  // rescaled, only when a later score exceeds it by more than 2^HEADROOM.
+  static __device__ __forceinline__ void settle(State& x, float m) {
+    const bool over = m > x.m_ref + HEADROOM || (x.m_ref == -INFINITY && m > -INFINITY);
+    if (__any(over)) {
+      const float f = over ? __builtin_amdgcn_exp2f(x.m_ref - m) : 1.f;
+      x.l_run *= f;
+#pragma unroll
+      for (int t = 0; t < NT; ++t) x.o[t] *= f;
+      x.m_ref = over ? m : x.m_ref;
+    }
+  }
+  static __device__ __forceinline__ void probabilities(State& x, f32x16& s, float qscale) {
+    const float ref = x.m_ref == -INFINITY ? 0.f : x.m_ref;  // nothing seen yet: every probability is 2^-inf
+    float sum[2] = {0.f, 0.f};
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], qscale, -ref));
+      sum[r & 1] += s[r];
+    }
+    x.l_run += sum[0] + sum[1];
+  }
+  // 16 keys each, registers 8u .. 8u + 7 of S^T
+  static __device__ __forceinline__ void round_p(const f32x16& s, bf16x8 (&p)[2]) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) p[u][e] = static_cast<bf16>(s[8 * u + e]);
+  }
+  static __device__ __forceinline__ bf16x8 v_operand(const char* const (&vl)[2], int i) {  // output tile i / 2, 16-key step i % 2
+    return read_vt(vl[i >> 1 & 1] + TL::step_v(i >> 1, i & 1, 0));
+  }
+  // O^T += V^T P^T of one tile, P^T in the registers of S^T
+  static __device__ __forceinline__ void weigh(State& x, const char* vt, f32x16& s, float qscale) {
+    const int lane = threadIdx.x & 63;
+    probabilities(x, s, qscale);
+    if constexpr (HALF) {
+      const char* const vl[2] = {vt + TL::base_v(lane, 0), vt + TL::base_v(lane, 1)};
+      bf16x8 p[2];
+      round_p(s, p);
+#pragma unroll
+      for (int i = 0; i < 2 * NT; ++i) x.o[i >> 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_operand(vl, i), p[i & 1], x.o[i >> 1], 0, 0, 0);
+      __builtin_amdgcn_sched_group_barrier(SCHED_DS_READ, 2 * VA, 0);
+#pragma unroll
+      for (int i = 0; i < 2 * NT; ++i) {
+        __builtin_amdgcn_sched_group_barrier(SCHED_MFMA, 1, 0);
+        if (i < 2 * NT - VA) __builtin_amdgcn_sched_group_barrier(SCHED_DS_READ, 2, 0);
+      }
+    } else {
+      const char* const vl = vt + (lane >> 5) * 512 + (lane & 31) * 4;
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const float v = *reinterpret_cast<const float*>(vl + t * 4096 + (r >> 2) * 1024 + (r & 3) * 128);
+          x.o[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, s[r], x.o[t], 0, 0, 0);
+        }
+    }
+  }
+  // One tile's probabilities and product with V, and the scores of the next, a full tile that all rows see (bf16).  A wave
+  // has the matrix unit to itself or shares it with one other, so the work is laid out by hand, a product and what fits
+  // beside it at a time: while the unit works on the next scores, the probabilities are formed; while it works on V, the
+  // maximum of the next scores is found and the ring's loads are issued (`load(i)`, i < 2 NT).  Operands are read from LDS
+  // AHEAD and VA products before they are used.
+  template <typename F>
+  static __device__ __forceinline__ void both(State& x, const char* vt, const char* kt, const chunk (&q)[KS], f32x16& s,
+                                              float qscale, F load) {
+    const int lane = threadIdx.x & 63;
+    const char* kl[4];
+    k_bases(kt, kl);
+    const char* const vl[2] = {vt + TL::base_v(lane, 0), vt + TL::base_v(lane, 1)};
+    const float ref = x.m_ref == -INFINITY ? 0.f : x.m_ref;
+    constexpr int PRE = 4;            // probabilities formed while the first operands are on their way
+    constexpr int PV = 2 * NT, WAIT = PV > 4 ? 2 : 1;  // products with V; of them before the scores are looked at
+    chunk kf[AHEAD];
+    bf16x8 vf[VA];
+    float sum[2] = {0.f, 0.f};
+    auto probability = [&](int r) __attribute__((always_inline)) {
+      s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], qscale, -ref));
+      sum[r & 1] += s[r];
+    };
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) kf[k] = *reinterpret_cast<const chunk*>(kl[k & 3] + TL::step(k));
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int r = 0; r < PRE; ++r) probability(r);
+    f32x16 n;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) n[r] = 0.f;
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int k = 0; k < KS; ++k) {
+      n = mfma_chunk<T>(kf[k % AHEAD], q[k], n);
+      if (k + AHEAD < KS) kf[k % AHEAD] = *reinterpret_cast<const chunk*>(kl[(k + AHEAD) & 3] + TL::step(k + AHEAD));
+      if (k >= KS - VA) vf[k - (KS - VA)] = v_operand(vl, k - (KS - VA));
+#pragma unroll
+      for (int r = PRE + k * (16 - PRE) / KS; r < PRE + (k + 1) * (16 - PRE) / KS; ++r) probability(r);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    x.l_run += sum[0] + sum[1];
+    bf16x8 p[2];
+    round_p(s, p);
+    float m = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < PV; ++i) {
+      x.o[i >> 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[i % VA], p[i & 1], x.o[i >> 1], 0, 0, 0);
+      if (i + VA < PV) vf[i % VA] = v_operand(vl, i + VA);
+      load(i);
+      if (i >= WAIT) {
+#pragma unroll
+        for (int r = (i - WAIT) * 8 / (PV - WAIT) * 2; r < (i + 1 - WAIT) * 8 / (PV - WAIT) * 2; r += 2) m = fmaxf(fmaxf(m, n[r]), n[r + 1]);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    s = n;
+    if (__any(m * qscale > x.m_ref + HEADROOM)) settle(x, halves_max(m) * qscale);
+  }
+};
+
+__device__ __forceinline__ u32 uniform(u32 v) { return __builtin_amdgcn_readfirstlane(v); }
+
+// Loads of a ring stage, K of a tile and V of the tile before it (whose probabilities are formed while the scores of the
+// next are), piece f of the two by wave f % NW, as direct-to-LDS loads (16 bytes of
+// each lane, written lane after lane; the order inside a piece is made by what each lane asks for).  Every stage has the
+// same number of loads, past the last tile too, so that waits can count them.
+template <typename T, int DH, int NW>
+struct Ring {
+  using TL = Tile<T, DH>;
+  static constexpr int PIECES = TL::PIECES;                  // of one operand
+  static constexpr int LOADS = 2 * PIECES / NW;              // of one wave and stage
+  static constexpr int STAGE = 2 * TL::BYTES;
+  static constexpr int FIT = 128 * 1024 / STAGE;
+  static constexpr int MOST = 2 + 63 / LOADS;                // the loads of all stages but two are counted in six bits
+  static constexpr int NS = FIT < MOST ? (FIT < 8 ? FIT : 8) : (MOST < 8 ? MOST : 8);  // stages
+  static_assert(PIECES % NW == 0 && NS >= 2 && (NS - 2) * LOADS < 64, "ring shape");
+  // Buffer resource over the valid rows: what lies past row n - 1 is read as zero.
+  static __device__ __forceinline__ u32x4 rows(const char* p, u32 stride, int n) {
+    const u32 bytes = n > 0 ? (n - 1) * stride + DH * (u32)sizeof(T) : 0;
+    return u32x4{uniform((u32)(uintptr_t)p), uniform((u32)((uintptr_t)p >> 32) & 0xffffu), uniform(bytes), 0x00020000u};
+  }
+  // 16 bytes per lane to LDS at `to` + 16 * lane.  Written as assembly, which has no register outputs, because the compiler
+  // makes the transposed LDS reads wait for every direct-to-LDS load that it knows of, the later stages' too.
+  static __device__ __forceinline__ void load(u32x4 rsrc, u32 offset, u32 to) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(uniform(to)), "v"(offset), "s"(rsrc) : "memory", "m0");
+  }
+  // What the loads of one stage share, and load u of them.  Load u fills piece w + NW u: its rows are one of ROWS groups
+  // of eight, its chunks 128 bytes further on with each piece of the same rows.
+  static constexpr int ROWS = NW < 4 ? 4 / NW : 1;
+  struct Issue {
+    u32x4 k, v;
+    u32 at_k[ROWS], at_v[ROWS];  // byte of the lane's chunk from the tile's first row on
+    u32 to;                      // LDS address of the wave's first piece
+  };
+  static __device__ __forceinline__ Issue prepare(u32 stage, const char* kb, u32 kr, int kn, const char* vb, u32 vr, int vn) {
+    int lane = threadIdx.x & 63;
+    const int w = uniform(threadIdx.x >> 6);
+    asm volatile("" : "+v"(lane));  // the lane's offsets are formed anew for each stage: kept, they cost spills
+    Issue x;
+    x.k = rows(kb, kr, kn), x.v = rows(vb, vr, vn);
+    x.to = uniform(stage + w * 1024);
+    u32 k0 = TL::row(lane) * kr + (w >> 2) * 128, v0 = TL::row(lane) * vr + TL::col_v(lane) * 16 + (w >> 2) * 128;
+    asm volatile("" : "+v"(k0), "+v"(v0));
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+      const int g = (w + NW * i) & 3;
+      x.at_k[i] = k0 + TL::col(g, lane) * 16 + 8 * g * kr;
+      x.at_v[i] = v0 + 8 * g * vr;
+    }
+    return x;
+  }
+  static __device__ __forceinline__ void forward(u32x4& rsrc, u32 by) {
+    const uint64_t p = ((uint64_t)rsrc[1] << 32 | rsrc[0]) + by;
+    rsrc[0] = (u32)p, rsrc[1] = (u32)(p >> 32);
+  }
+  static __device__ __forceinline__ void one(const Issue& x, int u) {
+    // with half of the loads each for K and V, whether load u is one of K does not depend on the wave
+    const bool is_k = u < LOADS / 2;
+    const int i = is_k ? u : u - LOADS / 2;
+    const u32 off = (NW > 4 ? i * (NW / 4) : i / ROWS) * 128;
+    load(is_k ? x.k : x.v, (is_k ? x.at_k[i % ROWS] : x.at_v[i % ROWS]) + off, x.to + u * NW * 1024);
+  }
+};
+
+// A place in a row tile's key sequence: the prefix's tiles, then those of the rollouts' tails one after another.
+// Kept such that a step inside a prefix or tail is a few scalar additions.
+struct Walk {
+  int seg;  // rollout of the row tile whose tail this is (-1: prefix)
+  int n;    // valid keys from the tile's first on; <= 0: past the end
+};
+struct Source {
+  Walk at;
+  int tile;       // its number in the sequence
+  const char* p;  // its first row of K or V
+  u32 stride;     // bytes from row to row
+};
+
+template <typename T, int DH, int NW>
+__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(NW == 8 ? 2 : 1))) void k_shared(SharedLaunch l) {
+  using TL = Tile<T, DH>;
+  using RG = Ring<T, DH, NW>;
+  using ST = Steps<T, DH>;
+  constexpr int ROWS = 32 * NW, NS = RG::NS;
+  __shared__ __attribute__((aligned(1024))) char lds[NS * RG::STAGE + 4 * (2 * ROWS + 1 + NW + 9)];
+  int* const cum = reinterpret_cast<int*>(lds + NS * RG::STAGE);  // tail tiles of the rollouts of this row tile, summed up
+  int* const wave_sum = cum + ROWS + 1;
+  u32* const kinds = reinterpret_cast<u32*>(wave_sum + NW);  // of this tile and the two next (take_out)
+  int* const lens = wave_sum + NW + 9;                       // of those tails
 
   // items (group, KV head, range, row tile): row tiles of one range are neighbours, and neighbours share an XCD's L2
   const int item = (int)(blockIdx.x % 8) * (int)(gridDim.x / 8) + (int)(blockIdx.x / 8);
@@ -219,109 +444,244 @@ __global__ __launch_bounds__(64 * NW) void k_shared(SharedLaunch l) {
   const int g = gk / l.n_kv, kv = gk - g * l.n_kv;
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, half = lane >> 5;
   const int n_rows = l.group * l.q_rows * l.per_kv, r0 = rt * ROWS;
-  const Row me = row_of(l, g, kv, r0 + w * 32 + (lane & 31));
 
-  typename TL::chunk q[TL::KS];
-  {
-    const char* p = l.q.data + max(me.b, 0) * l.q.outer + me.i * l.q.row + me.h * l.q.head;
-#pragma unroll
-    for (int k = 0; k < TL::KS; ++k) {
-      if (me.b >= 0) q[k] = *reinterpret_cast<const typename TL::chunk*>(p + (2 * k + half) * 16);
-      else
-#pragma unroll
-        for (int e = 0; e < TL::CE; ++e) q[k][e] = (T)0.f;
-    }
-  }
-
-  // the key sequence: prefix tiles, then the tiles of each rollout's tail
-  const int plen = clamp_len(l.plen, g, l.prefix), np = (plen + KEYS - 1) / KEYS;
+  // lengths and queries are asked for together
   const int b0 = g * l.group + r0 / (l.q_rows * l.per_kv);
   const int nb = l.suffix ? g * l.group + (min(r0 + ROWS, n_rows) - 1) / (l.q_rows * l.per_kv) - b0 + 1 : 0;
-  if (tid == 0) cum[0] = 0;
-  for (int t = tid; t < nb; t += 64 * NW) cum[t + 1] = (clamp_len(l.slen, b0 + t, l.suffix) + KEYS - 1) / KEYS;
-  __syncthreads();
-  if (tid == 0)
-    for (int t = 0; t < nb; ++t) cum[t + 1] += cum[t];
-  __syncthreads();
-  const int total = np + cum[nb];
+  const int prefix_len = clamp_len(l.plen, g, l.prefix);
+  const int some_len = tid < nb ? clamp_len(l.slen, b0 + tid, l.suffix) : 0;
+  typename TL::chunk q[TL::KS];
+  {
+    const Row any = row_of(l, g, kv, min(r0 + w * 32 + (lane & 31), n_rows - 1));  // rows past the last one repeat it
+    const char* p = l.q.data + any.b * l.q.outer + any.i * l.q.row + any.h * l.q.head + half * 16;
+#pragma unroll
+    for (int k = 0; k < TL::KS; ++k) q[k] = *reinterpret_cast<const typename TL::chunk*>(p + k * 32);
+  }
+
+  // the key sequence
+  const int plen = uniform(prefix_len), np = (plen + KEYS - 1) / KEYS;
+  if (l.suffix) {
+    int c = (some_len + KEYS - 1) / KEYS;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+      const int x = __shfl_up(c, d, 64);
+      c += lane >= d ? x : 0;
+    }
+    if (lane == 63) wave_sum[w] = c;
+    __syncthreads();
+    for (int v = 0; v < w; ++v) c += wave_sum[v];
+    if (tid < nb) cum[tid + 1] = c, lens[tid] = some_len;
+    if (tid == 0) cum[0] = 0;
+    if (tid < 9) kinds[tid] = 0;
+    __syncthreads();
+  }
+  const int total = np + (l.suffix ? __builtin_amdgcn_readfirstlane(cum[nb]) : 0);
   const int t0 = (int)((int64_t)split * total / l.splits), t1 = (int)((int64_t)(split + 1) * total / l.splits);
 
-  f32x16 o[TL::NT];
+  typename ST::State x;
 #pragma unroll
   for (int t = 0; t < TL::NT; ++t)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) o[t][r] = 0.f;
-  float m_ref = -INFINITY, l_run = 0.f;
-  const int own_len = me.b >= 0 && l.suffix ? clamp_len(l.slen, me.b, l.suffix) : 0;
-  const int own_lim = l.causal ? min(own_len, own_len - l.q_rows + me.i + 1) : own_len;
+    for (int r = 0; r < 16; ++r) x.o[t][r] = 0.f;
+  x.m_ref = -INFINITY, x.l_run = 0.f;
+  float taint = 0.f;
+  int own_b, own_lim = 0;  // the lane's rollout, and how many keys of its tail its row sees, less the tail's length
+  {
+    const Row me = row_of(l, g, kv, r0 + w * 32 + (lane & 31));
+    own_b = me.b;
+    if (me.b >= 0 && l.causal) own_lim = min(0, me.i + 1 - l.q_rows);
+  }
 
-  int seg = 0;  // rollout of the current tail tile
-  for (int t = t0; t < t1; ++t) {
-    const char *kb, *vb;
-    int64_t kr, vr;
-    int n, lim;
-    bool mixed = false, mine = true;
-    if (t < np) {
-      const int j = t * KEYS;
-      kr = l.kp.row, vr = l.vp.row;
-      kb = l.kp.data + g * l.kp.outer + kv * l.kp.head + j * kr;
-      vb = l.vp.data + g * l.vp.outer + kv * l.vp.head + j * vr;
-      lim = n = min(KEYS, plen - j);
-    } else {
-      while (t - np >= cum[seg + 1]) ++seg;
-      const int j = (t - np - cum[seg]) * KEYS, b = b0 + seg;
-      kr = l.ks.row, vr = l.vs.row;
-      kb = l.ks.data + b * l.ks.outer + kv * l.ks.head + j * kr;
-      vb = l.vs.data + b * l.vs.outer + kv * l.vs.head + j * vr;
-      n = min(KEYS, clamp_len(l.slen, b, l.suffix) - j);
-      mine = me.b == b;
-      mixed = !__all(mine);
-      lim = mine ? own_lim - j : 0;
+  auto tail_len = [&](int seg) { return (int)uniform(lens[seg]); };
+  auto seek = [&](int t) {  // tile t
+    if (t < np) return Walk{-1, plen - t * KEYS};
+    int lo = 0, hi = nb;  // the tail with cum[lo] <= t - np < cum[lo + 1]
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) / 2;
+      if ((int)uniform(cum[mid]) <= t - np) lo = mid;
+      else hi = mid;
     }
-    __syncthreads();
-    for (int c = tid; c < KEYS * TL::CPR; c += 64 * NW) {
-      const int r = c / TL::CPR, cc = c - r * TL::CPR;
-      u32x4 x = {0, 0, 0, 0}, y = {0, 0, 0, 0};
-      if (r < n) {
-        x = *reinterpret_cast<const u32x4*>(kb + r * kr + cc * 16);
-        y = *reinterpret_cast<const u32x4*>(vb + r * vr + cc * 16);
+    return Walk{lo, tail_len(lo) - (t - np - (int)uniform(cum[lo])) * KEYS};
+  };
+  auto step = [&](Walk& y) __attribute__((always_inline)) {  // one tile on; true: into another tail
+    y.n -= KEYS;
+    if (y.n > 0) return false;
+    while (y.n <= 0 && y.seg + 1 < nb) y.n = tail_len(++y.seg);
+    return true;
+  };
+  auto open = [&](Source& y, bool keys) __attribute__((always_inline)) {  // where its tile lies
+    const bool tail = y.at.seg >= 0;
+    const View& v = keys ? (tail ? l.ks : l.kp) : (tail ? l.vs : l.vp);
+    const int64_t o_at = tail ? b0 + y.at.seg : g, j = (tail ? tail_len(y.at.seg) : plen) - y.at.n;
+    y.p = v.data + o_at * v.outer + kv * v.head + j * v.row;
+    y.stride = (u32)v.row;
+  };
+  auto advance = [&](Source& y, bool keys) __attribute__((always_inline)) {
+    if (++y.tile <= t0 || y.tile >= t1) return;
+    if (step(y.at)) open(y, keys);
+    else y.p += KEYS * y.stride;
+  };
+
+  wait_vm<0>();  // the queries are there: waited for in the loop, they would have it wait for the ring's loads too
+  if (t0 < t1) {
+    Walk cur = seek(t0);
+    Source ks{cur, t0}, vs{cur, t0 - 1};
+    open(ks, true);
+    open(vs, false);
+    auto prepare = [&](int stage) __attribute__((always_inline)) {  // K and V of nothing before the first tile and past the last one
+      const auto x = RG::prepare((u32)(uintptr_t)(dma_lds_t*)lds + stage * RG::STAGE, ks.p, ks.stride,
+                                 ks.tile < t1 ? min(ks.at.n, KEYS) : 0, vs.p, vs.stride,
+                                 vs.tile >= t0 && vs.tile < t1 ? min(vs.at.n, KEYS) : 0);
+      advance(ks, true);
+      advance(vs, false);
+      return x;
+    };
+    auto load = [&](int stage) __attribute__((always_inline)) {
+      const auto x = prepare(stage);
+#pragma unroll
+      for (int u = 0; u < RG::LOADS; ++u) RG::one(x, u);
+    };
+    for (int u = 0; u < NS - 1; ++u) load(u);
+    int stage = 0;
+    const bool partly = nb > 1 || l.causal;  // rows may not see all of a tail's tile
+    auto next_stage = [&](u32* here = nullptr) __attribute__((always_inline)) -> char* {
+      wait_vm<(NS - 2) * RG::LOADS>();
+      if (here) {
+        take_out<T, DH, NW>(lds + stage * RG::STAGE + TL::BYTES + tid * 16, here);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
       }
-      *reinterpret_cast<u32x4*>(kt + (r * TL::CPR + TL::place(r, cc)) * 16) = x;
-      *reinterpret_cast<u32x4*>(vt + (r * TL::CPR + TL::place_v(r, cc)) * 16) = y;
+      // every wave's loads of this stage have landed, and every wave is done with the stage before it, which is free
+      asm volatile("" ::: "memory");
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+      char* const at = lds + stage * RG::STAGE;
+      stage = stage == NS - 1 ? 0 : stage + 1;
+      return at;
+    };
+    auto freed = [&]() { return stage < 2 ? stage + NS - 2 : stage - 2; };  // the stage before the one just taken
+    auto limit = [&](const Walk& y) { return y.seg < 0 ? y.n : own_b == b0 + y.seg ? y.n + own_lim : 0; };
+
+    f32x16 s;
+    int lim = limit(cur);
+    bool have = __any(lim > 0);  // whether some row sees a key of the tile: its scores are in s
+    {
+      const char* const at = next_stage();
+      load(freed());
+      if (have) {
+        s = ST::scores(at, q);
+        x.m_ref = ST::mask_max(s, lim, l.qscale);
+      }
     }
-    __syncthreads();
-    if (__any(lim > 0)) tile_step<T, DH>(kt, vt, q, o, m_ref, l_run, l.qscale, lim, mixed, mine);
+    int t = t0;
+    if constexpr (ST::HALF) {
+      // full tiles of the prefix
+      const int full = min(plen / KEYS, t1), start = t;
+      if (t + 1 < full && ks.tile < full) {  // so are the tiles loaded next: their loads differ by a step of the addresses
+        auto is = RG::prepare(0, ks.p, ks.stride, KEYS, vs.p, vs.stride, KEYS);
+        const u32 first = is.to, k_step = KEYS * ks.stride, v_step = KEYS * vs.stride;
+        const int run = full - ks.tile;  // t + run < full: a tile of K is loaded before its scores are wanted
+        for (int r = 0; r < run; ++r) {
+          const char* const at = next_stage();
+          is.to = first + freed() * RG::STAGE;
+          ST::both(x, at + TL::BYTES, at, q, s, l.qscale, [&](int i) __attribute__((always_inline)) {
+#pragma unroll
+            for (int u = i * RG::LOADS / (2 * TL::NT); u < (i + 1) * RG::LOADS / (2 * TL::NT); ++u) RG::one(is, u);
+          });
+          RG::forward(is.k, k_step);
+          RG::forward(is.v, v_step);
+        }
+        t += run;
+        ks.p += (int64_t)run * k_step, vs.p += (int64_t)run * v_step;
+        ks.at.n -= run * KEYS, vs.at.n -= run * KEYS;
+        ks.tile += run, vs.tile += run;
+        if (ks.at.n <= 0 && ks.tile < t1) {  // the prefix ended with a full tile
+          ks.at.n += KEYS;
+          step(ks.at);
+          open(ks, true);
+        }
+      }
+      for (; t + 1 < full; ++t) {
+        const char* const at = next_stage();
+        const auto is = prepare(freed());
+        ST::both(x, at + TL::BYTES, at, q, s, l.qscale, [&](int i) __attribute__((always_inline)) {
+#pragma unroll
+          for (int u = i * RG::LOADS / (2 * TL::NT); u < (i + 1) * RG::LOADS / (2 * TL::NT); ++u) RG::one(is, u);
+        });
+      }
+      cur.n -= (t - start) * KEYS;
+      lim = limit(cur);
+    }
+    for (; t < t1; ++t) {
+      const bool check = cur.seg >= 0 && partly;
+      u32* const here = kinds + 3 * (t % 3);
+      const char* const at = next_stage(check ? here : nullptr);
+      load(freed());
+      if (check) {
+        if (here[0] | here[1] | here[2]) taint += taint_of(here, lim);
+        // read last before this tile's barrier, noted in first after the next one's
+        if (tid < 3) kinds[3 * ((t + 2) % 3) + tid] = 0;
+      }
+      if (have) ST::weigh(x, at + TL::BYTES, s, l.qscale);
+      if (t + 1 < t1) {
+        step(cur);
+        lim = limit(cur);
+        have = __any(lim > 0);
+        if (have) {
+          s = ST::scores(at, q);
+          ST::settle(x, ST::mask_max(s, lim, l.qscale));
+        }
+      }
+    }
+    wait_vm<0>();  // no load is in flight into LDS when the workgroup ends
   }
 
-  l_run = halves_sum(l_run);
-  if (me.b < 0) return;
+  // The rows leave through the ring's memory, 32 x DH fp32 of each wave, so that stores are whole rows: chunk c (4 dims)
+  // of row r at c ^ r % 16.  With several ranges that is the sum of p v, else the output.
+  const float l_run = halves_sum(x.l_run);
+  const Row me = row_of(l, g, kv, r0 + w * 32 + (lane & 31));
   const int64_t row = ((int64_t)me.b * l.q_rows + me.i) * l.n_heads + me.h;
-  const float ref = m_ref == -INFINITY ? 0.f : m_ref;
-  if (l.part) {
-    const int64_t at = (int64_t)split * l.n_groups * l.group * l.q_rows * l.n_heads + row;
-    if (half == 0) l.stats[at] = l_run == 0.f ? float2{-INFINITY, 0.f} : float2{ref, l_run};
-    if (l_run == 0.f) return;
-#pragma unroll
-    for (int t = 0; t < TL::NT; ++t)
-#pragma unroll
-      for (int k = 0; k < 4; ++k)
-        *reinterpret_cast<f32x4*>(l.part + at * DH + 32 * t + 8 * k + 4 * half) =
-            f32x4{o[t][4 * k], o[t][4 * k + 1], o[t][4 * k + 2], o[t][4 * k + 3]};
-    return;
+  const int64_t at = (int64_t)split * l.n_groups * l.group * l.q_rows * l.n_heads + row;
+  const float ref = x.m_ref == -INFINITY ? 0.f : x.m_ref;
+  const float inv = l.part ? 1.f : l_run == 0.f ? 0.f : 1.f / l_run;
+  if (half == 0 && me.b >= 0) {
+    if (l.part) l.stats[at] = l_run == 0.f ? float2{-INFINITY, 0.f} : float2{ref, l_run};
+    else if (l.lse) l.lse[row] = l_run == 0.f ? -INFINITY : (ref + log2f(l_run)) * LN2;
   }
-  if (half == 0 && l.lse) l.lse[row] = l_run == 0.f ? -INFINITY : (ref + log2f(l_run)) * LN2;
-  const float inv = l_run == 0.f ? 0.f : 1.f / l_run;
-  T* out = reinterpret_cast<T*>(const_cast<char*>(l.out.data) + me.b * l.out.outer + me.i * l.out.row + me.h * l.out.head);
-  typedef T quad __attribute__((ext_vector_type(4)));
+  static_assert(NS * RG::STAGE >= NW * 32 * DH * 4, "room for the rows");
+  constexpr int CH = DH / 4;  // chunks of a row
+  __syncthreads();
+  f32x4* const mine = reinterpret_cast<f32x4*>(lds + w * 32 * DH * 4);
 #pragma unroll
   for (int t = 0; t < TL::NT; ++t)
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      quad x;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) x[e] = from_f32<T>(o[t][4 * k + e] * inv);
-      *reinterpret_cast<quad*>(out + 32 * t + 8 * k + 4 * half) = x;
+      const f32x4 y = {x.o[t][4 * k], x.o[t][4 * k + 1], x.o[t][4 * k + 2], x.o[t][4 * k + 3]};
+      const int r = lane & 31;
+      mine[r * CH + ((8 * t + 2 * k + half) ^ (r & 15))] = y * inv + taint;
     }
+  typedef T quad __attribute__((ext_vector_type(4)));
+  int64_t base = l.part ? (int64_t)(uintptr_t)(l.part + at * DH)
+                        : (int64_t)(uintptr_t)l.out.data + me.b * l.out.outer + me.i * l.out.row + me.h * l.out.head;
+  if (me.b < 0) base = 0;
+  constexpr int RW = 64 / CH;       // rows of one store
+  const int c = lane % CH, sub = lane / CH;
+  auto leave = [&](auto part) __attribute__((always_inline)) {
+#pragma unroll 8
+    for (int r = 0; r < 32; r += RW) {
+      const f32x4 y = mine[(r + sub) * CH + (c ^ ((r + sub) & 15))];
+      int64_t to = 0;
+#pragma unroll
+      for (int j = 0; j < RW; ++j) {
+        const u32 lo = __builtin_amdgcn_readlane((u32)base, r + j), hi = __builtin_amdgcn_readlane((u32)((uint64_t)base >> 32), r + j);
+        if (sub == j) to = (int64_t)((uint64_t)hi << 32 | lo);
+      }
+      if (to == 0) continue;
+      if constexpr (decltype(part)::value) *reinterpret_cast<f32x4*>(to + c * 16) = y;
+      else *reinterpret_cast<quad*>(to + c * 4 * sizeof(T)) = quad{from_f32<T>(y[0]), from_f32<T>(y[1]), from_f32<T>(y[2]), from_f32<T>(y[3])};
+    }
+  };
+  if (l.part) leave(std::true_type{});
+  else leave(std::false_type{});
 }
 
 // Join of a row's ranges, one wave per row: the ranges' sums brought to their largest reference.
@@ -334,18 +694,25 @@ __global__ __launch_bounds__(256) void k_shared_merge(SharedLaunch l) {
   const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
   if (row >= rows) return;
   const int lane = threadIdx.x & 63;
-  float m = -INFINITY;
-  for (int s = 0; s < l.splits; ++s) m = fmaxf(m, l.stats[s * rows + row].x);
-  float sum = 0.f;
+  const float2 st = lane < l.splits ? l.stats[lane * rows + row] : float2{-INFINITY, 0.f};  // at most 64 ranges
+  const float m = wave_max(st.x);
+  const float f = st.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(st.x - m);
+  const float sum = wave_sum(st.x == -INFINITY ? 0.f : st.y * f);
+  const unsigned long long there = __ballot(st.x != -INFINITY);  // a range without a visible key wrote nothing
   vec o;
 #pragma unroll
   for (int e = 0; e < N; ++e) o[e] = 0.f;
-  for (int s = 0; s < l.splits; ++s) {
-    const float2 st = l.stats[s * rows + row];
-    if (st.x == -INFINITY) continue;  // a range without a visible key wrote nothing
-    const float f = __builtin_amdgcn_exp2f(st.x - m);
-    sum += st.y * f;
-    o += f * *reinterpret_cast<const vec*>(l.part + (s * rows + row) * DH + lane * N);
+  constexpr int U = 8;
+  for (int s = 0; s < l.splits; s += U) {
+    vec v[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (there >> (s + u < 64 ? s + u : 63) & 1 && s + u < l.splits)
+        v[u] = *reinterpret_cast<const vec*>(l.part + ((s + u) * rows + row) * DH + lane * N);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (there >> (s + u < 64 ? s + u : 63) & 1 && s + u < l.splits)
+        o += __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, f), s + u)) * v[u];
   }
   const float inv = m == -INFINITY ? 0.f : 1.f / sum;
   const int h = (int)(row % l.n_heads);
@@ -396,13 +763,13 @@ __global__ __launch_bounds__(64 * NW) void k_weight(WeightLaunch l) {
   float sum = 0.f;
   for (int t = t0; t < t1; ++t) {
     __syncthreads();
-    for (int c = tid; c < KEYS * TL::CPR; c += 64 * NW) {
-      const int r = c / TL::CPR, cc = c - r * TL::CPR;
-      const Row x = row_of(a, g, kv, t * KEYS + r);
+    for (int c = tid; c < TL::PIECES * 64; c += 64 * NW) {
+      const Row x = row_of(a, g, kv, t * KEYS + 8 * (c / 64 % 4) + TL::row(c % 64));
       u32x4 v = {0, 0, 0, 0};
       if (x.b >= 0)
-        v = *reinterpret_cast<const u32x4*>(a.q.data + x.b * a.q.outer + x.i * a.q.row + x.h * a.q.head + cc * 16);
-      *reinterpret_cast<u32x4*>(lds + (r * TL::CPR + TL::place(r, cc)) * 16) = v;
+        v = *reinterpret_cast<const u32x4*>(a.q.data + x.b * a.q.outer + x.i * a.q.row + x.h * a.q.head +
+                                             (8 * (c / 256) + TL::col(c / 64, c % 64)) * 16);
+      *reinterpret_cast<u32x4*>(lds + c * 16) = v;
     }
     if (tid < KEYS) {
       const Row x = row_of(a, g, kv, t * KEYS + tid);
@@ -415,8 +782,7 @@ __global__ __launch_bounds__(64 * NW) void k_weight(WeightLaunch l) {
     for (int r = 0; r < 16; ++r) s[r] = 0.f;
 #pragma unroll
     for (int k = 0; k < TL::KS; ++k) {
-      const auto x = *reinterpret_cast<const typename TL::chunk*>(lds + (col * TL::CPR + TL::place(col, 2 * k + half)) * 16);
-      s = mfma_chunk<T>(x, key[k], s);
+      s = mfma_chunk<T>(*reinterpret_cast<const typename TL::chunk*>(lds + TL::base(lane, k & 3) + TL::step(k)), key[k], s);
     }
 #pragma unroll
     for (int r = 0; r < 16; ++r)
@@ -476,15 +842,32 @@ struct Plan {
   int waves, row_tiles, splits;
 };
 
+// Waves (32 rows each) of a workgroup and ranges of the key sequence, by estimated time.  A workgroup of most shapes fills
+// a compute unit's LDS, so workgroups beyond one per unit wait for another round.  Microseconds measured on 256 units:
+// a tile takes about 0.003 per element of a row in bf16 (0.75 at 256, 0.45 at 128) and 0.027 in fp32, the rest of a
+// workgroup 12; joining ranges takes a launch, 5, and writing and reading their sums, 3 bytes a picosecond.
 Plan shared_plan(const jpi_shared_attn& a) {
+  const double n_cu = 256;
   const int64_t rows = (int64_t)a.group * a.q_rows * (a.n_heads / a.n_kv_heads);
-  Plan p;
-  p.waves = rows <= 32 ? 1 : rows <= 64 ? 2 : 4;
-  p.row_tiles = (int)((rows + 32 * p.waves - 1) / (32 * p.waves));
-  const int64_t items = (int64_t)a.n_groups * a.n_kv_heads * p.row_tiles;
   const int64_t tiles = (a.prefix + KEYS - 1) / KEYS + (a.suffix + KEYS - 1) / KEYS;
-  p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({64, 512 / items, (tiles + 1) / 2}));
-  return p;
+  const double all = (double)a.n_groups * a.group * a.q_rows * a.n_heads;
+  const double tile_us = 0.1 + (a.dtype == JPI_BF16 ? 0.0026 : 0.027) * a.head_dim;
+  // eight waves share a unit's matrix cores two by two; their rings hold two of the pieces of a tile of 64 bf16 elements
+  const int most = a.head_dim == 256 || (a.dtype == JPI_BF16 && a.head_dim == 64) ? 4 : 8;
+  Plan best{};
+  double best_us = 1e30;
+  for (int w = 1; w <= most; w *= 2) {
+    if (w > 1 && 32 * (w / 2) >= rows) break;
+    const int64_t row_tiles = (rows + 32 * w - 1) / (32 * w), items = (int64_t)a.n_groups * a.n_kv_heads * row_tiles;
+    for (const int s : {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 48, 64}) {
+      if (s > 1 && s > tiles) break;
+      const double rounds = ceil(items * s / n_cu);
+      const double us = rounds * (((tiles + s - 1) / s) * tile_us * (w == 8 ? 1.5 : 1.0) + 12) +
+                        (s > 1 ? 5 + all * s * a.head_dim * 8 / 3e6 : 0);
+      if (us < best_us) best_us = us, best = Plan{w, (int)row_tiles, s};
+    }
+  }
+  return best;
 }
 
 Plan weight_plan(const jpi_shared_attn& a) {
@@ -514,7 +897,10 @@ hipError_t shared_typed(const jpi_shared_attn& a, void* ws, hipStream_t s) {
   switch (p.waves) {
     case 1: k_shared<T, DH, 1><<<grid, 64, 0, s>>>(l); break;
     case 2: k_shared<T, DH, 2><<<grid, 128, 0, s>>>(l); break;
-    default: k_shared<T, DH, 4><<<grid, 256, 0, s>>>(l); break;
+    case 4: k_shared<T, DH, 4><<<grid, 256, 0, s>>>(l); break;
+    default:
+      if constexpr (Tile<T, DH>::PIECES % 8 == 0 && DH < 256) k_shared<T, DH, 8><<<grid, 512, 0, s>>>(l);
+      break;
   }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.splits == 1) return e;
