@@ -187,13 +187,13 @@ _sig = {
     "jpi_corr_predict": (_i, [_vp, _vp, _vp, _i, _i, _vp, _vp, _vp]),
     "jpi_corr_last_error": (ctypes.c_char_p, [_vp]),
     "jpi_prefix_last_error": (ctypes.c_char_p, []),
-    "jpi_rope": (_i, [ctypes.POINTER(jpi_rope_config), _i, _i, _i, _vp, _i64, ctypes.POINTER(jpi_view),
-                      ctypes.POINTER(jpi_view), _i, ctypes.POINTER(jpi_view), ctypes.POINTER(jpi_view), _i, _vp]),
-    "jpi_shared_attention_workspace": (_i, [ctypes.POINTER(jpi_shared_attn), ctypes.POINTER(ctypes.c_size_t)]),
-    "jpi_prefix_weight_workspace": (_i, [ctypes.POINTER(jpi_shared_attn), ctypes.POINTER(ctypes.c_size_t)]),
-    "jpi_shared_attention": (_i, [ctypes.POINTER(jpi_shared_attn), _vp, ctypes.c_size_t, _vp]),
-    "jpi_prefix_weight": (_i, [ctypes.POINTER(jpi_shared_attn), _vp, _f, _vp, _vp, ctypes.c_size_t, _vp]),
-    "jpi_evict": (_i, [ctypes.POINTER(jpi_evict_args), _vp]),
+    # structures as addresses: ctypes.byref of one, or its bytes
+    "jpi_rope": (_i, [_vp, _i, _i, _i, _vp, _i64, _vp, _vp, _i, _vp, _vp, _i, _vp]),
+    "jpi_shared_attention_workspace": (_i, [_vp, _vp]),
+    "jpi_prefix_weight_workspace": (_i, [_vp, _vp]),
+    "jpi_shared_attention": (_i, [_vp, _vp, ctypes.c_size_t, _vp]),
+    "jpi_prefix_weight": (_i, [_vp, _vp, _f, _vp, _vp, ctypes.c_size_t, _vp]),
+    "jpi_evict": (_i, [_vp, _vp]),
 }
 for _name, (_res, _args) in _sig.items():
     _fn = getattr(_lib, _name)
@@ -429,37 +429,41 @@ def jpi_prefix_last_error() -> str:
     return (_lib.jpi_prefix_last_error() or b"").decode()
 
 
-def jpi_rope(cfg, dtype: int, batch: int, tokens: int, positions, pos_stride: int, q, q_out, q_heads: int, k=None, k_out=None,
-             k_heads: int = 0, stream=None) -> int:
-    """cfg a jpi_rope_config; q, q_out, k, k_out jpi_view structures (or references to them)."""
-    return _lib.jpi_rope(cfg, dtype, batch, tokens, addr(positions), pos_stride, q, q_out, q_heads, k, k_out, k_heads,
-                         stream_handle(stream))
+def _ref(x):
+    """Address of a ctypes structure for a call (None: NULL)."""
+    return None if x is None else ctypes.byref(x)
+
+
+def jpi_rope(cfg: jpi_rope_config, dtype: int, batch: int, tokens: int, positions, pos_stride: int, q: jpi_view, q_out: jpi_view,
+             q_heads: int, k: jpi_view | None = None, k_out: jpi_view | None = None, k_heads: int = 0, stream=None) -> int:
+    return _lib.jpi_rope(_ref(cfg), dtype, batch, tokens, addr(positions), pos_stride, _ref(q), _ref(q_out), q_heads, _ref(k),
+                         _ref(k_out), k_heads, stream_handle(stream))
 
 
 def jpi_shared_attention_workspace(args: jpi_shared_attn):
     n = ctypes.c_size_t()
-    st = _lib.jpi_shared_attention_workspace(args, n)
+    st = _lib.jpi_shared_attention_workspace(_ref(args), ctypes.byref(n))
     return st, n.value
 
 
 def jpi_prefix_weight_workspace(args: jpi_shared_attn):
     n = ctypes.c_size_t()
-    st = _lib.jpi_prefix_weight_workspace(args, n)
+    st = _lib.jpi_prefix_weight_workspace(_ref(args), ctypes.byref(n))
     return st, n.value
 
 
 def jpi_shared_attention(args: jpi_shared_attn, workspace=None, workspace_bytes: int = 0, stream=None) -> int:
-    return _lib.jpi_shared_attention(args, addr(workspace), workspace_bytes, stream_handle(stream))
+    return _lib.jpi_shared_attention(_ref(args), addr(workspace), workspace_bytes, stream_handle(stream))
 
 
 def jpi_prefix_weight(args: jpi_shared_attn, weight_in, decay: float, weight_out, workspace=None, workspace_bytes: int = 0,
                       stream=None) -> int:
-    return _lib.jpi_prefix_weight(args, addr(weight_in), decay, addr(weight_out), addr(workspace), workspace_bytes,
+    return _lib.jpi_prefix_weight(_ref(args), addr(weight_in), decay, addr(weight_out), addr(workspace), workspace_bytes,
                                   stream_handle(stream))
 
 
 def jpi_evict(args: jpi_evict_args, stream=None) -> int:
-    return _lib.jpi_evict(args, stream_handle(stream))
+    return _lib.jpi_evict(_ref(args), stream_handle(stream))
 
 
 class JpiError(RuntimeError):

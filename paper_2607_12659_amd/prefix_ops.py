@@ -12,6 +12,7 @@ raised as ``jpi.JpiError`` (the library's checks), ``ValueError`` or
 from __future__ import annotations
 
 import ctypes
+import struct
 
 import torch
 
@@ -20,6 +21,19 @@ from . import jpi as _j
 _LAYOUT = {"half": _j.JPI_ROPE_HALF, "interleaved": _j.JPI_ROPE_INTERLEAVED}
 _SCALING = {"none": _j.JPI_ROPE_PLAIN, "linear": _j.JPI_ROPE_LINEAR, "base": _j.JPI_ROPE_BASE, "parts": _j.JPI_ROPE_PARTS}
 _DTYPE = {torch.bfloat16: _j.JPI_BF16, torch.float32: _j.JPI_F32}
+_I32, _F32 = torch.int32, torch.float32
+_lib = _j._lib
+
+# The C structures as bytes, which cost a small call a third of what a ctypes structure filled field by field does
+_VIEW = "Pqqq"
+_ROPE = struct.Struct("@5i6d")
+_ROPE_VIEWS = struct.Struct("@" + _VIEW * 4)
+_ATTN = struct.Struct("@10if" + _VIEW * 5 + "PP" + _VIEW + "P")
+_EVICT = struct.Struct("@8iPqP" + _VIEW * 4 + "PqPP")
+assert (_ROPE.size, _ROPE_VIEWS.size, _ATTN.size, _EVICT.size) == (
+    ctypes.sizeof(_j.jpi_rope_config), 4 * ctypes.sizeof(_j.jpi_view), ctypes.sizeof(_j.jpi_shared_attn),
+    ctypes.sizeof(_j.jpi_evict_args))
+_NONE = (0, 0, 0, 0)
 
 
 def _check(status):
@@ -34,44 +48,45 @@ def _dtype(t):
     return dt
 
 
-def _want(name, t, shape, dtype, device):
-    """t has this shape, type and device; a size of None in `shape` fits any."""
-    if tuple(t.shape) != shape:
+def _want(name, t, shape, dtype, dev):
+    """t has this shape and type, and is on GPU number `dev`."""
+    if t.shape != shape:
         raise ValueError("%s must have shape %s, got %s" % (name, list(shape), list(t.shape)))
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         raise TypeError("%s must be %s, got %s" % (name, dtype, t.dtype))
-    if t.device != device:
-        raise ValueError("%s is on %s, other tensors on %s" % (name, t.device, device))
+    if t.get_device() != dev:
+        raise ValueError("%s is on %s, other tensors on GPU %d" % (name, t.device, dev) if dev >= 0 else
+                         "tensors must be on the GPU")
 
 
 def _view(name, t):
-    """[outer][row][head][head_dim]; strides of dimensions of size 1 do not count."""
+    """data, and the strides of [outer][row][head][head_dim]; those of dimensions of size 1 do not count."""
     n, s = t.shape, t.stride()
     if s[3] != 1 and n[3] != 1:
         raise ValueError("the elements of a head of %s must be contiguous" % name)
-    inner = n[3]
-    return _j.jpi_view(t.data_ptr() or None, s[0] if n[0] > 1 else inner, s[1] if n[1] > 1 else inner, s[2] if n[2] > 1 else inner)
+    return t.data_ptr(), s[0] if n[0] > 1 else 0, s[1] if n[1] > 1 else 0, s[2] if n[2] > 1 else 0
 
 
 def _dense(name, t):
     if not t.is_contiguous():
         raise ValueError("%s must be contiguous" % name)
-    return t.data_ptr() or None
+    return t.data_ptr()
 
 
 class _On:
-    """The tensors' device made current for a call, where it is not (None: nothing to do)."""
-    __slots__ = ("guard",)
+    """GPU `dev` made current for a call, where it is not; the handle of its current stream."""
+    __slots__ = ("dev", "guard")
 
-    def __init__(self, device):
-        if device.type != "cuda":
-            raise ValueError("tensors must be on the GPU, got %s" % device)
-        self.guard = None if device.index == torch.cuda.current_device() else torch.cuda.device(device)
+    def __init__(self, dev):
+        if dev < 0:
+            raise ValueError("tensors must be on the GPU")
+        self.dev = dev
+        self.guard = None if dev == torch.cuda.current_device() else torch.cuda.device(dev)
 
     def __enter__(self):
         if self.guard is not None:
             self.guard.__enter__()
-        return torch.cuda.current_stream().cuda_stream
+        return torch._C._cuda_getCurrentRawStream(self.dev)
 
     def __exit__(self, *e):
         if self.guard is not None:
@@ -88,65 +103,68 @@ def rope(q, k=None, positions=None, *, rot_dim=None, layout="half", base=1e4, sc
     if q.dim() != 4:
         raise ValueError("q must be [batch][tokens][heads][head_dim]")
     b, n, heads, dh = q.shape
-    dt, dev = _dtype(q), q.device
-    try:
-        cfg = _j.jpi_rope_config(dh, dh if rot_dim is None else rot_dim, _LAYOUT[layout], _SCALING[scaling], int(bool(inverse)),
-                                 base, factor, trained, beta_fast, beta_slow, amplitude)
-    except KeyError as e:
-        raise ValueError("unknown layout or scaling %s" % e) from None
+    dt, dev = _dtype(q), q.get_device()
+    if layout not in _LAYOUT or scaling not in _SCALING:
+        raise ValueError("unknown layout %r or scaling %r" % (layout, scaling))
+    cfg = _ROPE.pack(dh, dh if rot_dim is None else rot_dim, _LAYOUT[layout], _SCALING[scaling], int(bool(inverse)), base, factor,
+                     trained, beta_fast, beta_slow, amplitude)
+    if q_out is None:
+        q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
+    elif q_out is not q:
+        _want("q_out", q_out, q.shape, q.dtype, dev)
     if k is None:
-        kv = ko = None
-        k_heads = 0
+        kv = ko = _NONE
+        k_heads, k_out = 0, None
     else:
         k_heads = k.shape[2] if k.dim() == 4 else 0
         _want("k", k, (b, n, k_heads, dh), q.dtype, dev)
         if k_out is None:
             k_out = torch.empty_like(k, memory_format=torch.contiguous_format)
         elif k_out is not k:
-            _want("k_out", k_out, tuple(k.shape), q.dtype, dev)
-        kv, ko = ctypes.byref(_view("k", k)), ctypes.byref(_view("k_out", k_out))
-    if q_out is None:
-        q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
-    elif q_out is not q:
-        _want("q_out", q_out, tuple(q.shape), q.dtype, dev)
+            _want("k_out", k_out, k.shape, q.dtype, dev)
+        kv, ko = _view("k", k), _view("k_out", k_out)
     pos, pos_stride = None, 0
     if positions is not None:
         if positions.dim() == 2:
-            _want("positions", positions, (b, n), torch.int32, dev)
-            pos_stride = positions.stride(0)
+            _want("positions", positions, (b, n), _I32, dev)
+            pos_stride = positions.stride(0) if b > 1 else 0
         else:
-            _want("positions", positions, (n,), torch.int32, dev)
+            _want("positions", positions, (n,), _I32, dev)
         if n > 1 and positions.stride(-1) != 1:
             raise ValueError("positions of a batch row must be contiguous")
-        pos = positions.data_ptr() or None
-    qv, qo = ctypes.byref(_view("q", q)), ctypes.byref(_view("q_out", q_out))
+        pos = positions.data_ptr()
+    views = ctypes.create_string_buffer(_ROPE_VIEWS.pack(*_view("q", q), *_view("q_out", q_out), *kv, *ko), 128)
+    at = ctypes.addressof(views)
     with _On(dev) as stream:
-        _check(_j.jpi_rope(cfg, dt, b, n, pos, pos_stride, qv, qo, heads, kv, ko, k_heads, stream))
-    return q_out, k_out if k is not None else None
+        _check(_lib.jpi_rope(cfg, dt, b, n, pos, pos_stride, at, at + 32, heads, at + 64 if k_heads else None,
+                             at + 96 if k_heads else None, k_heads, stream))
+    return q_out, k_out
 
 
-def _attn_args(q, k_prefix, scale, prefix_len):
+def _shapes(q, k_prefix):
     if q.dim() != 4 or k_prefix.dim() != 4:
         raise ValueError("q and k_prefix must have four dimensions")
     b, rows, heads, dh = q.shape
     g, p, kv, _ = k_prefix.shape
-    _want("k_prefix", k_prefix, (g, p, kv, dh), q.dtype, q.device)
+    dev = q.get_device()
+    _want("k_prefix", k_prefix, (g, p, kv, dh), q.dtype, dev)
     if g < 1 or b < 1 or b % g:
         raise ValueError("the batch of %d must be a multiple of the %d prefixes" % (b, g))
-    a = _j.jpi_shared_attn(_dtype(q), g, b // g, rows, heads, kv, dh, p, 0, 0, dh ** -0.5 if scale is None else scale)
-    a.q = _view("q", q)
-    a.k_prefix = _view("k_prefix", k_prefix)
-    if prefix_len is not None:
-        _want("prefix_len", prefix_len, (g,), torch.int32, q.device)
-        a.prefix_len = _dense("prefix_len", prefix_len)
-    return a
+    return b, rows, heads, dh, g, p, kv, dev
 
 
-def _workspace(a, size_of, device):
-    need = size_of(a)
-    if not need:
-        return None, 0
-    return torch.empty(need, dtype=torch.uint8, device=device), need
+def _lens(name, t, n, dev):
+    if t is None:
+        return 0
+    _want(name, t, (n,), _I32, dev)
+    return _dense(name, t)
+
+
+def _workspace(size_of, args, dev):
+    n = ctypes.c_size_t()
+    _check(size_of(args, ctypes.byref(n)))
+    n = n.value
+    return (torch.empty(n, dtype=torch.uint8, device=dev), n) if n else (None, 0)
 
 
 def shared_attention(q, k_prefix, v_prefix, k_suffix=None, v_suffix=None, *, prefix_len=None, suffix_len=None, causal=False,
@@ -159,52 +177,36 @@ def shared_attention(q, k_prefix, v_prefix, k_suffix=None, v_suffix=None, *, pre
     prefix_len int32 [groups], suffix_len int32 [batch], None for all slots.  scale: head_dim^-1/2 unless given.
     Returns (out, lse): out like q, lse float32 [batch][rows][heads].
     """
-    a = _attn_args(q, k_prefix, scale, prefix_len)
-    b, rows, heads, dh = q.shape
-    dev = q.device
-    _want("v_prefix", v_prefix, tuple(k_prefix.shape), q.dtype, dev)
-    a.v_prefix = _view("v_prefix", v_prefix)
+    b, rows, heads, dh, g, p, kv, dev = _shapes(q, k_prefix)
+    dt = _dtype(q)
+    _want("v_prefix", v_prefix, k_prefix.shape, q.dtype, dev)
     if (k_suffix is None) != (v_suffix is None):
         raise ValueError("k_suffix and v_suffix go together")
-    if k_suffix is not None:
-        s = k_suffix.shape[1] if k_suffix.dim() == 4 else -1
-        shape = (b, s, a.n_kv_heads, dh)
-        _want("k_suffix", k_suffix, shape, q.dtype, dev)
-        _want("v_suffix", v_suffix, shape, q.dtype, dev)
-        a.suffix = s
-        a.k_suffix, a.v_suffix = _view("k_suffix", k_suffix), _view("v_suffix", v_suffix)
+    if k_suffix is None:
         if suffix_len is not None:
-            _want("suffix_len", suffix_len, (b,), torch.int32, dev)
-            a.suffix_len = _dense("suffix_len", suffix_len)
-    elif suffix_len is not None:
-        raise ValueError("suffix_len without k_suffix")
-    a.causal = int(bool(causal))
+            raise ValueError("suffix_len without k_suffix")
+        s, ks, vs = 0, _NONE, _NONE
+    else:
+        s = k_suffix.shape[1] if k_suffix.dim() == 4 else -1
+        _want("k_suffix", k_suffix, (b, s, kv, dh), q.dtype, dev)
+        _want("v_suffix", v_suffix, k_suffix.shape, q.dtype, dev)
+        ks, vs = _view("k_suffix", k_suffix), _view("v_suffix", v_suffix)
     if out is None:
-        out = torch.empty((b, rows, heads, dh), dtype=q.dtype, device=dev)
+        out = torch.empty((b, rows, heads, dh), dtype=q.dtype, device=q.device)
     else:
-        _want("out", out, (b, rows, heads, dh), q.dtype, dev)
-    a.out = _view("out", out)
+        _want("out", out, q.shape, q.dtype, dev)
     if lse is None:
-        lse = torch.empty((b, rows, heads), dtype=torch.float32, device=dev)
+        lse = torch.empty((b, rows, heads), dtype=_F32, device=q.device)
     else:
-        _want("lse", lse, (b, rows, heads), torch.float32, dev)
-    a.lse = _dense("lse", lse)
+        _want("lse", lse, (b, rows, heads), _F32, dev)
+    args = _ATTN.pack(dt, g, b // g, rows, heads, kv, dh, p, s, int(bool(causal)), dh ** -0.5 if scale is None else scale,
+                      *_view("q", q), *_view("k_prefix", k_prefix), *_view("v_prefix", v_prefix), *ks, *vs,
+                      _lens("prefix_len", prefix_len, g, dev), _lens("suffix_len", suffix_len, b, dev), *_view("out", out),
+                      _dense("lse", lse))
     with _On(dev) as stream:
-        ws, n = _workspace(a, _attention_bytes, dev)
-        _check(_j.jpi_shared_attention(a, ws, n, stream))
+        ws, n = _workspace(_lib.jpi_shared_attention_workspace, args, q.device)
+        _check(_lib.jpi_shared_attention(args, ws.data_ptr() if n else None, n, stream))
     return out, lse
-
-
-def _attention_bytes(a):
-    st, n = _j.jpi_shared_attention_workspace(a)
-    _check(st)
-    return n
-
-
-def _weight_bytes(a):
-    st, n = _j.jpi_prefix_weight_workspace(a)
-    _check(st)
-    return n
 
 
 def prefix_weight(q, k_prefix, lse, weight=None, *, prefix_len=None, decay=1.0, scale=None, out=None):
@@ -214,23 +216,35 @@ def prefix_weight(q, k_prefix, lse, weight=None, *, prefix_len=None, decay=1.0, 
     [groups][kv_heads][prefix] or None for zero.  out: None for a new tensor (slots past prefix_len are 0 in it), weight
     itself to accumulate in place.  Returns out.
     """
-    a = _attn_args(q, k_prefix, scale, prefix_len)
-    dev = q.device
-    shape = (a.n_groups, a.n_kv_heads, a.prefix)
-    _want("lse", lse, tuple(q.shape[:3]), torch.float32, dev)
-    a.lse = _dense("lse", lse)
+    b, rows, heads, dh, g, p, kv, dev = _shapes(q, k_prefix)
+    dt, shape = _dtype(q), (g, kv, p)
+    _want("lse", lse, (b, rows, heads), _F32, dev)
     w = None
     if weight is not None:
-        _want("weight", weight, shape, torch.float32, dev)
+        _want("weight", weight, shape, _F32, dev)
         w = _dense("weight", weight)
     if out is None:
-        out = torch.empty(shape, dtype=torch.float32, device=dev) if prefix_len is None else torch.zeros(shape, device=dev)
+        out = (torch.empty if prefix_len is None else torch.zeros)(shape, dtype=_F32, device=q.device)
     else:
-        _want("out", out, shape, torch.float32, dev)
+        _want("out", out, shape, _F32, dev)
+    args = _ATTN.pack(dt, g, b // g, rows, heads, kv, dh, p, 0, 0, dh ** -0.5 if scale is None else scale, *_view("q", q),
+                      *_view("k_prefix", k_prefix), *_NONE, *_NONE, *_NONE, _lens("prefix_len", prefix_len, g, dev), 0, *_NONE,
+                      _dense("lse", lse))
     with _On(dev) as stream:
-        ws, n = _workspace(a, _weight_bytes, dev)
-        _check(_j.jpi_prefix_weight(a, w, decay, _dense("out", out), ws, n, stream))
+        ws, n = _workspace(_lib.jpi_prefix_weight_workspace, args, q.device)
+        _check(_lib.jpi_prefix_weight(args, w, decay, _dense("out", out), ws.data_ptr() if n else None, n, stream))
     return out
+
+
+def _room(name, t, own, dtype, dim, most, dev):
+    """t, or `own` where it is None: like `own` but for dimension `dim`, which has room for `most`."""
+    if t is None or t is own:
+        return own
+    if t.dim() <= dim or t.shape[dim] < most:
+        raise ValueError("%s must have room for %d slots" % (name, most))
+    n = own.shape
+    _want(name, t, n[:dim] + t.shape[dim:dim + 1] + n[dim + 1:], dtype, dev)
+    return t
 
 
 def evict(k, v, weight, keep, *, lens=None, n_first=0, n_last=0, k_out=None, v_out=None, weight_out=None, index=None,
@@ -245,40 +259,24 @@ def evict(k, v, weight, keep, *, lens=None, n_first=0, n_last=0, k_out=None, v_o
     if k.dim() != 4:
         raise ValueError("k must be [outer][slots][heads][head_dim]")
     n, slots, heads, dh = k.shape
-    dev = k.device
-    _want("v", v, tuple(k.shape), k.dtype, dev)
-    _want("weight", weight, (n, heads, slots), torch.float32, dev)
+    dt, dev = _dtype(k), k.get_device()
+    _want("v", v, k.shape, k.dtype, dev)
+    _want("weight", weight, (n, heads, slots), _F32, dev)
     keep = int(keep)
     most = min(keep, slots)
-
-    def like(name, t, own, dtype, dim):
-        if t is None:
-            return own
-        if t is not own:
-            if t.dim() <= dim or t.shape[dim] < most:
-                raise ValueError("%s must have room for %d slots" % (name, most))
-            shape = list(own.shape)
-            shape[dim] = t.shape[dim]
-            _want(name, t, tuple(shape), dtype, dev)
-        return t
-
-    k_out, v_out = like("k_out", k_out, k, k.dtype, 1), like("v_out", v_out, v, k.dtype, 1)
-    weight_out = like("weight_out", weight_out, weight, torch.float32, 2)
+    k_out, v_out = _room("k_out", k_out, k, k.dtype, 1, most, dev), _room("v_out", v_out, v, k.dtype, 1, most, dev)
+    weight_out = _room("weight_out", weight_out, weight, _F32, 2, most, dev)
     if index is None:
-        index = torch.full((n, heads, max(keep, 0)), -1, dtype=torch.int32, device=dev)
+        index = torch.full((n, heads, max(keep, 0)), -1, dtype=_I32, device=k.device)
     else:
-        _want("index", index, (n, heads, keep), torch.int32, dev)
+        _want("index", index, (n, heads, keep), _I32, dev)
     if lens_out is None:
-        lens_out = torch.empty((n,), dtype=torch.int32, device=dev)
+        lens_out = torch.empty((n,), dtype=_I32, device=k.device)
     else:
-        _want("lens_out", lens_out, (n,), torch.int32, dev)
-    a = _j.jpi_evict_args(_dtype(k), n, heads, dh, slots, keep, n_first, n_last, _dense("weight", weight), slots)
-    if lens is not None:
-        _want("lens", lens, (n,), torch.int32, dev)
-        a.len = _dense("lens", lens)
-    a.k, a.v, a.k_out, a.v_out = _view("k", k), _view("v", v), _view("k_out", k_out), _view("v_out", v_out)
-    a.weight_out, a.weight_out_stride = _dense("weight_out", weight_out), weight_out.shape[2]
-    a.index, a.len_out = _dense("index", index), _dense("lens_out", lens_out)
+        _want("lens_out", lens_out, (n,), _I32, dev)
+    args = _EVICT.pack(dt, n, heads, dh, slots, keep, n_first, n_last, _dense("weight", weight), slots, _lens("lens", lens, n, dev),
+                       *_view("k", k), *_view("v", v), *_view("k_out", k_out), *_view("v_out", v_out),
+                       _dense("weight_out", weight_out), weight_out.shape[2], _dense("index", index), _dense("lens_out", lens_out))
     with _On(dev) as stream:
-        _check(_j.jpi_evict(a, stream))
+        _check(_lib.jpi_evict(args, stream))
     return index, lens_out
