@@ -189,7 +189,8 @@ typedef struct {
  * strides: the cache is compacted where it lies) or memory that overlaps no
  * input; K and V may not overlap each other.  Any alignment; 16-byte aligned
  * rows are fastest.  Errors: JPI_ERR_ARG (NULL, values out of the ranges above),
- * JPI_ERR_SHAPE (slots past 2^26, or n_outer * n_heads past 2^24), JPI_ERR_DTYPE, JPI_ERR_HIP. */
+ * JPI_ERR_SHAPE (more than 2^26 slots, 2^20 sequences n_outer * n_heads, or 2^40
+ * bytes of K), JPI_ERR_DTYPE, JPI_ERR_HIP. */
 jpi_status jpi_evict(const jpi_evict_args* a, void* stream);
 
 #ifdef __cplusplus

@@ -194,8 +194,9 @@ jpi_status jpi_evict(const jpi_evict_args* a, void* stream) {
     return fail(JPI_ERR_ARG, "%s: size out of range", call);
   if (a->n_first < 0 || a->n_last < 0 || (int64_t)a->n_first + a->n_last > a->keep)
     return fail(JPI_ERR_ARG, "%s: n_first + n_last must be 0 .. keep", call);
-  if (a->slots > 1 << 26 || (int64_t)a->n_outer * a->n_heads > 1 << 24)
-    return fail(JPI_ERR_SHAPE, "%s: more than 2^26 slots or 2^24 sequences", call);
+  if (a->slots > 1 << 26 || (int64_t)a->n_outer * a->n_heads > 1 << 20 ||
+      (double)a->n_outer * a->n_heads * a->slots * a->head_dim * (a->dtype == JPI_BF16 ? 2 : 4) > 1099511627776.0)
+    return fail(JPI_ERR_SHAPE, "%s: more than 2^26 slots, 2^20 sequences or 2^40 bytes of K", call);
   if (a->n_outer == 0) return JPI_OK;
   if (a->slots > 0 && (!a->weight || !a->index)) return fail(JPI_ERR_ARG, "%s: weight or index is NULL", call);
   const int most = a->keep < a->slots ? a->keep : a->slots;

@@ -30,6 +30,9 @@ typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef short i16x4 __attribute__((ext_vector_type(4)));
 
 constexpr int KEYS = 32;          // keys per tile
+// Share of a range that a tile of a tail counts for, in prefix tiles: 64 samples over 65536 slots with tails of up to 512
+// took 139, 124, 130 and 137 us with 1, 2, 3 and 4.
+constexpr int TAIL_COST = 2;
 constexpr float LOG2E = 1.44269504088896341f, LN2 = 0.693147180559945309f;
 constexpr float HEADROOM = 16.f;  // log2 of the most that a probability may exceed its row's reference by
 
@@ -99,6 +102,8 @@ __device__ __forceinline__ float halves_sum(float v) {
   halves(v, a, b);
   return a + b;
 }
+
+__device__ __forceinline__ u32 uniform(u32 v) { return __builtin_amdgcn_readfirstlane(v); }
 
 struct View {
   const char* data;
@@ -348,8 +353,6 @@ struct Steps {
   }
 };
 
-__device__ __forceinline__ u32 uniform(u32 v) { return __builtin_amdgcn_readfirstlane(v); }
-
 // Loads of a ring stage, K of a tile and V of the tile before it (whose probabilities are formed while the scores of the
 // next are), piece f of the two by wave f % NW, as direct-to-LDS loads (16 bytes of
 // each lane, written lane after lane; the order inside a piece is made by what each lane asks for).  Every stage has the
@@ -476,7 +479,13 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(NW == 8
     __syncthreads();
   }
   const int total = np + (l.suffix ? __builtin_amdgcn_readfirstlane(cum[nb]) : 0);
-  const int t0 = (int)((int64_t)split * total / l.splits), t1 = (int)((int64_t)(split + 1) * total / l.splits);
+  // Ranges of equal time: a tile of a tail takes TAIL_COST times a prefix tile's (it is one wave's or few waves' work).
+  const int64_t units = np + (int64_t)TAIL_COST * (total - np);
+  auto first_of = [&](int r) {
+    const int64_t u = r * units / l.splits;
+    return (int)(u <= np ? u : np + (u - np + TAIL_COST - 1) / TAIL_COST);
+  };
+  const int t0 = first_of(split), t1 = first_of(split + 1);
 
   typename ST::State x;
 #pragma unroll
@@ -728,82 +737,146 @@ __global__ __launch_bounds__(256) void k_shared_merge(SharedLaunch l) {
 // ---------------------------------------------------------------------------
 // weight of the prefix slots
 // ---------------------------------------------------------------------------
-// A wave keeps 32 keys in registers and reads the rows, 32 at a time, from LDS: S = q K^T puts one key in each lane,
-// and the sum over rows stays in its register.  Ranges of rows are summed by k_weight_sum in their order.
+// A wave keeps 64 keys (fp32 heads of 256: 32) in registers and takes the rows, 32 at a time, from LDS: S = q K^T puts one
+// key in each lane and 16 rows in its registers, so the sum over rows stays in a register, and a read of a row from LDS
+// serves two products.  Bound by the exponentials (24 of a SIMD's cycles for 64 of them, against 16 of a product over 128
+// dims).  A workgroup's range of rows has its lse in LDS from the start, as the exponent's summand; ranges are summed by
+// k_weight_sum in their order.
 struct WeightLaunch {
-  SharedLaunch a;  // q, kp, sizes; lse read; splits: ranges of rows
+  SharedLaunch a;  // q, kp, sizes; splits: ranges of rows
   const float *lse, *w_in;
   float *w_out, *part;  // part: [splits][n_groups][n_kv][prefix] (null: one range)
   float decay;
   int key_tiles;
 };
 
-template <typename T, int DH, int NW>
-__global__ __launch_bounds__(64 * NW) void k_weight(WeightLaunch l) {
+constexpr int WEIGHT_WAVES = 4;
+constexpr int WEIGHT_ROWS = 2048;  // rows of a range at most
+
+template <typename T, int DH>
+struct WeightShape {
   using TL = Tile<T, DH>;
-  __shared__ __attribute__((aligned(1024))) char lds[TL::BYTES];
-  __shared__ float lse2[KEYS];
+  static constexpr int KT = sizeof(T) == 4 && DH == 256 ? 1 : 2;  // 32-key tiles of a wave
+  static constexpr int KEYS_WG = KEYS * KT * WEIGHT_WAVES;
+  static constexpr int NS = 4;                                    // stages of rows; the same memory first takes the keys
+  static constexpr int LOADS = TL::PIECES / WEIGHT_WAVES;         // of one wave and stage
+};
+
+template <typename T, int DH>
+__global__ __launch_bounds__(64 * WEIGHT_WAVES) void k_weight(WeightLaunch l) {
+  using TL = Tile<T, DH>;
+  using WS = WeightShape<T, DH>;
+  constexpr int NW = WEIGHT_WAVES, NS = WS::NS, KT = WS::KT;
+  static_assert(NW == 4 && NS >= NW, "a wave's pieces are eight rows of all chunks; each wave stages its keys");
+  __shared__ __attribute__((aligned(1024))) char lds[NS * TL::BYTES];
+  __shared__ float lse2[WEIGHT_ROWS];
   const SharedLaunch& a = l.a;
   const int item = (int)(blockIdx.x % 8) * (int)(gridDim.x / 8) + (int)(blockIdx.x / 8);
   if (item >= a.n_groups * a.n_kv * l.key_tiles * a.splits) return;
   const int kt = item % l.key_tiles, split = item / l.key_tiles % a.splits, gk = item / (l.key_tiles * a.splits);
   const int g = gk / a.n_kv, kv = gk - g * a.n_kv;
-  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, half = lane >> 5, col = lane & 31;
-  const int plen = clamp_len(a.plen, g, a.prefix);
-  if (kt * KEYS * NW >= plen) return;
-  const int j = (kt * NW + w) * KEYS + col;
-  typename TL::chunk key[TL::KS];
-  {
-    const char* p = a.kp.data + g * a.kp.outer + kv * a.kp.head + (int64_t)min(j, plen - 1) * a.kp.row;
+  const int tid = threadIdx.x, lane = tid & 63, w = uniform(tid >> 6), half = lane >> 5, col = lane & 31;
+  const int plen = uniform(clamp_len(a.plen, g, a.prefix));
+  if (kt * WS::KEYS_WG >= plen) return;
+  const u32 ring = (u32)(uintptr_t)(dma_lds_t*)lds;
+  auto load = [&](const char* p, u32 to) __attribute__((always_inline)) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(uniform(to)), "v"(p) : "memory", "m0");
+  };
+
+  // keys into registers, by way of LDS so that whole lines are asked for
+  const int key0 = kt * WS::KEYS_WG + w * KEYS * KT;
+  typename TL::chunk key[KT][TL::KS];
 #pragma unroll
-    for (int k = 0; k < TL::KS; ++k) key[k] = *reinterpret_cast<const typename TL::chunk*>(p + (2 * k + half) * 16);
+  for (int u = 0; u < KT; ++u) {
+#pragma unroll
+    for (int f = 0; f < TL::PIECES; ++f) {
+      const int r = min(key0 + u * KEYS + 8 * (f & 3) + TL::row(lane), plen - 1);
+      load(a.kp.data + g * a.kp.outer + kv * a.kp.head + (int64_t)r * a.kp.row + (8 * (f >> 2) + TL::col(f, lane)) * 16,
+           ring + w * TL::BYTES + f * 1024);
+    }
+    wait_vm<0>();
+    asm volatile("" ::: "memory");
+#pragma unroll
+    for (int k = 0; k < TL::KS; ++k)
+      key[u][k] = *reinterpret_cast<const typename TL::chunk*>(lds + w * TL::BYTES + TL::base(lane, k & 3) + TL::step(k));
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
   }
+
   const int n_rows = a.group * a.q_rows * a.per_kv, tiles = (n_rows + KEYS - 1) / KEYS;
   const int t0 = (int)((int64_t)split * tiles / a.splits), t1 = (int)((int64_t)(split + 1) * tiles / a.splits);
-  float sum = 0.f;
-  for (int t = t0; t < t1; ++t) {
-    __syncthreads();
-    for (int c = tid; c < TL::PIECES * 64; c += 64 * NW) {
-      const Row x = row_of(a, g, kv, t * KEYS + 8 * (c / 64 % 4) + TL::row(c % 64));
-      u32x4 v = {0, 0, 0, 0};
-      if (x.b >= 0)
-        v = *reinterpret_cast<const u32x4*>(a.q.data + x.b * a.q.outer + x.i * a.q.row + x.h * a.q.head +
-                                             (8 * (c / 256) + TL::col(c / 64, c % 64)) * 16);
-      *reinterpret_cast<u32x4*>(lds + c * 16) = v;
-    }
-    if (tid < KEYS) {
-      const Row x = row_of(a, g, kv, t * KEYS + tid);
-      const float v = x.b >= 0 ? l.lse[((int64_t)x.b * a.q_rows + x.i) * a.n_heads + x.h] : -INFINITY;
-      lse2[tid] = v == -INFINITY ? INFINITY : v * LOG2E;  // rows that see nothing, or are none, add 2^-inf
-    }
-    __syncthreads();
-    f32x16 s;
+  for (int r = tid; r < (t1 - t0) * KEYS; r += 64 * NW) {
+    const Row x = row_of(a, g, kv, t0 * KEYS + r);
+    const float v = x.b >= 0 ? l.lse[((int64_t)x.b * a.q_rows + x.i) * a.n_heads + x.h] : -INFINITY;
+    lse2[r] = v == -INFINITY ? -INFINITY : -v * LOG2E;  // rows that see nothing, or are none, add 2^-inf
+  }
+  __syncthreads();
+
+  auto rows = [&](int t, int stage) __attribute__((always_inline)) {  // past the last tile: the last row again
+    const Row x = row_of(a, g, kv, min(t * KEYS + 8 * w + TL::row(lane), n_rows - 1));
+    const char* p = a.q.data + x.b * a.q.outer + x.i * a.q.row + x.h * a.q.head + TL::col(w, lane) * 16;
 #pragma unroll
-    for (int r = 0; r < 16; ++r) s[r] = 0.f;
+    for (int i = 0; i < WS::LOADS; ++i) load(p + i * 128, ring + stage * TL::BYTES + (w + NW * i) * 1024);
+  };
+#pragma unroll
+  for (int u = 0; u < NS - 1; ++u) rows(t0 + u, u);
+  float sum[KT][2] = {};
+  int stage = 0;
+  for (int t = t0; t < t1; ++t) {
+    wait_vm<(NS - 2) * WS::LOADS>();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    rows(t + NS - 1, stage == 0 ? NS - 1 : stage - 1);
+    const char* const at = lds + stage * TL::BYTES;
+    stage = stage == NS - 1 ? 0 : stage + 1;
+    f32x16 s[KT];
+#pragma unroll
+    for (int u = 0; u < KT; ++u)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[u][r] = 0.f;
 #pragma unroll
     for (int k = 0; k < TL::KS; ++k) {
-      s = mfma_chunk<T>(*reinterpret_cast<const typename TL::chunk*>(lds + TL::base(lane, k & 3) + TL::step(k)), key[k], s);
-    }
+      const auto x = *reinterpret_cast<const typename TL::chunk*>(at + TL::base(lane, k & 3) + TL::step(k));
 #pragma unroll
-    for (int r = 0; r < 16; ++r)
-      sum += __builtin_amdgcn_exp2f(fmaf(s[r], a.qscale, -lse2[8 * (r >> 2) + 4 * half + (r & 3)]));
+      for (int u = 0; u < KT; ++u) s[u] = mfma_chunk<T>(x, key[u][k], s[u]);
+    }
+    f32x4 e[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) e[j] = *reinterpret_cast<const f32x4*>(&lse2[(t - t0) * KEYS + 8 * j + 4 * half]);
+#pragma unroll
+    for (int u = 0; u < KT; ++u)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) sum[u][r & 1] += __builtin_amdgcn_exp2f(fmaf(s[u][r], a.qscale, e[r >> 2][r & 3]));
   }
-  sum = halves_sum(sum);
-  if (half || j >= plen) return;
-  const int64_t at = (int64_t)gk * a.prefix + j;
-  if (l.part) l.part[(int64_t)split * a.n_groups * a.n_kv * a.prefix + at] = sum;
-  else l.w_out[at] = (l.w_in ? l.decay * l.w_in[at] : 0.f) + sum;
+  wait_vm<0>();  // no load is in flight into LDS when the workgroup ends
+#pragma unroll
+  for (int u = 0; u < KT; ++u) {
+    const float x = halves_sum(sum[u][0] + sum[u][1]);
+    const int j = key0 + u * KEYS + col;
+    if (half || j >= plen) continue;
+    const int64_t at = (int64_t)gk * a.prefix + j;
+    if (l.part) l.part[(int64_t)split * a.n_groups * a.n_kv * a.prefix + at] = x;
+    else l.w_out[at] = (l.w_in ? l.decay * l.w_in[at] : 0.f) + x;
+  }
 }
 
+// 64 slots a workgroup; each wave sums every fourth range, the four sums are added in order
 __global__ __launch_bounds__(256) void k_weight_sum(WeightLaunch l) {
+  __shared__ float sums[4][64];
   const SharedLaunch& a = l.a;
-  const int64_t n = (int64_t)a.n_groups * a.n_kv * a.prefix, at = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (at >= n) return;
-  const int gk = (int)(at / a.prefix), j = (int)(at - (int64_t)gk * a.prefix);
-  if (j >= clamp_len(a.plen, gk / a.n_kv, a.prefix)) return;
+  const int64_t n = (int64_t)a.n_groups * a.n_kv * a.prefix, at = (int64_t)blockIdx.x * 64 + (threadIdx.x & 63);
+  const int w = threadIdx.x >> 6, gk = (int)(at / a.prefix), j = (int)(at - (int64_t)gk * a.prefix);
+  const bool on = at < n && j < clamp_len(a.plen, gk / a.n_kv, a.prefix);
   float sum = 0.f;
-  for (int s = 0; s < a.splits; ++s) sum += l.part[s * n + at];
-  l.w_out[at] = (l.w_in ? l.decay * l.w_in[at] : 0.f) + sum;
+  if (on) {
+#pragma unroll 8
+    for (int s = w; s < a.splits; s += 4) sum += l.part[s * n + at];
+  }
+  sums[w][threadIdx.x & 63] = sum;
+  __syncthreads();
+  if (w || !on) return;
+  const int c = threadIdx.x;
+  l.w_out[at] = (l.w_in ? l.decay * l.w_in[at] : 0.f) + (((sums[0][c] + sums[1][c]) + sums[2][c]) + sums[3][c]);
 }
 
 // ---------------------------------------------------------------------------
@@ -870,13 +943,17 @@ Plan shared_plan(const jpi_shared_attn& a) {
   return best;
 }
 
+// Key blocks of a workgroup, and ranges of rows: enough workgroups for two on each unit, ranges of at most WEIGHT_ROWS.
 Plan weight_plan(const jpi_shared_attn& a) {
-  const int64_t rows = (int64_t)a.group * a.q_rows * (a.n_heads / a.n_kv_heads);
-  Plan p;
-  p.waves = 4;
-  p.row_tiles = (int)((a.prefix + KEYS * p.waves - 1) / (KEYS * p.waves));
+  const int64_t rows = (int64_t)a.group * a.q_rows * (a.n_heads / a.n_kv_heads), tiles = (rows + KEYS - 1) / KEYS;
+  const int keys = KEYS * (a.dtype == JPI_F32 && a.head_dim == 256 ? 1 : 2) * WEIGHT_WAVES;
+  Plan p{};
+  p.waves = WEIGHT_WAVES;
+  p.row_tiles = (a.prefix + keys - 1) / keys;
   const int64_t items = (int64_t)a.n_groups * a.n_kv_heads * p.row_tiles;
-  p.splits = items ? (int)std::max<int64_t>(1, std::min<int64_t>({64, 512 / items, (rows + KEYS - 1) / KEYS})) : 1;
+  const int64_t least = (tiles + WEIGHT_ROWS / KEYS - 1) / (WEIGHT_ROWS / KEYS);
+  p.splits = items ? (int)std::max(least, std::min<int64_t>({64, 512 / items, tiles})) : 1;
+  if (p.splits < 1) p.splits = 1;
   return p;
 }
 
@@ -922,10 +999,10 @@ hipError_t weight_typed(const jpi_shared_attn& a, const float* w_in, float decay
   l.key_tiles = p.row_tiles;
   const int64_t slots = (int64_t)a.n_groups * a.n_kv_heads * a.prefix;
   if (p.splits > 1) l.part = (float*)ws;
-  k_weight<T, DH, 4><<<grid8((int64_t)a.n_groups * a.n_kv_heads * p.row_tiles * p.splits), 256, 0, s>>>(l);
+  k_weight<T, DH><<<grid8((int64_t)a.n_groups * a.n_kv_heads * p.row_tiles * p.splits), 64 * WEIGHT_WAVES, 0, s>>>(l);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.splits == 1) return e;
-  k_weight_sum<<<(unsigned)((slots + 255) / 256), 256, 0, s>>>(l);
+  k_weight_sum<<<(unsigned)((slots + 63) / 64), 256, 0, s>>>(l);
   return hipGetLastError();
 }
 
