@@ -29,51 +29,55 @@ typedef u32 u32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef short i16x4 __attribute__((ext_vector_type(4)));
 
-constexpr int KEYS = 32;          // keys per tile
+// Keys of a tile.  Two 32-key halves in bf16 share the waits, the first reads from LDS and the bookkeeping of a tile, and
+// the products of one half fill the latency of the other's; 64 fp32 keys of 256 dims would not leave room for two stages.
+template <typename T>
+constexpr int KEYS = sizeof(T) == 2 ? 64 : 32;
 // Share of a range that a tile of a tail counts for, in prefix tiles: 64 samples over 65536 slots with tails of up to 512
 // took 139, 124, 130 and 137 us with 1, 2, 3 and 4.
 constexpr int TAIL_COST = 2;
 constexpr float LOG2E = 1.44269504088896341f, LN2 = 0.693147180559945309f;
 constexpr float HEADROOM = 16.f;  // log2 of the most that a probability may exceed its row's reference by
 
-// A tile of 32 rows (keys, or queries) of DH elements in LDS, in 1 KB pieces of 8 rows x 128 bytes.  A load instruction
+// A tile of R rows (keys, or queries) of DH elements in LDS, in 1 KB pieces of 8 rows x 128 bytes.  A load instruction
 // fills a piece lane after lane, and it is fast only where neighbouring lanes ask for neighbouring memory, so rows stay
 // whole in a piece and their eight 16-byte chunks are permuted, row by row, such that the lanes of one LDS read share
 // out the 64 banks evenly.  A read's address is one of a few bases of its lane plus a constant.
-template <typename T, int DH>
+template <typename T, int DH, int R>
 struct Tile {
   static constexpr int CE = 16 / sizeof(T);      // elements of a chunk
   static constexpr int CPR = DH / CE;            // chunks of a row
   static constexpr int KS = CPR / 2;             // k-steps: a chunk for each lane half
   static constexpr int NT = DH / 32;             // 32-wide output tiles
-  static constexpr int BYTES = KEYS * DH * (int)sizeof(T);
-  static constexpr int PIECES = BYTES / 1024;    // piece f: chunks 8 (f / 4) .. + 7 of rows 8 (f % 4) .. + 7
+  static constexpr int BYTES = R * DH * (int)sizeof(T);
+  static constexpr int GROUPS = R / 8;           // of rows
+  static constexpr int PIECES = BYTES / 1024;    // piece f: chunks 8 (f / GROUPS) .. + 7 of rows 8 (f % GROUPS) .. + 7
   typedef T chunk __attribute__((ext_vector_type(CE)));
   // Rows of a product over DH (K, or queries) are read 32 at a time at one chunk: chunk c of row r lies at c ^ swz(r).
   static __device__ __forceinline__ int swz(int r) { return (r & 7) ^ (r >> 3 & 1); }
   // V in bf16 is read transposed, 16 lanes addressing 4 keys x 16 dims: keys 4 .. 7, 2 keys apart, change 64-byte halves.
   static __device__ __forceinline__ int swz_v(int r) { return sizeof(T) == 2 ? (r & 2) << 1 : 0; }
-  // what chunk `at` of a piece holds: a row of its eight, and a chunk of the row's eight
+  // what chunk `at` of a piece (of row group g) holds: a row of its eight, and a chunk of the row's eight
   static __device__ __forceinline__ int row(int at) { return at >> 3; }
-  static __device__ __forceinline__ int col(int f, int at) { return (at & 7) ^ swz(8 * (f & 3) + (at >> 3)); }
+  static __device__ __forceinline__ int col(int g, int at) { return (at & 7) ^ swz(8 * g + (at >> 3)); }
   static __device__ __forceinline__ int col_v(int at) { return (at & 7) ^ swz_v(at >> 3); }
-  // the chunk of k-step k that a lane (row lane % 32, half lane / 32) reads: base(lane, k % 4) + step(k)
+  // the chunk of k-step k that a lane (row 32 hh + lane % 32, half lane / 32) reads: base(lane, k % 4) + step(k, hh)
   static __device__ __forceinline__ int base(int lane, int j) {
     const int r = lane & 31, h = lane >> 5;
     return r * 128 + ((2 * j + h) ^ swz(r)) * 16;
   }
-  static constexpr int step(int k) { return (k >> 2) * 4096; }
+  static constexpr int step(int k, int hh) { return (k >> 2) * GROUPS * 1024 + hh * 4096; }
   // V, bf16: the 8 bytes that a lane addresses for 16-key step u, output tile t and keys 8 z .. of it:
   // base_v(lane, t % 2) + step_v(t, u, z)
   static __device__ __forceinline__ int base_v(int lane, int tp) {
     const int key = 4 * (lane >> 5) + (lane >> 2 & 3);
     return key * 128 + ((tp ^ (key >> 1 & 1)) * 64) + (lane >> 4 & 1) * 32 + (lane & 3) * 8;
   }
-  static constexpr int step_v(int t, int u, int z) { return (t >> 1) * 4096 + (2 * u + z) * 1024; }
+  static constexpr int step_v(int t, int u, int z) { return (t >> 1) * GROUPS * 1024 + (2 * u + z) * 1024; }
 };
 
 template <typename T>
-__device__ __forceinline__ f32x16 mfma_chunk(const typename Tile<T, 64>::chunk& a, const typename Tile<T, 64>::chunk& b,
+__device__ __forceinline__ f32x16 mfma_chunk(const typename Tile<T, 64, 32>::chunk& a, const typename Tile<T, 64, 32>::chunk& b,
                                              f32x16 c) {
   if constexpr (sizeof(T) == 2) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
@@ -138,10 +142,10 @@ __device__ __forceinline__ int clamp_len(const int32_t* len, int i, int most) {
 // Rows that do not see a key have probability 0 for it, and 0 * V of the matrix product would carry NaN or infinity of
 // its V into them.  In a tile of a tail that not all rows see, such values are therefore taken out of LDS, by each wave in
 // the pieces that it loaded, and their keys noted; the rows that see one add its kind to all their elements at the end.
-// kinds[0 .. 2]: keys with +inf, -inf, NaN.
+// kinds[3 i ..]: those of keys 32 i .. + 31 with +inf, -inf, NaN.
 template <typename T, int DH, int NW>
 __device__ __forceinline__ void take_out(char* vt, u32* kinds) {
-  using TL = Tile<T, DH>;
+  using TL = Tile<T, DH, KEYS<T>>;
   constexpr u32 ones = sizeof(T) == 2 ? 0x7f807f80u : 0x7f800000u, step = sizeof(T) == 2 ? 0x00800080u : 0x00800000u;
   constexpr u32 carry = sizeof(T) == 2 ? 0x80008000u : 0x80000000u;
   u32x4 x[TL::PIECES / NW];
@@ -156,21 +160,27 @@ __device__ __forceinline__ void take_out(char* vt, u32* kinds) {
 #pragma unroll 1
   for (int i = 0; i < TL::PIECES / NW; ++i) {
     T* v = reinterpret_cast<T*>(vt + i * NW * 1024);
-    const int f = (threadIdx.x >> 6) + i * NW, key = 8 * (f & 3) + TL::row(threadIdx.x & 63);
+    const int f = (threadIdx.x >> 6) + i * NW, key = 8 * (f % TL::GROUPS) + TL::row(threadIdx.x & 63);
 #pragma unroll 1
     for (int e = 0; e < TL::CE; ++e) {
       const float y = (float)v[e];
       if (__builtin_isfinite(y)) continue;
-      atomicOr(&kinds[y == INFINITY ? 0 : y == -INFINITY ? 1 : 2], 1u << key);
+      atomicOr(&kinds[3 * (key >> 5) + (y == INFINITY ? 0 : y == -INFINITY ? 1 : 2)], 1u << (key & 31));
       v[e] = (T)0.f;
     }
   }
 }
 
 // what the keys below `lim` among those add to a row
+template <int N>
 __device__ __forceinline__ float taint_of(const u32* kinds, int lim) {
-  const u32 seen = lim >= KEYS ? ~0u : (1u << max(lim, 0)) - 1;
-  const bool pos = (kinds[0] & seen) != 0, neg = (kinds[1] & seen) != 0, nan = (kinds[2] & seen) != 0;
+  bool pos = false, neg = false, nan = false;
+#pragma unroll
+  for (int i = 0; i < N / 32; ++i) {
+    const int rest = lim - 32 * i;
+    const u32 seen = rest >= 32 ? ~0u : (1u << max(rest, 0)) - 1;
+    pos |= (kinds[3 * i] & seen) != 0, neg |= (kinds[3 * i + 1] & seen) != 0, nan |= (kinds[3 * i + 2] & seen) != 0;
+  }
   return nan || (pos && neg) ? __builtin_nanf("") : pos ? INFINITY : neg ? -INFINITY : 0.f;
 }
 
@@ -185,16 +195,19 @@ __device__ __forceinline__ bf16x8 read_vt(const char* p) {
   return __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
-// S^T = K q^T of one tile.  LDS reads run AHEAD operands before the products, each of which takes less time than a read.
+// The work of a wave's 32 rows on a tile: S^T = K q^T, the softmax, O^T += V^T P^T.
 template <typename T, int DH>
 struct Steps {
-  using TL = Tile<T, DH>;
+  static constexpr int N = KEYS<T>, HT = N / 32;  // keys of a tile, 32-key halves
+  using TL = Tile<T, DH, N>;
   typedef typename TL::chunk chunk;
   static constexpr bool HALF = sizeof(T) == 2;
   static constexpr int KS = TL::KS, NT = TL::NT;
-  static constexpr int AHEAD = KS < 8 ? KS : 8, VA = 4;  // operands of K, of V (bf16), that are read ahead
+  static constexpr int QK = KS * HT, PV = NT * 2 * HT;      // products of a tile (bf16)
+  // Operands of K, of V (bf16), that are read ahead: a read takes longer than a product.
+  static constexpr int AHEAD = QK < 8 ? QK : 8, VA = 4;
 
-  struct State {  // of this wave's 32 rows: a row in each lane, its keys and dims shared by the lane halves
+  struct State {  // a row in each lane, its keys and dims shared by the lane halves
     f32x16 o[NT];   // sum of p v
     float m_ref;    // reference of the row's probabilities: 2^(s - m_ref)
     float l_run;    // sum of p over this half's keys
@@ -205,33 +218,38 @@ struct Steps {
 #pragma unroll
     for (int j = 0; j < 4; ++j) kl[j] = kt + TL::base(lane, j);
   }
-  static __device__ __forceinline__ f32x16 scores(const char* kt, const chunk (&q)[KS]) {
+  static __device__ __forceinline__ chunk k_operand(const char* const (&kl)[4], int f) {  // k-step f / HT, half f % HT
+    return *reinterpret_cast<const chunk*>(kl[f / HT & 3] + TL::step(f / HT, f % HT));
+  }
+  static __device__ __forceinline__ void scores(const char* kt, const chunk (&q)[KS], f32x16 (&s)[HT]) {
     const char* kl[4];
     k_bases(kt, kl);
-    f32x16 s;
 #pragma unroll
-    for (int r = 0; r < 16; ++r) s[r] = 0.f;
+    for (int h = 0; h < HT; ++h)
 #pragma unroll
-    for (int k = 0; k < KS; ++k) s = mfma_chunk<T>(*reinterpret_cast<const chunk*>(kl[k & 3] + TL::step(k)), q[k], s);
+      for (int r = 0; r < 16; ++r) s[h][r] = 0.f;
+#pragma unroll
+    for (int f = 0; f < QK; ++f) s[f % HT] = mfma_chunk<T>(k_operand(kl, f), q[f / HT], s[f % HT]);
     if constexpr (HALF) {
       __builtin_amdgcn_sched_group_barrier(SCHED_DS_READ, AHEAD, 0);
 #pragma unroll
-      for (int k = 0; k < KS; ++k) {
+      for (int f = 0; f < QK; ++f) {
         __builtin_amdgcn_sched_group_barrier(SCHED_MFMA, 1, 0);
-        if (k < KS - AHEAD) __builtin_amdgcn_sched_group_barrier(SCHED_DS_READ, 1, 0);
+        if (f < QK - AHEAD) __builtin_amdgcn_sched_group_barrier(SCHED_DS_READ, 1, 0);
       }
     }
-    return s;
   }
   // Keys from `lim` on are not visible to the row.  Returns the row's largest score in powers of two.
-  static __device__ __forceinline__ float mask_max(f32x16& s, int lim, float qscale) {
+  static __device__ __forceinline__ float mask_max(f32x16 (&s)[HT], int lim, float qscale) {
     const int rest = lim - 4 * ((threadIdx.x & 63) >> 5);
     float m = -INFINITY;
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      s[r] = 8 * (r >> 2) + (r & 3) < rest ? s[r] : -INFINITY;
-      m = fmaxf(m, s[r]);
-    }
+    for (int h = 0; h < HT; ++h)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        s[h][r] = 32 * h + 8 * (r >> 2) + (r & 3) < rest ? s[h][r] : -INFINITY;
+        m = fmaxf(m, s[h][r]);
+      }
     return halves_max(m) * qscale;
   }
   // The row's reference is the maximum of its first tile with a visible key; it moves up, and the row's sums are
@@ -246,41 +264,47 @@ struct Steps {
       x.m_ref = over ? m : x.m_ref;
     }
   }
-  static __device__ __forceinline__ void probabilities(State& x, f32x16& s, float qscale) {
+  static __device__ __forceinline__ void probabilities(State& x, f32x16 (&s)[HT], float qscale) {
     const float ref = x.m_ref == -INFINITY ? 0.f : x.m_ref;  // nothing seen yet: every probability is 2^-inf
     float sum[2] = {0.f, 0.f};
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], qscale, -ref));
-      sum[r & 1] += s[r];
-    }
+    for (int h = 0; h < HT; ++h)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        s[h][r] = __builtin_amdgcn_exp2f(fmaf(s[h][r], qscale, -ref));
+        sum[r & 1] += s[h][r];
+      }
     x.l_run += sum[0] + sum[1];
   }
-  // 16 keys each, registers 8u .. 8u + 7 of S^T
-  static __device__ __forceinline__ void round_p(const f32x16& s, bf16x8 (&p)[2]) {
+  // 16 keys each: registers 8 (u % 2) .. + 7 of half u / 2 of S^T
+  static __device__ __forceinline__ void round_p(const f32x16 (&s)[HT], bf16x8 (&p)[2 * HT]) {
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
+    for (int u = 0; u < 2 * HT; ++u)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) p[u][e] = static_cast<bf16>(s[8 * u + e]);
+      for (int e = 0; e < 8; ++e) p[u][e] = static_cast<bf16>(s[u >> 1][8 * (u & 1) + e]);
   }
-  static __device__ __forceinline__ bf16x8 v_operand(const char* const (&vl)[2], int i) {  // output tile i / 2, 16-key step i % 2
-    return read_vt(vl[i >> 1 & 1] + TL::step_v(i >> 1, i & 1, 0));
+  // product i with V: output tile, 16-key step; two output tiles take turns, so that no product waits for the last one's sum
+  static constexpr int out_tile(int i) { return i / (4 * HT) * 2 + (i & 1); }
+  static constexpr int key_step(int i) { return i / 2 % (2 * HT); }
+  static __device__ __forceinline__ bf16x8 v_operand(const char* const (&vl)[2], int i) {
+    return read_vt(vl[out_tile(i) & 1] + TL::step_v(out_tile(i), key_step(i), 0));
   }
   // O^T += V^T P^T of one tile, P^T in the registers of S^T
-  static __device__ __forceinline__ void weigh(State& x, const char* vt, f32x16& s, float qscale) {
+  static __device__ __forceinline__ void weigh(State& x, const char* vt, f32x16 (&s)[HT], float qscale) {
     const int lane = threadIdx.x & 63;
     probabilities(x, s, qscale);
     if constexpr (HALF) {
       const char* const vl[2] = {vt + TL::base_v(lane, 0), vt + TL::base_v(lane, 1)};
-      bf16x8 p[2];
+      bf16x8 p[2 * HT];
       round_p(s, p);
 #pragma unroll
-      for (int i = 0; i < 2 * NT; ++i) x.o[i >> 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_operand(vl, i), p[i & 1], x.o[i >> 1], 0, 0, 0);
+      for (int i = 0; i < PV; ++i)
+        x.o[out_tile(i)] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_operand(vl, i), p[key_step(i)], x.o[out_tile(i)], 0, 0, 0);
       __builtin_amdgcn_sched_group_barrier(SCHED_DS_READ, 2 * VA, 0);
 #pragma unroll
-      for (int i = 0; i < 2 * NT; ++i) {
+      for (int i = 0; i < PV; ++i) {
         __builtin_amdgcn_sched_group_barrier(SCHED_MFMA, 1, 0);
-        if (i < 2 * NT - VA) __builtin_amdgcn_sched_group_barrier(SCHED_DS_READ, 2, 0);
+        if (i < PV - VA) __builtin_amdgcn_sched_group_barrier(SCHED_DS_READ, 2, 0);
       }
     } else {
       const char* const vl = vt + (lane >> 5) * 512 + (lane & 31) * 4;
@@ -289,66 +313,71 @@ struct Steps {
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           const float v = *reinterpret_cast<const float*>(vl + t * 4096 + (r >> 2) * 1024 + (r & 3) * 128);
-          x.o[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, s[r], x.o[t], 0, 0, 0);
+          x.o[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, s[0][r], x.o[t], 0, 0, 0);
         }
     }
   }
   // One tile's probabilities and product with V, and the scores of the next, a full tile that all rows see (bf16).  A wave
   // has the matrix unit to itself or shares it with one other, so the work is laid out by hand, a product and what fits
   // beside it at a time: while the unit works on the next scores, the probabilities are formed; while it works on V, the
-  // maximum of the next scores is found and the ring's loads are issued (`load(i)`, i < 2 NT).  Operands are read from LDS
+  // maximum of the next scores is found and the ring's loads are issued (`load(i)`, i < PV).  Operands are read from LDS
   // AHEAD and VA products before they are used.
   template <typename F>
-  static __device__ __forceinline__ void both(State& x, const char* vt, const char* kt, const chunk (&q)[KS], f32x16& s,
+  static __device__ __forceinline__ void both(State& x, const char* vt, const char* kt, const chunk (&q)[KS], f32x16 (&s)[HT],
                                               float qscale, F load) {
     const int lane = threadIdx.x & 63;
     const char* kl[4];
     k_bases(kt, kl);
     const char* const vl[2] = {vt + TL::base_v(lane, 0), vt + TL::base_v(lane, 1)};
     const float ref = x.m_ref == -INFINITY ? 0.f : x.m_ref;
-    constexpr int PRE = 4;            // probabilities formed while the first operands are on their way
-    constexpr int PV = 2 * NT, WAIT = PV > 4 ? 2 : 1;  // products with V; of them before the scores are looked at
+    constexpr int E = 16 * HT, PRE = 4;  // probabilities; of them formed while the first operands are on their way
+    constexpr int WAIT = 2;              // products with V before the scores are looked at
     chunk kf[AHEAD];
     bf16x8 vf[VA];
     float sum[2] = {0.f, 0.f};
-    auto probability = [&](int r) __attribute__((always_inline)) {
-      s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], qscale, -ref));
-      sum[r & 1] += s[r];
+    auto probability = [&](int e) __attribute__((always_inline)) {
+      float& y = reinterpret_cast<float*>(&s[e >> 4])[e & 15];
+      y = __builtin_amdgcn_exp2f(fmaf(y, qscale, -ref));
+      sum[e & 1] += y;
     };
 #pragma unroll
-    for (int k = 0; k < AHEAD; ++k) kf[k] = *reinterpret_cast<const chunk*>(kl[k & 3] + TL::step(k));
+    for (int f = 0; f < AHEAD; ++f) kf[f] = k_operand(kl, f);
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int r = 0; r < PRE; ++r) probability(r);
-    f32x16 n;
+    for (int e = 0; e < PRE; ++e) probability(e);
+    f32x16 n[HT];
 #pragma unroll
-    for (int r = 0; r < 16; ++r) n[r] = 0.f;
+    for (int h = 0; h < HT; ++h)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) n[h][r] = 0.f;
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int k = 0; k < KS; ++k) {
-      n = mfma_chunk<T>(kf[k % AHEAD], q[k], n);
-      if (k + AHEAD < KS) kf[k % AHEAD] = *reinterpret_cast<const chunk*>(kl[(k + AHEAD) & 3] + TL::step(k + AHEAD));
-      if (k >= KS - VA) vf[k - (KS - VA)] = v_operand(vl, k - (KS - VA));
+    for (int f = 0; f < QK; ++f) {
+      n[f % HT] = mfma_chunk<T>(kf[f % AHEAD], q[f / HT], n[f % HT]);
+      if (f + AHEAD < QK) kf[f % AHEAD] = k_operand(kl, f + AHEAD);
+      if (f >= QK - VA) vf[f - (QK - VA)] = v_operand(vl, f - (QK - VA));
 #pragma unroll
-      for (int r = PRE + k * (16 - PRE) / KS; r < PRE + (k + 1) * (16 - PRE) / KS; ++r) probability(r);
+      for (int e = PRE + f * (E - PRE) / QK; e < PRE + (f + 1) * (E - PRE) / QK; ++e) probability(e);
       __builtin_amdgcn_sched_barrier(0);
     }
     x.l_run += sum[0] + sum[1];
-    bf16x8 p[2];
+    bf16x8 p[2 * HT];
     round_p(s, p);
     float m = -INFINITY;
 #pragma unroll
     for (int i = 0; i < PV; ++i) {
-      x.o[i >> 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[i % VA], p[i & 1], x.o[i >> 1], 0, 0, 0);
+      x.o[out_tile(i)] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[i % VA], p[key_step(i)], x.o[out_tile(i)], 0, 0, 0);
       if (i + VA < PV) vf[i % VA] = v_operand(vl, i + VA);
       load(i);
       if (i >= WAIT) {
 #pragma unroll
-        for (int r = (i - WAIT) * 8 / (PV - WAIT) * 2; r < (i + 1 - WAIT) * 8 / (PV - WAIT) * 2; r += 2) m = fmaxf(fmaxf(m, n[r]), n[r + 1]);
+        for (int e = (i - WAIT) * (E / 2) / (PV - WAIT) * 2; e < (i + 1 - WAIT) * (E / 2) / (PV - WAIT) * 2; e += 2)
+          m = fmaxf(fmaxf(m, n[e >> 4][e & 15]), n[e >> 4][(e & 15) + 1]);
       }
       __builtin_amdgcn_sched_barrier(0);
     }
-    s = n;
+#pragma unroll
+    for (int h = 0; h < HT; ++h) s[h] = n[h];
     if (__any(m * qscale > x.m_ref + HEADROOM)) settle(x, halves_max(m) * qscale);
   }
 };
@@ -359,7 +388,7 @@ struct Steps {
 // same number of loads, past the last tile too, so that waits can count them.
 template <typename T, int DH, int NW>
 struct Ring {
-  using TL = Tile<T, DH>;
+  using TL = Tile<T, DH, KEYS<T>>;
   static constexpr int PIECES = TL::PIECES;                  // of one operand
   static constexpr int LOADS = 2 * PIECES / NW;              // of one wave and stage
   static constexpr int STAGE = 2 * TL::BYTES;
@@ -379,7 +408,7 @@ struct Ring {
   }
   // What the loads of one stage share, and load u of them.  Load u fills piece w + NW u: its rows are one of ROWS groups
   // of eight, its chunks 128 bytes further on with each piece of the same rows.
-  static constexpr int ROWS = NW < 4 ? 4 / NW : 1;
+  static constexpr int GROUPS = TL::GROUPS, ROWS = NW < GROUPS ? GROUPS / NW : 1;
   struct Issue {
     u32x4 k, v;
     u32 at_k[ROWS], at_v[ROWS];  // byte of the lane's chunk from the tile's first row on
@@ -392,11 +421,11 @@ struct Ring {
     Issue x;
     x.k = rows(kb, kr, kn), x.v = rows(vb, vr, vn);
     x.to = uniform(stage + w * 1024);
-    u32 k0 = TL::row(lane) * kr + (w >> 2) * 128, v0 = TL::row(lane) * vr + TL::col_v(lane) * 16 + (w >> 2) * 128;
+    u32 k0 = TL::row(lane) * kr + w / GROUPS * 128, v0 = TL::row(lane) * vr + TL::col_v(lane) * 16 + w / GROUPS * 128;
     asm volatile("" : "+v"(k0), "+v"(v0));
 #pragma unroll
     for (int i = 0; i < ROWS; ++i) {
-      const int g = (w + NW * i) & 3;
+      const int g = (w + NW * i) % GROUPS;
       x.at_k[i] = k0 + TL::col(g, lane) * 16 + 8 * g * kr;
       x.at_v[i] = v0 + 8 * g * vr;
     }
@@ -410,7 +439,7 @@ struct Ring {
     // with half of the loads each for K and V, whether load u is one of K does not depend on the wave
     const bool is_k = u < LOADS / 2;
     const int i = is_k ? u : u - LOADS / 2;
-    const u32 off = (NW > 4 ? i * (NW / 4) : i / ROWS) * 128;
+    const u32 off = (NW > GROUPS ? i * (NW / GROUPS) : i / ROWS) * 128;
     load(is_k ? x.k : x.v, (is_k ? x.at_k[i % ROWS] : x.at_v[i % ROWS]) + off, x.to + u * NW * 1024);
   }
 };
@@ -430,15 +459,15 @@ struct Source {
 
 template <typename T, int DH, int NW>
 __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(NW == 8 ? 2 : 1))) void k_shared(SharedLaunch l) {
-  using TL = Tile<T, DH>;
+  using TL = Tile<T, DH, KEYS<T>>;
   using RG = Ring<T, DH, NW>;
   using ST = Steps<T, DH>;
-  constexpr int ROWS = 32 * NW, NS = RG::NS;
-  __shared__ __attribute__((aligned(1024))) char lds[NS * RG::STAGE + 4 * (2 * ROWS + 1 + NW + 9)];
+  constexpr int ROWS = 32 * NW, NS = RG::NS, KT = KEYS<T>, KINDS = 3 * (KT / 32);
+  __shared__ __attribute__((aligned(1024))) char lds[NS * RG::STAGE + 4 * (2 * ROWS + 1 + NW + 3 * KINDS)];
   int* const cum = reinterpret_cast<int*>(lds + NS * RG::STAGE);  // tail tiles of the rollouts of this row tile, summed up
   int* const wave_sum = cum + ROWS + 1;
   u32* const kinds = reinterpret_cast<u32*>(wave_sum + NW);  // of this tile and the two next (take_out)
-  int* const lens = wave_sum + NW + 9;                       // of those tails
+  int* const lens = wave_sum + NW + 3 * KINDS;               // of those tails
 
   // items (group, KV head, range, row tile): row tiles of one range are neighbours, and neighbours share an XCD's L2
   const int item = (int)(blockIdx.x % 8) * (int)(gridDim.x / 8) + (int)(blockIdx.x / 8);
@@ -462,9 +491,9 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(NW == 8
   }
 
   // the key sequence
-  const int plen = uniform(prefix_len), np = (plen + KEYS - 1) / KEYS;
+  const int plen = uniform(prefix_len), np = (plen + KT - 1) / KT;
   if (l.suffix) {
-    int c = (some_len + KEYS - 1) / KEYS;
+    int c = (some_len + KT - 1) / KT;
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) {
       const int x = __shfl_up(c, d, 64);
@@ -475,7 +504,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(NW == 8
     for (int v = 0; v < w; ++v) c += wave_sum[v];
     if (tid < nb) cum[tid + 1] = c, lens[tid] = some_len;
     if (tid == 0) cum[0] = 0;
-    if (tid < 9) kinds[tid] = 0;
+    if (tid < 3 * KINDS) kinds[tid] = 0;
     __syncthreads();
   }
   const int total = np + (l.suffix ? __builtin_amdgcn_readfirstlane(cum[nb]) : 0);
@@ -503,17 +532,17 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(NW == 8
 
   auto tail_len = [&](int seg) { return (int)uniform(lens[seg]); };
   auto seek = [&](int t) {  // tile t
-    if (t < np) return Walk{-1, plen - t * KEYS};
+    if (t < np) return Walk{-1, plen - t * KT};
     int lo = 0, hi = nb;  // the tail with cum[lo] <= t - np < cum[lo + 1]
     while (hi - lo > 1) {
       const int mid = (lo + hi) / 2;
       if ((int)uniform(cum[mid]) <= t - np) lo = mid;
       else hi = mid;
     }
-    return Walk{lo, tail_len(lo) - (t - np - (int)uniform(cum[lo])) * KEYS};
+    return Walk{lo, tail_len(lo) - (t - np - (int)uniform(cum[lo])) * KT};
   };
   auto step = [&](Walk& y) __attribute__((always_inline)) {  // one tile on; true: into another tail
-    y.n -= KEYS;
+    y.n -= KT;
     if (y.n > 0) return false;
     while (y.n <= 0 && y.seg + 1 < nb) y.n = tail_len(++y.seg);
     return true;
@@ -528,7 +557,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(NW == 8
   auto advance = [&](Source& y, bool keys) __attribute__((always_inline)) {
     if (++y.tile <= t0 || y.tile >= t1) return;
     if (step(y.at)) open(y, keys);
-    else y.p += KEYS * y.stride;
+    else y.p += KT * y.stride;
   };
 
   wait_vm<0>();  // the queries are there: waited for in the loop, they would have it wait for the ring's loads too
@@ -539,8 +568,8 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(NW == 8
     open(vs, false);
     auto prepare = [&](int stage) __attribute__((always_inline)) {  // K and V of nothing before the first tile and past the last one
       const auto x = RG::prepare((u32)(uintptr_t)(dma_lds_t*)lds + stage * RG::STAGE, ks.p, ks.stride,
-                                 ks.tile < t1 ? min(ks.at.n, KEYS) : 0, vs.p, vs.stride,
-                                 vs.tile >= t0 && vs.tile < t1 ? min(vs.at.n, KEYS) : 0);
+                                 ks.tile < t1 ? min(ks.at.n, KT) : 0, vs.p, vs.stride,
+                                 vs.tile >= t0 && vs.tile < t1 ? min(vs.at.n, KT) : 0);
       advance(ks, true);
       advance(vs, false);
       return x;
@@ -570,41 +599,41 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(NW == 8
     auto freed = [&]() { return stage < 2 ? stage + NS - 2 : stage - 2; };  // the stage before the one just taken
     auto limit = [&](const Walk& y) { return y.seg < 0 ? y.n : own_b == b0 + y.seg ? y.n + own_lim : 0; };
 
-    f32x16 s;
+    f32x16 s[ST::HT];
     int lim = limit(cur);
     bool have = __any(lim > 0);  // whether some row sees a key of the tile: its scores are in s
     {
       const char* const at = next_stage();
       load(freed());
       if (have) {
-        s = ST::scores(at, q);
+        ST::scores(at, q, s);
         x.m_ref = ST::mask_max(s, lim, l.qscale);
       }
     }
     int t = t0;
     if constexpr (ST::HALF) {
       // full tiles of the prefix
-      const int full = min(plen / KEYS, t1), start = t;
+      const int full = min(plen / KT, t1), start = t;
       if (t + 1 < full && ks.tile < full) {  // so are the tiles loaded next: their loads differ by a step of the addresses
-        auto is = RG::prepare(0, ks.p, ks.stride, KEYS, vs.p, vs.stride, KEYS);
-        const u32 first = is.to, k_step = KEYS * ks.stride, v_step = KEYS * vs.stride;
+        auto is = RG::prepare(0, ks.p, ks.stride, KT, vs.p, vs.stride, KT);
+        const u32 first = is.to, k_step = KT * ks.stride, v_step = KT * vs.stride;
         const int run = full - ks.tile;  // t + run < full: a tile of K is loaded before its scores are wanted
         for (int r = 0; r < run; ++r) {
           const char* const at = next_stage();
           is.to = first + freed() * RG::STAGE;
           ST::both(x, at + TL::BYTES, at, q, s, l.qscale, [&](int i) __attribute__((always_inline)) {
 #pragma unroll
-            for (int u = i * RG::LOADS / (2 * TL::NT); u < (i + 1) * RG::LOADS / (2 * TL::NT); ++u) RG::one(is, u);
+            for (int u = i * RG::LOADS / ST::PV; u < (i + 1) * RG::LOADS / ST::PV; ++u) RG::one(is, u);
           });
           RG::forward(is.k, k_step);
           RG::forward(is.v, v_step);
         }
         t += run;
         ks.p += (int64_t)run * k_step, vs.p += (int64_t)run * v_step;
-        ks.at.n -= run * KEYS, vs.at.n -= run * KEYS;
+        ks.at.n -= run * KT, vs.at.n -= run * KT;
         ks.tile += run, vs.tile += run;
         if (ks.at.n <= 0 && ks.tile < t1) {  // the prefix ended with a full tile
-          ks.at.n += KEYS;
+          ks.at.n += KT;
           step(ks.at);
           open(ks, true);
         }
@@ -614,21 +643,24 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(NW == 8
         const auto is = prepare(freed());
         ST::both(x, at + TL::BYTES, at, q, s, l.qscale, [&](int i) __attribute__((always_inline)) {
 #pragma unroll
-          for (int u = i * RG::LOADS / (2 * TL::NT); u < (i + 1) * RG::LOADS / (2 * TL::NT); ++u) RG::one(is, u);
+          for (int u = i * RG::LOADS / ST::PV; u < (i + 1) * RG::LOADS / ST::PV; ++u) RG::one(is, u);
         });
       }
-      cur.n -= (t - start) * KEYS;
+      cur.n -= (t - start) * KT;
       lim = limit(cur);
     }
     for (; t < t1; ++t) {
       const bool check = cur.seg >= 0 && partly;
-      u32* const here = kinds + 3 * (t % 3);
+      u32* const here = kinds + KINDS * (t % 3);
       const char* const at = next_stage(check ? here : nullptr);
       load(freed());
       if (check) {
-        if (here[0] | here[1] | here[2]) taint += taint_of(here, lim);
+        u32 any = 0;
+#pragma unroll
+        for (int i = 0; i < KINDS; ++i) any |= here[i];
+        if (any) taint += taint_of<KT>(here, lim);
         // read last before this tile's barrier, noted in first after the next one's
-        if (tid < 3) kinds[3 * ((t + 2) % 3) + tid] = 0;
+        if (tid < KINDS) kinds[KINDS * ((t + 2) % 3) + tid] = 0;
       }
       if (have) ST::weigh(x, at + TL::BYTES, s, l.qscale);
       if (t + 1 < t1) {
@@ -636,7 +668,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(NW == 8
         lim = limit(cur);
         have = __any(lim > 0);
         if (have) {
-          s = ST::scores(at, q);
+          ST::scores(at, q, s);
           ST::settle(x, ST::mask_max(s, lim, l.qscale));
         }
       }
@@ -693,16 +725,18 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(NW == 8
   else leave(std::false_type{});
 }
 
-// Join of a row's ranges, one wave per row: the ranges' sums brought to their largest reference.
-template <typename T, int DH>
+// Join of a row's ranges: the ranges' sums brought to their largest reference.  WPR waves a row, each for a part of the
+// ranges: with one, 64 ranges of few rows are eight trips to memory one after another.
+template <typename T, int DH, int WPR>
 __global__ __launch_bounds__(256) void k_shared_merge(SharedLaunch l) {
-  constexpr int N = DH / 64;
+  constexpr int N = DH / 64, RPW = 4 / WPR;
   typedef float vec __attribute__((ext_vector_type(N)));
   typedef T tvec __attribute__((ext_vector_type(N)));
+  __shared__ vec parts[WPR > 1 ? WPR : 1][64];
   const int64_t rows = (int64_t)l.n_groups * l.group * l.q_rows * l.n_heads;
-  const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (row >= rows) return;
-  const int lane = threadIdx.x & 63;
+  const int lane = threadIdx.x & 63, w = uniform(threadIdx.x >> 6), share = w % WPR;
+  const int64_t row = (int64_t)blockIdx.x * RPW + w / WPR;
+  if (row >= rows) return;  // WPR == 4: all of the workgroup
   const float2 st = lane < l.splits ? l.stats[lane * rows + row] : float2{-INFINITY, 0.f};  // at most 64 ranges
   const float m = wave_max(st.x);
   const float f = st.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(st.x - m);
@@ -711,17 +745,27 @@ __global__ __launch_bounds__(256) void k_shared_merge(SharedLaunch l) {
   vec o;
 #pragma unroll
   for (int e = 0; e < N; ++e) o[e] = 0.f;
-  constexpr int U = 8;
-  for (int s = 0; s < l.splits; s += U) {
+  constexpr int U = 4;  // loads in flight; where fewer ranges are left, the last one again
+  const int s0 = share * l.splits / WPR, s1 = (share + 1) * l.splits / WPR;
+  const float* const at = l.part + row * DH + lane * N;
+  for (int s = s0; s < s1; s += U) {
     vec v[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (there >> (s + u < 64 ? s + u : 63) & 1 && s + u < l.splits)
-        v[u] = *reinterpret_cast<const vec*>(l.part + ((s + u) * rows + row) * DH + lane * N);
+    for (int u = 0; u < U; ++u) v[u] = *reinterpret_cast<const vec*>(at + min(s + u, s1 - 1) * rows * DH);
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (there >> (s + u < 64 ? s + u : 63) & 1 && s + u < l.splits)
-        o += __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, f), s + u)) * v[u];
+    for (int u = 0; u < U; ++u) {
+      const bool on = s + u < s1 && (there >> (s + u) & 1);
+      const float g = on ? __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, f), min(s + u, 63))) : 0.f;
+#pragma unroll
+      for (int e = 0; e < N; ++e) o[e] = fmaf(g, on ? v[u][e] : 0.f, o[e]);
+    }
+  }
+  if constexpr (WPR > 1) {
+    parts[share][lane] = o;
+    __syncthreads();
+    if (share) return;
+#pragma unroll
+    for (int i = 1; i < WPR; ++i) o += parts[i][lane];
   }
   const float inv = m == -INFINITY ? 0.f : 1.f / sum;
   const int h = (int)(row % l.n_heads);
@@ -755,16 +799,16 @@ constexpr int WEIGHT_ROWS = 2048;  // rows of a range at most
 
 template <typename T, int DH>
 struct WeightShape {
-  using TL = Tile<T, DH>;
+  using TL = Tile<T, DH, 32>;
   static constexpr int KT = sizeof(T) == 4 && DH == 256 ? 1 : 2;  // 32-key tiles of a wave
-  static constexpr int KEYS_WG = KEYS * KT * WEIGHT_WAVES;
+  static constexpr int KEYS_WG = 32 * KT * WEIGHT_WAVES;
   static constexpr int NS = 4;                                    // stages of rows; the same memory first takes the keys
   static constexpr int LOADS = TL::PIECES / WEIGHT_WAVES;         // of one wave and stage
 };
 
 template <typename T, int DH>
 __global__ __launch_bounds__(64 * WEIGHT_WAVES) void k_weight(WeightLaunch l) {
-  using TL = Tile<T, DH>;
+  using TL = Tile<T, DH, 32>;
   using WS = WeightShape<T, DH>;
   constexpr int NW = WEIGHT_WAVES, NS = WS::NS, KT = WS::KT;
   static_assert(NW == 4 && NS >= NW, "a wave's pieces are eight rows of all chunks; each wave stages its keys");
@@ -784,35 +828,35 @@ __global__ __launch_bounds__(64 * WEIGHT_WAVES) void k_weight(WeightLaunch l) {
   };
 
   // keys into registers, by way of LDS so that whole lines are asked for
-  const int key0 = kt * WS::KEYS_WG + w * KEYS * KT;
+  const int key0 = kt * WS::KEYS_WG + w * 32 * KT;
   typename TL::chunk key[KT][TL::KS];
 #pragma unroll
   for (int u = 0; u < KT; ++u) {
 #pragma unroll
     for (int f = 0; f < TL::PIECES; ++f) {
-      const int r = min(key0 + u * KEYS + 8 * (f & 3) + TL::row(lane), plen - 1);
-      load(a.kp.data + g * a.kp.outer + kv * a.kp.head + (int64_t)r * a.kp.row + (8 * (f >> 2) + TL::col(f, lane)) * 16,
+      const int r = min(key0 + u * 32 + 8 * (f & 3) + TL::row(lane), plen - 1);
+      load(a.kp.data + g * a.kp.outer + kv * a.kp.head + (int64_t)r * a.kp.row + (8 * (f >> 2) + TL::col(f & 3, lane)) * 16,
            ring + w * TL::BYTES + f * 1024);
     }
     wait_vm<0>();
     asm volatile("" ::: "memory");
 #pragma unroll
     for (int k = 0; k < TL::KS; ++k)
-      key[u][k] = *reinterpret_cast<const typename TL::chunk*>(lds + w * TL::BYTES + TL::base(lane, k & 3) + TL::step(k));
+      key[u][k] = *reinterpret_cast<const typename TL::chunk*>(lds + w * TL::BYTES + TL::base(lane, k & 3) + TL::step(k, 0));
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
   }
 
-  const int n_rows = a.group * a.q_rows * a.per_kv, tiles = (n_rows + KEYS - 1) / KEYS;
+  const int n_rows = a.group * a.q_rows * a.per_kv, tiles = (n_rows + 32 - 1) / 32;
   const int t0 = (int)((int64_t)split * tiles / a.splits), t1 = (int)((int64_t)(split + 1) * tiles / a.splits);
-  for (int r = tid; r < (t1 - t0) * KEYS; r += 64 * NW) {
-    const Row x = row_of(a, g, kv, t0 * KEYS + r);
+  for (int r = tid; r < (t1 - t0) * 32; r += 64 * NW) {
+    const Row x = row_of(a, g, kv, t0 * 32 + r);
     const float v = x.b >= 0 ? l.lse[((int64_t)x.b * a.q_rows + x.i) * a.n_heads + x.h] : -INFINITY;
     lse2[r] = v == -INFINITY ? -INFINITY : -v * LOG2E;  // rows that see nothing, or are none, add 2^-inf
   }
   __syncthreads();
 
   auto rows = [&](int t, int stage) __attribute__((always_inline)) {  // past the last tile: the last row again
-    const Row x = row_of(a, g, kv, min(t * KEYS + 8 * w + TL::row(lane), n_rows - 1));
+    const Row x = row_of(a, g, kv, min(t * 32 + 8 * w + TL::row(lane), n_rows - 1));
     const char* p = a.q.data + x.b * a.q.outer + x.i * a.q.row + x.h * a.q.head + TL::col(w, lane) * 16;
 #pragma unroll
     for (int i = 0; i < WS::LOADS; ++i) load(p + i * 128, ring + stage * TL::BYTES + (w + NW * i) * 1024);
@@ -836,13 +880,13 @@ __global__ __launch_bounds__(64 * WEIGHT_WAVES) void k_weight(WeightLaunch l) {
       for (int r = 0; r < 16; ++r) s[u][r] = 0.f;
 #pragma unroll
     for (int k = 0; k < TL::KS; ++k) {
-      const auto x = *reinterpret_cast<const typename TL::chunk*>(at + TL::base(lane, k & 3) + TL::step(k));
+      const auto x = *reinterpret_cast<const typename TL::chunk*>(at + TL::base(lane, k & 3) + TL::step(k, 0));
 #pragma unroll
       for (int u = 0; u < KT; ++u) s[u] = mfma_chunk<T>(x, key[u][k], s[u]);
     }
     f32x4 e[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) e[j] = *reinterpret_cast<const f32x4*>(&lse2[(t - t0) * KEYS + 8 * j + 4 * half]);
+    for (int j = 0; j < 4; ++j) e[j] = *reinterpret_cast<const f32x4*>(&lse2[(t - t0) * 32 + 8 * j + 4 * half]);
 #pragma unroll
     for (int u = 0; u < KT; ++u)
 #pragma unroll
@@ -852,7 +896,7 @@ __global__ __launch_bounds__(64 * WEIGHT_WAVES) void k_weight(WeightLaunch l) {
 #pragma unroll
   for (int u = 0; u < KT; ++u) {
     const float x = halves_sum(sum[u][0] + sum[u][1]);
-    const int j = key0 + u * KEYS + col;
+    const int j = key0 + u * 32 + col;
     if (half || j >= plen) continue;
     const int64_t at = (int64_t)gk * a.prefix + j;
     if (l.part) l.part[(int64_t)split * a.n_groups * a.n_kv * a.prefix + at] = x;
@@ -915,28 +959,30 @@ struct Plan {
   int waves, row_tiles, splits;
 };
 
-// Waves (32 rows each) of a workgroup and ranges of the key sequence, by estimated time.  A workgroup of most shapes fills
-// a compute unit's LDS, so workgroups beyond one per unit wait for another round.  Microseconds measured on 256 units:
-// a tile takes about 0.003 per element of a row in bf16 (0.75 at 256, 0.45 at 128) and 0.027 in fp32, the rest of a
-// workgroup 12; joining ranges takes a launch, 5, and writing and reading their sums, 3 bytes a picosecond.
+// Waves (32 rows each) of a workgroup and ranges of the key sequence, by estimated time.  A workgroup fills a compute
+// unit's LDS, so workgroups beyond one per unit wait for another round.  Microseconds, fitted to heads of 64 to 256 on 256
+// units (estimates within a fifth of what was measured): a tile takes 0.9 + 0.002 of head_dim in bf16, four tenths more
+// where waves share matrix cores, and 0.4 + 0.022 of head_dim in fp32; the rest of a workgroup 12; joining ranges a launch,
+// 4, and their sums, written and read, 6.6 TB/s.  Lengths are on the device: the slots count, and all tails as full.
 Plan shared_plan(const jpi_shared_attn& a) {
   const double n_cu = 256;
-  const int64_t rows = (int64_t)a.group * a.q_rows * (a.n_heads / a.n_kv_heads);
-  const int64_t tiles = (a.prefix + KEYS - 1) / KEYS + (a.suffix + KEYS - 1) / KEYS;
-  const double all = (double)a.n_groups * a.group * a.q_rows * a.n_heads;
-  const double tile_us = 0.1 + (a.dtype == JPI_BF16 ? 0.0026 : 0.027) * a.head_dim;
-  // eight waves share a unit's matrix cores two by two; their rings hold two of the pieces of a tile of 64 bf16 elements
-  const int most = a.head_dim == 256 || (a.dtype == JPI_BF16 && a.head_dim == 64) ? 4 : 8;
+  const bool half = a.dtype == JPI_BF16;
+  const int64_t per_rollout = (int64_t)a.q_rows * (a.n_heads / a.n_kv_heads), rows = a.group * per_rollout;
+  const int keys = half ? KEYS<bf16> : KEYS<float>;
+  const int64_t prefix = (a.prefix + keys - 1) / keys, tail = (a.suffix + keys - 1) / keys;
+  const double all_mb = (double)a.n_groups * rows * a.n_kv_heads * a.head_dim * 4e-6;
+  const int most = a.head_dim == 256 ? 4 : 8;  // eight waves share a unit's matrix cores and registers two by two
   Plan best{};
   double best_us = 1e30;
   for (int w = 1; w <= most; w *= 2) {
     if (w > 1 && 32 * (w / 2) >= rows) break;
     const int64_t row_tiles = (rows + 32 * w - 1) / (32 * w), items = (int64_t)a.n_groups * a.n_kv_heads * row_tiles;
+    const int64_t rollouts = std::min<int64_t>(a.group, (32 * w + per_rollout - 1) / per_rollout);
+    const double tiles = (double)prefix + (double)TAIL_COST * tail * rollouts;
+    const double tile_us = (half ? 0.9 + 0.002 * a.head_dim : 0.4 + 0.022 * a.head_dim) * (w == 8 ? 1.4 : 1.0);
     for (const int s : {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 48, 64}) {
-      if (s > 1 && s > tiles) break;
-      const double rounds = ceil(items * s / n_cu);
-      const double us = rounds * (((tiles + s - 1) / s) * tile_us * (w == 8 ? 1.5 : 1.0) + 12) +
-                        (s > 1 ? 5 + all * s * a.head_dim * 8 / 3e6 : 0);
+      if (s > 1 && s > prefix + tail) break;
+      const double us = ceil(items * s / n_cu) * (ceil(tiles / s) * tile_us + 12) + (s > 1 ? 4 + all_mb * s / 3.3 : 0);
       if (us < best_us) best_us = us, best = Plan{w, (int)row_tiles, s};
     }
   }
@@ -945,13 +991,13 @@ Plan shared_plan(const jpi_shared_attn& a) {
 
 // Key blocks of a workgroup, and ranges of rows: enough workgroups for two on each unit, ranges of at most WEIGHT_ROWS.
 Plan weight_plan(const jpi_shared_attn& a) {
-  const int64_t rows = (int64_t)a.group * a.q_rows * (a.n_heads / a.n_kv_heads), tiles = (rows + KEYS - 1) / KEYS;
-  const int keys = KEYS * (a.dtype == JPI_F32 && a.head_dim == 256 ? 1 : 2) * WEIGHT_WAVES;
+  const int64_t rows = (int64_t)a.group * a.q_rows * (a.n_heads / a.n_kv_heads), tiles = (rows + 32 - 1) / 32;
+  const int keys = 32 * (a.dtype == JPI_F32 && a.head_dim == 256 ? 1 : 2) * WEIGHT_WAVES;
   Plan p{};
   p.waves = WEIGHT_WAVES;
   p.row_tiles = (a.prefix + keys - 1) / keys;
   const int64_t items = (int64_t)a.n_groups * a.n_kv_heads * p.row_tiles;
-  const int64_t least = (tiles + WEIGHT_ROWS / KEYS - 1) / (WEIGHT_ROWS / KEYS);
+  const int64_t least = (tiles + WEIGHT_ROWS / 32 - 1) / (WEIGHT_ROWS / 32);
   p.splits = items ? (int)std::max(least, std::min<int64_t>({64, 512 / items, tiles})) : 1;
   if (p.splits < 1) p.splits = 1;
   return p;
@@ -976,12 +1022,13 @@ hipError_t shared_typed(const jpi_shared_attn& a, void* ws, hipStream_t s) {
     case 2: k_shared<T, DH, 2><<<grid, 128, 0, s>>>(l); break;
     case 4: k_shared<T, DH, 4><<<grid, 256, 0, s>>>(l); break;
     default:
-      if constexpr (Tile<T, DH>::PIECES % 8 == 0 && DH < 256) k_shared<T, DH, 8><<<grid, 512, 0, s>>>(l);
+      if constexpr (DH < 256) k_shared<T, DH, 8><<<grid, 512, 0, s>>>(l);
       break;
   }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.splits == 1) return e;
-  k_shared_merge<T, DH><<<(unsigned)((rows + 3) / 4), 256, 0, s>>>(l);
+  if (p.splits > 8) k_shared_merge<T, DH, 4><<<(unsigned)rows, 256, 0, s>>>(l);
+  else k_shared_merge<T, DH, 1><<<(unsigned)((rows + 3) / 4), 256, 0, s>>>(l);
   return hipGetLastError();
 }
 
