@@ -114,6 +114,12 @@ struct View {
   int64_t outer, row, head;  // bytes
 };
 
+// n / d for n < 2^31 by a product (round-up method: m = floor(2^32 (2^s - d) / d) + 1 with 2^s >= d)
+struct Divisor {
+  u32 d, m, s;
+  __device__ __forceinline__ u32 of(u32 n) const { return (__umulhi(n, m) + n) >> s; }
+};
+
 struct SharedLaunch {
   View q, kp, vp, ks, vs, out;
   const int32_t *plen, *slen;
@@ -122,6 +128,7 @@ struct SharedLaunch {
   float2* stats;  // [splits][rows in all]: its reference and sum of p
   int n_groups, group, q_rows, n_heads, n_kv, per_kv, prefix, suffix;
   int causal, splits, row_tiles;
+  Divisor by_kv_heads, by_rows, by_splits, by_tiles, by_rollout;  // per_kv, q_rows, splits, row_tiles, q_rows * per_kv
   float qscale;  // scale * log2(e): scores in powers of two
 };
 
@@ -131,7 +138,7 @@ struct Row {
 };
 __device__ __forceinline__ Row row_of(const SharedLaunch& l, int g, int kv, int r) {
   if (r >= l.group * l.q_rows * l.per_kv) return Row{-1, 0, 0};
-  const int qi = (int)((unsigned)r / (unsigned)l.per_kv), bl = (int)((unsigned)qi / (unsigned)l.q_rows);
+  const int qi = (int)l.by_kv_heads.of(r), bl = (int)l.by_rows.of(qi);
   return Row{g * l.group + bl, qi - bl * l.q_rows, kv * l.per_kv + r - qi * l.per_kv};
 }
 
@@ -385,7 +392,7 @@ struct Steps {
 // Loads of a ring stage, K of a tile and V of the tile before it (whose probabilities are formed while the scores of the
 // next are), piece f of the two by wave f % NW, as direct-to-LDS loads (16 bytes of
 // each lane, written lane after lane; the order inside a piece is made by what each lane asks for).  Every stage has the
-// same number of loads, past the last tile too, so that waits can count them.
+// same number of loads, so that waits can count them.
 template <typename T, int DH, int NW>
 struct Ring {
   using TL = Tile<T, DH, KEYS<T>>;
@@ -472,14 +479,15 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(NW == 8
   // items (group, KV head, range, row tile): row tiles of one range are neighbours, and neighbours share an XCD's L2
   const int item = (int)(blockIdx.x % 8) * (int)(gridDim.x / 8) + (int)(blockIdx.x / 8);
   if (item >= l.n_groups * l.n_kv * l.splits * l.row_tiles) return;
-  const int rt = item % l.row_tiles, split = item / l.row_tiles % l.splits, gk = item / (l.row_tiles * l.splits);
+  const int by_tile = (int)l.by_tiles.of(item), rt = item - by_tile * l.row_tiles;
+  const int gk = (int)l.by_splits.of(by_tile), split = by_tile - gk * l.splits;
   const int g = gk / l.n_kv, kv = gk - g * l.n_kv;
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, half = lane >> 5;
   const int n_rows = l.group * l.q_rows * l.per_kv, r0 = rt * ROWS;
 
   // lengths and queries are asked for together
-  const int b0 = g * l.group + r0 / (l.q_rows * l.per_kv);
-  const int nb = l.suffix ? g * l.group + (min(r0 + ROWS, n_rows) - 1) / (l.q_rows * l.per_kv) - b0 + 1 : 0;
+  const int first = (int)l.by_rollout.of(r0), b0 = g * l.group + first;
+  const int nb = l.suffix ? (int)l.by_rollout.of(min(r0 + ROWS, n_rows) - 1) - first + 1 : 0;
   const int prefix_len = clamp_len(l.plen, g, l.prefix);
   const int some_len = tid < nb ? clamp_len(l.slen, b0 + tid, l.suffix) : 0;
   typename TL::chunk q[TL::KS];
@@ -566,24 +574,23 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(NW == 8
     Source ks{cur, t0}, vs{cur, t0 - 1};
     open(ks, true);
     open(vs, false);
-    auto prepare = [&](int stage) __attribute__((always_inline)) {  // K and V of nothing before the first tile and past the last one
-      const auto x = RG::prepare((u32)(uintptr_t)(dma_lds_t*)lds + stage * RG::STAGE, ks.p, ks.stride,
-                                 ks.tile < t1 ? min(ks.at.n, KT) : 0, vs.p, vs.stride,
-                                 vs.tile >= t0 && vs.tile < t1 ? min(vs.at.n, KT) : 0);
+    // One stage more, as long as V of some tile is to come: K of nothing past the last tile, V of nothing before the first.
+    auto load = [&](int stage) __attribute__((always_inline)) {
+      if (vs.tile >= t1) return;
+      const auto y = RG::prepare((u32)(uintptr_t)(dma_lds_t*)lds + stage * RG::STAGE, ks.p, ks.stride,
+                                 ks.tile < t1 ? min(ks.at.n, KT) : 0, vs.p, vs.stride, vs.tile >= t0 ? min(vs.at.n, KT) : 0);
+#pragma unroll
+      for (int u = 0; u < RG::LOADS; ++u) RG::one(y, u);
       advance(ks, true);
       advance(vs, false);
-      return x;
-    };
-    auto load = [&](int stage) __attribute__((always_inline)) {
-      const auto x = prepare(stage);
-#pragma unroll
-      for (int u = 0; u < RG::LOADS; ++u) RG::one(x, u);
     };
     for (int u = 0; u < NS - 1; ++u) load(u);
-    int stage = 0;
+    int stage = 0, taken = 0;
     const bool partly = nb > 1 || l.causal;  // rows may not see all of a tail's tile
-    auto next_stage = [&](u32* here = nullptr) __attribute__((always_inline)) -> char* {
-      wait_vm<(NS - 2) * RG::LOADS>();
+    auto next_stage = [&](auto full_ring, u32* here) __attribute__((always_inline)) -> char* {
+      // of the stages asked for, vs.tile - (t0 - 1), those after the next one may still be on their way
+      if constexpr (decltype(full_ring)::value) wait_vm<(NS - 2) * RG::LOADS>();
+      else wait_later<RG::LOADS, NS - 2>(vs.tile - t0 - taken);
       if (here) {
         take_out<T, DH, NW>(lds + stage * RG::STAGE + TL::BYTES + tid * 16, here);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -594,8 +601,10 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(NW == 8
       asm volatile("" ::: "memory");
       char* const at = lds + stage * RG::STAGE;
       stage = stage == NS - 1 ? 0 : stage + 1;
+      ++taken;
       return at;
     };
+    const std::false_type some{};
     auto freed = [&]() { return stage < 2 ? stage + NS - 2 : stage - 2; };  // the stage before the one just taken
     auto limit = [&](const Walk& y) { return y.seg < 0 ? y.n : own_b == b0 + y.seg ? y.n + own_lim : 0; };
 
@@ -603,7 +612,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(NW == 8
     int lim = limit(cur);
     bool have = __any(lim > 0);  // whether some row sees a key of the tile: its scores are in s
     {
-      const char* const at = next_stage();
+      const char* const at = next_stage(some, nullptr);
       load(freed());
       if (have) {
         ST::scores(at, q, s);
@@ -619,7 +628,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(NW == 8
         const u32 first = is.to, k_step = KT * ks.stride, v_step = KT * vs.stride;
         const int run = full - ks.tile;  // t + run < full: a tile of K is loaded before its scores are wanted
         for (int r = 0; r < run; ++r) {
-          const char* const at = next_stage();
+          const char* const at = next_stage(std::true_type{}, nullptr);
           is.to = first + freed() * RG::STAGE;
           ST::both(x, at + TL::BYTES, at, q, s, l.qscale, [&](int i) __attribute__((always_inline)) {
 #pragma unroll
@@ -639,12 +648,9 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(NW == 8
         }
       }
       for (; t + 1 < full; ++t) {
-        const char* const at = next_stage();
-        const auto is = prepare(freed());
-        ST::both(x, at + TL::BYTES, at, q, s, l.qscale, [&](int i) __attribute__((always_inline)) {
-#pragma unroll
-          for (int u = i * RG::LOADS / ST::PV; u < (i + 1) * RG::LOADS / ST::PV; ++u) RG::one(is, u);
-        });
+        const char* const at = next_stage(some, nullptr);
+        load(freed());
+        ST::both(x, at + TL::BYTES, at, q, s, l.qscale, [](int) {});
       }
       cur.n -= (t - start) * KT;
       lim = limit(cur);
@@ -652,7 +658,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(NW == 8
     for (; t < t1; ++t) {
       const bool check = cur.seg >= 0 && partly;
       u32* const here = kinds + KINDS * (t % 3);
-      const char* const at = next_stage(check ? here : nullptr);
+      const char* const at = next_stage(some, check ? here : nullptr);
       load(freed());
       if (check) {
         u32 any = 0;
@@ -707,18 +713,28 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(NW == 8
   constexpr int RW = 64 / CH;       // rows of one store
   const int c = lane % CH, sub = lane / CH;
   auto leave = [&](auto part) __attribute__((always_inline)) {
-#pragma unroll 8
-    for (int r = 0; r < 32; r += RW) {
-      const f32x4 y = mine[(r + sub) * CH + (c ^ ((r + sub) & 15))];
-      int64_t to = 0;
+    constexpr int U = 8;
+#pragma unroll 1
+    for (int r0 = 0; r0 < 32; r0 += U * RW) {
+      f32x4 y[U];
 #pragma unroll
-      for (int j = 0; j < RW; ++j) {
-        const u32 lo = __builtin_amdgcn_readlane((u32)base, r + j), hi = __builtin_amdgcn_readlane((u32)((uint64_t)base >> 32), r + j);
-        if (sub == j) to = (int64_t)((uint64_t)hi << 32 | lo);
+      for (int u = 0; u < U; ++u) {
+        const int r = r0 + u * RW + sub;
+        y[u] = mine[r * CH + (c ^ (r & 15))];
       }
-      if (to == 0) continue;
-      if constexpr (decltype(part)::value) *reinterpret_cast<f32x4*>(to + c * 16) = y;
-      else *reinterpret_cast<quad*>(to + c * 4 * sizeof(T)) = quad{from_f32<T>(y[0]), from_f32<T>(y[1]), from_f32<T>(y[2]), from_f32<T>(y[3])};
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        int64_t to = 0;
+#pragma unroll
+        for (int j = 0; j < RW; ++j) {
+          const int r = r0 + u * RW + j;
+          const u32 lo = __builtin_amdgcn_readlane((u32)base, r), hi = __builtin_amdgcn_readlane((u32)((uint64_t)base >> 32), r);
+          if (sub == j) to = (int64_t)((uint64_t)hi << 32 | lo);
+        }
+        if (to == 0) continue;
+        if constexpr (decltype(part)::value) *reinterpret_cast<f32x4*>(to + c * 16) = y[u];
+        else *reinterpret_cast<quad*>(to + c * 4 * sizeof(T)) = quad{from_f32<T>(y[u][0]), from_f32<T>(y[u][1]), from_f32<T>(y[u][2]), from_f32<T>(y[u][3])};
+      }
     }
   };
   if (l.part) leave(std::true_type{});
@@ -930,6 +946,12 @@ View view_of(const jpi_view& v, int es) {
   return View{(const char*)v.data, v.outer * es, v.row * es, v.head * es};
 }
 
+Divisor divisor(int64_t d) {
+  u32 s = 0;
+  while (((int64_t)1 << s) < d) ++s;
+  return Divisor{(u32)d, (u32)((((uint64_t)1 << 32) * (((uint64_t)1 << s) - d)) / d + 1), s};
+}
+
 SharedLaunch launch_of(const jpi_shared_attn& a) {
   const int es = a.dtype == JPI_BF16 ? 2 : 4;
   SharedLaunch l{};
@@ -952,6 +974,9 @@ SharedLaunch launch_of(const jpi_shared_attn& a) {
   l.suffix = a.suffix;
   l.causal = a.causal != 0;
   l.qscale = a.scale * LOG2E;
+  l.by_kv_heads = divisor(l.per_kv);
+  l.by_rows = divisor(l.q_rows);
+  l.by_rollout = divisor((int64_t)l.q_rows * l.per_kv);
   return l;
 }
 
@@ -1011,6 +1036,8 @@ hipError_t shared_typed(const jpi_shared_attn& a, void* ws, hipStream_t s) {
   SharedLaunch l = launch_of(a);
   l.splits = p.splits;
   l.row_tiles = p.row_tiles;
+  l.by_splits = divisor(p.splits);
+  l.by_tiles = divisor(p.row_tiles);
   const int64_t rows = (int64_t)a.n_groups * a.group * a.q_rows * a.n_heads;
   if (p.splits > 1) {
     l.part = (float*)ws;
