@@ -25,20 +25,14 @@ _I32, _F32 = torch.int32, torch.float32
 _lib = _j._lib
 
 # The C structures as bytes, which cost a small call a third of what a ctypes structure filled field by field does
-_VIEW = "Pqqq"
+_V = "Pqqq"
+_VIEW = struct.Struct("@" + _V)
 _ROPE = struct.Struct("@5i6d")
-_ROPE_VIEWS = struct.Struct("@" + _VIEW * 4)
-_ATTN = struct.Struct("@10if" + _VIEW * 5 + "PP" + _VIEW + "P")
-_EVICT = struct.Struct("@8iPqP" + _VIEW * 4 + "PqPP")
-assert (_ROPE.size, _ROPE_VIEWS.size, _ATTN.size, _EVICT.size) == (
-    ctypes.sizeof(_j.jpi_rope_config), 4 * ctypes.sizeof(_j.jpi_view), ctypes.sizeof(_j.jpi_shared_attn),
-    ctypes.sizeof(_j.jpi_evict_args))
+_ATTN = struct.Struct("@10if" + _V * 5 + "PP" + _V + "P")
+_EVICT = struct.Struct("@8iPqP" + _V * 4 + "PqPP")
+assert (_ROPE.size, _VIEW.size, _ATTN.size, _EVICT.size) == tuple(
+    ctypes.sizeof(c) for c in (_j.jpi_rope_config, _j.jpi_view, _j.jpi_shared_attn, _j.jpi_evict_args))
 _NONE = (0, 0, 0, 0)
-
-
-def _check(status):
-    if status != _j.JPI_OK:
-        raise _j.JpiError(status, _j.jpi_prefix_last_error())
 
 
 def _dtype(t):
@@ -73,24 +67,20 @@ def _dense(name, t):
     return t.data_ptr()
 
 
-class _On:
-    """GPU `dev` made current for a call, where it is not; the handle of its current stream."""
-    __slots__ = ("dev", "guard")
+_current_device, _raw_stream = getattr(torch._C, "_cuda_getDevice", None), getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
-    def __init__(self, dev):
-        if dev < 0:
-            raise ValueError("tensors must be on the GPU")
-        self.dev = dev
-        self.guard = None if dev == torch.cuda.current_device() else torch.cuda.device(dev)
 
-    def __enter__(self):
-        if self.guard is not None:
-            self.guard.__enter__()
-        return torch._C._cuda_getCurrentRawStream(self.dev)
-
-    def __exit__(self, *e):
-        if self.guard is not None:
-            self.guard.__exit__(*e)
+def _launch(dev, f, *args):
+    """f of the library on the current stream of GPU `dev`, which is made current for the call where it is not."""
+    if dev < 0:
+        raise ValueError("tensors must be on the GPU")
+    if dev == _current_device():
+        status = f(*args, _raw_stream(dev))
+    else:
+        with torch.cuda.device(dev):
+            status = f(*args, _raw_stream(dev))
+    if status != _j.JPI_OK:
+        raise _j.JpiError(status, _j.jpi_prefix_last_error())
 
 
 def rope(q, k=None, positions=None, *, rot_dim=None, layout="half", base=1e4, scaling="none", factor=1.0, trained=0,
@@ -113,8 +103,8 @@ def rope(q, k=None, positions=None, *, rot_dim=None, layout="half", base=1e4, sc
     elif q_out is not q:
         _want("q_out", q_out, q.shape, q.dtype, dev)
     if k is None:
-        kv = ko = _NONE
-        k_heads, k_out = 0, None
+        kv = ko = k_out = None
+        k_heads = 0
     else:
         k_heads = k.shape[2] if k.dim() == 4 else 0
         _want("k", k, (b, n, k_heads, dh), q.dtype, dev)
@@ -122,7 +112,10 @@ def rope(q, k=None, positions=None, *, rot_dim=None, layout="half", base=1e4, sc
             k_out = torch.empty_like(k, memory_format=torch.contiguous_format)
         elif k_out is not k:
             _want("k_out", k_out, k.shape, q.dtype, dev)
-        kv, ko = _view("k", k), _view("k_out", k_out)
+        if k_heads:
+            kv, ko = _VIEW.pack(*_view("k", k)), _VIEW.pack(*_view("k_out", k_out))
+        else:
+            kv = ko = None
     pos, pos_stride = None, 0
     if positions is not None:
         if positions.dim() == 2:
@@ -133,11 +126,9 @@ def rope(q, k=None, positions=None, *, rot_dim=None, layout="half", base=1e4, sc
         if n > 1 and positions.stride(-1) != 1:
             raise ValueError("positions of a batch row must be contiguous")
         pos = positions.data_ptr()
-    views = ctypes.create_string_buffer(_ROPE_VIEWS.pack(*_view("q", q), *_view("q_out", q_out), *kv, *ko), 128)
-    at = ctypes.addressof(views)
-    with _On(dev) as stream:
-        _check(_lib.jpi_rope(cfg, dt, b, n, pos, pos_stride, at, at + 32, heads, at + 64 if k_heads else None,
-                             at + 96 if k_heads else None, k_heads, stream))
+    pack = _VIEW.pack
+    _launch(dev, _lib.jpi_rope, cfg, dt, b, n, pos, pos_stride, pack(*_view("q", q)), pack(*_view("q_out", q_out)), heads, kv, ko,
+            k_heads)
     return q_out, k_out
 
 
@@ -160,11 +151,13 @@ def _lens(name, t, n, dev):
     return _dense(name, t)
 
 
-def _workspace(size_of, args, dev):
+def _workspace(size_of, args, q):
     n = ctypes.c_size_t()
-    _check(size_of(args, ctypes.byref(n)))
+    status = size_of(args, ctypes.byref(n))
+    if status != _j.JPI_OK:
+        raise _j.JpiError(status, _j.jpi_prefix_last_error())
     n = n.value
-    return (torch.empty(n, dtype=torch.uint8, device=dev), n) if n else (None, 0)
+    return (torch.empty(n, dtype=torch.uint8, device=q.device), n) if n else (None, 0)
 
 
 def shared_attention(q, k_prefix, v_prefix, k_suffix=None, v_suffix=None, *, prefix_len=None, suffix_len=None, causal=False,
@@ -203,9 +196,8 @@ def shared_attention(q, k_prefix, v_prefix, k_suffix=None, v_suffix=None, *, pre
                       *_view("q", q), *_view("k_prefix", k_prefix), *_view("v_prefix", v_prefix), *ks, *vs,
                       _lens("prefix_len", prefix_len, g, dev), _lens("suffix_len", suffix_len, b, dev), *_view("out", out),
                       _dense("lse", lse))
-    with _On(dev) as stream:
-        ws, n = _workspace(_lib.jpi_shared_attention_workspace, args, q.device)
-        _check(_lib.jpi_shared_attention(args, ws.data_ptr() if n else None, n, stream))
+    ws, n = _workspace(_lib.jpi_shared_attention_workspace, args, q)
+    _launch(dev, _lib.jpi_shared_attention, args, ws.data_ptr() if n else None, n)
     return out, lse
 
 
@@ -230,9 +222,8 @@ def prefix_weight(q, k_prefix, lse, weight=None, *, prefix_len=None, decay=1.0, 
     args = _ATTN.pack(dt, g, b // g, rows, heads, kv, dh, p, 0, 0, dh ** -0.5 if scale is None else scale, *_view("q", q),
                       *_view("k_prefix", k_prefix), *_NONE, *_NONE, *_NONE, _lens("prefix_len", prefix_len, g, dev), 0, *_NONE,
                       _dense("lse", lse))
-    with _On(dev) as stream:
-        ws, n = _workspace(_lib.jpi_prefix_weight_workspace, args, q.device)
-        _check(_lib.jpi_prefix_weight(args, w, decay, _dense("out", out), ws.data_ptr() if n else None, n, stream))
+    ws, n = _workspace(_lib.jpi_prefix_weight_workspace, args, q)
+    _launch(dev, _lib.jpi_prefix_weight, args, w, decay, _dense("out", out), ws.data_ptr() if n else None, n)
     return out
 
 
@@ -277,6 +268,5 @@ def evict(k, v, weight, keep, *, lens=None, n_first=0, n_last=0, k_out=None, v_o
     args = _EVICT.pack(dt, n, heads, dh, slots, keep, n_first, n_last, _dense("weight", weight), slots, _lens("lens", lens, n, dev),
                        *_view("k", k), *_view("v", v), *_view("k_out", k_out), *_view("v_out", v_out),
                        _dense("weight_out", weight_out), weight_out.shape[2], _dense("index", index), _dense("lens_out", lens_out))
-    with _On(dev) as stream:
-        _check(_lib.jpi_evict(args, stream))
+    _launch(dev, _lib.jpi_evict, args)
     return index, lens_out
