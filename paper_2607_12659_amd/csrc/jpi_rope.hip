@@ -9,6 +9,8 @@
 // which for position 10^5 is 6e-3 radians; here the angle is formed in turns in
 // fp64 (position exact, f_i / 2 pi to 2^-52), reduced to [-1/2, 1/2] turns there,
 // and only then rounded to fp32 for sincospi.
+#include <algorithm>
+
 #include "jpi_device.h"
 #include "jpi_prefix_internal.h"
 
@@ -64,10 +66,10 @@ struct Piece {
 
 // A unit is N elements of a head, with JPI_ROPE_HALF and their N partners half a rotation further on.
 template <typename T, int N, bool VEC, bool INTER>
-__global__ __launch_bounds__(ROPE_THREADS) void k_rope(RopeLaunch l, int n_tok, int tile) {
+__global__ __launch_bounds__(ROPE_THREADS) void k_rope(RopeLaunch l, int first, int n_tok, int tile) {
   __shared__ float2 table[ROPE_TOKENS * ROPE_MAX_PAIRS];
   const int pairs = l.rot_dim >> 1;
-  const int tok0 = (int)blockIdx.x * tile, here = min(tile, n_tok - tok0);
+  const int tok0 = first + (int)blockIdx.x * tile, here = min(tile, n_tok - tok0);
 
   int have = -1;
   double f = 0.0;
@@ -145,16 +147,21 @@ hipError_t rope_typed(const RopeLaunch& l, hipStream_t s) {
   constexpr int N = 16 / sizeof(T);
   const int n = l.batch * l.tokens;
   const int tile = n < 1024 ? 1 : ROPE_TOKENS;
-  const dim3 grid((unsigned)((n + (int64_t)tile - 1) / tile));
-  if (rope_aligned<T>(l)) {
-    if (l.interleaved) k_rope<T, N, true, true><<<grid, ROPE_THREADS, 0, s>>>(l, n, tile);
-    else k_rope<T, N, true, false><<<grid, ROPE_THREADS, 0, s>>>(l, n, tile);
-  } else if (l.interleaved) {
-    k_rope<T, 2, false, true><<<grid, ROPE_THREADS, 0, s>>>(l, n, tile);
-  } else {
-    k_rope<T, 1, false, false><<<grid, ROPE_THREADS, 0, s>>>(l, n, tile);
+  const int64_t most = (int64_t)tile << 22;  // tokens of a launch, whose threads are counted in 32 bits
+  for (int64_t first = 0; first < n; first += most) {
+    const dim3 grid((unsigned)((std::min(most, n - first) + tile - 1) / tile));
+    if (rope_aligned<T>(l)) {
+      if (l.interleaved) k_rope<T, N, true, true><<<grid, ROPE_THREADS, 0, s>>>(l, (int)first, n, tile);
+      else k_rope<T, N, true, false><<<grid, ROPE_THREADS, 0, s>>>(l, (int)first, n, tile);
+    } else if (l.interleaved) {
+      k_rope<T, 2, false, true><<<grid, ROPE_THREADS, 0, s>>>(l, (int)first, n, tile);
+    } else {
+      k_rope<T, 1, false, false><<<grid, ROPE_THREADS, 0, s>>>(l, (int)first, n, tile);
+    }
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
   }
-  return hipGetLastError();
+  return hipSuccess;
 }
 
 }  // namespace

@@ -592,3 +592,16 @@ def test_evicted_prefix_in_the_denoiser(ops):
             ae.close()
     # the same keys in the same order, but ranges of the key axis follow the buffer's size: fp32 sums in another order
     within(acts[1], acts[0].cpu(), 1e-5)
+
+
+def test_rope_of_many_tokens(ops):
+    """More tokens than one launch's threads can be counted for: the same as for a few tokens at their positions."""
+    n, part = (1 << 26) + 100, 70
+    x = torch.empty(1, n, 1, 2, dtype=torch.bfloat16, device="cuda")
+    at = torch.tensor([0, (1 << 24) - 33, (1 << 25) - 2, (1 << 26) - 35, n - part])
+    rows = (at[:, None] + torch.arange(part)).cuda()
+    x[0, rows] = rand(5, len(at), part, 1, 2, dtype=torch.bfloat16).cuda()
+    few = x[0, rows]
+    got, _ = ops.rope(x)
+    want, _ = ops.rope(few, positions=rows.int())
+    assert torch.equal(got[0, rows], want)
