@@ -49,9 +49,9 @@ jpi_status check_sizes(const char* call, const jpi_shared_attn* a) {
   if (a->prefix < 0 || a->suffix < 0) return fail(JPI_ERR_ARG, "%s: negative prefix or suffix", call);
   if (!isfinite(a->scale) || a->scale <= 0.f) return fail(JPI_ERR_ARG, "%s: scale must be finite and > 0", call);
   const double rows = (double)a->n_groups * a->group * a->q_rows * a->n_heads;
-  if (rows > 1073741824.0 || a->prefix > 1 << 27 || a->suffix > 1 << 27 ||
-      (double)a->n_groups * a->n_kv_heads * a->prefix > 4294967296.0)
-    return fail(JPI_ERR_SHAPE, "%s: more than 2^30 rows, 2^27 slots or 2^32 slots in all", call);
+  if (rows > 1073741824.0 || a->prefix > 1 << 27 || a->suffix > 1 << 27 || (int64_t)a->n_groups * a->n_kv_heads > 1 << 22 ||
+      (double)a->n_groups * a->n_kv_heads * a->prefix > 1073741824.0)
+    return fail(JPI_ERR_SHAPE, "%s: more than 2^30 rows, 2^27 slots, 2^22 prefixes x KV heads or 2^30 slots in all", call);
   return JPI_OK;
 }
 
@@ -168,6 +168,9 @@ jpi_status jpi_shared_attention(const jpi_shared_attn* a, void* workspace, size_
     if ((st = check_view(call, "v_suffix", a->v_suffix, es, true)) != JPI_OK) return st;
   }
   if ((st = check_workspace(call, shared_attention_bytes(*a), workspace, workspace_bytes)) != JPI_OK) return st;
+  if (a->out.data == a->q.data || (a->prefix > 0 && (a->out.data == a->k_prefix.data || a->out.data == a->v_prefix.data)) ||
+      (a->suffix > 0 && (a->out.data == a->k_suffix.data || a->out.data == a->v_suffix.data)))
+    return fail(JPI_ERR_ARG, "%s: out may not be an input", call);
   return launched(call, launch_shared_attention(*a, workspace, (hipStream_t)stream));
 }
 

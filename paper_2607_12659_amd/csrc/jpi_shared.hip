@@ -864,12 +864,14 @@ __global__ __launch_bounds__(64 * WEIGHT_WAVES) void k_weight(WeightLaunch l) {
 
   const int n_rows = a.group * a.q_rows * a.per_kv, tiles = (n_rows + 32 - 1) / 32;
   const int t0 = (int)((int64_t)split * tiles / a.splits), t1 = (int)((int64_t)(split + 1) * tiles / a.splits);
+  bool silent = false;  // a row that adds nothing, whatever its queries hold
   for (int r = tid; r < (t1 - t0) * 32; r += 64 * NW) {
     const Row x = row_of(a, g, kv, t0 * 32 + r);
     const float v = x.b >= 0 ? l.lse[((int64_t)x.b * a.q_rows + x.i) * a.n_heads + x.h] : -INFINITY;
     lse2[r] = v == -INFINITY ? -INFINITY : -v * LOG2E;  // rows that see nothing, or are none, add 2^-inf
+    silent = silent || (x.b >= 0 && v == -INFINITY);
   }
-  __syncthreads();
+  const bool some_silent = __syncthreads_or(silent);
 
   auto rows = [&](int t, int stage) __attribute__((always_inline)) {  // past the last tile: the last row again
     const Row x = row_of(a, g, kv, min(t * 32 + 8 * w + TL::row(lane), n_rows - 1));
@@ -903,6 +905,12 @@ __global__ __launch_bounds__(64 * WEIGHT_WAVES) void k_weight(WeightLaunch l) {
     f32x4 e[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) e[j] = *reinterpret_cast<const f32x4*>(&lse2[(t - t0) * 32 + 8 * j + 4 * half]);
+    if (some_silent) {  // their scores may be NaN or infinite
+#pragma unroll
+      for (int u = 0; u < KT; ++u)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[u][r] = e[r >> 2][r & 3] == -INFINITY ? 0.f : s[u][r];
+    }
 #pragma unroll
     for (int u = 0; u < KT; ++u)
 #pragma unroll
@@ -1029,6 +1037,7 @@ Plan weight_plan(const jpi_shared_attn& a) {
 }
 
 unsigned grid8(int64_t items) { return (unsigned)((items + 7) / 8 * 8); }
+bool too_many(int64_t groups, int threads) { return groups * threads >= (int64_t)1 << 32; }  // for one launch
 
 template <typename T, int DH>
 hipError_t shared_typed(const jpi_shared_attn& a, void* ws, hipStream_t s) {
@@ -1073,7 +1082,9 @@ hipError_t weight_typed(const jpi_shared_attn& a, const float* w_in, float decay
   l.key_tiles = p.row_tiles;
   const int64_t slots = (int64_t)a.n_groups * a.n_kv_heads * a.prefix;
   if (p.splits > 1) l.part = (float*)ws;
-  k_weight<T, DH><<<grid8((int64_t)a.n_groups * a.n_kv_heads * p.row_tiles * p.splits), 64 * WEIGHT_WAVES, 0, s>>>(l);
+  const int64_t items = (int64_t)a.n_groups * a.n_kv_heads * p.row_tiles * p.splits;
+  if (too_many(items + 7, 64 * WEIGHT_WAVES) || too_many(slots / 64 + 1, 256)) return hipErrorInvalidConfiguration;
+  k_weight<T, DH><<<grid8(items), 64 * WEIGHT_WAVES, 0, s>>>(l);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.splits == 1) return e;
   k_weight_sum<<<(unsigned)((slots + 63) / 64), 256, 0, s>>>(l);

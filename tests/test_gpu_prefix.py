@@ -605,3 +605,72 @@ def test_rope_of_many_tokens(ops):
     got, _ = ops.rope(x)
     want, _ = ops.rope(few, positions=rows.int())
     assert torch.equal(got[0, rows], want)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("prefix,rollouts", [(40, 3), (700, 9)])
+def test_prefix_weight_of_padding_rows(ops, dtype, prefix, rollouts):
+    """Rows whose lse is -inf add nothing, whatever their queries hold."""
+    nh, D = 4, 128
+    q, kp = rand(1, rollouts, 5, nh, D, dtype=dtype), rand(2, 1, prefix, 2, D, dtype=dtype)
+    lse = torch.full((rollouts, 5, nh), 3.0)
+    lse[1, 2:], lse[2, :, 1], lse[-1, -1] = -INF, -INF, -INF
+    ref, err = weight64(q, kp, lse, [prefix], D ** -0.5)
+    q[1, 2:], q[2, :, 1], q[-1, -1] = math.nan, INF, -INF
+    within(ops.prefix_weight(dev(q), dev(kp), dev(lse)), ref, err + 1e-30)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_prefix_weight_of_many_rows(ops, dtype):
+    """More rows on one KV head than a workgroup's range holds."""
+    case = (1, 13, 50, 8, 1, 64, [90], 97, 0, None, False)
+    x = attn_inputs(case, dtype)
+    lse = attn64(*x, 0.125)[1].float()
+    ref, err = weight64(x[0], x[1], lse, [90], 0.125)
+    within(ops.prefix_weight(dev(x[0]), dev(x[1]), dev(lse), prefix_len=i32([90])), ref, err + 1e-30)
+
+
+def test_caches_past_32_bit_offsets(ops):
+    """Slots 2^20 elements apart: the last of 4100 lies 8.6 GB behind the first."""
+    P, D, apart, dtype = 4100, 64, 1 << 20, torch.bfloat16
+    free, _ = torch.cuda.mem_get_info()
+    if free < 24 << 30:
+        pytest.skip("needs 24 GB of device memory")
+    room = torch.empty(P * apart, dtype=dtype, device="cuda").view(1, P, 1, apart)
+    far_k, far_v, far_q = room[..., :D], room[..., D:2 * D], room[..., 4 * D:5 * D].view(P, 1, 1, D)
+    q, kp, vp = (rand(i, n, m, 2 if i == 1 else 1, D, dtype=dtype) for i, n, m in ((1, 3, 2), (2, 1, P), (3, 1, P)))
+    far_k.copy_(kp), far_v.copy_(vp)
+    want, want_lse = ops.shared_attention(dev(q), dev(kp), dev(vp))
+    out, lse = ops.shared_attention(dev(q), far_k, far_v)
+    assert torch.equal(out, want) and torch.equal(lse, want_lse)
+    w = ops.prefix_weight(dev(q), far_k, lse)
+    assert torch.equal(w, ops.prefix_weight(dev(q), dev(kp), lse))
+    # as the tails of one-row rollouts, each a cache of its own
+    far_q.copy_(rand(7, P, 1, 1, D, dtype=dtype))
+    tails = far_k.view(P, 1, 1, D), far_v.view(P, 1, 1, D)
+    near = tuple(t.contiguous() for t in (far_q, *tails))
+    few = dev(kp)[:, :5], dev(vp)[:, :5]
+    assert torch.equal(ops.shared_attention(far_q, *few, *tails)[0], ops.shared_attention(near[0], *few, *near[1:])[0])
+    # turned where they lie, and evicted
+    turned, _ = ops.rope(dev(kp))
+    ops.rope(far_k, q_out=far_k)
+    assert torch.equal(far_k, turned)
+    index, _ = ops.evict(far_k, far_v, w, 100)
+    kept = index[0, 0].long()
+    assert torch.equal(far_k[:, :100], turned[:, kept]) and torch.equal(far_v[:, :100], dev(vp)[:, kept])
+
+
+def test_shared_attention_of_no_keys(ops):
+    q, none = torch.randn(2, 3, 4, 64, device="cuda"), torch.empty(1, 0, 2, 64, device="cuda")
+    out, lse = ops.shared_attention(q, none, none)
+    assert (out == 0).all() and (lse == -INF).all()
+    tail = torch.empty(2, 0, 2, 64, device="cuda")
+    out, lse = ops.shared_attention(q, none, none, tail, tail, causal=True)
+    assert (out == 0).all() and (lse == -INF).all()
+    assert ops.prefix_weight(q, none, lse).shape == (1, 2, 0)
+
+
+def test_shared_attention_refuses_its_inputs_as_output(ops):
+    q, kp = torch.randn(2, 3, 4, 64, device="cuda"), torch.randn(1, 9, 2, 64, device="cuda")
+    with pytest.raises(Exception, match="may not be an input"):
+        ops.shared_attention(q, kp, kp, out=q)

@@ -160,3 +160,10 @@ def test_tensors_on_the_cpu_are_refused():
         ops.rope(q, layout="other")
     with pytest.raises(ValueError, match="contiguous"):
         ops.rope(torch.zeros(2, 3, 4, 128)[..., ::2])
+
+
+def test_shared_attention_refuses_more_than_a_launch_holds_and_overlap():
+    assert j.jpi_shared_attention(attn_args(n_groups=(1 << 22) + 1, group=1, q_rows=1, prefix=1)) == j.JPI_ERR_SHAPE
+    assert j.jpi_shared_attention(attn_args(n_groups=17, prefix=1 << 26)) == j.JPI_ERR_SHAPE
+    a = attn_args(prefix=0, suffix=0, q=view(2 * FAKE), out=view(2 * FAKE))
+    assert j.jpi_shared_attention(a, FAKE, 1 << 40) == j.JPI_ERR_ARG and "may not be an input" in j.jpi_prefix_last_error()
