@@ -22,6 +22,7 @@ constexpr int SEL = 1024;         // threads of a selection
 constexpr int SEL_WAVES = SEL / 64;
 constexpr int DIGIT = 11;         // bits of a radix digit: three passes
 constexpr int BINS = 1 << DIGIT;
+constexpr int TOGETHER = 8;       // chunks of SEL slots that are read, and placed, together
 
 // Order-preserving image of a weight: larger weight, larger integer; NaN as -inf, -0 as 0; never 0.
 __device__ __forceinline__ u32 weight_key(float w) {
@@ -38,6 +39,7 @@ struct SelectLds {
   int bins[BINS];
   int sums[SEL_WAVES];
   int found[2];
+  int ties[TOGETHER * SEL_WAVES], kept[TOGETHER * SEL_WAVES];  // of each wave, chunk by chunk
 };
 
 // Sum over the threads of lower index; `all` the sum over all of them.
@@ -61,6 +63,25 @@ __device__ __forceinline__ int before_me(int v, int* sums, int& all) {
     all += y;
   }
   return add + x - v;
+}
+
+// From each wave's counts of C chunks: the sum over all that come before this wave's, for each chunk; returns the whole sum.
+// Every wave makes the one scan for itself.
+template <int C>
+__device__ __forceinline__ int before_chunks(const int* counts, int (&before)[C]) {
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const bool on = 2 * lane < C * SEL_WAVES;
+  const int a = on ? counts[2 * lane] : 0, b = on ? counts[2 * lane + 1] : 0;
+  int x = a + b;
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const int y = __shfl_up(x, d, 64);
+    x += lane >= d ? y : 0;
+  }
+  const int first = x - a - b, second = x - b;
+#pragma unroll
+  for (int c = 0; c < C; ++c) before[c] = __shfl(w & 1 ? second : first, (c * SEL_WAVES + w) / 2, 64);
+  return __builtin_amdgcn_readlane(x, 63);
 }
 
 // The slots of a sequence that stay, n > keep.  N: weights that a thread keeps in registers (up to N * SEL slots); 0: they
@@ -105,7 +126,13 @@ __device__ __forceinline__ void select(const jpi_evict_args& a, const float* wt,
         for (int c = 0; c < N; ++c)
           if (c < chunks) count(key[c]);
       } else {
-        for (int c = 0; c < chunks; ++c) count(load(c));
+        for (int c0 = 0; c0 < chunks; c0 += TOGETHER) {
+          u32 k[TOGETHER];
+#pragma unroll
+          for (int c = 0; c < TOGETHER; ++c) k[c] = load(c0 + c);  // 0 past the last slot
+#pragma unroll
+          for (int c = 0; c < TOGETHER; ++c) count(k[c]);
+        }
       }
       __syncthreads();
       // from the largest bin down, two a thread: the one that holds the need-th
@@ -123,23 +150,44 @@ __device__ __forceinline__ void select(const jpi_evict_args& a, const float* wt,
   }
 
   // places in slot order
+  constexpr int C = N != 0 && N < TOGETHER ? N : TOGETHER;
   int ties_before = 0, kept_before = 0;
-  auto place = [&](int c, u32 k) __attribute__((always_inline)) {
-    const int j = c * SEL + tid;
-    const bool tie = k == last;
-    int ties, kept;
-    const int tb = ties_before + before_me(tie, lds.sums, ties);
-    const bool stay = j < n && (j < lo || j >= hi || k > last || (tie && tb < need));
-    const int t = kept_before + before_me(stay, lds.sums, kept);
+  auto place = [&](int c0, const u32* k) __attribute__((always_inline)) {
+    const int w = tid >> 6;
+    int before[C];
+    unsigned long long in[C];  // of this wave
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      in[c] = __ballot(k[c] == last);
+      if (lane == 0) lds.ties[c * SEL_WAVES + w] = __builtin_popcountll(in[c]);
+    }
+    __syncthreads();
+    const int ties = before_chunks<C>(lds.ties, before);
+    const unsigned long long lower = (1ull << lane) - 1;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const int j = (c0 + c) * SEL + tid, tie = ties_before + before[c] + __builtin_popcountll(in[c] & lower);
+      in[c] = __ballot(j < n && (j < lo || j >= hi || k[c] > last || (k[c] == last && tie < need)));
+      if (lane == 0) lds.kept[c * SEL_WAVES + w] = __builtin_popcountll(in[c]);
+    }
+    __syncthreads();
+    const int kept = before_chunks<C>(lds.kept, before);
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+      if (in[c] >> lane & 1) stays(kept_before + before[c] + __builtin_popcountll(in[c] & lower), (c0 + c) * SEL + tid);
     ties_before += ties, kept_before += kept;
-    if (stay) stays(t, j);
   };
   if constexpr (N != 0) {
 #pragma unroll
-    for (int c = 0; c < N; ++c)
-      if (c < chunks) place(c, key[c]);
+    for (int c0 = 0; c0 < N; c0 += C)
+      if (c0 < chunks) place(c0, key + c0);
   } else {
-    for (int c = 0; c < chunks; ++c) place(c, load(c));
+    for (int c0 = 0; c0 < chunks; c0 += C) {
+      u32 k[C];
+#pragma unroll
+      for (int c = 0; c < C; ++c) k[c] = load(c0 + c);
+      place(c0, k);
+    }
   }
 }
 
@@ -301,7 +349,8 @@ hipError_t evict_pieces(MoveLaunch l, bool gather, int row_bytes, hipStream_t s)
   const int64_t seqs = (int64_t)a.n_outer * a.n_heads;
   const int most = std::min(a.keep, a.slots);
   if (!gather && l.t[0].src != l.t[0].dst && l.t[1].src != l.t[1].dst) {
-    l.per = std::max(1, 1024 / l.pieces);
+    // 16 KB a workgroup; more where a launch, whose threads are counted in 32 bits, would not hold them
+    l.per = (int)std::max<int64_t>(std::max(1, 1024 / l.pieces), (seqs * l.n_t * most >> 23) + 1);
     l.parts = std::max(1, (most + l.per - 1) / l.per);
     k_evict_copy<P><<<(unsigned)(seqs * l.n_t * l.parts), 256, 0, s>>>(l);
     return hipGetLastError();
@@ -320,8 +369,7 @@ hipError_t evict_pieces(MoveLaunch l, bool gather, int row_bytes, hipStream_t s)
   const unsigned grid = (unsigned)(seqs * l.parts);
   if (a.slots <= SEL) k_evict_gather<1, P><<<grid, SEL, 0, s>>>(l);
   else if (a.slots <= 4 * SEL) k_evict_gather<4, P><<<grid, SEL, 0, s>>>(l);
-  else if (a.slots <= 16 * SEL) k_evict_gather<16, P><<<grid, SEL, 0, s>>>(l);
-  else k_evict_gather<0, P><<<grid, SEL, 0, s>>>(l);
+  else k_evict_gather<16, P><<<grid, SEL, 0, s>>>(l);
   return hipGetLastError();
 }
 
@@ -335,7 +383,7 @@ hipError_t launch_evict(const jpi_evict_args& a, hipStream_t s) {
   l.a = a;
   l.n_t = 2;
   // one launch where nothing that a workgroup writes is read by another
-  bool gather = a.weight_out != a.weight && (!a.len || a.len_out != a.len);
+  bool gather = a.slots <= 16 * SEL && a.weight_out != a.weight && (!a.len || a.len_out != a.len);
   int64_t any = a.head_dim * es;
   for (int i = 0; i < 2; ++i) {
     l.t[i] = MoveTensor{(const char*)in[i]->data, (char*)out[i]->data, in[i]->outer * es, in[i]->row * es, in[i]->head * es,

@@ -674,3 +674,33 @@ def test_shared_attention_refuses_its_inputs_as_output(ops):
     q, kp = torch.randn(2, 3, 4, 64, device="cuda"), torch.randn(1, 9, 2, 64, device="cuda")
     with pytest.raises(Exception, match="may not be an input"):
         ops.shared_attention(q, kp, kp, out=q)
+
+
+EVICT_MORE = [
+    (1, 2, 64, 16384, 5000, 3, 9, None, "ties"),            # weights in registers, two rounds of places
+    (3, 1, 64, 9000, 7000, 0, 0, [9000, 8193, 7001], "odd"),
+    (2, 1, 5, 17000, 9000, 1, 0, [17000, 16385], "ties"),   # weights read anew; rows of no whole pieces
+    (80, 1, 128, 2100, 1700, 4, 8, None, "plain"),          # more bytes than one launch moves
+]
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("case", EVICT_MORE, ids=lambda c: "n%dx%d-d%d-p%d-k%d-%s" % (*c[:5], c[8]))
+def test_evict_long_and_large(ops, case, in_place):
+    n, heads, dh, slots, keep, first, last, lens, kind = case
+    k, v = (rand(i, n, slots, heads, dh, dtype=torch.bfloat16) for i in (4, 5))
+    w = weights(kind, 6, n, heads, slots)
+    lengths = [slots] * n if lens is None else lens
+    dk, dv, dw = dev(k), dev(v), dev(w)
+    ko, vo, wo = (dk, dv, dw) if in_place else (torch.zeros_like(dk[:, :keep]), torch.zeros_like(dv[:, :keep]),
+                                                torch.zeros_like(dw[:, :, :keep]))
+    index, out_len = ops.evict(dk, dv, dw, keep, lens=None if lens is None else i32(lens), n_first=first, n_last=last, k_out=ko,
+                               v_out=vo, weight_out=wo)
+    assert out_len.tolist() == [min(x, keep) for x in lengths]
+    index = index.cpu()
+    for o in range(n):
+        for h in range(heads):
+            kept = kept_slots(w[o, h], lengths[o], keep, first, last)
+            assert index[o, h].tolist() == kept
+            assert torch.equal(ko[o, :keep, h].cpu(), k[o, kept, h]) and torch.equal(vo[o, :keep, h].cpu(), v[o, kept, h])
+            assert torch.equal(wo[o, h, :keep].cpu().nan_to_num(nan=-1), w[o, h, kept].nan_to_num(nan=-1))
