@@ -823,7 +823,7 @@ struct WeightShape {
 };
 
 template <typename T, int DH>
-__global__ __launch_bounds__(64 * WEIGHT_WAVES) void k_weight(WeightLaunch l) {
+__global__ __launch_bounds__(64 * WEIGHT_WAVES) __attribute__((amdgpu_waves_per_eu(2))) void k_weight(WeightLaunch l) {
   using TL = Tile<T, DH, 32>;
   using WS = WeightShape<T, DH>;
   constexpr int NW = WEIGHT_WAVES, NS = WS::NS, KT = WS::KT;
