@@ -742,35 +742,36 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(NW == 8
 }
 
 // Join of a row's ranges: the ranges' sums brought to their largest reference.  WPR waves a row, each for a part of the
-// ranges: with one, 64 ranges of few rows are eight trips to memory one after another.
+// ranges (at most 64): with one, 64 ranges of few rows are eight trips to memory one after another.
 template <typename T, int DH, int WPR>
-__global__ __launch_bounds__(256) void k_shared_merge(SharedLaunch l) {
-  constexpr int N = DH / 64, RPW = 4 / WPR;
+__global__ __launch_bounds__(WPR > 4 ? 64 * WPR : 256) void k_shared_merge(SharedLaunch l) {
+  constexpr int N = DH / 64, RPW = WPR < 4 ? 4 / WPR : 1;  // rows of a workgroup
   typedef float vec __attribute__((ext_vector_type(N)));
   typedef T tvec __attribute__((ext_vector_type(N)));
   __shared__ vec parts[WPR > 1 ? WPR : 1][64];
+  __shared__ float2 stats[WPR];
   const int64_t rows = (int64_t)l.n_groups * l.group * l.q_rows * l.n_heads;
   const int lane = threadIdx.x & 63, w = uniform(threadIdx.x >> 6), share = w % WPR;
   const int64_t row = (int64_t)blockIdx.x * RPW + w / WPR;
-  if (row >= rows) return;  // WPR == 4: all of the workgroup
-  const float2 st = lane < l.splits ? l.stats[lane * rows + row] : float2{-INFINITY, 0.f};  // at most 64 ranges
-  const float m = wave_max(st.x);
+  if (row >= rows) return;  // WPR > 1: all of the workgroup
+  const int s0 = share * l.splits / WPR, n = (share + 1) * l.splits / WPR - s0;
+  const float2 st = lane < n ? l.stats[(s0 + lane) * rows + row] : float2{-INFINITY, 0.f};
+  float m = wave_max(st.x);
   const float f = st.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(st.x - m);
-  const float sum = wave_sum(st.x == -INFINITY ? 0.f : st.y * f);
+  float sum = wave_sum(st.x == -INFINITY ? 0.f : st.y * f);
   const unsigned long long there = __ballot(st.x != -INFINITY);  // a range without a visible key wrote nothing
   vec o;
 #pragma unroll
   for (int e = 0; e < N; ++e) o[e] = 0.f;
   constexpr int U = 4;  // loads in flight; where fewer ranges are left, the last one again
-  const int s0 = share * l.splits / WPR, s1 = (share + 1) * l.splits / WPR;
-  const float* const at = l.part + row * DH + lane * N;
-  for (int s = s0; s < s1; s += U) {
+  const float* const at = l.part + (s0 * rows + row) * DH + lane * N;
+  for (int s = 0; s < n; s += U) {
     vec v[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) v[u] = *reinterpret_cast<const vec*>(at + min(s + u, s1 - 1) * rows * DH);
+    for (int u = 0; u < U; ++u) v[u] = *reinterpret_cast<const vec*>(at + min(s + u, n - 1) * rows * DH);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const bool on = s + u < s1 && (there >> (s + u) & 1);
+      const bool on = s + u < n && (there >> (s + u) & 1);
       const float g = on ? __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, f), min(s + u, 63))) : 0.f;
 #pragma unroll
       for (int e = 0; e < N; ++e) o[e] = fmaf(g, on ? v[u][e] : 0.f, o[e]);
@@ -778,10 +779,20 @@ __global__ __launch_bounds__(256) void k_shared_merge(SharedLaunch l) {
   }
   if constexpr (WPR > 1) {
     parts[share][lane] = o;
+    if (lane == 0) stats[share] = float2{m, sum};
     __syncthreads();
     if (share) return;
 #pragma unroll
-    for (int i = 1; i < WPR; ++i) o += parts[i][lane];
+    for (int i = 1; i < WPR; ++i) m = fmaxf(m, stats[i].x);
+    sum = 0.f;
+#pragma unroll
+    for (int e = 0; e < N; ++e) o[e] = 0.f;
+#pragma unroll
+    for (int i = 0; i < WPR; ++i) {
+      const float g = stats[i].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(stats[i].x - m);
+      sum = fmaf(g, stats[i].y, sum);
+      if (g != 0.f) o += parts[i][lane] * g;
+    }
   }
   const float inv = m == -INFINITY ? 0.f : 1.f / sum;
   const int h = (int)(row % l.n_heads);
@@ -1013,7 +1024,7 @@ Plan shared_plan(const jpi_shared_attn& a) {
     const int64_t rollouts = std::min<int64_t>(a.group, (32 * w + per_rollout - 1) / per_rollout);
     const double tiles = (double)prefix + (double)TAIL_COST * tail * rollouts;
     const double tile_us = (half ? 0.9 + 0.002 * a.head_dim : 0.4 + 0.022 * a.head_dim) * (w == 8 ? 1.4 : 1.0);
-    for (const int s : {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 48, 64}) {
+    for (const int s : {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 48, 64, 96, 128, 192, 256}) {
       if (s > 1 && s > prefix + tail) break;
       const double us = ceil(items * s / n_cu) * (ceil(tiles / s) * tile_us + 12) + (s > 1 ? 4 + all_mb * s / 3.3 : 0);
       if (us < best_us) best_us = us, best = Plan{w, (int)row_tiles, s};
@@ -1063,7 +1074,8 @@ hipError_t shared_typed(const jpi_shared_attn& a, void* ws, hipStream_t s) {
   }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.splits == 1) return e;
-  if (p.splits > 8) k_shared_merge<T, DH, 4><<<(unsigned)rows, 256, 0, s>>>(l);
+  if (p.splits > 64) k_shared_merge<T, DH, 16><<<(unsigned)rows, 1024, 0, s>>>(l);
+  else if (p.splits > 8) k_shared_merge<T, DH, 4><<<(unsigned)rows, 256, 0, s>>>(l);
   else k_shared_merge<T, DH, 1><<<(unsigned)((rows + 3) / 4), 256, 0, s>>>(l);
   return hipGetLastError();
 }

@@ -704,3 +704,18 @@ def test_evict_long_and_large(ops, case, in_place):
             assert index[o, h].tolist() == kept
             assert torch.equal(ko[o, :keep, h].cpu(), k[o, kept, h]) and torch.equal(vo[o, :keep, h].cpu(), v[o, kept, h])
             assert torch.equal(wo[o, h, :keep].cpu().nan_to_num(nan=-1), w[o, h, kept].nan_to_num(nan=-1))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("case", [(1, 1, 1, 8, 1, 64, [20000], 20000, 0, None, False),
+                                  (2, 3, 2, 4, 2, 128, [12345, 3], 12346, 7, [7, 1, 0, 2, 7, 3], True)],
+                         ids=lambda c: "g%dx%d-q%d-h%d/%d-d%d-p%d-s%d" % (*c[:6], c[7], c[8]))
+def test_shared_attention_of_few_rows_over_a_long_prefix(ops, case, dtype):
+    """More ranges of the prefix than a wave joins, most of them without a key where the prefix is short."""
+    x = attn_inputs(case, dtype)
+    D, scale = case[5], case[5] ** -0.5
+    ref, lse, mag, err = attn64(*x, scale)
+    out, got_lse = run_attn(ops, *x)
+    tol, lse_tol = attn_tolerance(dtype, ref, lse, mag, err, case[7] + case[8], D)
+    within(out, ref, tol)
+    within(got_lse, lse, lse_tol)
