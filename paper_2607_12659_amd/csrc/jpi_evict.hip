@@ -3,9 +3,12 @@
 // Bound by memory: the kept rows of K and V are read and written once.  Which rows those are is found by a radix
 // selection of the last weight that stays, over an order-preserving integer image of the weights (counts only, so no
 // order of atomics could show), and a prefix sum in slot order.
-//   Into other memory: one launch.  Every workgroup of a sequence makes the selection for itself, 3 us at 816 slots and
-//   4 at 4096 in which the card is otherwise idle, and moves its share of the rows; a selection in a launch of its own
-//   took as long, and its end and the next launch's start another 5.
+//   Into other memory, few rows: one launch.  Every workgroup of a sequence makes the selection for itself, in which the
+//   card is otherwise idle, and moves its share of the rows: 18 sequences of 816 slots cut to 408 (15 MB) take 10 us, with
+//   the selection in a launch of its own 13.
+//   Into other memory, many rows or slots: k_evict_select, then k_evict_copy (144 sequences of up to 4096 slots cut to
+//   1024, 305 MB: 12 and 48 us; 74 with data that no cache holds, 4.1 TB/s).  The selection is one workgroup's work for
+//   each sequence: 65536 slots take 100 us.
 //   In place: k_evict_select, then k_evict_shift, since weights and lengths change where other workgroups read them.
 #include <algorithm>
 
@@ -285,7 +288,7 @@ __global__ __launch_bounds__(SEL) void k_evict_select(jpi_evict_args a) {
   }
 }
 
-// Kept rows into other memory after a selection in a launch of its own.
+// Kept rows into other memory after a selection in a launch of its own, 16 KB a workgroup.
 template <typename P>
 __global__ __launch_bounds__(256) void k_evict_copy(MoveLaunch l) {
   const int part = blockIdx.x % l.parts, ti = blockIdx.x / l.parts % l.n_t, seq = blockIdx.x / (l.parts * l.n_t);
@@ -382,7 +385,8 @@ hipError_t launch_evict(const jpi_evict_args& a, hipStream_t s) {
   MoveLaunch l{};
   l.a = a;
   l.n_t = 2;
-  // one launch where nothing that a workgroup writes is read by another
+  // One launch where nothing that a workgroup writes is read by another, and where a thread's weights stay in registers:
+  // read anew by every workgroup, the selection of 65536 slots took 320 us against 166 in a launch of its own.
   bool gather = a.slots <= 16 * SEL && a.weight_out != a.weight && (!a.len || a.len_out != a.len);
   int64_t any = a.head_dim * es;
   for (int i = 0; i < 2; ++i) {
@@ -393,7 +397,7 @@ hipError_t launch_evict(const jpi_evict_args& a, hipStream_t s) {
            l.t[i].dr | l.t[i].dh;
   }
   // With many rows to move, small workgroups that do nothing else are faster by more than the other launch costs:
-  // 302 MB (144 sequences, 1024 of 4096 slots) in 68 us against 81, 15 MB (18, 408 of 816) in 14 against 10.
+  // 302 MB (144 sequences, 1024 of 4096 slots) in 68 us against 81, 15 MB (18, 408 of 816) in 13 against 10.
   gather = gather && (int64_t)a.n_outer * a.n_heads * std::min(a.keep, a.slots) * a.head_dim * es < (int64_t)32 << 20;
   if (!gather) {
     const unsigned seqs = (unsigned)(a.n_outer * a.n_heads);

@@ -4,16 +4,25 @@
 // All query rows of a group that read one KV head (rollouts x query rows x the
 // heads on that KV head) form one matrix against one key sequence: the prefix,
 // which every row sees, and behind it the tails of the rollouts, each seen by
-// its own rows only.  A workgroup takes 32 rows per wave and a range of 32-key
-// tiles of that sequence, so each prefix tile that it loads serves all its rows,
-// whichever rollouts they belong to.  A running maximum and sum per row give the
-// softmax in one pass; ranges of one row tile are joined by k_shared_merge.
+// its own rows only.  A workgroup takes 32 rows per wave and a range of tiles of
+// that sequence (64 keys in bf16, 32 in fp32), so each prefix tile that it loads
+// serves all its rows, whichever rollouts they belong to.  A running maximum and
+// sum per row give the softmax in one pass; ranges of one row tile are joined by
+// k_shared_merge.
 //
 // Products use 32 x 32 matrix instructions with the operands swapped:
 // S^T = K q^T puts one query row in each lane (lane % 32) and 16 of the tile's
 // keys in its registers, register r <-> key 8 (r / 4) + 4 (lane / 32) + r % 4, so
 // the row maximum and sum are in-lane but for one lane swap, and P^T is the B
 // operand of O^T = V^T P^T without leaving its registers.
+//
+// What bounds it.  With many rows the products: a tile of 64 keys x 128 rows of
+// 256 dims takes a workgroup 1.4 us, 1.5 PFLOP/s if all 256 units had one.  Four
+// prefixes of up to 1600 slots against 6400 rows each, 58 us: the workgroups of
+// the longest prefix are the call's time, since lengths are on the device when
+// ranges are chosen.  With few rows memory: 65536 slots x 8 KV heads of 128 dims
+// and 64 tails of up to 512, 104 us, 3.2 TB/s.  A workgroup's start, first tile
+// and rows' way out take 12 us whatever its range, and the join 4 to 9.
 #include <algorithm>
 #include <type_traits>
 
@@ -810,9 +819,9 @@ __global__ __launch_bounds__(WPR > 4 ? 64 * WPR : 256) void k_shared_merge(Share
 // ---------------------------------------------------------------------------
 // A wave keeps 64 keys (fp32 heads of 256: 32) in registers and takes the rows, 32 at a time, from LDS: S = q K^T puts one
 // key in each lane and 16 rows in its registers, so the sum over rows stays in a register, and a read of a row from LDS
-// serves two products.  Bound by the exponentials (24 of a SIMD's cycles for 64 of them, against 16 of a product over 128
-// dims).  A workgroup's range of rows has its lse in LDS from the start, as the exponent's summand; ranges are summed by
-// k_weight_sum in their order.
+// serves two products.  65536 slots x 8 KV heads of 128 dims against 256 rows take 52 us: 28 to read the keys, which only
+// partly overlap the 33 of products and exponentials (the loop's slope over more rows).  A workgroup's range of rows has
+// its lse in LDS from the start, as the exponent's summand; ranges are summed by k_weight_sum in their order.
 struct WeightLaunch {
   SharedLaunch a;  // q, kp, sizes; splits: ranges of rows
   const float *lse, *w_in;
