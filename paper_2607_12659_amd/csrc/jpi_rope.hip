@@ -4,8 +4,8 @@
 // all heads of its token, so the call is bound by memory: a workgroup takes a
 // few tokens, forms their table of (cos, sin) in LDS once, and then streams the
 // heads of both tensors through it in 16-byte pieces.  6528 tokens of 8 + 1 heads
-// of 256 (bf16, 60 MB) take 13 us, 8198 of 32 + 8 of 128 in fp32 (336 MB) 83:
-// 4.6 and 4.1 TB/s, where a copy reaches 4.8.
+// of 256 (bf16, 60 MB) take 13 us, 8198 of 32 + 8 of 128 in fp32 (336 MB) 66:
+// 4.7 and 5.1 TB/s, where a copy of 4 GiB reaches 4.8.
 //
 // Angles.  A position times f_i in fp32 is off by 2^-24 of the angle itself,
 // which for position 10^5 is 6e-3 radians; here the angle is formed in turns in
@@ -21,7 +21,7 @@ namespace {
 
 constexpr int ROPE_THREADS = 256;
 constexpr int ROPE_MAX_PAIRS = 256;
-constexpr int ROPE_TOKENS = 4;  // tokens per workgroup at most; one where few tokens would leave units idle
+constexpr int ROPE_TOKENS = 4;  // tokens per workgroup at most
 
 // f_i / 2 pi: turns per position of pair i
 __device__ __forceinline__ double rope_turns(const RopeLaunch& l, int i) {
@@ -148,7 +148,11 @@ template <typename T>
 hipError_t rope_typed(const RopeLaunch& l, hipStream_t s) {
   constexpr int N = 16 / sizeof(T);
   const int n = l.batch * l.tokens;
-  const int tile = n < 1024 ? 1 : ROPE_TOKENS;
+  // As many tokens as make 16 KB to read: a table costs a workgroup the same few us whatever follows it, and more tokens
+  // leave fewer workgroups, whose tables and streams then overlap less.  4.6 KB a token (6528 tokens): 17.5, 14.5 and 14.0 us
+  // with 1, 2 and 4; 20 KB (8198 tokens): 68, 71 and 80.
+  const int64_t bytes = (int64_t)(l.t[0].heads + l.t[1].heads) * l.head_dim * sizeof(T);
+  const int tile = n < 1024 ? 1 : (int)std::min<int64_t>(ROPE_TOKENS, (16384 + bytes - 1) / bytes);
   const int64_t most = (int64_t)tile << 22;  // tokens of a launch, whose threads are counted in 32 bits
   for (int64_t first = 0; first < n; first += most) {
     const dim3 grid((unsigned)((std::min(most, n - first) + tile - 1) / tile));
