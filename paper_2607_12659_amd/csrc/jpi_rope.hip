@@ -20,8 +20,7 @@ namespace jpi {
 namespace {
 
 constexpr int ROPE_THREADS = 256;
-constexpr int ROPE_MAX_PAIRS = 256;
-constexpr int ROPE_TOKENS = 4;  // tokens per workgroup at most
+constexpr int ROPE_TABLE = 1024;  // (cos, sin) of a workgroup at most: four tokens of 256 pairs
 
 // f_i / 2 pi: turns per position of pair i
 __device__ __forceinline__ double rope_turns(const RopeLaunch& l, int i) {
@@ -69,7 +68,7 @@ struct Piece {
 // A unit is N elements of a head, with JPI_ROPE_HALF and their N partners half a rotation further on.
 template <typename T, int N, bool VEC, bool INTER>
 __global__ __launch_bounds__(ROPE_THREADS) void k_rope(RopeLaunch l, int first, int n_tok, int tile) {
-  __shared__ float2 table[ROPE_TOKENS * ROPE_MAX_PAIRS];
+  __shared__ float2 table[ROPE_TABLE];
   const int pairs = l.rot_dim >> 1;
   const int tok0 = first + (int)blockIdx.x * tile, here = min(tile, n_tok - tok0);
 
@@ -148,11 +147,12 @@ template <typename T>
 hipError_t rope_typed(const RopeLaunch& l, hipStream_t s) {
   constexpr int N = 16 / sizeof(T);
   const int n = l.batch * l.tokens;
-  // As many tokens as make 16 KB to read: a table costs a workgroup the same few us whatever follows it, and more tokens
-  // leave fewer workgroups, whose tables and streams then overlap less.  4.6 KB a token (6528 tokens): 17.5, 14.5 and 14.0 us
-  // with 1, 2 and 4; 20 KB (8198 tokens): 68, 71 and 80.
+  // As many tokens as make 16 KB to read and fit the table: a table costs a workgroup the same few us whatever follows it,
+  // and more tokens leave fewer workgroups, whose tables and streams then overlap less; at least 512 workgroups where there
+  // are as many tokens.  20 KB a token (8198 tokens): 68, 71 and 80 us with 1, 2 and 4; 4.6 KB (6528): 17.5, 14.5 and 14.0;
+  // 768 bytes (131072): 56 with 4, 34 with 22.
   const int64_t bytes = (int64_t)(l.t[0].heads + l.t[1].heads) * l.head_dim * sizeof(T);
-  const int tile = n < 1024 ? 1 : (int)std::min<int64_t>(ROPE_TOKENS, (16384 + bytes - 1) / bytes);
+  const int tile = (int)std::min<int64_t>({(16384 + bytes - 1) / bytes, ROPE_TABLE / (l.rot_dim / 2), std::max(1, n / 512)});
   const int64_t most = (int64_t)tile << 22;  // tokens of a launch, whose threads are counted in 32 bits
   for (int64_t first = 0; first < n; first += most) {
     const dim3 grid((unsigned)((std::min(most, n - first) + tile - 1) / tile));

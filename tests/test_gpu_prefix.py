@@ -719,3 +719,30 @@ def test_shared_attention_of_few_rows_over_a_long_prefix(ops, case, dtype):
     tol, lse_tol = attn_tolerance(dtype, ref, lse, mag, err, case[7] + case[8], D)
     within(out, ref, tol)
     within(got_lse, lse, lse_tol)
+
+
+def test_rope_of_more_wide_tokens_than_one_launch_holds(ops):
+    """Four tokens of 256 pairs a workgroup: past 2^24 of them there is a second launch."""
+    n, part, dh = (1 << 24) + 200, 70, 512
+    free, _ = torch.cuda.mem_get_info()
+    if free < 24 << 30:
+        pytest.skip("needs 24 GB of device memory")
+    x = torch.empty(1, n, 1, dh, dtype=torch.bfloat16, device="cuda")
+    at = torch.tensor([0, (1 << 24) - 35, n - part])
+    rows = (at[:, None] + torch.arange(part)).cuda()
+    few = rand(5, len(at), part, 1, dh, dtype=torch.bfloat16).cuda()
+    x[0, rows] = few
+    want, _ = ops.rope(few, positions=rows.int())
+    ops.rope(x, q_out=x)
+    assert torch.equal(x[0, rows], want)
+
+
+@pytest.mark.parametrize("heads,dh,rot,tokens", [(1, 2, 2, 70001), (3, 64, 16, 5003), (6, 64, 64, 9001), (1, 512, 512, 2051)])
+def test_rope_of_small_tokens(ops, heads, dh, rot, tokens):
+    """Many tokens a workgroup, the last one's part of them: the same as one call for each stretch of few."""
+    x = dev(rand(6, 1, tokens, heads, dh, dtype=torch.bfloat16))
+    pos = dev(torch.randint(0, 100000, (tokens,), generator=torch.Generator().manual_seed(7)).int())
+    got, _ = ops.rope(x, positions=pos, rot_dim=rot)
+    for t in (0, 1000, tokens - 333):
+        want, _ = ops.rope(x[:, t:t + 333], positions=pos[t:t + 333], rot_dim=rot)
+        assert torch.equal(got[:, t:t + 333], want)
