@@ -5,7 +5,8 @@ tensors, fills in the C arguments and enqueues libjpi's kernels on the current
 stream of the tensors' device, which may be capturing a graph.  Outputs and
 workspaces are allocated by torch on that stream unless they are given.
 Floating tensors are bfloat16 or float32, lengths and positions int32; tensors
-may be strided as long as the elements of a head are contiguous.  Errors are
+may be strided as long as the elements of a head are contiguous.  No gradients
+are recorded (that of a rotation is the rotation with inverse=True).  Errors are
 raised as ``jpi.JpiError`` (the library's checks), ``ValueError`` or
 ``TypeError`` (shapes, devices and types).
 """
@@ -157,7 +158,7 @@ def _workspace(size_of, args, q):
     if status != _j.JPI_OK:
         raise _j.JpiError(status, _j.jpi_prefix_last_error())
     n = n.value
-    return (torch.empty(n, dtype=torch.uint8, device=q.device), n) if n else (None, 0)
+    return (q.new_empty(n, dtype=torch.uint8), n) if n else (None, 0)
 
 
 def shared_attention(q, k_prefix, v_prefix, k_suffix=None, v_suffix=None, *, prefix_len=None, suffix_len=None, causal=False,
@@ -185,11 +186,11 @@ def shared_attention(q, k_prefix, v_prefix, k_suffix=None, v_suffix=None, *, pre
         _want("v_suffix", v_suffix, k_suffix.shape, q.dtype, dev)
         ks, vs = _view("k_suffix", k_suffix), _view("v_suffix", v_suffix)
     if out is None:
-        out = torch.empty((b, rows, heads, dh), dtype=q.dtype, device=q.device)
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
     else:
         _want("out", out, q.shape, q.dtype, dev)
     if lse is None:
-        lse = torch.empty((b, rows, heads), dtype=_F32, device=q.device)
+        lse = q.new_empty((b, rows, heads), dtype=_F32)
     else:
         _want("lse", lse, (b, rows, heads), _F32, dev)
     args = _ATTN.pack(dt, g, b // g, rows, heads, kv, dh, p, s, int(bool(causal)), dh ** -0.5 if scale is None else scale,
@@ -216,7 +217,7 @@ def prefix_weight(q, k_prefix, lse, weight=None, *, prefix_len=None, decay=1.0, 
         _want("weight", weight, shape, _F32, dev)
         w = _dense("weight", weight)
     if out is None:
-        out = (torch.empty if prefix_len is None else torch.zeros)(shape, dtype=_F32, device=q.device)
+        out = (q.new_empty if prefix_len is None else q.new_zeros)(shape, dtype=_F32)
     else:
         _want("out", out, shape, _F32, dev)
     args = _ATTN.pack(dt, g, b // g, rows, heads, kv, dh, p, 0, 0, dh ** -0.5 if scale is None else scale, *_view("q", q),
