@@ -207,6 +207,7 @@ struct MoveLaunch {
   int pieces;  // of a row
   int parts;   // workgroups of one sequence: ranges of rows (gather); of one tensor, too: ranges of pieces (shift)
   int per;     // rows (gather) or pieces (shift) of one of them
+  int first;   // first sequence of this launch (shift)
 };
 
 constexpr int GATHER_ROWS = 2048;  // rows of a workgroup at most
@@ -313,7 +314,7 @@ __global__ __launch_bounds__(256) void k_evict_copy(MoveLaunch l) {
 template <typename P>
 __global__ __launch_bounds__(256) void k_evict_shift(MoveLaunch l) {
   constexpr int U = 4;
-  const int part = blockIdx.x % l.parts, ti = blockIdx.x / l.parts % l.n_t, seq = blockIdx.x / (l.parts * l.n_t);
+  const int part = blockIdx.x % l.parts, ti = blockIdx.x / l.parts % l.n_t, seq = l.first + (int)(blockIdx.x / (l.parts * l.n_t));
   const int o = seq / l.a.n_heads, h = seq - o * l.a.n_heads;
   const int m = min(evict_len(l.a, o), l.a.keep);  // the same before and after len_out, where that is len
   const MoveTensor& x = l.t[ti];
@@ -362,8 +363,15 @@ hipError_t evict_pieces(MoveLaunch l, bool gather, int row_bytes, hipStream_t s)
     // 64 bytes of a row: half of a line, so that few sequences make enough workgroups
     l.per = std::min(l.pieces, std::max(1, 64 / (int)sizeof(P)));
     l.parts = (l.pieces + l.per - 1) / l.per;
-    k_evict_shift<P><<<(unsigned)(seqs * l.n_t * l.parts), 256, 0, s>>>(l);
-    return hipGetLastError();
+    // a launch's threads are counted in 32 bits: as many launches as the sequences need
+    const int64_t each = ((1 << 24) - 1) / (l.n_t * l.parts);
+    for (int64_t first = 0; first < seqs; first += each) {
+      l.first = (int)first;
+      k_evict_shift<P><<<(unsigned)(std::min(each, seqs - first) * l.n_t * l.parts), 256, 0, s>>>(l);
+      const hipError_t e = hipGetLastError();
+      if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
   }
   // two workgroups for each of 256 units, but no fewer than 32 rows in one
   const int64_t want = std::max<int64_t>(1, 512 / seqs);

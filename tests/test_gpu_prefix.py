@@ -746,3 +746,30 @@ def test_rope_of_small_tokens(ops, heads, dh, rot, tokens):
     for t in (0, 1000, tokens - 333):
         want, _ = ops.rope(x[:, t:t + 333], positions=pos[t:t + 333], rot_dim=rot)
         assert torch.equal(got[:, t:t + 333], want)
+
+
+@pytest.mark.parametrize("dtype,heads,dh", [(torch.float32, 4, 512), (torch.bfloat16, 1, 257)])
+def test_evict_in_place_of_more_sequences_than_one_launch_holds(ops, dtype, heads, dh):
+    """A row of 512 fp32 is moved by 32 workgroups, one of 257 bf16 by nine: 2^18 and 2^20 sequences make 2^32 threads and more."""
+    n, slots = (1 << (18 if heads > 1 else 20)) // heads, 2
+    free, _ = torch.cuda.mem_get_info()
+    if free < 24 << 30:
+        pytest.skip("needs 24 GB of device memory")
+    g = torch.Generator(device="cuda").manual_seed(9)
+    # a sequence's slots hold its number and theirs, so that rows and sequences cannot be taken for one another
+    at = torch.arange(n, device="cuda").view(n, 1, 1, 1)
+    tag = torch.cat([at % 256, at // 256 % 256, at // 65536], -1).expand(n, slots, heads, 3).contiguous()
+    k = torch.zeros(n, slots, heads, dh, dtype=dtype, device="cuda")
+    k[..., :3], k[..., dh - 3:] = tag, tag
+    k[..., 3] = torch.arange(heads, device="cuda") + 8 * torch.arange(slots, device="cuda")[:, None]
+    v = -k
+    w = torch.randint(0, 3, (n, heads, slots), generator=g, device="cuda").float()
+    lens = torch.randint(0, slots + 1, (n,), generator=g, device="cuda").int()
+    second = (lens.view(n, 1) == 2) & (w[..., 1] > w[..., 0])  # ties: the lower slot
+    want = torch.where(second[..., None], k[:, 1], k[:, 0])
+    was, want_w = k[:, 1].clone(), torch.where(second, w[..., 1], w[..., 0])
+    want_lens = lens.clamp(max=1)
+    ops.evict(k, v, w, 1, lens=lens, lens_out=lens)
+    assert torch.equal(lens, want_lens)
+    assert torch.equal(k[:, 0], want) and torch.equal(v[:, 0], -want) and torch.equal(w[..., 0], want_w)
+    assert torch.equal(k[:, 1], was) and torch.equal(v[:, 1], -was)
