@@ -144,7 +144,9 @@ jpi_status jpi_prefix_weight_workspace(const jpi_shared_attn* a, size_t* bytes);
  * Errors: JPI_ERR_ARG (NULL, values out of the ranges above, alignment, a
  * workspace that is too small, out at an input's address), JPI_ERR_SHAPE (more
  * than 2^30 rows, 2^27 slots of one prefix or tail, 2^22 prefixes x KV heads, or
- * 2^30 prefix slots x KV heads in all), JPI_ERR_DTYPE, JPI_ERR_HIP. */
+ * 2^30 prefix slots x KV heads in all; or more workgroups than a launch holds,
+ * which takes millions of rows over millions of slots), JPI_ERR_DTYPE,
+ * JPI_ERR_HIP. */
 jpi_status jpi_shared_attention(const jpi_shared_attn* a, void* workspace, size_t workspace_bytes, void* stream);
 
 /* The weight that the rows lay on each prefix slot, accumulated:

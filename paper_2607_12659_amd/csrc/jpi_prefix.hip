@@ -37,7 +37,7 @@ bool same(const jpi_view& a, const jpi_view& b) {
 }
 
 // everything about the arguments that does not depend on pointers
-jpi_status check_sizes(const char* call, const jpi_shared_attn* a) {
+jpi_status check_sizes(const char* call, const jpi_shared_attn* a, bool (*launches_fit)(const jpi_shared_attn&)) {
   if (!a) return fail(JPI_ERR_ARG, "%s: NULL arguments", call);
   if (!known(a->dtype)) return fail(JPI_ERR_DTYPE, "%s: dtype must be JPI_BF16 or JPI_F32", call);
   if (a->n_groups < 1 || a->group < 1 || a->q_rows < 1)
@@ -52,6 +52,7 @@ jpi_status check_sizes(const char* call, const jpi_shared_attn* a) {
   if (rows > 1073741824.0 || a->prefix > 1 << 27 || a->suffix > 1 << 27 || (int64_t)a->n_groups * a->n_kv_heads > 1 << 22 ||
       (double)a->n_groups * a->n_kv_heads * a->prefix > 1073741824.0)
     return fail(JPI_ERR_SHAPE, "%s: more than 2^30 rows, 2^27 slots, 2^22 prefixes x KV heads or 2^30 slots in all", call);
+  if (!launches_fit(*a)) return fail(JPI_ERR_SHAPE, "%s: more workgroups than one launch holds", call);
   return JPI_OK;
 }
 
@@ -138,7 +139,7 @@ jpi_status jpi_shared_attention_workspace(const jpi_shared_attn* a, size_t* byte
   const char* call = "jpi_shared_attention_workspace";
   if (!bytes) return fail(JPI_ERR_ARG, "%s: NULL bytes", call);
   *bytes = 0;
-  const jpi_status st = check_sizes(call, a);
+  const jpi_status st = check_sizes(call, a, shared_attention_fits);
   if (st == JPI_OK) *bytes = shared_attention_bytes(*a);
   return st;
 }
@@ -147,14 +148,14 @@ jpi_status jpi_prefix_weight_workspace(const jpi_shared_attn* a, size_t* bytes) 
   const char* call = "jpi_prefix_weight_workspace";
   if (!bytes) return fail(JPI_ERR_ARG, "%s: NULL bytes", call);
   *bytes = 0;
-  const jpi_status st = check_sizes(call, a);
+  const jpi_status st = check_sizes(call, a, prefix_weight_fits);
   if (st == JPI_OK) *bytes = prefix_weight_bytes(*a);
   return st;
 }
 
 jpi_status jpi_shared_attention(const jpi_shared_attn* a, void* workspace, size_t workspace_bytes, void* stream) {
   const char* call = "jpi_shared_attention";
-  jpi_status st = check_sizes(call, a);
+  jpi_status st = check_sizes(call, a, shared_attention_fits);
   if (st != JPI_OK) return st;
   const int es = a->dtype == JPI_BF16 ? 2 : 4;
   if ((st = check_view(call, "q", a->q, es, false)) != JPI_OK) return st;
@@ -177,7 +178,7 @@ jpi_status jpi_shared_attention(const jpi_shared_attn* a, void* workspace, size_
 jpi_status jpi_prefix_weight(const jpi_shared_attn* a, const float* weight_in, float decay, float* weight_out,
                              void* workspace, size_t workspace_bytes, void* stream) {
   const char* call = "jpi_prefix_weight";
-  jpi_status st = check_sizes(call, a);
+  jpi_status st = check_sizes(call, a, prefix_weight_fits);
   if (st != JPI_OK) return st;
   if (!isfinite(decay)) return fail(JPI_ERR_ARG, "%s: decay must be finite", call);
   if (a->prefix == 0) return JPI_OK;

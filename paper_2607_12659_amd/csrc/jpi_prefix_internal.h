@@ -28,6 +28,10 @@ struct RopeLaunch {
 };
 hipError_t launch_rope(jpi_dtype dt, const RopeLaunch& l, hipStream_t s);
 
+// whether every launch of the call holds its workgroups
+bool shared_attention_fits(const jpi_shared_attn& a);
+bool prefix_weight_fits(const jpi_shared_attn& a);
+
 size_t shared_attention_bytes(const jpi_shared_attn& a);
 hipError_t launch_shared_attention(const jpi_shared_attn& a, void* ws, hipStream_t s);
 

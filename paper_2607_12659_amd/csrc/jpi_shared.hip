@@ -1059,7 +1059,9 @@ Plan weight_plan(const jpi_shared_attn& a) {
 }
 
 unsigned grid8(int64_t items) { return (unsigned)((items + 7) / 8 * 8); }
-bool too_many(int64_t groups, int threads) { return groups * threads >= (int64_t)1 << 32; }  // for one launch
+bool fits(int64_t groups, int threads) { return groups * threads < (int64_t)1 << 32; }  // a launch's threads are counted in 32 bits
+
+int merge_waves(int splits) { return splits > 64 ? 16 : splits > 8 ? 4 : 1; }  // of a row
 
 template <typename T, int DH>
 hipError_t shared_typed(const jpi_shared_attn& a, void* ws, hipStream_t s) {
@@ -1085,8 +1087,9 @@ hipError_t shared_typed(const jpi_shared_attn& a, void* ws, hipStream_t s) {
   }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.splits == 1) return e;
-  if (p.splits > 64) k_shared_merge<T, DH, 16><<<(unsigned)rows, 1024, 0, s>>>(l);
-  else if (p.splits > 8) k_shared_merge<T, DH, 4><<<(unsigned)rows, 256, 0, s>>>(l);
+  const int waves = merge_waves(p.splits);
+  if (waves == 16) k_shared_merge<T, DH, 16><<<(unsigned)rows, 1024, 0, s>>>(l);
+  else if (waves == 4) k_shared_merge<T, DH, 4><<<(unsigned)rows, 256, 0, s>>>(l);
   else k_shared_merge<T, DH, 1><<<(unsigned)((rows + 3) / 4), 256, 0, s>>>(l);
   return hipGetLastError();
 }
@@ -1105,9 +1108,7 @@ hipError_t weight_typed(const jpi_shared_attn& a, const float* w_in, float decay
   l.key_tiles = p.row_tiles;
   const int64_t slots = (int64_t)a.n_groups * a.n_kv_heads * a.prefix;
   if (p.splits > 1) l.part = (float*)ws;
-  const int64_t items = (int64_t)a.n_groups * a.n_kv_heads * p.row_tiles * p.splits;
-  if (too_many(items + 7, 64 * WEIGHT_WAVES) || too_many(slots / 64 + 1, 256)) return hipErrorInvalidConfiguration;
-  k_weight<T, DH><<<grid8(items), 64 * WEIGHT_WAVES, 0, s>>>(l);
+  k_weight<T, DH><<<grid8((int64_t)a.n_groups * a.n_kv_heads * p.row_tiles * p.splits), 64 * WEIGHT_WAVES, 0, s>>>(l);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.splits == 1) return e;
   k_weight_sum<<<(unsigned)((slots + 63) / 64), 256, 0, s>>>(l);
@@ -1127,6 +1128,19 @@ hipError_t by_type(const jpi_shared_attn& a, F f) {
 }
 
 }  // namespace
+
+bool shared_attention_fits(const jpi_shared_attn& a) {
+  const Plan p = shared_plan(a);
+  const int64_t rows = (int64_t)a.n_groups * a.group * a.q_rows * a.n_heads;
+  return fits((int64_t)a.n_groups * a.n_kv_heads * p.row_tiles * p.splits + 7, 64 * p.waves) &&
+         (p.splits == 1 || fits(rows + 3, 64 * merge_waves(p.splits)));
+}
+
+bool prefix_weight_fits(const jpi_shared_attn& a) {
+  const Plan p = weight_plan(a);
+  const int64_t kv = (int64_t)a.n_groups * a.n_kv_heads;
+  return fits(kv * p.row_tiles * p.splits + 7, 64 * WEIGHT_WAVES) && (p.splits == 1 || fits(kv * a.prefix / 64 + 1, 256));
+}
 
 size_t shared_attention_bytes(const jpi_shared_attn& a) {
   const Plan p = shared_plan(a);

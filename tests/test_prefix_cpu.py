@@ -167,3 +167,20 @@ def test_shared_attention_refuses_more_than_a_launch_holds_and_overlap():
     assert j.jpi_shared_attention(attn_args(n_groups=17, prefix=1 << 26)) == j.JPI_ERR_SHAPE
     a = attn_args(prefix=0, suffix=0, q=view(2 * FAKE), out=view(2 * FAKE))
     assert j.jpi_shared_attention(a, FAKE, 1 << 40) == j.JPI_ERR_ARG and "may not be an input" in j.jpi_prefix_last_error()
+
+
+@pytest.mark.parametrize("of_weight,sizes", [
+    (False, dict(dtype=j.JPI_F32, n_groups=1, group=(1 << 22) + 1, q_rows=1, n_heads=1, prefix=1 << 27, suffix=0)),  # the join
+    (False, dict(dtype=j.JPI_F32, n_groups=(1 << 21) + 1, group=5, q_rows=1, n_heads=1, head_dim=256, prefix=1, suffix=1 << 27)),
+    (True, dict(n_groups=1, group=1 << 13, q_rows=1, n_heads=8, n_kv_heads=8, prefix=1 << 27, suffix=0)),            # slots x rows
+])
+def test_calls_that_no_launch_holds_are_refused_before_anything_is_enqueued(of_weight, sizes):
+    """Sizes that pass every limit by themselves, but make 2^32 threads or more."""
+    a = attn_args(lse=FAKE, **sizes)
+    if of_weight:
+        assert j.jpi_prefix_weight_workspace(a) == (j.JPI_ERR_SHAPE, 0)
+        assert j.jpi_prefix_weight(a, None, 1.0, FAKE, FAKE, 1 << 50) == j.JPI_ERR_SHAPE
+    else:
+        assert j.jpi_shared_attention_workspace(a) == (j.JPI_ERR_SHAPE, 0)
+        assert j.jpi_shared_attention(a, FAKE, 1 << 50) == j.JPI_ERR_SHAPE
+    assert "workgroups" in j.jpi_prefix_last_error()
