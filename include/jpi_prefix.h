@@ -87,9 +87,9 @@ typedef struct {
 
 /* Turn q [batch][tokens][q_heads][head_dim] into q_out and, where k is not NULL,
  * k [batch][tokens][k_heads][head_dim] into k_out, in one launch.  An output may
- * be its input (same data and strides); other overlaps of an output with an
- * input or with itself are not allowed (a stride of 0 on an input is: all heads
- * read the same row).  positions: device int32, token t of batch b at
+ * be its input (same data and strides, but for dimensions of size 1); other
+ * overlaps of an output with an input or with itself are not allowed (a stride of
+ * 0 on an input is: all heads read the same row).  positions: device int32, token t of batch b at
  * positions[b * pos_stride + t] (pos_stride 0: shared by the batch), or NULL for
  * 0, 1, 2 ...  Any alignment and strides; 16-byte aligned rows are fastest.
  * batch or tokens 0: nothing is done.  Errors: JPI_ERR_ARG (NULL, values out of
@@ -188,11 +188,11 @@ typedef struct {
 } jpi_evict_args;
 
 /* k_out, v_out and weight_out may be k, v and weight themselves (same data and
- * strides: the cache is compacted where it lies) or memory that overlaps no
- * input; K and V may not overlap each other.  Any alignment; 16-byte aligned
- * rows are fastest.  Errors: JPI_ERR_ARG (NULL, values out of the ranges above),
- * JPI_ERR_SHAPE (more than 2^26 slots, 2^20 sequences n_outer * n_heads, or 2^40
- * bytes of K), JPI_ERR_DTYPE, JPI_ERR_HIP. */
+ * strides, but for dimensions of size 1: the cache is compacted where it lies)
+ * or memory that overlaps no input; K and V may not overlap each other.  Any
+ * alignment; 16-byte aligned rows are fastest.  Errors: JPI_ERR_ARG (NULL, values
+ * out of the ranges above), JPI_ERR_SHAPE (more than 2^26 slots, 2^20 sequences
+ * n_outer * n_heads, or 2^40 bytes of K), JPI_ERR_DTYPE, JPI_ERR_HIP. */
 jpi_status jpi_evict(const jpi_evict_args* a, void* stream);
 
 #ifdef __cplusplus

@@ -32,8 +32,9 @@ bool negative(const jpi_view& v) { return v.outer < 0 || v.row < 0 || v.head < 0
 bool aligned16(const jpi_view& v, int es) {
   return ((uintptr_t)v.data & 15) == 0 && (v.outer * es) % 16 == 0 && (v.row * es) % 16 == 0 && (v.head * es) % 16 == 0;
 }
-bool same(const jpi_view& a, const jpi_view& b) {
-  return a.outer == b.outer && a.row == b.row && a.head == b.head;
+// the same places for [outer][rows][heads]: strides of a dimension of size 1 are not used
+bool same(const jpi_view& a, const jpi_view& b, int outer, int rows, int heads) {
+  return (outer <= 1 || a.outer == b.outer) && (rows <= 1 || a.row == b.row) && (heads <= 1 || a.head == b.head);
 }
 
 // everything about the arguments that does not depend on pointers
@@ -111,7 +112,7 @@ jpi_status jpi_rope(const jpi_rope_config* cfg, jpi_dtype dt, int batch, int tok
   for (int i = 0; i < (k ? 2 : 1); ++i) {
     if (!in[i]->data || !out[i]->data) return fail(JPI_ERR_ARG, "%s: NULL data", call);
     if (negative(*in[i]) || negative(*out[i])) return fail(JPI_ERR_ARG, "%s: negative stride", call);
-    if (in[i]->data == out[i]->data && !same(*in[i], *out[i]))
+    if (in[i]->data == out[i]->data && !same(*in[i], *out[i], batch, tokens, i ? k_heads : q_heads))
       return fail(JPI_ERR_ARG, "%s: in place, input and output need the same strides", call);
     l.t[i] = RopeTensor{in[i]->data, out[i]->data, in[i]->outer, in[i]->row, in[i]->head, out[i]->outer, out[i]->row,
                         out[i]->head, i ? k_heads : q_heads};
@@ -206,14 +207,14 @@ jpi_status jpi_evict(const jpi_evict_args* a, void* stream) {
   const int most = a->keep < a->slots ? a->keep : a->slots;
   if (a->weight_stride < a->slots || (a->weight_out && a->weight_out_stride < most))
     return fail(JPI_ERR_ARG, "%s: weight stride below the number of slots", call);
-  if (a->weight_out == a->weight && a->weight_out_stride != a->weight_stride)
+  if (a->weight_out && a->weight_out == a->weight && a->weight_out_stride != a->weight_stride && a->n_outer * a->n_heads > 1)
     return fail(JPI_ERR_ARG, "%s: in place, the weights need the same stride", call);
   const jpi_view* in[2] = {&a->k, &a->v};
   const jpi_view* out[2] = {&a->k_out, &a->v_out};
   for (int i = 0; i < 2; ++i) {
     if (a->slots > 0 && (!in[i]->data || !out[i]->data)) return fail(JPI_ERR_ARG, "%s: NULL data", call);
     if (negative(*in[i]) || negative(*out[i])) return fail(JPI_ERR_ARG, "%s: negative stride", call);
-    if (in[i]->data == out[i]->data && !same(*in[i], *out[i]))
+    if (in[i]->data == out[i]->data && !same(*in[i], *out[i], a->n_outer, most, a->n_heads))
       return fail(JPI_ERR_ARG, "%s: in place, input and output need the same strides", call);
   }
   return launched(call, launch_evict(*a, (hipStream_t)stream));

@@ -773,3 +773,27 @@ def test_evict_in_place_of_more_sequences_than_one_launch_holds(ops, dtype, head
     assert torch.equal(lens, want_lens)
     assert torch.equal(k[:, 0], want) and torch.equal(v[:, 0], -want) and torch.equal(w[..., 0], want_w)
     assert torch.equal(k[:, 1], was) and torch.equal(v[:, 1], -was)
+
+
+@pytest.mark.parametrize("heads", [1, 2])
+@pytest.mark.parametrize("keep", [1, 2, 5])
+def test_evict_into_the_first_slots_of_its_own_cache(ops, keep, heads):
+    """Outputs that are the first slots of the inputs: the same memory and strides, a single slot too."""
+    n, slots, dh = 3, 40, 64
+    k, v, w = rand(1, n, slots, heads, dh), rand(2, n, slots, heads, dh), rand(3, n, heads, slots)
+    dk, dv, dw = dev(k), dev(v), dev(w)
+    wo = torch.zeros(n, heads, keep, device="cuda")
+    ops.evict(dk, dv, dw, keep, k_out=dk[:, :keep], v_out=dv[:, :keep], weight_out=wo)
+    for o in range(n):
+        for h in range(heads):
+            kept = kept_slots(w[o, h], slots, keep, 0, 0)
+            for got, src in ((dk.cpu(), k), (dv.cpu(), v)):
+                assert torch.equal(got[o, :keep, h], src[o, kept, h]) and torch.equal(got[o, keep:, h], src[o, keep:, h])
+            assert torch.equal(wo[o, h].cpu(), w[o, h, kept])
+    assert torch.equal(dw.cpu(), w)
+    # one sequence: the weights' first slots are contiguous as well
+    one = [t[:1, :, :1].contiguous() for t in (dev(k), dev(v))] + [dev(w)[:1, :1].contiguous()]
+    ops.evict(*one, keep, k_out=one[0][:, :keep], v_out=one[1][:, :keep], weight_out=one[2][:, :, :keep])
+    kept = kept_slots(w[0, 0], slots, keep, 0, 0)
+    assert torch.equal(one[0][0, :keep, 0].cpu(), k[0, kept, 0]) and torch.equal(one[2][0, 0, :keep].cpu(), w[0, 0, kept])
+    assert torch.equal(one[2][0, 0, keep:].cpu(), w[0, 0, keep:])

@@ -184,3 +184,14 @@ def test_calls_that_no_launch_holds_are_refused_before_anything_is_enqueued(of_w
         assert j.jpi_shared_attention_workspace(a) == (j.JPI_ERR_SHAPE, 0)
         assert j.jpi_shared_attention(a, FAKE, 1 << 50) == j.JPI_ERR_SHAPE
     assert "workgroups" in j.jpi_prefix_last_error()
+
+
+def test_strides_in_place_count_where_there_are_several():
+    """Two kept slots in place want the inputs' row stride, two sequences their weights' stride."""
+    def call(most, n_outer=1, outer=0):
+        a = evict_args(n_outer=n_outer, slots=100, keep=most, n_first=0, n_last=0, weight_out=FAKE, weight_out_stride=50)
+        a.k = j.jpi_view(FAKE, 25600, 256, 256)
+        a.k_out = j.jpi_view(FAKE, outer, 0, 0)
+        return j.jpi_evict(a), j.jpi_prefix_last_error()
+    assert call(2)[0] == j.JPI_ERR_ARG and "same strides" in call(2)[1]
+    assert call(1, n_outer=2, outer=25600)[0] == j.JPI_ERR_ARG and "same stride" in call(1, n_outer=2, outer=25600)[1]
