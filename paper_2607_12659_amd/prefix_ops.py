@@ -6,9 +6,11 @@ stream of the tensors' device, which may be capturing a graph.  Outputs and
 workspaces are allocated by torch on that stream unless they are given.
 Floating tensors are bfloat16 or float32, lengths and positions int32; tensors
 may be strided as long as the elements of a head are contiguous.  No gradients
-are recorded (that of a rotation is the rotation with inverse=True).  Errors are
-raised as ``jpi.JpiError`` (the library's checks), ``ValueError`` or
-``TypeError`` (shapes, devices and types).
+are recorded (that of a rotation is the rotation with inverse=True), so tensors
+that require them are refused while torch records gradients, as torch refuses
+them for its own out= arguments; tensors that a call writes into count as
+changed in place.  Errors are raised as ``jpi.JpiError`` (the library's checks),
+``ValueError`` or ``TypeError`` (shapes, devices and types).
 """
 from __future__ import annotations
 
@@ -71,6 +73,16 @@ def _dense(name, t):
 _current_device, _raw_stream = getattr(torch._C, "_cuda_getDevice", None), getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
+_recording, _written = torch.is_grad_enabled, torch.autograd.graph.increment_version
+
+
+def _no_gradients(*tensors):
+    """None of the tensors wants a gradient that the call would not record; asked for while torch records them."""
+    for t in tensors:
+        if t is not None and t.requires_grad:
+            raise ValueError("no gradients are recorded through this call: detach its tensors, or call it under torch.no_grad()")
+
+
 def _launch(dev, f, *args):
     """f of the library on the current stream of GPU `dev`, which is made current for the call where it is not."""
     if dev < 0:
@@ -93,6 +105,9 @@ def rope(q, k=None, positions=None, *, rot_dim=None, layout="half", base=1e4, sc
     """
     if q.dim() != 4:
         raise ValueError("q must be [batch][tokens][heads][head_dim]")
+    if _recording():
+        _no_gradients(q, k, q_out, k_out)
+    given = [t for t in (q_out, k_out) if t is not None]
     b, n, heads, dh = q.shape
     dt, dev = _dtype(q), q.get_device()
     if layout not in _LAYOUT or scaling not in _SCALING:
@@ -130,6 +145,8 @@ def rope(q, k=None, positions=None, *, rot_dim=None, layout="half", base=1e4, sc
     pack = _VIEW.pack
     _launch(dev, _lib.jpi_rope, cfg, dt, b, n, pos, pos_stride, pack(*_view("q", q)), pack(*_view("q_out", q_out)), heads, kv, ko,
             k_heads)
+    if given:
+        _written(given)
     return q_out, k_out
 
 
@@ -172,6 +189,9 @@ def shared_attention(q, k_prefix, v_prefix, k_suffix=None, v_suffix=None, *, pre
     Returns (out, lse): out like q, lse float32 [batch][rows][heads].
     """
     b, rows, heads, dh, g, p, kv, dev = _shapes(q, k_prefix)
+    if _recording():
+        _no_gradients(q, k_prefix, v_prefix, k_suffix, v_suffix, out, lse)
+    given = [t for t in (out, lse) if t is not None]
     dt = _dtype(q)
     _want("v_prefix", v_prefix, k_prefix.shape, q.dtype, dev)
     if (k_suffix is None) != (v_suffix is None):
@@ -199,6 +219,8 @@ def shared_attention(q, k_prefix, v_prefix, k_suffix=None, v_suffix=None, *, pre
                       _dense("lse", lse))
     ws, n = _workspace(_lib.jpi_shared_attention_workspace, args, q)
     _launch(dev, _lib.jpi_shared_attention, args, ws.data_ptr() if n else None, n)
+    if given:
+        _written(given)
     return out, lse
 
 
@@ -210,13 +232,16 @@ def prefix_weight(q, k_prefix, lse, weight=None, *, prefix_len=None, decay=1.0, 
     itself to accumulate in place.  Returns out.
     """
     b, rows, heads, dh, g, p, kv, dev = _shapes(q, k_prefix)
+    if _recording():
+        _no_gradients(q, k_prefix, lse, weight, out)
     dt, shape = _dtype(q), (g, kv, p)
     _want("lse", lse, (b, rows, heads), _F32, dev)
     w = None
     if weight is not None:
         _want("weight", weight, shape, _F32, dev)
         w = _dense("weight", weight)
-    if out is None:
+    given = out is not None
+    if not given:
         out = (q.new_empty if prefix_len is None else q.new_zeros)(shape, dtype=_F32)
     else:
         _want("out", out, shape, _F32, dev)
@@ -225,6 +250,8 @@ def prefix_weight(q, k_prefix, lse, weight=None, *, prefix_len=None, decay=1.0, 
                       _dense("lse", lse))
     ws, n = _workspace(_lib.jpi_prefix_weight_workspace, args, q)
     _launch(dev, _lib.jpi_prefix_weight, args, w, decay, _dense("out", out), ws.data_ptr() if n else None, n)
+    if given:
+        _written(out)
     return out
 
 
@@ -250,6 +277,9 @@ def evict(k, v, weight, keep, *, lens=None, n_first=0, n_last=0, k_out=None, v_o
     """
     if k.dim() != 4:
         raise ValueError("k must be [outer][slots][heads][head_dim]")
+    if _recording():
+        _no_gradients(k, v, weight, k_out, v_out, weight_out)
+    given = [t for t in (index, lens_out) if t is not None]
     n, slots, heads, dh = k.shape
     dt, dev = _dtype(k), k.get_device()
     _want("v", v, k.shape, k.dtype, dev)
@@ -270,4 +300,5 @@ def evict(k, v, weight, keep, *, lens=None, n_first=0, n_last=0, k_out=None, v_o
                        *_view("k", k), *_view("v", v), *_view("k_out", k_out), *_view("v_out", v_out),
                        _dense("weight_out", weight_out), weight_out.shape[2], _dense("index", index), _dense("lens_out", lens_out))
     _launch(dev, _lib.jpi_evict, args)
+    _written([k_out, v_out, weight_out, *given])
     return index, lens_out

@@ -797,3 +797,27 @@ def test_evict_into_the_first_slots_of_its_own_cache(ops, keep, heads):
     kept = kept_slots(w[0, 0], slots, keep, 0, 0)
     assert torch.equal(one[0][0, :keep, 0].cpu(), k[0, kept, 0]) and torch.equal(one[2][0, 0, :keep].cpu(), w[0, 0, kept])
     assert torch.equal(one[2][0, 0, keep:].cpu(), w[0, 0, keep:])
+
+
+def test_tensors_written_in_place_are_known_to_have_changed(ops):
+    """Outputs that the caller gave count as changed, so that a backward pass that wants their old values refuses."""
+    s = serving_state(5)
+    before = {n: s[n]._version for n in s}
+    serve(ops, s, 100)
+    written = ("q_rot", "cache_k", "out", "lse", "w", "k2", "v2", "w2", "index", "lens", "out2", "lse2")
+    for n in s:
+        assert (s[n]._version > before[n]) == (n in written), n
+    q, k = dev(rand(1, 1, 4, 2, 64)), dev(rand(2, 1, 4, 2, 64))
+    v, w = k.clone(), torch.rand(1, 2, 4, device="cuda")
+    leaf = torch.ones(1, 4, 2, 64, device="cuda", requires_grad=True)
+    losses = [(leaf * t).sum() for t in (q, k, v)]
+    ops.rope(q, q_out=q)
+    ops.evict(k, v, w, 2)
+    for loss in losses:
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            loss.backward()
+    with torch.inference_mode():
+        x = torch.ones(1, 4, 2, 64, device="cuda")
+    ops.rope(x, q_out=x)
+    with torch.no_grad():
+        ops.rope(leaf, q_out=leaf)

@@ -195,3 +195,22 @@ def test_strides_in_place_count_where_there_are_several():
         return j.jpi_evict(a), j.jpi_prefix_last_error()
     assert call(2)[0] == j.JPI_ERR_ARG and "same strides" in call(2)[1]
     assert call(1, n_outer=2, outer=25600)[0] == j.JPI_ERR_ARG and "same stride" in call(1, n_outer=2, outer=25600)[1]
+
+
+def test_tensors_that_want_gradients_are_refused():
+    torch = pytest.importorskip("torch")
+    from paper_2607_12659_amd import prefix_ops as ops
+    q, lse = torch.zeros(2, 3, 4, 64), torch.zeros(2, 3, 4)
+    w, leaf = torch.zeros(2, 4, 3), torch.zeros(2, 3, 4, 64, requires_grad=True)
+    calls = [lambda t: ops.rope(t), lambda t: ops.rope(q, t), lambda t: ops.rope(q, q_out=t),
+             lambda t: ops.shared_attention(t, q, q), lambda t: ops.shared_attention(q, q, t),
+             lambda t: ops.shared_attention(q, q, q, q, t), lambda t: ops.prefix_weight(q, t, lse),
+             lambda t: ops.evict(q, t, w, 2), lambda t: ops.evict(t, q, w, 2)]
+    for call in calls:
+        with pytest.raises(ValueError, match="gradients"):
+            call(leaf)
+        for off in (torch.no_grad, torch.inference_mode):  # taken, up to the next check
+            with off(), pytest.raises(ValueError, match="GPU"):
+                call(leaf)
+        with pytest.raises(ValueError, match="GPU"):
+            call(leaf.detach())
