@@ -36,6 +36,14 @@ _EVICT = struct.Struct("@8iPqP" + _V * 4 + "PqPP")
 assert (_ROPE.size, _VIEW.size, _ATTN.size, _EVICT.size) == tuple(
     ctypes.sizeof(c) for c in (_j.jpi_rope_config, _j.jpi_view, _j.jpi_shared_attn, _j.jpi_evict_args))
 _NONE = (0, 0, 0, 0)
+_INT_MAX = 2 ** 31 - 1  # C's int, to which ctypes would cut a larger one without a word
+
+
+def _pack(structure, *values):
+    try:
+        return structure.pack(*values)
+    except (struct.error, OverflowError) as e:
+        raise ValueError("an argument is no number or out of its C type's range: %s" % e) from None
 
 
 def _dtype(t):
@@ -112,8 +120,10 @@ def rope(q, k=None, positions=None, *, rot_dim=None, layout="half", base=1e4, sc
     dt, dev = _dtype(q), q.get_device()
     if layout not in _LAYOUT or scaling not in _SCALING:
         raise ValueError("unknown layout %r or scaling %r" % (layout, scaling))
-    cfg = _ROPE.pack(dh, dh if rot_dim is None else rot_dim, _LAYOUT[layout], _SCALING[scaling], int(bool(inverse)), base, factor,
-                     trained, beta_fast, beta_slow, amplitude)
+    cfg = _pack(_ROPE, dh, dh if rot_dim is None else rot_dim, _LAYOUT[layout], _SCALING[scaling], int(bool(inverse)), base,
+                factor, trained, beta_fast, beta_slow, amplitude)
+    if b > _INT_MAX or n > _INT_MAX or heads > _INT_MAX:
+        raise ValueError("q is larger than 2^31 - 1 in a dimension")
     if q_out is None:
         q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
     elif q_out is not q:
@@ -124,6 +134,8 @@ def rope(q, k=None, positions=None, *, rot_dim=None, layout="half", base=1e4, sc
     else:
         k_heads = k.shape[2] if k.dim() == 4 else 0
         _want("k", k, (b, n, k_heads, dh), q.dtype, dev)
+        if k_heads > _INT_MAX:
+            raise ValueError("k has more than 2^31 - 1 heads")
         if k_out is None:
             k_out = torch.empty_like(k, memory_format=torch.contiguous_format)
         elif k_out is not k:
@@ -213,10 +225,10 @@ def shared_attention(q, k_prefix, v_prefix, k_suffix=None, v_suffix=None, *, pre
         lse = q.new_empty((b, rows, heads), dtype=_F32)
     else:
         _want("lse", lse, (b, rows, heads), _F32, dev)
-    args = _ATTN.pack(dt, g, b // g, rows, heads, kv, dh, p, s, int(bool(causal)), dh ** -0.5 if scale is None else scale,
-                      *_view("q", q), *_view("k_prefix", k_prefix), *_view("v_prefix", v_prefix), *ks, *vs,
-                      _lens("prefix_len", prefix_len, g, dev), _lens("suffix_len", suffix_len, b, dev), *_view("out", out),
-                      _dense("lse", lse))
+    args = _pack(_ATTN, dt, g, b // g, rows, heads, kv, dh, p, s, int(bool(causal)), dh ** -0.5 if scale is None else scale,
+                 *_view("q", q), *_view("k_prefix", k_prefix), *_view("v_prefix", v_prefix), *ks, *vs,
+                 _lens("prefix_len", prefix_len, g, dev), _lens("suffix_len", suffix_len, b, dev), *_view("out", out),
+                 _dense("lse", lse))
     ws, n = _workspace(_lib.jpi_shared_attention_workspace, args, q)
     _launch(dev, _lib.jpi_shared_attention, args, ws.data_ptr() if n else None, n)
     if given:
@@ -245,11 +257,11 @@ def prefix_weight(q, k_prefix, lse, weight=None, *, prefix_len=None, decay=1.0, 
         out = (q.new_empty if prefix_len is None else q.new_zeros)(shape, dtype=_F32)
     else:
         _want("out", out, shape, _F32, dev)
-    args = _ATTN.pack(dt, g, b // g, rows, heads, kv, dh, p, 0, 0, dh ** -0.5 if scale is None else scale, *_view("q", q),
-                      *_view("k_prefix", k_prefix), *_NONE, *_NONE, *_NONE, _lens("prefix_len", prefix_len, g, dev), 0, *_NONE,
-                      _dense("lse", lse))
+    args = _pack(_ATTN, dt, g, b // g, rows, heads, kv, dh, p, 0, 0, dh ** -0.5 if scale is None else scale, *_view("q", q),
+                 *_view("k_prefix", k_prefix), *_NONE, *_NONE, *_NONE, _lens("prefix_len", prefix_len, g, dev), 0, *_NONE,
+                 _dense("lse", lse))
     ws, n = _workspace(_lib.jpi_prefix_weight_workspace, args, q)
-    _launch(dev, _lib.jpi_prefix_weight, args, w, decay, _dense("out", out), ws.data_ptr() if n else None, n)
+    _launch(dev, _lib.jpi_prefix_weight, args, w, float(decay), _dense("out", out), ws.data_ptr() if n else None, n)
     if given:
         _written(out)
     return out
@@ -285,6 +297,8 @@ def evict(k, v, weight, keep, *, lens=None, n_first=0, n_last=0, k_out=None, v_o
     _want("v", v, k.shape, k.dtype, dev)
     _want("weight", weight, (n, heads, slots), _F32, dev)
     keep = int(keep)
+    if keep > _INT_MAX:
+        raise ValueError("keep is larger than 2^31 - 1")
     most = min(keep, slots)
     k_out, v_out = _room("k_out", k_out, k, k.dtype, 1, most, dev), _room("v_out", v_out, v, k.dtype, 1, most, dev)
     weight_out = _room("weight_out", weight_out, weight, _F32, 2, most, dev)
@@ -296,9 +310,9 @@ def evict(k, v, weight, keep, *, lens=None, n_first=0, n_last=0, k_out=None, v_o
         lens_out = torch.empty((n,), dtype=_I32, device=k.device)
     else:
         _want("lens_out", lens_out, (n,), _I32, dev)
-    args = _EVICT.pack(dt, n, heads, dh, slots, keep, n_first, n_last, _dense("weight", weight), slots, _lens("lens", lens, n, dev),
-                       *_view("k", k), *_view("v", v), *_view("k_out", k_out), *_view("v_out", v_out),
-                       _dense("weight_out", weight_out), weight_out.shape[2], _dense("index", index), _dense("lens_out", lens_out))
+    args = _pack(_EVICT, dt, n, heads, dh, slots, keep, n_first, n_last, _dense("weight", weight), slots,
+                 _lens("lens", lens, n, dev), *_view("k", k), *_view("v", v), *_view("k_out", k_out), *_view("v_out", v_out),
+                 _dense("weight_out", weight_out), weight_out.shape[2], _dense("index", index), _dense("lens_out", lens_out))
     _launch(dev, _lib.jpi_evict, args)
     _written([k_out, v_out, weight_out, *given])
     return index, lens_out

@@ -214,3 +214,25 @@ def test_tensors_that_want_gradients_are_refused():
                 call(leaf)
         with pytest.raises(ValueError, match="GPU"):
             call(leaf.detach())
+
+
+def test_sizes_past_c_ints_and_numbers_that_are_none_are_refused():
+    """2^32 + 5 tokens are not five of them; what does not fit the C structures raises what the module documents."""
+    torch = pytest.importorskip("torch")
+    from paper_2607_12659_amd import prefix_ops as ops
+    many = torch.zeros(1, 1, 1, 2).expand(1, 2 ** 32 + 5, 1, 2)
+    for x in (many, many.transpose(0, 1), many.transpose(1, 2)):
+        with pytest.raises(ValueError, match="2\\^31"):
+            ops.rope(x, q_out=x)
+    few = torch.zeros(1, 1, 1, 2)
+    with pytest.raises(ValueError, match="2\\^31"):
+        ops.rope(few, many.transpose(1, 2), k_out=many.transpose(1, 2))
+    q, w = torch.zeros(2, 3, 4, 64), torch.zeros(2, 4, 3)
+    with pytest.raises(ValueError, match="2\\^31"):
+        ops.evict(q, q.clone(), w, 2 ** 40)
+    for call in (lambda: ops.rope(q, rot_dim=2.5), lambda: ops.rope(q, base="ten"), lambda: ops.rope(q, rot_dim=2 ** 31),
+                 lambda: ops.rope(q, factor=10 ** 400), lambda: ops.shared_attention(q, q, q, scale="one"),
+                 lambda: ops.evict(q, q.clone(), w, 2, n_first=2 ** 31), lambda: ops.evict(q, q.clone(), w, 2, n_last=0.5),
+                 lambda: ops.prefix_weight(q, q, torch.zeros(2, 3, 4), decay="half")):
+        with pytest.raises(ValueError, match="range|could not convert"):
+            call()
