@@ -82,7 +82,7 @@ typedef struct {
   double base;   /* > 1 */
   double factor; /* >= 1; ignored by JPI_ROPE_PLAIN */
   double trained, beta_fast, beta_slow; /* JPI_ROPE_PARTS: trained > 0, beta_fast > beta_slow >= 0 */
-  double amplitude;                     /* finite */
+  double amplitude;                     /* finite, as a float too */
 } jpi_rope_config;
 
 /* Turn q [batch][tokens][q_heads][head_dim] into q_out and, where k is not NULL,
@@ -120,7 +120,7 @@ typedef struct {
   int n_heads, n_kv_heads, head_dim;   /* n_heads a multiple of n_kv_heads; head_dim 64, 128 or 256 */
   int prefix, suffix;                  /* slots per group and per rollout, >= 0 */
   int causal;
-  float scale;                         /* finite, > 0 (usually head_dim^-1/2) */
+  float scale;                         /* > 0, scale / ln 2 finite (usually head_dim^-1/2) */
   jpi_view q;                          /* [batch][q_rows][n_heads][head_dim] */
   jpi_view k_prefix, v_prefix;         /* [n_groups][prefix][n_kv_heads][head_dim]; not read if prefix is 0 */
   jpi_view k_suffix, v_suffix;         /* [batch][suffix][n_kv_heads][head_dim]; not read if suffix is 0 */

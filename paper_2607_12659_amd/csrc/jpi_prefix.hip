@@ -48,7 +48,9 @@ jpi_status check_sizes(const char* call, const jpi_shared_attn* a, bool (*launch
   if (a->head_dim != 64 && a->head_dim != 128 && a->head_dim != 256)
     return fail(JPI_ERR_ARG, "%s: head_dim must be 64, 128 or 256", call);
   if (a->prefix < 0 || a->suffix < 0) return fail(JPI_ERR_ARG, "%s: negative prefix or suffix", call);
-  if (!isfinite(a->scale) || a->scale <= 0.f) return fail(JPI_ERR_ARG, "%s: scale must be finite and > 0", call);
+  // the kernels take scores in powers of two
+  if (!isfinite(a->scale * 1.44269504f) || !(a->scale > 0.f))
+    return fail(JPI_ERR_ARG, "%s: scale, and scale / ln 2, must be finite and > 0", call);
   const double rows = (double)a->n_groups * a->group * a->q_rows * a->n_heads;
   if (rows > 1073741824.0 || a->prefix > 1 << 27 || a->suffix > 1 << 27 || (int64_t)a->n_groups * a->n_kv_heads > 1 << 22 ||
       (double)a->n_groups * a->n_kv_heads * a->prefix > 1073741824.0)
@@ -93,7 +95,7 @@ jpi_status jpi_rope(const jpi_rope_config* cfg, jpi_dtype dt, int batch, int tok
   if (c.layout != JPI_ROPE_HALF && c.layout != JPI_ROPE_INTERLEAVED) return fail(JPI_ERR_ARG, "%s: unknown layout", call);
   if (c.scaling < JPI_ROPE_PLAIN || c.scaling > JPI_ROPE_PARTS) return fail(JPI_ERR_ARG, "%s: unknown scaling", call);
   if (!isfinite(c.base) || c.base <= 1.0) return fail(JPI_ERR_ARG, "%s: base must be finite and > 1", call);
-  if (!isfinite(c.amplitude)) return fail(JPI_ERR_ARG, "%s: amplitude must be finite", call);
+  if (!isfinite((float)c.amplitude)) return fail(JPI_ERR_ARG, "%s: amplitude must be finite as a float", call);
   if (c.scaling != JPI_ROPE_PLAIN && (!isfinite(c.factor) || c.factor < 1.0))
     return fail(JPI_ERR_ARG, "%s: factor must be finite and >= 1", call);
   if (c.scaling == JPI_ROPE_BASE && c.rot_dim == 2)

@@ -236,3 +236,11 @@ def test_sizes_past_c_ints_and_numbers_that_are_none_are_refused():
                  lambda: ops.prefix_weight(q, q, torch.zeros(2, 3, 4), decay="half")):
         with pytest.raises(ValueError, match="range|could not convert"):
             call()
+
+
+def test_numbers_that_are_infinite_in_fp32_are_refused():
+    """An amplitude past fp32, and a scale whose scores in powers of two would be 0 * inf."""
+    assert rope_call(amplitude=1e39) == j.JPI_ERR_ARG and rope_call(amplitude=-1e300) == j.JPI_ERR_ARG
+    for call in (lambda a: j.jpi_shared_attention(a, FAKE, 1 << 40), lambda a: j.jpi_prefix_weight(a, None, 1.0, FAKE, FAKE, 1 << 40)):
+        assert call(attn_args(lse=FAKE, scale=3e38)) == j.JPI_ERR_ARG
+        assert "scale" in j.jpi_prefix_last_error()
