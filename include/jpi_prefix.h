@@ -24,7 +24,10 @@
  *     jpi_prefix_last_error().
  *   - Arrays are given as jpi_view: element (o, r, h, d) of
  *     [outer][row][head][head_dim] lies at data[o * outer + r * row + h * head
- *     + d].  Strides are in elements and may be in any order, but not negative.
+ *     + d].  Strides are in elements and may be in any order, but not negative;
+ *     an input's may be 0.  Outputs may not overlap each other, themselves or,
+ *     but where a call says so, an input; what shows it at first sight (equal
+ *     addresses, a stride of 0) is JPI_ERR_ARG.
  *   - Lengths are int32 arrays on the device (or NULL: all slots).  They are
  *     read when the kernels run; values outside [0, slots] count as the nearer
  *     end.  Slots at or past a length are never read, so they may hold

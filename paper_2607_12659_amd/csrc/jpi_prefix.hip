@@ -37,6 +37,15 @@ bool same(const jpi_view& a, const jpi_view& b, int outer, int rows, int heads) 
   return (outer <= 1 || a.outer == b.outer) && (rows <= 1 || a.row == b.row) && (heads <= 1 || a.head == b.head);
 }
 
+// an output of which several elements are one
+bool folded(const jpi_view& v, int outer, int rows, int heads) {
+  return (outer > 1 && v.outer == 0) || (rows > 1 && v.row == 0) || (heads > 1 && v.head == 0);
+}
+// one of a pair of tensors is written where the other one is read or written
+bool crossed(const jpi_view* const in[2], const jpi_view* const out[2]) {
+  return out[0]->data == out[1]->data || out[0]->data == in[1]->data || out[1]->data == in[0]->data;
+}
+
 // everything about the arguments that does not depend on pointers
 jpi_status check_sizes(const char* call, const jpi_shared_attn* a, bool (*launches_fit)(const jpi_shared_attn&)) {
   if (!a) return fail(JPI_ERR_ARG, "%s: NULL arguments", call);
@@ -116,9 +125,11 @@ jpi_status jpi_rope(const jpi_rope_config* cfg, jpi_dtype dt, int batch, int tok
     if (negative(*in[i]) || negative(*out[i])) return fail(JPI_ERR_ARG, "%s: negative stride", call);
     if (in[i]->data == out[i]->data && !same(*in[i], *out[i], batch, tokens, i ? k_heads : q_heads))
       return fail(JPI_ERR_ARG, "%s: in place, input and output need the same strides", call);
+    if (folded(*out[i], batch, tokens, i ? k_heads : q_heads)) return fail(JPI_ERR_ARG, "%s: an output has a stride of 0", call);
     l.t[i] = RopeTensor{in[i]->data, out[i]->data, in[i]->outer, in[i]->row, in[i]->head, out[i]->outer, out[i]->row,
                         out[i]->head, i ? k_heads : q_heads};
   }
+  if (k && crossed(in, out)) return fail(JPI_ERR_ARG, "%s: q_out or k_out is where another tensor is", call);
   l.pos = positions;
   l.pos_stride = pos_stride;
   l.batch = batch;
@@ -175,6 +186,7 @@ jpi_status jpi_shared_attention(const jpi_shared_attn* a, void* workspace, size_
   if (a->out.data == a->q.data || (a->prefix > 0 && (a->out.data == a->k_prefix.data || a->out.data == a->v_prefix.data)) ||
       (a->suffix > 0 && (a->out.data == a->k_suffix.data || a->out.data == a->v_suffix.data)))
     return fail(JPI_ERR_ARG, "%s: out may not be an input", call);
+  if (folded(a->out, a->n_groups * a->group, a->q_rows, a->n_heads)) return fail(JPI_ERR_ARG, "%s: out has a stride of 0", call);
   return launched(call, launch_shared_attention(*a, workspace, (hipStream_t)stream));
 }
 
@@ -216,9 +228,11 @@ jpi_status jpi_evict(const jpi_evict_args* a, void* stream) {
   for (int i = 0; i < 2; ++i) {
     if (a->slots > 0 && (!in[i]->data || !out[i]->data)) return fail(JPI_ERR_ARG, "%s: NULL data", call);
     if (negative(*in[i]) || negative(*out[i])) return fail(JPI_ERR_ARG, "%s: negative stride", call);
-    if (in[i]->data == out[i]->data && !same(*in[i], *out[i], a->n_outer, most, a->n_heads))
+    if (most > 0 && in[i]->data == out[i]->data && !same(*in[i], *out[i], a->n_outer, most, a->n_heads))
       return fail(JPI_ERR_ARG, "%s: in place, input and output need the same strides", call);
+    if (folded(*out[i], a->n_outer, most, a->n_heads)) return fail(JPI_ERR_ARG, "%s: an output has a stride of 0", call);
   }
+  if (most > 0 && crossed(in, out)) return fail(JPI_ERR_ARG, "%s: k_out or v_out is where another tensor is", call);
   return launched(call, launch_evict(*a, (hipStream_t)stream));
 }
 

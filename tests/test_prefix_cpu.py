@@ -244,3 +244,21 @@ def test_numbers_that_are_infinite_in_fp32_are_refused():
     for call in (lambda a: j.jpi_shared_attention(a, FAKE, 1 << 40), lambda a: j.jpi_prefix_weight(a, None, 1.0, FAKE, FAKE, 1 << 40)):
         assert call(attn_args(lse=FAKE, scale=3e38)) == j.JPI_ERR_ARG
         assert "scale" in j.jpi_prefix_last_error()
+
+
+def test_outputs_that_overlap_at_first_sight_are_refused():
+    """Outputs at each other's address or at the other tensor's, and outputs whose elements are one."""
+    at = [view(i * FAKE, outer=1024) for i in range(1, 5)]
+    for q_out, k_out in ((at[2], at[2]), (at[1], at[2]), (at[2], at[0]), (at[1], at[0])):
+        assert rope_call(q=at[0], k=at[1], q_out=q_out, k_out=k_out, k_heads=2) == j.JPI_ERR_ARG
+        assert "another tensor" in j.jpi_prefix_last_error()
+        assert j.jpi_evict(evict_args(k=at[0], v=at[1], k_out=q_out, v_out=k_out)) == j.JPI_ERR_ARG
+        assert "another tensor" in j.jpi_prefix_last_error()
+    for fold in (dict(outer=0), dict(outer=1024, row=0), dict(outer=1024, head=0)):
+        out = view(3 * FAKE, **fold)
+        assert rope_call(q=at[0], q_out=out, batch=2) == j.JPI_ERR_ARG and "stride of 0" in j.jpi_prefix_last_error()
+        assert rope_call(q=out, q_out=out, batch=2) == j.JPI_ERR_ARG and "stride of 0" in j.jpi_prefix_last_error()
+        a = attn_args(out=out, lse=FAKE)
+        assert j.jpi_shared_attention(a, FAKE, 1 << 40) == j.JPI_ERR_ARG and "stride of 0" in j.jpi_prefix_last_error()
+        a = evict_args(n_heads=2, k=at[0], v=at[1], k_out=out, v_out=at[3])
+        assert j.jpi_evict(a) == j.JPI_ERR_ARG and "stride of 0" in j.jpi_prefix_last_error()
