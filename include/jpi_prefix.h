@@ -165,6 +165,13 @@ jpi_status jpi_shared_attention(const jpi_shared_attn* a, void* workspace, size_
 jpi_status jpi_prefix_weight(const jpi_shared_attn* a, const float* weight_in, float decay, float* weight_out,
                              void* workspace, size_t workspace_bytes, void* stream);
 
+/* How a call with these sizes is cut, for tests that want a certain cut:
+ * of_weight 0, jpi_shared_attention: waves of a workgroup (32 rows each), row
+ * tiles of a (prefix, KV head), ranges of its keys.  of_weight 1,
+ * jpi_prefix_weight: waves, key tiles, ranges of its rows.  Errors as the
+ * workspace queries. */
+jpi_status jpi_debug_prefix_plan(const jpi_shared_attn* a, int of_weight, int* waves, int* tiles, int* ranges);
+
 /* ---- eviction by weight ----------------------------------------------------
  * n_outer x n_heads sequences of up to `slots` cache slots, e.g. layer x
  * rollout, KV head.  A sequence of n = len[o] slots keeps all of them if n <=

@@ -167,6 +167,16 @@ jpi_status jpi_prefix_weight_workspace(const jpi_shared_attn* a, size_t* bytes) 
   return st;
 }
 
+jpi_status jpi_debug_prefix_plan(const jpi_shared_attn* a, int of_weight, int* waves, int* tiles, int* ranges) {
+  const char* call = "jpi_debug_prefix_plan";
+  if (!waves || !tiles || !ranges) return fail(JPI_ERR_ARG, "%s: NULL argument", call);
+  const jpi_status st = check_sizes(call, a, of_weight ? prefix_weight_fits : shared_attention_fits);
+  if (st != JPI_OK) return st;
+  const PrefixPlan p = of_weight ? weight_plan(*a) : shared_plan(*a);
+  *waves = p.waves, *tiles = p.tiles, *ranges = p.splits;
+  return JPI_OK;
+}
+
 jpi_status jpi_shared_attention(const jpi_shared_attn* a, void* workspace, size_t workspace_bytes, void* stream) {
   const char* call = "jpi_shared_attention";
   jpi_status st = check_sizes(call, a, shared_attention_fits);

@@ -28,6 +28,12 @@ struct RopeLaunch {
 };
 hipError_t launch_rope(jpi_dtype dt, const RopeLaunch& l, hipStream_t s);
 
+// how a call is cut: 32-row waves of a workgroup, row tiles and ranges of keys (weights: key tiles and ranges of rows)
+struct PrefixPlan {
+  int waves, tiles, splits;
+};
+PrefixPlan shared_plan(const jpi_shared_attn& a);
+PrefixPlan weight_plan(const jpi_shared_attn& a);
 // whether every launch of the call holds its workgroups
 bool shared_attention_fits(const jpi_shared_attn& a);
 bool prefix_weight_fits(const jpi_shared_attn& a);

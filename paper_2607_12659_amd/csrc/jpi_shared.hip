@@ -1008,9 +1008,7 @@ SharedLaunch launch_of(const jpi_shared_attn& a) {
   return l;
 }
 
-struct Plan {
-  int waves, row_tiles, splits;
-};
+}  // namespace
 
 // Waves (32 rows each) of a workgroup and ranges of the key sequence, by estimated time.  A workgroup fills a compute
 // unit's LDS, so workgroups beyond one per unit wait for another round.  Microseconds, fitted to heads of 64 to 256 on 256
@@ -1019,7 +1017,7 @@ struct Plan {
 // 4, and their sums, written and read, 6.6 TB/s.  Lengths are on the device: the slots count, and all tails as full.
 // Few rows over a long prefix want as many ranges as units: 32 rows of 256 dims over 65536 slots took 47 us with 64 ranges at
 // most and take 30 with 256.
-Plan shared_plan(const jpi_shared_attn& a) {
+PrefixPlan shared_plan(const jpi_shared_attn& a) {
   const double n_cu = 256;
   const bool half = a.dtype == JPI_BF16;
   const int64_t per_rollout = (int64_t)a.q_rows * (a.n_heads / a.n_kv_heads), rows = a.group * per_rollout;
@@ -1027,7 +1025,7 @@ Plan shared_plan(const jpi_shared_attn& a) {
   const int64_t prefix = (a.prefix + keys - 1) / keys, tail = (a.suffix + keys - 1) / keys;
   const double all_mb = (double)a.n_groups * rows * a.n_kv_heads * a.head_dim * 4e-6;
   const int most = a.head_dim == 256 ? 4 : 8;  // eight waves share a unit's matrix cores and registers two by two
-  Plan best{};
+  PrefixPlan best{};
   double best_us = 1e30;
   for (int w = 1; w <= most; w *= 2) {
     if (w > 1 && 32 * (w / 2) >= rows) break;
@@ -1038,25 +1036,27 @@ Plan shared_plan(const jpi_shared_attn& a) {
     for (const int s : {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 48, 64, 96, 128, 192, 256}) {
       if (s > 1 && s > prefix + tail) break;
       const double us = ceil(items * s / n_cu) * (ceil(tiles / s) * tile_us + 12) + (s > 1 ? 4 + all_mb * s / 3.3 : 0);
-      if (us < best_us) best_us = us, best = Plan{w, (int)row_tiles, s};
+      if (us < best_us) best_us = us, best = PrefixPlan{w, (int)row_tiles, s};
     }
   }
   return best;
 }
 
 // Key blocks of a workgroup, and ranges of rows: enough workgroups for two on each unit, ranges of at most WEIGHT_ROWS.
-Plan weight_plan(const jpi_shared_attn& a) {
+PrefixPlan weight_plan(const jpi_shared_attn& a) {
   const int64_t rows = (int64_t)a.group * a.q_rows * (a.n_heads / a.n_kv_heads), tiles = (rows + 32 - 1) / 32;
   const int keys = 32 * (a.dtype == JPI_F32 && a.head_dim == 256 ? 1 : 2) * WEIGHT_WAVES;
-  Plan p{};
+  PrefixPlan p{};
   p.waves = WEIGHT_WAVES;
-  p.row_tiles = (a.prefix + keys - 1) / keys;
-  const int64_t items = (int64_t)a.n_groups * a.n_kv_heads * p.row_tiles;
+  p.tiles = (a.prefix + keys - 1) / keys;
+  const int64_t items = (int64_t)a.n_groups * a.n_kv_heads * p.tiles;
   const int64_t least = (tiles + WEIGHT_ROWS / 32 - 1) / (WEIGHT_ROWS / 32);
   p.splits = items ? (int)std::max(least, std::min<int64_t>({64, 512 / items, tiles})) : 1;
   if (p.splits < 1) p.splits = 1;
   return p;
 }
+
+namespace {
 
 unsigned grid8(int64_t items) { return (unsigned)((items + 7) / 8 * 8); }
 bool fits(int64_t groups, int threads) { return groups * threads < (int64_t)1 << 32; }  // a launch's threads are counted in 32 bits
@@ -1065,18 +1065,18 @@ int merge_waves(int splits) { return splits > 64 ? 16 : splits > 8 ? 4 : 1; }  /
 
 template <typename T, int DH>
 hipError_t shared_typed(const jpi_shared_attn& a, void* ws, hipStream_t s) {
-  const Plan p = shared_plan(a);
+  const PrefixPlan p = shared_plan(a);
   SharedLaunch l = launch_of(a);
   l.splits = p.splits;
-  l.row_tiles = p.row_tiles;
+  l.row_tiles = p.tiles;
   l.by_splits = divisor(p.splits);
-  l.by_tiles = divisor(p.row_tiles);
+  l.by_tiles = divisor(p.tiles);
   const int64_t rows = (int64_t)a.n_groups * a.group * a.q_rows * a.n_heads;
   if (p.splits > 1) {
     l.part = (float*)ws;
     l.stats = (float2*)(l.part + p.splits * rows * DH);
   }
-  const unsigned grid = grid8((int64_t)a.n_groups * a.n_kv_heads * p.row_tiles * p.splits);
+  const unsigned grid = grid8((int64_t)a.n_groups * a.n_kv_heads * p.tiles * p.splits);
   switch (p.waves) {
     case 1: k_shared<T, DH, 1><<<grid, 64, 0, s>>>(l); break;
     case 2: k_shared<T, DH, 2><<<grid, 128, 0, s>>>(l); break;
@@ -1097,7 +1097,7 @@ hipError_t shared_typed(const jpi_shared_attn& a, void* ws, hipStream_t s) {
 template <typename T, int DH>
 hipError_t weight_typed(const jpi_shared_attn& a, const float* w_in, float decay, float* w_out, void* ws, hipStream_t s) {
   if (a.prefix == 0) return hipSuccess;
-  const Plan p = weight_plan(a);
+  const PrefixPlan p = weight_plan(a);
   WeightLaunch l{};
   l.a = launch_of(a);
   l.a.splits = p.splits;
@@ -1105,10 +1105,10 @@ hipError_t weight_typed(const jpi_shared_attn& a, const float* w_in, float decay
   l.w_in = w_in;
   l.w_out = w_out;
   l.decay = decay;
-  l.key_tiles = p.row_tiles;
+  l.key_tiles = p.tiles;
   const int64_t slots = (int64_t)a.n_groups * a.n_kv_heads * a.prefix;
   if (p.splits > 1) l.part = (float*)ws;
-  k_weight<T, DH><<<grid8((int64_t)a.n_groups * a.n_kv_heads * p.row_tiles * p.splits), 64 * WEIGHT_WAVES, 0, s>>>(l);
+  k_weight<T, DH><<<grid8((int64_t)a.n_groups * a.n_kv_heads * p.tiles * p.splits), 64 * WEIGHT_WAVES, 0, s>>>(l);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.splits == 1) return e;
   k_weight_sum<<<(unsigned)((slots + 63) / 64), 256, 0, s>>>(l);
@@ -1130,20 +1130,20 @@ hipError_t by_type(const jpi_shared_attn& a, F f) {
 }  // namespace
 
 bool shared_attention_fits(const jpi_shared_attn& a) {
-  const Plan p = shared_plan(a);
+  const PrefixPlan p = shared_plan(a);
   const int64_t rows = (int64_t)a.n_groups * a.group * a.q_rows * a.n_heads;
-  return fits((int64_t)a.n_groups * a.n_kv_heads * p.row_tiles * p.splits + 7, 64 * p.waves) &&
+  return fits((int64_t)a.n_groups * a.n_kv_heads * p.tiles * p.splits + 7, 64 * p.waves) &&
          (p.splits == 1 || fits(rows + 3, 64 * merge_waves(p.splits)));
 }
 
 bool prefix_weight_fits(const jpi_shared_attn& a) {
-  const Plan p = weight_plan(a);
+  const PrefixPlan p = weight_plan(a);
   const int64_t kv = (int64_t)a.n_groups * a.n_kv_heads;
-  return fits(kv * p.row_tiles * p.splits + 7, 64 * WEIGHT_WAVES) && (p.splits == 1 || fits(kv * a.prefix / 64 + 1, 256));
+  return fits(kv * p.tiles * p.splits + 7, 64 * WEIGHT_WAVES) && (p.splits == 1 || fits(kv * a.prefix / 64 + 1, 256));
 }
 
 size_t shared_attention_bytes(const jpi_shared_attn& a) {
-  const Plan p = shared_plan(a);
+  const PrefixPlan p = shared_plan(a);
   if (p.splits == 1) return 0;
   return (size_t)p.splits * a.n_groups * a.group * a.q_rows * a.n_heads * (a.head_dim * sizeof(float) + sizeof(float2));
 }
@@ -1153,7 +1153,7 @@ hipError_t launch_shared_attention(const jpi_shared_attn& a, void* ws, hipStream
 }
 
 size_t prefix_weight_bytes(const jpi_shared_attn& a) {
-  const Plan p = weight_plan(a);
+  const PrefixPlan p = weight_plan(a);
   return p.splits == 1 ? 0 : (size_t)p.splits * a.n_groups * a.n_kv_heads * a.prefix * sizeof(float);
 }
 

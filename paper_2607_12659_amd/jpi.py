@@ -32,7 +32,7 @@ EXPORTED = ["jpi_abi_version", "jpi_status_str", "jpi_last_error", "jpi_create",
             "jpi_corr_destroy", "jpi_corr_set_weight", "jpi_corr_finalize_weights", "jpi_corr_compress",
             "jpi_corr_predict", "jpi_corr_last_error", "jpi_prefix_last_error", "jpi_rope",
             "jpi_shared_attention_workspace", "jpi_prefix_weight_workspace", "jpi_shared_attention", "jpi_prefix_weight",
-            "jpi_evict"]
+            "jpi_evict", "jpi_debug_prefix_plan"]
 JPI_ROPE_HALF, JPI_ROPE_INTERLEAVED = 0, 1
 JPI_ROPE_PLAIN, JPI_ROPE_LINEAR, JPI_ROPE_BASE, JPI_ROPE_PARTS = range(4)
 JPI_KERNEL_NONE, JPI_KERNEL_QKV, JPI_KERNEL_ATTENTION, JPI_KERNEL_OPROJ, JPI_KERNEL_GATEUP, JPI_KERNEL_DOWN, \
@@ -194,6 +194,7 @@ _sig = {
     "jpi_shared_attention": (_i, [_vp, _vp, ctypes.c_size_t, _vp]),
     "jpi_prefix_weight": (_i, [_vp, _vp, _f, _vp, _vp, ctypes.c_size_t, _vp]),
     "jpi_evict": (_i, [_vp, _vp]),
+    "jpi_debug_prefix_plan": (_i, [_vp, _i, _vp, _vp, _vp]),
 }
 for _name, (_res, _args) in _sig.items():
     _fn = getattr(_lib, _name)
@@ -464,6 +465,13 @@ def jpi_prefix_weight(args: jpi_shared_attn, weight_in, decay: float, weight_out
 
 def jpi_evict(args: jpi_evict_args, stream=None) -> int:
     return _lib.jpi_evict(_ref(args), stream_handle(stream))
+
+
+def jpi_debug_prefix_plan(args: jpi_shared_attn, of_weight: int):
+    """(status, waves, tiles, ranges)"""
+    v = [ctypes.c_int() for _ in range(3)]
+    st = _lib.jpi_debug_prefix_plan(_ref(args), of_weight, *(ctypes.byref(x) for x in v))
+    return (st, *(x.value for x in v))
 
 
 class JpiError(RuntimeError):

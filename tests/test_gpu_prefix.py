@@ -821,3 +821,74 @@ def test_tensors_written_in_place_are_known_to_have_changed(ops):
     ops.rope(x, q_out=x)
     with torch.no_grad():
         ops.rope(leaf, q_out=leaf)
+
+
+LARGE = [
+    # groups, rollouts, rows, heads, kv heads, dim, prefix lengths (of slots), tail slots, tail lengths, causal;
+    # waves of a workgroup, full tiles of the prefix that a range has at least (of 64 keys in bf16, of 32 in fp32)
+    (torch.bfloat16, 1, 33, 50, 8, 1, 64, [3489], 3500, 70, [70 - (i * 9) % 71 for i in range(33)], True, 8, 13),
+    (torch.bfloat16, 1, 33, 50, 8, 1, 128, [2300], 2300, 33, [(i * 5) % 34 for i in range(33)], False, 8, 8),
+    (torch.bfloat16, 4, 33, 17, 8, 1, 64, [777, 704, 0, 701], 777, 33, [(i * 7) % 34 for i in range(132)], True, 4, 12),
+    (torch.bfloat16, 1, 9, 50, 8, 1, 128, [4999], 5000, 33, [33 - i for i in range(9)], False, 4, 9),
+    (torch.bfloat16, 1, 9, 50, 8, 1, 256, [3456], 3500, 70, [70, 0, 1, 64, 65, 50, 49, 3, 70], True, 4, 6),
+    (torch.bfloat16, 1, 9, 50, 8, 1, 256, [3500], 3500, 0, None, False, 4, 6),
+    (torch.bfloat16, 3, 16, 50, 6, 3, 64, [777, 768, 64], 777, 33, [(i * 7) % 34 for i in range(48)], False, 2, 12),
+    (torch.bfloat16, 1, 33, 50, 8, 1, 128, [769], 777, 33, [(i * 5) % 34 for i in range(33)], True, 2, 12),
+    (torch.bfloat16, 3, 9, 50, 6, 3, 256, [500, 448, 0], 500, 33, [(i * 5) % 34 for i in range(27)], True, 2, 7),
+    (torch.bfloat16, 1, 16, 50, 8, 1, 256, [500], 500, 33, [33 - 2 * i for i in range(16)], False, 1, 7),
+    (torch.bfloat16, 16, 1, 1, 8, 8, 64, [1600 - 64 * i for i in range(16)], 1600, 33, [33 - i for i in range(16)], False, 1, 12),
+    (torch.float32, 1, 33, 17, 8, 1, 64, [4992], 5000, 33, [(i * 5) % 34 for i in range(33)], True, 8, 13),
+    (torch.float32, 1, 33, 17, 8, 1, 128, [3500], 3500, 33, [(i * 7) % 34 for i in range(33)], False, 8, 9),
+    (torch.float32, 3, 16, 17, 8, 1, 64, [2300, 2273, 5], 2300, 130, [(i * 11) % 131 for i in range(48)], False, 4, 14),
+    (torch.float32, 1, 33, 50, 6, 3, 128, [770], 777, 33, [(i * 5) % 34 for i in range(33)], True, 4, 8),
+    (torch.float32, 1, 5, 50, 8, 1, 256, [3456], 3500, 33, [33, 0, 32, 1, 17], True, 4, 6),
+    (torch.float32, 16, 9, 17, 6, 3, 64, [500 - 31 * i for i in range(16)], 500, 70, [(i * 7) % 71 for i in range(144)], True, 2, 15),
+    (torch.float32, 2, 33, 1, 8, 1, 256, [5000, 4991], 5000, 130, [(i * 13) % 131 for i in range(66)], False, 2, 6),
+    (torch.float32, 3, 33, 1, 16, 4, 256, [777, 768, 300], 777, 33, [(i * 7) % 34 for i in range(99)], False, 1, 6),
+]
+
+
+def plan_of(case, dtype, weight):
+    from paper_2607_12659_amd import jpi
+    G, R, Hq, nh, kv, D, _, P, S = case[:9]
+    a = jpi.jpi_shared_attn(jpi.JPI_BF16 if dtype == torch.bfloat16 else jpi.JPI_F32, G, R, Hq, nh, kv, D, P, S, 0, 1.0)
+    st, waves, tiles, ranges = jpi.jpi_debug_prefix_plan(a, weight)
+    assert st == jpi.JPI_OK
+    return waves, tiles, ranges
+
+
+@pytest.mark.parametrize("case", LARGE, ids=lambda c: "%s-w%d-g%dx%d-q%d-h%d/%d-d%d-p%d-s%d" % (
+    "bf16" if c[0] == torch.bfloat16 else "f32", c[12], *c[1:7], c[8], c[9]))
+def test_shared_attention_of_many_rows_over_long_ranges(ops, case):
+    """Every number of waves, over ranges in which each stage of the ring is filled and read several times."""
+    dtype, case, waves, full = case[0], case[1:12], *case[12:]
+    D, scale, keys = case[5], case[5] ** -0.5, 64 if dtype == torch.bfloat16 else 32
+    got_waves, _, ranges = plan_of(case, dtype, 0)
+    assert got_waves == waves and case[7] // keys // ranges >= full
+    x = attn_inputs(case, dtype)
+    ref, lse, mag, err = attn64(*x, scale)
+    out, got_lse = run_attn(ops, *x)
+    tol, lse_tol = attn_tolerance(dtype, ref, lse, mag, err, case[7] + case[8], D)
+    within(out, ref, tol)
+    within(got_lse, lse, lse_tol)
+    n = ref.norm()
+    assert (out.double().cpu() - ref).norm() <= 1.5 * H[dtype] * n + (mag * tol.new_tensor(64 * U)).norm()
+    assert (out.cpu()[lse == -INF] == 0).all()
+    # the same bits again, and other rollouts' rows untouched by NaN and infinity of a tail and of queries
+    again, _ = run_attn(ops, *x)
+    assert torch.equal(again, out)
+    q, kp, vp, ks, vs, plen, slen, causal = x
+    if ks is None:
+        return
+    q, ks, vs = q.clone(), ks.clone(), vs.clone()
+    B = len(q)
+    some = [b for b in range(B) if slen[b] > 0]
+    in_k, in_v, in_q = some[len(some) // 3], some[2 * len(some) // 3], some[-1]
+    ks[in_k, slen[in_k] - 1], vs[in_v, 0, :, 5], q[in_q, -1, 0, 3] = math.nan, INF, math.nan
+    sick, _ = run_attn(ops, q, kp, vp, ks, vs, plen, slen, causal)
+    well = [b for b in range(B) if b not in (in_k, in_v, in_q)]
+    assert torch.equal(sick[well], out[well])
+    # the last row of a rollout sees its whole tail
+    assert torch.isnan(sick[in_k, -1]).all() and torch.isnan(sick[in_q, -1, 0]).all()
+    assert not torch.isfinite(sick[in_v, -1, :, 5]).any()
+    assert torch.equal(sick[in_q, :-1], out[in_q, :-1]) and torch.equal(sick[in_q, -1, 1:], out[in_q, -1, 1:])

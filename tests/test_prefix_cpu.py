@@ -262,3 +262,15 @@ def test_outputs_that_overlap_at_first_sight_are_refused():
         assert j.jpi_shared_attention(a, FAKE, 1 << 40) == j.JPI_ERR_ARG and "stride of 0" in j.jpi_prefix_last_error()
         a = evict_args(n_heads=2, k=at[0], v=at[1], k_out=out, v_out=at[3])
         assert j.jpi_evict(a) == j.JPI_ERR_ARG and "stride of 0" in j.jpi_prefix_last_error()
+
+
+def test_the_plan_of_a_call():
+    a = attn_args(prefix=5000)
+    st, waves, tiles, ranges = j.jpi_debug_prefix_plan(a, 0)
+    assert st == j.JPI_OK and waves in (1, 2, 4) and tiles == -(-3 * 5 * 8 // (32 * waves)) and ranges > 1
+    _, n = j.jpi_shared_attention_workspace(a)
+    assert n == ranges * 2 * 3 * 5 * 8 * (64 * 4 + 8)  # a sum and two statistics of each row in each range
+    st, waves, tiles, ranges = j.jpi_debug_prefix_plan(a, 1)
+    assert st == j.JPI_OK and waves == 4 and tiles == -(-5000 // 256)
+    assert j._lib.jpi_debug_prefix_plan(ctypes.byref(a), 0, None, None, None) == j.JPI_ERR_ARG
+    assert j.jpi_debug_prefix_plan(attn_args(head_dim=32), 0)[0] == j.JPI_ERR_ARG
