@@ -892,3 +892,55 @@ def test_shared_attention_of_many_rows_over_long_ranges(ops, case):
     assert torch.isnan(sick[in_k, -1]).all() and torch.isnan(sick[in_q, -1, 0]).all()
     assert not torch.isfinite(sick[in_v, -1, :, 5]).any()
     assert torch.equal(sick[in_q, :-1], out[in_q, :-1]) and torch.equal(sick[in_q, -1, 1:], out[in_q, -1, 1:])
+
+
+LONG_WEIGHT = [
+    # groups, rollouts, rows, heads, kv heads, dim, prefix lengths (of slots); ranges, row tiles of 32 in the longest of them
+    (3, 9, 10, 8, 2, 64, [22000, 21777, 100], 22000, 1, 12),      # one range, written directly
+    (1, 5, 12, 6, 3, 128, [44000], 44001, 1, 4),
+    (1, 21, 50, 8, 4, 64, [33000], 33000, 2, 33),                 # more rows than a range holds, many key tiles
+    (1, 21, 52, 8, 4, 128, [32990], 33000, 2, 35),
+    (2, 15, 50, 4, 2, 128, [8000, 4011], 8000, 4, 12),            # ranges summed afterwards
+]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("case", LONG_WEIGHT, ids=lambda c: "g%dx%d-q%d-h%d/%d-d%d-p%d" % (*c[:6], c[7]))
+def test_prefix_weight_over_long_ranges(ops, case, dtype):
+    """Ranges of more row tiles than the ring has stages, one that is written directly among them."""
+    case, ranges, longest = (*case[:8], 0, None, False), *case[8:]
+    G, R, Hq, nh, kv, D, plen, P = case[:8]
+    row_tiles = -(-R * Hq * (nh // kv) // 32)
+    assert plan_of(case, dtype, 1)[2] == ranges and -(-row_tiles // ranges) == longest
+    check_weight(ops, case, dtype)
+
+
+def test_prefix_weight_of_wide_fp32_heads(ops):
+    """fp32 heads of 256: a wave keeps 32 keys."""
+    case = (2, 9, 25, 6, 3, 256, [11000, 9001], 11000, 0, None, False)
+    assert plan_of(case, torch.float32, 1)[2] == 1
+    check_weight(ops, case, torch.float32)
+
+
+def check_weight(ops, case, dtype):
+    G, R, Hq, nh, kv, D, plen, P = case[:8]
+    scale = D ** -0.5
+    q, kp = attn_inputs(case, dtype)[:2]
+    lse = 9.0 + 0.1 * rand(21, G * R, Hq, nh)
+    # compared in 64 bits: the slots around tile borders and lengths, and every 37th
+    near = [j + d for j in (0, 64, 128, 256, *plen, P) for d in (-2, -1, 0, 1)]
+    slots = torch.tensor(sorted({j for j in near if 0 <= j < P} | set(range(0, P, 37))))
+    inside = slots < torch.tensor(plen)[:, None, None]
+    ref, err = weight64(q, kp[:, slots], lse, [int((slots < n).sum()) for n in plen], scale)
+    args = (dev(q), dev(kp), dev(lse))
+    got = ops.prefix_weight(*args, prefix_len=i32(plen))
+    within(got[..., slots], ref, err + 1e-30)
+    w0 = rand(77, G, kv, P).abs()
+    w = dev(w0)
+    ops.prefix_weight(*args, w, prefix_len=i32(plen), decay=0.75, out=w)
+    at = w0[..., slots]
+    acc = torch.where(inside, 0.75 * at.double() + ref, at.double())
+    within(w[..., slots], acc, err + 4 * U * acc)
+    outside = (torch.arange(P) >= torch.tensor(plen)[:, None, None]).expand_as(w0)
+    assert torch.equal(w.cpu()[outside], w0[outside]) and (got.cpu()[outside] == 0).all()
+    assert torch.equal(ops.prefix_weight(*args, prefix_len=i32(plen)), got)
