@@ -4,12 +4,14 @@
 // selection of the last weight that stays, over an order-preserving integer image of the weights (counts only, so no
 // order of atomics could show), and a prefix sum in slot order.
 //   Into other memory, few rows: one launch.  Every workgroup of a sequence makes the selection for itself, in which the
-//   card is otherwise idle, and moves its share of the rows: 18 sequences of 816 slots cut to 408 (15 MB) take 10 us, with
+//   card is otherwise idle, and moves its share of the rows: 18 sequences of 816 slots cut to 408 (15 MB) take 10.5 us, with
 //   the selection in a launch of its own 13.
-//   Into other memory, many rows or slots: k_evict_select, then k_evict_copy (144 sequences of up to 4096 slots cut to
-//   1024, 305 MB: 12 and 48 us; 74 with data that no cache holds, 4.1 TB/s).  The selection is one workgroup's work for
-//   each sequence: 65536 slots take 100 us.
-//   In place: k_evict_select, then k_evict_shift, since weights and lengths change where other workgroups read them.
+//   Into other memory, many rows or slots: k_evict_select, then k_evict_copy.  144 sequences of 4096 slots cut to 1024
+//   (302 MB) take 75 us, 4.0 TB/s; on inputs that the last-level cache holds 12 and 48.  The selection is one workgroup's
+//   work for each sequence: 65536 slots take 120 us.
+//   In place: k_evict_select, then k_evict_shift, since weights and lengths change where other workgroups read them.  The
+//   same 18 sequences take 18 us, the 144 105 (11 and 88): a workgroup's rows follow each other, 256 at a time, and few
+//   sequences make few workgroups (one of 65536 slots cut to half: 121 and 361).
 #include <algorithm>
 
 #include "jpi_device.h"
@@ -210,13 +212,13 @@ struct MoveLaunch {
   int first;   // first sequence of this launch (shift)
 };
 
-constexpr int GATHER_ROWS = 2048;  // rows of a workgroup at most
+constexpr int GATHER_LEAST = 32, GATHER_MOST = SEL;  // rows of a workgroup
 
 // Selection and move into other memory.  P: a piece of a row, 16 bytes where everything is aligned, else an element.
 template <int N, typename P>
 __global__ __launch_bounds__(SEL) void k_evict_gather(MoveLaunch l) {
   __shared__ SelectLds lds;
-  __shared__ int from[GATHER_ROWS];
+  __shared__ int from[GATHER_MOST];
   const jpi_evict_args& a = l.a;
   const int part = blockIdx.x % l.parts, seq = blockIdx.x / l.parts, o = seq / a.n_heads, h = seq - o * a.n_heads;
   const int n = evict_len(a, o), m = min(n, a.keep);
@@ -373,9 +375,10 @@ hipError_t evict_pieces(MoveLaunch l, bool gather, int row_bytes, hipStream_t s)
     }
     return hipSuccess;
   }
-  // two workgroups for each of 256 units, but no fewer than 32 rows in one
+  // two workgroups for each of 256 units, but no fewer than GATHER_LEAST rows in one.  At most GATHER_MOST: up to SEL slots
+  // there are no more rows, past them the rule of launch_evict leaves at most 256 times GATHER_LEAST rows in all
   const int64_t want = std::max<int64_t>(1, 512 / seqs);
-  l.per = (int)std::min<int64_t>(GATHER_ROWS, std::max<int64_t>(32, (most + want - 1) / want));
+  l.per = (int)std::max<int64_t>(GATHER_LEAST, (most + want - 1) / want);
   l.parts = std::max(1, (most + l.per - 1) / l.per);
   const unsigned grid = (unsigned)(seqs * l.parts);
   if (a.slots <= SEL) k_evict_gather<1, P><<<grid, SEL, 0, s>>>(l);
@@ -393,8 +396,9 @@ hipError_t launch_evict(const jpi_evict_args& a, hipStream_t s) {
   MoveLaunch l{};
   l.a = a;
   l.n_t = 2;
-  // One launch where nothing that a workgroup writes is read by another, and where a thread's weights stay in registers:
-  // read anew by every workgroup, the selection of 65536 slots took 320 us against 166 in a launch of its own.
+  // One launch where nothing that a workgroup writes is read by another, and where a thread's weights stay in registers: read
+  // anew by every workgroup, the selection of one sequence of 65536 slots took 214 us against 135 in a launch of its own, of
+  // 20000 slots 79 against 51.
   bool gather = a.slots <= 16 * SEL && a.weight_out != a.weight && (!a.len || a.len_out != a.len);
   int64_t any = a.head_dim * es;
   for (int i = 0; i < 2; ++i) {
@@ -404,11 +408,17 @@ hipError_t launch_evict(const jpi_evict_args& a, hipStream_t s) {
     any |= (int64_t)((uintptr_t)l.t[i].src | (uintptr_t)l.t[i].dst) | l.t[i].so | l.t[i].sr | l.t[i].sh | l.t[i].d_o |
            l.t[i].dr | l.t[i].dh;
   }
-  // With many rows to move, small workgroups that do nothing else are faster by more than the other launch costs:
-  // 302 MB (144 sequences, 1024 of 4096 slots) in 68 us against 81, 15 MB (18, 408 of 816) in 13 against 10.
-  gather = gather && (int64_t)a.n_outer * a.n_heads * std::min(a.keep, a.slots) * a.head_dim * es < (int64_t)32 << 20;
+  // One launch or two, in us, heads of 256 in bf16 unless said; of 211 calls timed the rule's side was the faster one or within a
+  // fifth of it, and half a percent slower on average.
+  //   Up to SEL slots a selection is cheap, and one launch wins until the move is long: 18 sequences, 408 of 816 slots (K 4 MB),
+  //   10 and 13; 512, 408 of 816 slots of 64 (27 MB), 28 and 34; 512, 900 of 1024 slots of 64 (59 MB), 68 and 60.
+  //   Past them it wins while no unit has two workgroups, whose selections take twice as long: eight sequences, 1024 of 4096
+  //   slots, 14 and 16, sixteen 27 and 19; one, 8192 of 16384 slots, 28 and 32, two 56 and 38.
+  const int64_t n_seqs = (int64_t)a.n_outer * a.n_heads, most = std::min(a.keep, a.slots);
+  gather = gather && n_seqs * most * a.head_dim * es < (int64_t)32 << 20 &&
+           (a.slots <= SEL || n_seqs * ((most + GATHER_LEAST - 1) / GATHER_LEAST) <= 256);
   if (!gather) {
-    const unsigned seqs = (unsigned)(a.n_outer * a.n_heads);
+    const unsigned seqs = (unsigned)n_seqs;
     if (a.slots <= SEL) k_evict_select<1><<<seqs, SEL, 0, s>>>(a);
     else if (a.slots <= 4 * SEL) k_evict_select<4><<<seqs, SEL, 0, s>>>(a);
     else if (a.slots <= 16 * SEL) k_evict_select<16><<<seqs, SEL, 0, s>>>(a);

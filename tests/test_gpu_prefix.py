@@ -944,3 +944,20 @@ def check_weight(ops, case, dtype):
     outside = (torch.arange(P) >= torch.tensor(plen)[:, None, None]).expand_as(w0)
     assert torch.equal(w.cpu()[outside], w0[outside]) and (got.cpu()[outside] == 0).all()
     assert torch.equal(ops.prefix_weight(*args, prefix_len=i32(plen)), got)
+
+
+EVICT_LAUNCHES = [
+    # on either side of where one launch gives way to two: past 1024 slots by workgroups, up to them by bytes
+    (8, 1, 64, 4096, 1024, 4, 64, None, "ties"),
+    (9, 1, 64, 4096, 1024, 4, 64, [4096 - 300 * i for i in range(9)], "odd"),
+    (1, 2, 64, 16384, 4096, 0, 7, None, "ties"),
+    (1, 2, 64, 16384, 4097, 0, 7, None, "ties"),
+    (64, 8, 64, 512, 511, 1, 2, None, "plain"),
+    (65, 8, 64, 513, 512, 1, 2, None, "plain"),
+    (300, 1, 8, 1030, 5, 1, 1, None, "equal"),
+]
+
+
+@pytest.mark.parametrize("case", EVICT_LAUNCHES, ids=lambda c: "n%dx%d-d%d-p%d-k%d-%s" % (*c[:5], c[8]))
+def test_evict_in_one_launch_and_in_two(ops, case):
+    test_evict_long_and_large(ops, case, False)
