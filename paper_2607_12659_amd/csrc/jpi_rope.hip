@@ -10,7 +10,12 @@
 // Angles.  A position times f_i in fp32 is off by 2^-24 of the angle itself,
 // which for position 10^5 is 6e-3 radians; here the angle is formed in turns in
 // fp64 (position exact, f_i / 2 pi to 2^-52), reduced to [-1/2, 1/2] turns there,
-// and only then rounded to fp32 for sincospi.
+// and only then rounded to fp32 for sincospi.  That angle, the sine and the
+// amplitude are each rounded to fp32, which leaves fp32 rotations 4.7e-8 from 64
+// bits, where sines and cosines formed in fp64 leave 3.5e-8; bf16 ones are the same.
+//
+// Rows or halves that are no whole 16-byte pieces go element by element: 6528
+// tokens of 8 + 1 heads of 250 take 33 us in bf16 and 34 in fp32 (floors 12, 25).
 #include <algorithm>
 
 #include "jpi_device.h"

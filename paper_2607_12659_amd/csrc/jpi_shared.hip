@@ -21,8 +21,10 @@
 // prefixes of up to 1600 slots against 6400 rows each, 58 us: the workgroups of
 // the longest prefix are the call's time, since lengths are on the device when
 // ranges are chosen.  With few rows memory: 65536 slots x 8 KV heads of 128 dims
-// and 64 tails of up to 512, 104 us, 3.2 TB/s.  A workgroup's start, first tile
-// and rows' way out take 12 us whatever its range, and the join 4 to 9.
+// and 64 tails of up to 512, 107 us, 3.2 TB/s.  A launch of one tile takes 14 us
+// whatever its range, 9 of them inside its workgroup (32 rows of 256 dims: 2.9
+// until the first tile is there, 1.7 for its scores, 1.4 for the product with V,
+// 2.8 for the rows' way out), and the join 4 to 9.
 #include <algorithm>
 #include <type_traits>
 
@@ -42,8 +44,10 @@ typedef short i16x4 __attribute__((ext_vector_type(4)));
 // the products of one half fill the latency of the other's; 64 fp32 keys of 256 dims would not leave room for two stages.
 template <typename T>
 constexpr int KEYS = sizeof(T) == 2 ? 64 : 32;
-// Share of a range that a tile of a tail counts for, in prefix tiles: 64 samples over 65536 slots with tails of up to 512
-// took 139, 124, 130 and 137 us with 1, 2, 3 and 4.
+// Share of a range that a tile of a tail counts for, in prefix tiles.  us with 1, 2 and 3 (and their plans), tails of up to 512
+// slots: eight waves (64 samples, 32 heads on 8 of 128 dims, 65536 slots) 126, 111 and 128; four (8 chunks of 50 rows, 8 heads
+// of 256, 3200 slots) 46, 37 and 37; two (16 samples, 32 heads on 8 of 128, 16384 slots) 40, 31 and 30; one (32 samples, 8 heads
+// on 8 of 64, 8192 slots) 30, 26 and 26, in fp32 65, 80 and 106: there a tail's tile costs what a prefix tile does.
 constexpr int TAIL_COST = 2;
 constexpr float LOG2E = 1.44269504088896341f, LN2 = 0.693147180559945309f;
 constexpr float HEADROOM = 16.f;  // log2 of the most that a probability may exceed its row's reference by
@@ -292,7 +296,9 @@ struct Steps {
       }
     x.l_run += sum[0] + sum[1];
   }
-  // 16 keys each: registers 8 (u % 2) .. + 7 of half u / 2 of S^T
+  // 16 keys each: registers 8 (u % 2) .. + 7 of half u / 2 of S^T.  Rounded to bf16, as V is, for the bf16 matrix instructions;
+  // half a step of each probability, which leaves outputs 2.0e-3 to 2.3e-3 from 64 bits where fp32 probabilities leave 1.7e-3
+  // (the output's own rounding).  Row sums and lse take them in fp32.
   static __device__ __forceinline__ void round_p(const f32x16 (&s)[HT], bf16x8 (&p)[2 * HT]) {
 #pragma unroll
     for (int u = 0; u < 2 * HT; ++u)
@@ -751,7 +757,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(NW == 8
 }
 
 // Join of a row's ranges: the ranges' sums brought to their largest reference.  WPR waves a row, each for a part of the
-// ranges (at most 64): with one, 64 ranges of few rows are eight trips to memory one after another.
+// ranges (at most 64): with one, 64 ranges of few rows would be sixteen trips to memory one after another, with four, four.
 template <typename T, int DH, int WPR>
 __global__ __launch_bounds__(WPR > 4 ? 64 * WPR : 256) void k_shared_merge(SharedLaunch l) {
   constexpr int N = DH / 64, RPW = WPR < 4 ? 4 / WPR : 1;  // rows of a workgroup
@@ -888,7 +894,9 @@ __global__ __launch_bounds__(64 * WEIGHT_WAVES) __attribute__((amdgpu_waves_per_
   for (int r = tid; r < (t1 - t0) * 32; r += 64 * NW) {
     const Row x = row_of(a, g, kv, t0 * 32 + r);
     const float v = x.b >= 0 ? l.lse[((int64_t)x.b * a.q_rows + x.i) * a.n_heads + x.h] : -INFINITY;
-    lse2[r] = v == -INFINITY ? -INFINITY : -v * LOG2E;  // rows that see nothing, or are none, add 2^-inf
+    // rows that see nothing, or are none, add 2^-inf.  The product's rounding is 2^-24 of the summand (about 15 for a long
+    // prefix), 6e-7 of a weight at most; sums of 3200 rows come out 9.0e-8 from 64 bits, 7.3e-8 where lse is subtracted first
+    lse2[r] = v == -INFINITY ? -INFINITY : -v * LOG2E;
     silent = silent || (x.b >= 0 && v == -INFINITY);
   }
   const bool some_silent = __syncthreads_or(silent);
@@ -1042,7 +1050,8 @@ PrefixPlan shared_plan(const jpi_shared_attn& a) {
   return best;
 }
 
-// Key blocks of a workgroup, and ranges of rows: enough workgroups for two on each unit, ranges of at most WEIGHT_ROWS.
+// Key blocks of a workgroup, and ranges of rows: 512 workgroups where there are as many pieces, ranges of at most WEIGHT_ROWS.
+// A unit holds three in bf16 with heads of 64 and 128 and in fp32 with 64, two with bf16 256 and fp32 128, one with fp32 256.
 PrefixPlan weight_plan(const jpi_shared_attn& a) {
   const int64_t rows = (int64_t)a.group * a.q_rows * (a.n_heads / a.n_kv_heads), tiles = (rows + 32 - 1) / 32;
   const int keys = 32 * (a.dtype == JPI_F32 && a.head_dim == 256 ? 1 : 2) * WEIGHT_WAVES;

@@ -5,12 +5,13 @@ tensors, fills in the C arguments and enqueues libjpi's kernels on the current
 stream of the tensors' device, which may be capturing a graph.  Outputs and
 workspaces are allocated by torch on that stream unless they are given.
 Floating tensors are bfloat16 or float32, lengths and positions int32; tensors
-may be strided as long as the elements of a head are contiguous.  No gradients
-are recorded (that of a rotation is the rotation with inverse=True), so tensors
-that require them are refused while torch records gradients, as torch refuses
-them for its own out= arguments; tensors that a call writes into count as
-changed in place.  Errors are raised as ``jpi.JpiError`` (the library's checks),
-``ValueError`` or ``TypeError`` (shapes, devices and types).
+may be strided as long as the elements of a head are contiguous (attention and
+slot weights want 16-byte aligned rows as well).  No gradients are recorded
+(that of a rotation is the rotation with inverse=True), so tensors that require
+them are refused while torch records gradients, as torch refuses them for its
+own out= arguments; tensors that a call writes into count as changed in place.
+Errors are raised as ``jpi.JpiError`` (the library's checks), ``ValueError`` or
+``TypeError`` (shapes, devices and types).
 """
 from __future__ import annotations
 
