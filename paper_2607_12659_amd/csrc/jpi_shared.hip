@@ -1139,8 +1139,10 @@ hipError_t by_type(const jpi_shared_attn& a, F f) {
 }  // namespace
 
 bool shared_attention_fits(const jpi_shared_attn& a) {
-  const PrefixPlan p = shared_plan(a);
   const int64_t rows = (int64_t)a.n_groups * a.group * a.q_rows * a.n_heads;
+  // whatever the plan: at most 2 threads a row and 512 a (group, KV head) in each of 256 ranges, and 1024 a row of the join
+  if (rows <= 1 << 21 && (int64_t)a.n_groups * a.n_kv_heads <= 1 << 13) return true;
+  const PrefixPlan p = shared_plan(a);
   return fits((int64_t)a.n_groups * a.n_kv_heads * p.tiles * p.splits + 7, 64 * p.waves) &&
          (p.splits == 1 || fits(rows + 3, 64 * merge_waves(p.splits)));
 }
