@@ -396,7 +396,7 @@ def _append_one(st, x, codes, scale, of_keys):
     amax = torch.where(fresh, y, 0.0).abs().amax((-2, -1))
     had = older.any(-2)[:, :, 0]
     old = scale[at]
-    new = torch.where(had & ~(amax > top * old), old, _scale_of(amax, code))
+    new = torch.where(had & (amax <= top * old), old, _scale_of(amax, code))
     new = torch.where(had & torch.isnan(old), old, new)
     was = _natural(codes.view(torch.uint8)[at].view(codes.dtype), of_keys)
     kept = torch.where((new == old)[..., None, None], was.float(), was.float() * (old / new)[..., None, None])
