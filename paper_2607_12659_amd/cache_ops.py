@@ -1,0 +1,297 @@
+"""Operators of a paged 8-bit KV cache on torch tensors (include/jpi_cache.h).
+
+As in ``prefix_ops``, PyTorch provides device memory and streams only: every
+function checks its tensors, fills in the C arguments and enqueues libjpi's
+kernels on the current stream of the tensors' device, which may be capturing a
+graph.  Outputs and workspaces are allocated by torch on that stream unless they
+are given.  Queries, keys, values and outputs are bfloat16 or float32, codes int8
+or float8_e4m3fn, scales float32, lengths, tables and counts int32.  No gradients
+are recorded: tensors that require them are refused while torch records them.
+Tensors that a call writes into count as changed in place.  Errors are raised as
+``jpi.JpiError`` (the library's checks), ``ValueError`` or ``TypeError`` (shapes,
+devices and types).
+
+Sequence s holds slots 0 .. lens[s] - 1, slot j in the page that table[s][j //
+page] names; refs counts the sequences that hold each page, and a page that none
+holds is free.  A step of a program that samples texts::
+
+    starts = lens.clone()
+    resize(table, lens, refs, lens + n, pool)         # room, in all layers
+    for each layer:
+        q, k = norm_rope(q, k, positions, q_weight=..., k_weight=...)
+        append(pool.layer(i), table, starts, k, v)
+        out, lse = attention(q, pool.layer(i), table, lens)
+    reorder(table, lens, refs, parents, page)         # fork, free, reorder
+"""
+from __future__ import annotations
+
+import ctypes
+import struct
+from typing import NamedTuple
+
+import torch
+
+from . import jpi as _j
+from .prefix_ops import (_DTYPE, _F32, _I32, _INT_MAX, _LAST_ERROR, _V, _VIEW, _dense, _dtype, _launch, _lib, _no_gradients, _pack,
+                         _recording, _turned, _view, _want, _written)
+
+_CODE = {torch.int8: _j.JPI_INT8, torch.float8_e4m3fn: _j.JPI_E4M3}
+_LAST_ERROR.update(dict.fromkeys(("jpi_norm_rope", "jpi_cache_append", "jpi_cache_attention", "jpi_cache_resize", "jpi_cache_reorder",
+                                  "jpi_cache_compact"), _j.jpi_cache_last_error))
+
+_NORM = struct.Struct("@PP2iqd")
+_POOL = struct.Struct("@5iPPPP")
+_SEQS = struct.Struct("@2iqPP")
+_ATTN = struct.Struct("@6if" + _V + "P" + _V + "P")
+_MOVES = struct.Struct("@2iqPPPPqPP2iPi4x")
+assert (_NORM.size, _POOL.size, _SEQS.size, _ATTN.size, _MOVES.size) == tuple(
+    ctypes.sizeof(c) for c in (_j.jpi_head_norm, _j.jpi_cache_pool, _j.jpi_cache_seqs, _j.jpi_cache_attn, _j.jpi_cache_moves))
+
+
+class Pool(NamedTuple):
+    """The pages of one layer, or of several in a leading dimension: codes k [pages][kv_heads][head_dim / 16][page][16] and
+    v [pages][kv_heads][page / 16][head_dim][16], scales [pages][kv_heads]; all contiguous."""
+    k: torch.Tensor
+    v: torch.Tensor
+    k_scale: torch.Tensor
+    v_scale: torch.Tensor
+
+    @classmethod
+    def zeros(cls, n_pages, kv_heads, head_dim, page, *, code=torch.float8_e4m3fn, layers=None, device="cuda"):
+        """A new pool; without `layers` of one layer."""
+        if code not in _CODE:
+            raise TypeError("codes must be int8 or float8_e4m3fn, got %s" % code)
+        lead = (n_pages, kv_heads) if layers is None else (layers, n_pages, kv_heads)
+        shapes = ((head_dim // 16, page, 16), (page // 16, head_dim, 16))
+        return cls(*(torch.zeros(lead + s, dtype=torch.uint8, device=device).view(code) for s in shapes),
+                   *(torch.zeros(lead, dtype=_F32, device=device) for _ in shapes))
+
+    def layer(self, i):
+        return Pool(self.k[i], self.v[i], self.k_scale[i], self.v_scale[i])
+
+
+def _pool(pool, layers):
+    """The C structure, layers, pages, slots of a page, KV heads, head_dim and device of a pool, of one layer unless `layers`."""
+    k, v, ks, vs = pool
+    shape = k.shape
+    if len(shape) != 5 and not (layers and len(shape) == 6):
+        raise ValueError("codes of K must be %s[pages][kv_heads][head_dim / 16][page][16]" % ("[layers]" if layers else ""))
+    lead, (pieces, page, width), dev = shape[:-3], shape[-3:], k.get_device()
+    code = _CODE.get(k.dtype)
+    if code is None:
+        raise TypeError("codes must be int8 or float8_e4m3fn, got %s" % k.dtype)
+    n_pages, kv = lead[-2:]
+    if width != 16 or page % 16 or max(n_pages, kv, pieces * 16, page) > _INT_MAX:
+        raise ValueError("codes of K must be [pages][kv_heads][head_dim / 16][page][16], got %s" % list(shape))
+    _want("codes of V", v, lead + (page // 16, pieces * 16, 16), k.dtype, dev)
+    _want("k_scale", ks, lead, _F32, dev)
+    _want("v_scale", vs, lead, _F32, dev)
+    packed = _POOL.pack(code, kv, pieces * 16, n_pages, page, _dense("codes of K", k), _dense("codes of V", v), _dense("k_scale", ks),
+                        _dense("v_scale", vs))
+    return packed, (lead[0] if len(lead) == 3 else 1), n_pages, page, kv, pieces * 16, dev
+
+
+def _rows(name, table, n, dev):
+    """n_seqs, max_pages and the row stride of a table."""
+    if table.dim() != 2:
+        raise ValueError("%s must be [sequences][pages]" % name)
+    shape = table.shape
+    _want(name, table, shape if n is None else (n, shape[1]), _I32, dev)
+    if max(shape) > _INT_MAX:
+        raise ValueError("%s is larger than 2^31 - 1 in a dimension" % name)
+    if shape[1] > 1 and table.stride(1) != 1:
+        raise ValueError("the entries of a row of %s must be contiguous" % name)
+    return shape[0], shape[1], table.stride(0) if shape[0] > 1 else shape[1]
+
+
+def _seqs(table, lens, dev):
+    n, width, stride = _rows("table", table, None, dev)
+    _want("lens", lens, (n,), _I32, dev)
+    return n, width, stride, table.data_ptr(), _dense("lens", lens)
+
+
+def _workspace(size_of, like, *args):
+    n = ctypes.c_size_t()
+    status = size_of(*args, ctypes.byref(n))
+    if status != _j.JPI_OK:
+        raise _j.JpiError(status, _j.jpi_cache_last_error())
+    n = n.value
+    return (torch.empty(n, dtype=torch.uint8, device=like.device), n) if n else (None, 0)
+
+
+def norm_rope(q, k=None, positions=None, *, q_weight=None, k_weight=None, eps=1e-6, unit_offset=False, rot_dim=None, layout="half",
+              base=1e4, scaling="none", factor=1.0, trained=0, beta_fast=32.0, beta_slow=1.0, amplitude=1.0, inverse=False,
+              q_out=None, k_out=None):
+    """Norms of the heads of q and k, then their rotary positions, in one pass: ``jpi_norm_rope``.
+
+    q_weight, k_weight: [head_dim], or [heads][head_dim] of each tensor, both of one type (bfloat16 or float32); None: the
+    norm alone.  unit_offset: the factor is 1 + weight.  Everything else as ``prefix_ops.rope``.  Returns (q_out, k_out).
+    """
+    if q.dim() != 4 or (k is not None and k.dim() != 4):
+        raise ValueError("q and k must be [batch][tokens][heads][head_dim]")
+    if _recording():
+        _no_gradients(q_weight, k_weight)
+    if k is None and k_weight is not None:
+        raise ValueError("k_weight without k")
+    dh, dev, given = q.shape[3], q.get_device(), [(x, w) for x, w in ((q, q_weight), (k, k_weight)) if w is not None]
+    dtype = given[0][1].dtype if given else _F32
+    if dtype not in _DTYPE:
+        raise TypeError("weights must be bfloat16 or float32, got %s" % dtype)
+    stride = 0
+    for x, w in given:
+        _want("a weight", w, (dh,) if w.dim() == 1 else (x.shape[2], dh), dtype, dev)
+        if w.dim() == 2:
+            stride = dh
+        _dense("a weight", w)
+    if stride and any(w.dim() == 1 for _, w in given):
+        raise ValueError("weights are [head_dim] for both tensors or [heads][head_dim] for both")
+    norm = _pack(_NORM, 0 if q_weight is None else q_weight.data_ptr(), 0 if k_weight is None else k_weight.data_ptr(), _DTYPE[dtype],
+                 int(bool(unit_offset)), stride, eps)
+    return _turned(norm, q, k, positions, rot_dim, layout, base, scaling, factor, trained, beta_fast, beta_slow, amplitude, inverse,
+                   q_out, k_out)
+
+
+def append(pool, table, starts, k, v, *, n_new=None):
+    """Write token t of k and v [sequences][tokens][kv_heads][head_dim] as slot starts[s] + t of sequence s into the pages of
+    its row of table: ``jpi_cache_append``.  n_new: int32 [sequences], how many of its tokens are new, None for all.
+    """
+    packed, _, _, _, kv, dh, dev = _pool(pool, False)
+    if k.dim() != 4:
+        raise ValueError("k must be [sequences][tokens][kv_heads][head_dim]")
+    if _recording():
+        _no_gradients(k, v, *pool)
+    n, width, stride, *at = _seqs(table, starts, dev)
+    tokens = k.shape[1]
+    if tokens > _INT_MAX:
+        raise ValueError("k has more than 2^31 - 1 tokens")
+    dt = _dtype(k)
+    _want("k", k, (n, tokens, kv, dh), k.dtype, dev)
+    _want("v", v, k.shape, k.dtype, dev)
+    if n_new is not None:
+        _want("n_new", n_new, (n,), _I32, dev)
+        _dense("n_new", n_new)
+    _launch(dev, _lib.jpi_cache_append, packed, _SEQS.pack(n, width, stride, *at), dt, tokens, _VIEW.pack(*_view("k", k)),
+            _VIEW.pack(*_view("v", v)),
+            None if n_new is None else n_new.data_ptr())
+    _written(list(pool))
+
+
+def attention(q, pool, table, lens, *, q_lens=None, causal=True, window=0, sinks=0, scale=None, out=None, lse=None):
+    """Attention of q [sequences][rows][heads][head_dim] to the slots of each sequence: ``jpi_cache_attention``.
+
+    causal: the last q_lens[s] slots are the queries' own, and a row sees no later ones; window: it sees the last `window`
+    of those only, and the first `sinks` of the sequence.  q_lens: int32 [sequences], rows of each, None for all; rows past
+    them are left as they were.  scale: head_dim^-1/2 unless given.  Returns (out, lse): out like q, lse float32
+    [sequences][rows][heads].
+    """
+    packed, _, _, _, kv, dh, dev = _pool(pool, False)
+    if q.dim() != 4:
+        raise ValueError("q must be [sequences][rows][heads][head_dim]")
+    if _recording():
+        _no_gradients(q, out, lse, *pool)
+    given = [t for t in (out, lse) if t is not None]
+    n, width, stride, *at = _seqs(table, lens, dev)
+    dt = _dtype(q)
+    _, rows, heads, _ = q.shape
+    _want("q", q, (n, rows, heads, dh), q.dtype, dev)
+    if max(rows, heads) > _INT_MAX:
+        raise ValueError("q is larger than 2^31 - 1 in a dimension")
+    ql = 0
+    if q_lens is not None:
+        _want("q_lens", q_lens, (n,), _I32, dev)
+        ql = _dense("q_lens", q_lens)
+    if out is None:
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
+    else:
+        _want("out", out, q.shape, q.dtype, dev)
+    if lse is None:
+        lse = q.new_empty((n, rows, heads), dtype=_F32)
+    else:
+        _want("lse", lse, (n, rows, heads), _F32, dev)
+    args = _pack(_ATTN, dt, rows, heads, int(bool(causal)), window, sinks, dh ** -0.5 if scale is None else scale, *_view("q", q), ql,
+                 *_view("out", out), _dense("lse", lse))
+    seqs = _SEQS.pack(n, width, stride, *at)
+    ws, size = _workspace(_lib.jpi_cache_attention_workspace, q, args, packed, seqs)
+    _launch(dev, _lib.jpi_cache_attention, args, packed, seqs, ws.data_ptr() if size else None, size)
+    if given:
+        _written(given)
+    return out, lse
+
+
+def _moves(table, lens, refs, pool, page, table_out, lens_out, refs_out):
+    """The C structure of a move, the workspace, the device, the outputs, and whether torch is told of them."""
+    if pool is not None:
+        packed, layers, n_pages, slots, _, _, dev = _pool(pool, True)
+        if page not in (None, slots):
+            raise ValueError("page is %s, that of the pool %d" % (page, slots))
+    else:
+        packed, layers, n_pages, slots, dev = None, 0, refs.shape[0] if refs.dim() == 1 else 0, page, refs.get_device()
+        if n_pages > _INT_MAX:
+            raise ValueError("refs has more than 2^31 - 1 pages")
+    _want("refs", refs, (n_pages,), _I32, dev)
+    n, width, stride = _rows("table", table, None, dev)
+    table_out = table if table_out is None else table_out
+    _, _, out_stride = _rows("table_out", table_out, n, dev)
+    _want("table_out", table_out, table.shape, _I32, dev)
+    refs_out = refs if refs_out is None else refs_out
+    _want("refs_out", refs_out, (n_pages,), _I32, dev)
+    at = out = 0
+    if lens is not None:
+        _want("lens", lens, (n,), _I32, dev)
+        at = _dense("lens", lens)
+        lens_out = lens if lens_out is None else lens_out
+        _want("lens_out", lens_out, (n,), _I32, dev)
+        out = _dense("lens_out", lens_out)
+    held = ctypes.create_string_buffer(packed, len(packed)) if packed else None
+    m = _pack(_MOVES, n, width, stride, table.data_ptr(), at, _dense("refs", refs), table_out.data_ptr(), out_stride, out,
+              _dense("refs_out", refs_out), n_pages, slots, ctypes.addressof(held) if packed else 0, layers)
+    ws, size = _workspace(_lib.jpi_cache_moves_workspace, table, m)
+    changed = [table_out, refs_out] + ([] if lens is None else [lens_out])
+    return m, held, ws, size, dev, n, changed
+
+
+def _one(name, t, like, dev):
+    if t is None:
+        return torch.empty(1, dtype=_I32, device=like.device)
+    _want(name, t, (1,), _I32, dev)
+    return t
+
+
+def resize(table, lens, refs, new_lens, pool=None, *, page=None, short=None, table_out=None, lens_out=None, refs_out=None):
+    """Give sequence s room for new_lens[s] slots, or take what lies behind them back; a partly filled last page that others
+    hold too is copied before it grows: ``jpi_cache_resize``.
+
+    table int32 [sequences][pages], lens and new_lens int32 [sequences] (negative: as it is), refs int32 [pages]; each is
+    changed in place unless it has an output of its own.  pool: all layers whose pages are copied; None for tables alone,
+    with `page` slots of a page.  Returns (lens_out, short), short int32 [1]: pages that were lacking.
+    """
+    m, held, ws, size, dev, n, changed = _moves(table, lens, refs, pool, page, table_out, lens_out, refs_out)
+    _want("new_lens", new_lens, (n,), _I32, dev)
+    short = _one("short", short, table, dev)
+    _launch(dev, _lib.jpi_cache_resize, m, _dense("new_lens", new_lens), short.data_ptr(), ws.data_ptr(), size)
+    _written(changed + [short] + list(pool or ()))
+    return changed[2], short
+
+
+def reorder(table, lens, refs, parents, page, *, table_out=None, lens_out=None, refs_out=None):
+    """Sequence s takes over what sequence parents[s] holds, nothing where there is no such sequence: ``jpi_cache_reorder``.
+    Forks share their pages until they grow.  Arguments as resize; returns lens_out.
+    """
+    m, held, ws, size, dev, n, changed = _moves(table, lens, refs, None, page, table_out, lens_out, refs_out)
+    _want("parents", parents, (n,), _I32, dev)
+    _launch(dev, _lib.jpi_cache_reorder, m, _dense("parents", parents), ws.data_ptr(), size)
+    _written(changed)
+    return changed[2]
+
+
+def compact(table, refs, pool=None, *, page=None, n_live=None, table_out=None, refs_out=None):
+    """Move the pages in use to the lowest numbers: ``jpi_cache_compact``.  Arguments as resize; returns n_live, int32 [1]:
+    pages in use.
+    """
+    if pool is None and page is None:
+        page = 16  # tables alone: of no consequence
+    m, held, ws, size, dev, _, changed = _moves(table, None, refs, pool, page, table_out, None, refs_out)
+    n_live = _one("n_live", n_live, table, dev)
+    _launch(dev, _lib.jpi_cache_compact, m, n_live.data_ptr(), ws.data_ptr(), size)
+    _written(changed + [n_live] + list(pool or ()))
+    return n_live

@@ -96,6 +96,25 @@ __device__ __forceinline__ float wave_max(float v) {
   return fmaxf(fmaxf(r0, r1), fmaxf(r2, r3));
 }
 
+// this lane's value and that of the lane 32 away (one swap; the pair is copied before the bit casts,
+// since a bit cast of an element of the returned vector reads element 0 for both)
+__device__ __forceinline__ void halves(float v, float& a, float& b) {
+  const auto p = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, v), __builtin_bit_cast(unsigned, v), false, false);
+  const unsigned x = p[0], y = p[1];
+  a = __builtin_bit_cast(float, x);
+  b = __builtin_bit_cast(float, y);
+}
+__device__ __forceinline__ float halves_max(float v) {
+  float a, b;
+  halves(v, a, b);
+  return fmaxf(a, b);
+}
+__device__ __forceinline__ float halves_sum(float v) {
+  float a, b;
+  halves(v, a, b);
+  return a + b;
+}
+
 __device__ __forceinline__ double wave_sum_d(double v) {
 #pragma unroll
   for (int o = 32; o >= 1; o >>= 1) v += __shfl_xor(v, o, 64);

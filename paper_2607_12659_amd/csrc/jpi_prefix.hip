@@ -1,9 +1,5 @@
 // C entry points of the prefix-cache operators (include/jpi_prefix.h): argument checks, then the launches.
 #include <math.h>
-#include <stdarg.h>
-#include <stdio.h>
-
-#include <cstdint>
 
 #include "jpi_prefix_internal.h"
 
@@ -11,36 +7,15 @@ using namespace jpi;
 
 namespace {
 
-thread_local char g_err[256] = "";  // no allocation on the error path: nothing here can throw
+thread_local ErrorText fail{};
 
-__attribute__((format(printf, 2, 3))) jpi_status fail(jpi_status st, const char* fmt, ...) {
-  va_list ap;
-  va_start(ap, fmt);
-  vsnprintf(g_err, sizeof g_err, fmt, ap);
-  va_end(ap);
-  return st;
-}
+jpi_status launched(const char* call, hipError_t e) { return fail.launched(call, e); }
 
-jpi_status launched(const char* call, hipError_t e) {
-  if (e == hipSuccess) return JPI_OK;
-  (void)hipGetLastError();
-  return fail(JPI_ERR_HIP, "%s: %s", call, hipGetErrorString(e));
-}
-
-bool known(jpi_dtype dt) { return dt == JPI_BF16 || dt == JPI_F32; }
-bool negative(const jpi_view& v) { return v.outer < 0 || v.row < 0 || v.head < 0; }
-bool aligned16(const jpi_view& v, int es) {
-  return ((uintptr_t)v.data & 15) == 0 && (v.outer * es) % 16 == 0 && (v.row * es) % 16 == 0 && (v.head * es) % 16 == 0;
-}
 // the same places for [outer][rows][heads]: strides of a dimension of size 1 are not used
 bool same(const jpi_view& a, const jpi_view& b, int outer, int rows, int heads) {
   return (outer <= 1 || a.outer == b.outer) && (rows <= 1 || a.row == b.row) && (heads <= 1 || a.head == b.head);
 }
 
-// an output of which several elements are one
-bool folded(const jpi_view& v, int outer, int rows, int heads) {
-  return (outer > 1 && v.outer == 0) || (rows > 1 && v.row == 0) || (heads > 1 && v.head == 0);
-}
 // one of a pair of tensors is written where the other one is read or written
 bool crossed(const jpi_view* const in[2], const jpi_view* const out[2]) {
   return out[0]->data == out[1]->data || out[0]->data == in[1]->data || out[1]->data == in[0]->data;
@@ -86,14 +61,11 @@ jpi_status check_workspace(const char* call, size_t need, const void* ws, size_t
 
 }  // namespace
 
-extern "C" {
+namespace jpi {
 
-const char* jpi_prefix_last_error(void) { return g_err; }
-
-jpi_status jpi_rope(const jpi_rope_config* cfg, jpi_dtype dt, int batch, int tokens, const int32_t* positions,
-                    int64_t pos_stride, const jpi_view* q, const jpi_view* q_out, int q_heads, const jpi_view* k,
-                    const jpi_view* k_out, int k_heads, void* stream) {
-  const char* call = "jpi_rope";
+jpi_status check_rope(ErrorText& fail, const char* call, const jpi_rope_config* cfg, jpi_dtype dt, int batch, int tokens,
+                      const int32_t* positions, int64_t pos_stride, const jpi_view* q, const jpi_view* q_out, int q_heads,
+                      const jpi_view* k, const jpi_view* k_out, int k_heads, RopeLaunch& l) {
   if (!cfg || !q || !q_out || (k && !k_out)) return fail(JPI_ERR_ARG, "%s: NULL argument", call);
   if (!known(dt)) return fail(JPI_ERR_DTYPE, "%s: dtype must be JPI_BF16 or JPI_F32", call);
   const jpi_rope_config& c = *cfg;
@@ -119,7 +91,6 @@ jpi_status jpi_rope(const jpi_rope_config* cfg, jpi_dtype dt, int batch, int tok
   if (batch == 0 || tokens == 0) return JPI_OK;
   const jpi_view* in[2] = {q, k};
   const jpi_view* out[2] = {q_out, k_out};
-  RopeLaunch l{};
   for (int i = 0; i < (k ? 2 : 1); ++i) {
     if (!in[i]->data || !out[i]->data) return fail(JPI_ERR_ARG, "%s: NULL data", call);
     if (negative(*in[i]) || negative(*out[i])) return fail(JPI_ERR_ARG, "%s: negative stride", call);
@@ -146,6 +117,23 @@ jpi_status jpi_rope(const jpi_rope_config* cfg, jpi_dtype dt, int batch, int tok
   l.beta_fast = c.beta_fast;
   l.beta_slow = c.beta_slow;
   l.amplitude = (float)c.amplitude;
+  return JPI_OK;
+}
+
+}  // namespace jpi
+
+extern "C" {
+
+const char* jpi_prefix_last_error(void) { return fail.text; }
+
+jpi_status jpi_rope(const jpi_rope_config* cfg, jpi_dtype dt, int batch, int tokens, const int32_t* positions,
+                    int64_t pos_stride, const jpi_view* q, const jpi_view* q_out, int q_heads, const jpi_view* k,
+                    const jpi_view* k_out, int k_heads, void* stream) {
+  const char* call = "jpi_rope";
+  RopeLaunch l{};
+  const jpi_status st =
+      check_rope(fail, call, cfg, dt, batch, tokens, positions, pos_stride, q, q_out, q_heads, k, k_out, k_heads, l);
+  if (st != JPI_OK || batch == 0 || tokens == 0) return st;
   return launched(call, launch_rope(dt, l, (hipStream_t)stream));
 }
 

@@ -18,57 +18,10 @@
 // tokens of 8 + 1 heads of 250 take 33 us in bf16 and 34 in fp32 (floors 12, 25).
 #include <algorithm>
 
-#include "jpi_device.h"
-#include "jpi_prefix_internal.h"
+#include "jpi_rope_device.h"
 
 namespace jpi {
 namespace {
-
-constexpr int ROPE_THREADS = 256;
-constexpr int ROPE_TABLE = 1024;  // (cos, sin) of a workgroup at most: four tokens of 256 pairs
-
-// f_i / 2 pi: turns per position of pair i
-__device__ __forceinline__ double rope_turns(const RopeLaunch& l, int i) {
-  constexpr double inv_2pi = 0.15915494309189533577;
-  const double f = exp2(-(double)i * l.log2_step);
-  double g = f;
-  if (l.scaling == JPI_ROPE_LINEAR) {
-    g = f / l.factor;
-  } else if (l.scaling == JPI_ROPE_PARTS) {
-    const double r = l.trained * f * inv_2pi;
-    const double keep = fmin(1.0, fmax(0.0, (r - l.beta_slow) / (l.beta_fast - l.beta_slow)));
-    g = f * (keep + (1.0 - keep) / l.factor);
-  }
-  return g * inv_2pi;
-}
-
-// N consecutive elements: one piece where they are aligned to their size, else one by one
-template <typename T, int N, bool VEC>
-struct Piece {
-  typedef T vec __attribute__((ext_vector_type(N)));
-  T v[N];
-  __device__ __forceinline__ void load(const T* p) {
-    if constexpr (VEC) {
-      const vec x = *reinterpret_cast<const vec*>(p);
-#pragma unroll
-      for (int e = 0; e < N; ++e) v[e] = x[e];
-    } else {
-#pragma unroll
-      for (int e = 0; e < N; ++e) v[e] = p[e];
-    }
-  }
-  __device__ __forceinline__ void store(T* p) const {
-    if constexpr (VEC) {
-      vec x;
-#pragma unroll
-      for (int e = 0; e < N; ++e) x[e] = v[e];
-      *reinterpret_cast<vec*>(p) = x;
-    } else {
-#pragma unroll
-      for (int e = 0; e < N; ++e) p[e] = v[e];
-    }
-  }
-};
 
 // A unit is N elements of a head, with JPI_ROPE_HALF and their N partners half a rotation further on.
 template <typename T, int N, bool VEC, bool INTER>
@@ -77,17 +30,7 @@ __global__ __launch_bounds__(ROPE_THREADS) void k_rope(RopeLaunch l, int first, 
   const int pairs = l.rot_dim >> 1;
   const int tok0 = first + (int)blockIdx.x * tile, here = min(tile, n_tok - tok0);
 
-  int have = -1;
-  double f = 0.0;
-  for (int e = threadIdx.x; e < here * pairs; e += ROPE_THREADS) {
-    const int tt = e / pairs, i = e - tt * pairs, n = tok0 + tt;
-    if (i != have) f = rope_turns(l, i), have = i;
-    const int b = n / l.tokens, t = n - b * l.tokens;
-    const double turns = (double)(l.pos ? l.pos[b * l.pos_stride + t] : t) * f;
-    float sn, cs;
-    sincospif(2.f * (float)(turns - rint(turns)), &sn, &cs);
-    table[e] = float2{l.amplitude * cs, l.inverse ? -l.amplitude * sn : l.amplitude * sn};
-  }
+  rope_table(l, tok0, here, table);
   __syncthreads();
 
   const unsigned rot_units = (INTER ? l.rot_dim : pairs) / N, per_head = rot_units + (l.head_dim - l.rot_dim) / N;

@@ -101,25 +101,6 @@ __device__ __forceinline__ f32x16 mfma_chunk(const typename Tile<T, 64, 32>::chu
   }
 }
 
-// the larger of this lane's value and that of the lane 32 away (one swap; the pair is copied before the bit casts,
-// since a bit cast of an element of the returned vector reads element 0 for both)
-__device__ __forceinline__ void halves(float v, float& a, float& b) {
-  const auto p = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(u32, v), __builtin_bit_cast(u32, v), false, false);
-  const u32 x = p[0], y = p[1];
-  a = __builtin_bit_cast(float, x);
-  b = __builtin_bit_cast(float, y);
-}
-__device__ __forceinline__ float halves_max(float v) {
-  float a, b;
-  halves(v, a, b);
-  return fmaxf(a, b);
-}
-__device__ __forceinline__ float halves_sum(float v) {
-  float a, b;
-  halves(v, a, b);
-  return a + b;
-}
-
 __device__ __forceinline__ u32 uniform(u32 v) { return __builtin_amdgcn_readfirstlane(v); }
 
 struct View {

@@ -32,9 +32,12 @@ EXPORTED = ["jpi_abi_version", "jpi_status_str", "jpi_last_error", "jpi_create",
             "jpi_corr_destroy", "jpi_corr_set_weight", "jpi_corr_finalize_weights", "jpi_corr_compress",
             "jpi_corr_predict", "jpi_corr_last_error", "jpi_prefix_last_error", "jpi_rope",
             "jpi_shared_attention_workspace", "jpi_prefix_weight_workspace", "jpi_shared_attention", "jpi_prefix_weight",
-            "jpi_evict", "jpi_debug_prefix_plan"]
+            "jpi_evict", "jpi_debug_prefix_plan", "jpi_cache_last_error", "jpi_norm_rope", "jpi_cache_append",
+            "jpi_cache_attention_workspace", "jpi_cache_attention", "jpi_debug_cache_plan", "jpi_cache_moves_workspace",
+            "jpi_cache_resize", "jpi_cache_reorder", "jpi_cache_compact"]
 JPI_ROPE_HALF, JPI_ROPE_INTERLEAVED = 0, 1
 JPI_ROPE_PLAIN, JPI_ROPE_LINEAR, JPI_ROPE_BASE, JPI_ROPE_PARTS = range(4)
+JPI_E4M3, JPI_INT8 = 0, 1
 JPI_KERNEL_NONE, JPI_KERNEL_QKV, JPI_KERNEL_ATTENTION, JPI_KERNEL_OPROJ, JPI_KERNEL_GATEUP, JPI_KERNEL_DOWN, \
     JPI_KERNEL_PERSISTENT = range(-1, 6)
 
@@ -93,6 +96,35 @@ class jpi_evict_args(ctypes.Structure):
                 ("k", jpi_view), ("v", jpi_view), ("k_out", jpi_view), ("v_out", jpi_view),
                 ("weight_out", ctypes.c_void_p), ("weight_out_stride", ctypes.c_int64), ("index", ctypes.c_void_p),
                 ("len_out", ctypes.c_void_p)]
+
+
+# include/jpi_cache.h
+class jpi_cache_pool(ctypes.Structure):
+    _fields_ = [("code", ctypes.c_int), ("n_kv_heads", ctypes.c_int), ("head_dim", ctypes.c_int), ("n_pages", ctypes.c_int),
+                ("page", ctypes.c_int), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p),
+                ("v_scale", ctypes.c_void_p)]
+
+
+class jpi_cache_seqs(ctypes.Structure):
+    _fields_ = [("n_seqs", ctypes.c_int), ("max_pages", ctypes.c_int), ("table_stride", ctypes.c_int64),
+                ("table", ctypes.c_void_p), ("len", ctypes.c_void_p)]
+
+
+class jpi_head_norm(ctypes.Structure):
+    _fields_ = [("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p), ("weight_dtype", ctypes.c_int),
+                ("unit_offset", ctypes.c_int), ("weight_stride", ctypes.c_int64), ("eps", ctypes.c_double)]
+
+
+class jpi_cache_attn(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int), ("q_rows", ctypes.c_int), ("n_heads", ctypes.c_int), ("causal", ctypes.c_int),
+                ("window", ctypes.c_int), ("sinks", ctypes.c_int), ("scale", ctypes.c_float), ("q", jpi_view),
+                ("q_len", ctypes.c_void_p), ("out", jpi_view), ("lse", ctypes.c_void_p)]
+
+
+class jpi_cache_moves(ctypes.Structure):
+    _fields_ = [("seqs", jpi_cache_seqs), ("refs", ctypes.c_void_p), ("table_out", ctypes.c_void_p),
+                ("table_out_stride", ctypes.c_int64), ("len_out", ctypes.c_void_p), ("refs_out", ctypes.c_void_p),
+                ("n_pages", ctypes.c_int), ("page", ctypes.c_int), ("pool", ctypes.c_void_p), ("layers", ctypes.c_int)]
 
 
 # include/jpi_sched.h
@@ -195,6 +227,16 @@ _sig = {
     "jpi_prefix_weight": (_i, [_vp, _vp, _f, _vp, _vp, ctypes.c_size_t, _vp]),
     "jpi_evict": (_i, [_vp, _vp]),
     "jpi_debug_prefix_plan": (_i, [_vp, _i, _vp, _vp, _vp]),
+    "jpi_cache_last_error": (ctypes.c_char_p, []),
+    "jpi_norm_rope": (_i, [_vp, _vp, _i, _i, _i, _vp, _i64, _vp, _vp, _i, _vp, _vp, _i, _vp]),
+    "jpi_cache_append": (_i, [_vp, _vp, _i, _i, _vp, _vp, _vp, _vp]),
+    "jpi_cache_attention_workspace": (_i, [_vp, _vp, _vp, _vp]),
+    "jpi_cache_attention": (_i, [_vp, _vp, _vp, _vp, ctypes.c_size_t, _vp]),
+    "jpi_debug_cache_plan": (_i, [_vp, _vp, _vp, _vp, _vp, _vp]),
+    "jpi_cache_moves_workspace": (_i, [_vp, _vp]),
+    "jpi_cache_resize": (_i, [_vp, _vp, _vp, _vp, ctypes.c_size_t, _vp]),
+    "jpi_cache_reorder": (_i, [_vp, _vp, _vp, ctypes.c_size_t, _vp]),
+    "jpi_cache_compact": (_i, [_vp, _vp, _vp, ctypes.c_size_t, _vp]),
 }
 for _name, (_res, _args) in _sig.items():
     _fn = getattr(_lib, _name)
@@ -472,6 +514,58 @@ def jpi_debug_prefix_plan(args: jpi_shared_attn, of_weight: int):
     v = [ctypes.c_int() for _ in range(3)]
     st = _lib.jpi_debug_prefix_plan(_ref(args), of_weight, *(ctypes.byref(x) for x in v))
     return (st, *(x.value for x in v))
+
+
+def jpi_cache_last_error() -> str:
+    return (_lib.jpi_cache_last_error() or b"").decode()
+
+
+def jpi_norm_rope(norm: jpi_head_norm, cfg: jpi_rope_config, dtype: int, batch: int, tokens: int, positions, pos_stride: int,
+                  q: jpi_view, q_out: jpi_view, q_heads: int, k: jpi_view | None = None, k_out: jpi_view | None = None,
+                  k_heads: int = 0, stream=None) -> int:
+    return _lib.jpi_norm_rope(_ref(norm), _ref(cfg), dtype, batch, tokens, addr(positions), pos_stride, _ref(q), _ref(q_out),
+                              q_heads, _ref(k), _ref(k_out), k_heads, stream_handle(stream))
+
+
+def jpi_cache_append(pool: jpi_cache_pool, seqs: jpi_cache_seqs, dtype: int, tokens: int, k: jpi_view, v: jpi_view, n_new=None,
+                     stream=None) -> int:
+    return _lib.jpi_cache_append(_ref(pool), _ref(seqs), dtype, tokens, _ref(k), _ref(v), addr(n_new), stream_handle(stream))
+
+
+def jpi_cache_attention_workspace(args: jpi_cache_attn, pool: jpi_cache_pool, seqs: jpi_cache_seqs):
+    n = ctypes.c_size_t()
+    st = _lib.jpi_cache_attention_workspace(_ref(args), _ref(pool), _ref(seqs), ctypes.byref(n))
+    return st, n.value
+
+
+def jpi_cache_attention(args: jpi_cache_attn, pool: jpi_cache_pool, seqs: jpi_cache_seqs, workspace=None, workspace_bytes: int = 0,
+                        stream=None) -> int:
+    return _lib.jpi_cache_attention(_ref(args), _ref(pool), _ref(seqs), addr(workspace), workspace_bytes, stream_handle(stream))
+
+
+def jpi_debug_cache_plan(args: jpi_cache_attn, pool: jpi_cache_pool, seqs: jpi_cache_seqs):
+    """(status, waves, tiles, ranges)"""
+    v = [ctypes.c_int() for _ in range(3)]
+    st = _lib.jpi_debug_cache_plan(_ref(args), _ref(pool), _ref(seqs), *(ctypes.byref(x) for x in v))
+    return (st, *(x.value for x in v))
+
+
+def jpi_cache_moves_workspace(args: jpi_cache_moves):
+    n = ctypes.c_size_t()
+    st = _lib.jpi_cache_moves_workspace(_ref(args), ctypes.byref(n))
+    return st, n.value
+
+
+def jpi_cache_resize(args: jpi_cache_moves, new_len, short_out=None, workspace=None, workspace_bytes: int = 0, stream=None) -> int:
+    return _lib.jpi_cache_resize(_ref(args), addr(new_len), addr(short_out), addr(workspace), workspace_bytes, stream_handle(stream))
+
+
+def jpi_cache_reorder(args: jpi_cache_moves, parents, workspace=None, workspace_bytes: int = 0, stream=None) -> int:
+    return _lib.jpi_cache_reorder(_ref(args), addr(parents), addr(workspace), workspace_bytes, stream_handle(stream))
+
+
+def jpi_cache_compact(args: jpi_cache_moves, n_live_out=None, workspace=None, workspace_bytes: int = 0, stream=None) -> int:
+    return _lib.jpi_cache_compact(_ref(args), addr(n_live_out), addr(workspace), workspace_bytes, stream_handle(stream))
 
 
 class JpiError(RuntimeError):

@@ -102,7 +102,10 @@ def _launch(dev, f, *args):
         with torch.cuda.device(dev):
             status = f(*args, _raw_stream(dev))
     if status != _j.JPI_OK:
-        raise _j.JpiError(status, _j.jpi_prefix_last_error())
+        raise _j.JpiError(status, _LAST_ERROR.get(f.__name__, _j.jpi_prefix_last_error)())
+
+
+_LAST_ERROR = {}  # of functions of another header than include/jpi_prefix.h
 
 
 def rope(q, k=None, positions=None, *, rot_dim=None, layout="half", base=1e4, scaling="none", factor=1.0, trained=0,
@@ -112,6 +115,13 @@ def rope(q, k=None, positions=None, *, rot_dim=None, layout="half", base=1e4, sc
     positions: int32 [batch][tokens] or [tokens], None for 0, 1, 2 ...  q_out, k_out: None for new tensors; q and k
     themselves to turn them in place.  Returns (q_out, k_out), k_out None without k.
     """
+    return _turned(None, q, k, positions, rot_dim, layout, base, scaling, factor, trained, beta_fast, beta_slow, amplitude, inverse,
+                   q_out, k_out)
+
+
+def _turned(norm, q, k, positions, rot_dim, layout, base, scaling, factor, trained, beta_fast, beta_slow, amplitude, inverse, q_out,
+            k_out):
+    """jpi_rope, or jpi_norm_rope with the norm's arguments."""
     if q.dim() != 4:
         raise ValueError("q must be [batch][tokens][heads][head_dim]")
     if _recording():
@@ -156,8 +166,11 @@ def rope(q, k=None, positions=None, *, rot_dim=None, layout="half", base=1e4, sc
             raise ValueError("positions of a batch row must be contiguous")
         pos = positions.data_ptr()
     pack = _VIEW.pack
-    _launch(dev, _lib.jpi_rope, cfg, dt, b, n, pos, pos_stride, pack(*_view("q", q)), pack(*_view("q_out", q_out)), heads, kv, ko,
-            k_heads)
+    args = (cfg, dt, b, n, pos, pos_stride, pack(*_view("q", q)), pack(*_view("q_out", q_out)), heads, kv, ko, k_heads)
+    if norm is None:
+        _launch(dev, _lib.jpi_rope, *args)
+    else:
+        _launch(dev, _lib.jpi_norm_rope, norm, *args)
     if given:
         _written(given)
     return q_out, k_out

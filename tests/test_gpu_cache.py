@@ -1,0 +1,695 @@
+"""The operators of a paged 8-bit cache (include/jpi_cache.h) against plain implementations in 64 bits on the CPU.
+
+Codes, scales, tables and counts have to be equal.  Tolerances of the others come from the formats: h is half a step of the
+output type relative to the value (bf16 2^-8, fp32 2^-24), u = 2^-24 a rounding in fp32.
+"""
+import math
+
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+
+import cache_reference as ref  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+H = {torch.bfloat16: 2.0 ** -8, torch.float32: U}
+TYPES = [torch.bfloat16, torch.float32]
+CODES = {"int8": torch.int8, "e4m3": torch.float8_e4m3fn}
+INF = float("inf")
+
+
+@pytest.fixture(scope="module")
+def ops():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2607_12659_amd import cache_ops
+    return cache_ops
+
+
+def rand(seed, *shape, dtype=torch.float32):
+    g = torch.Generator().manual_seed(seed)
+    return torch.randn(shape, generator=g).to(dtype)
+
+
+def dev(t):
+    return None if t is None else t.cuda() if torch.is_tensor(t) else torch.from_numpy(np.ascontiguousarray(t)).cuda()
+
+
+def i32(values):
+    return torch.tensor(values, dtype=torch.int32, device="cuda")
+
+
+def within(got, want, tol):
+    """Every element within its own tolerance; non-finite ones equal."""
+    got, want = got.double().cpu(), torch.as_tensor(want, dtype=torch.float64)
+    fin = torch.isfinite(want)
+    assert torch.equal(torch.isfinite(got), fin)
+    assert torch.equal(torch.isnan(got), torch.isnan(want))
+    assert torch.equal(got[~fin & ~torch.isnan(want)], want[~fin & ~torch.isnan(want)])
+    tol = torch.as_tensor(tol, dtype=torch.float64).expand_as(want)
+    over = ((got - want).abs() - tol)[fin]
+    assert over.numel() == 0 or over.max() <= 0, "off by %g past the tolerance" % over.max()
+
+
+# ---------------------------------------------------------------------------
+# norms with rotation
+# ---------------------------------------------------------------------------
+def norm64(x, w, offset, eps, pos, rot, layout="half", base=1e4, scaling="none", factor=1.0, trained=0, beta_fast=32.0, beta_slow=1.0,
+           amplitude=1.0, inverse=False):
+    """The result, and the size of each element's pair, the scale of its errors."""
+    x = x.double()
+    y = x / torch.sqrt(x.square().mean(-1, keepdim=True) + eps)
+    if w is not None:
+        y = y * (w.double() + offset)
+    if scaling == "base":
+        base = base * factor ** (rot / (rot - 2))
+    f = torch.tensor([base ** (-2 * i / rot) for i in range(rot // 2)], dtype=torch.float64)
+    if scaling == "linear":
+        f = f / factor
+    if scaling == "parts":
+        keep = ((trained * f / (2 * math.pi) - beta_slow) / (beta_fast - beta_slow)).clamp(0, 1)
+        f = f * keep + f / factor * (1 - keep)
+    ang = pos.double()[..., None, None] * f * (-1 if inverse else 1)
+    c, s = amplitude * torch.cos(ang), amplitude * torch.sin(ang)
+    out, size = y.clone(), y.abs()
+    lo, hi = (slice(0, rot // 2), slice(rot // 2, rot)) if layout == "half" else (slice(0, rot, 2), slice(1, rot, 2))
+    a, b = y[..., lo], y[..., hi]
+    out[..., lo], out[..., hi] = a * c - b * s, a * s + b * c
+    size[..., lo] = size[..., hi] = amplitude * (a.abs() + b.abs())
+    return out, size
+
+
+def norm_close(got, x, w, offset, eps, pos, rot, **kw):
+    """Squares are summed in fp32: D / 2 u of the factor at most (it is a root), and a few u for the mean, the root, the
+    division and the products; the rotation as jpi_rope's (8 u of the pair's size); then the output's rounding."""
+    want, size = norm64(x, w, offset, eps, pos, rot, **kw)
+    within(got, want, H[x.dtype] * want.abs() + (x.shape[-1] / 2 + 16) * U * size * 1.01)
+
+
+NORM = [
+    # batch, tokens, heads, kv heads, head dim, rot, weights (0 none, 1 shared, 2 of each head), offset, what else
+    (1, 1, 8, 1, 256, 256, 1, 1, {}),
+    (2, 7, 3, 2, 64, 32, 1, 0, dict(layout="interleaved")),
+    (3, 1030, 2, 0, 128, 128, 2, 0, dict(scaling="linear", factor=4.0)),
+    (2, 513, 4, 1, 64, 64, 2, 1, dict(layout="interleaved", scaling="base", factor=8.0)),
+    (1, 90, 2, 1, 128, 64, 0, 0, dict(scaling="parts", factor=5.5, trained=4096, amplitude=1.125)),
+    (2, 5, 3, 1, 10, 6, 1, 0, {}),                           # pieces of single elements
+    (2, 5, 3, 1, 10, 6, 2, 1, dict(layout="interleaved")),
+    (2, 3, 2, 1, 512, 2, 1, 0, {}),                          # nearly all of it passes by, element by element
+    (1, 3, 1, 1, 512, 512, 1, 0, dict(inverse=True, amplitude=0.5)),
+    (1, 3, 1, 1, 512, 512, 0, 1, dict(layout="interleaved")),
+    (1, 3, 2, 1, 2, 2, 1, 0, dict(base=500.0)),
+    (1, 2, 3, 3, 96, 48, 1, 0, {}),                          # a head that is no power of two
+]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("wtype", TYPES)
+@pytest.mark.parametrize("case", NORM, ids=lambda c: "b%d-n%d-h%d+%d-d%d-r%d-w%d%d" % c[:8])
+def test_norm_rope(ops, case, dtype, wtype):
+    b, n, heads, kv, dh, rot, kind, offset, kw = case
+    q, k = 3 * rand(1, b, n, heads, dh), 3 * rand(2, b, n, kv, dh) if kv else None
+    q, k = q.to(dtype), None if k is None else k.to(dtype)
+    shape = lambda h: () if kind == 0 else (dh,) if kind == 1 else (h, dh)  # noqa: E731
+    qw = (1 - offset + 0.3 * rand(3, *shape(heads))).to(wtype) if kind else None
+    kw_ = (1 - offset + 0.3 * rand(4, *shape(kv))).to(wtype) if kind and kv else None
+    pos = torch.randint(0, 1 << 20, (b, n), generator=torch.Generator().manual_seed(3)).int()
+    qo, ko = ops.norm_rope(dev(q), dev(k), dev(pos), q_weight=dev(qw), k_weight=dev(kw_), unit_offset=bool(offset), eps=1e-3,
+                           rot_dim=rot, **kw)
+    norm_close(qo, q, qw, offset, 1e-3, pos, rot, **kw)
+    if kv:
+        norm_close(ko, k, kw_, offset, 1e-3, pos, rot, **kw)
+    else:
+        assert ko is None
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_norm_rope_positions_strides_and_in_place(ops, dtype):
+    # q and k as slices of one projection whose rows start off 16-byte boundaries, k_out a longer tensor's middle
+    b, n, dh = 2, 9, 64
+    both = rand(5, b, n, 6, dh + 3, dtype=dtype)
+    d = dev(both)
+    q, k = d[:, :, :4, :dh], d[:, :, 4:, :dh]
+    longer = torch.full((b, 20, 2, dh), 7.0, dtype=dtype, device="cuda")
+    w = rand(6, dh)
+    pos = torch.tensor([3, -5, 0, 100000, 2, 2, 1 << 24, -(1 << 24), 8]).int()
+    qo, ko = ops.norm_rope(q, k, dev(pos), q_weight=dev(w), q_out=q, k_out=longer[:, 5:14])  # k: the norm alone
+    assert qo is q
+    norm_close(qo, both[:, :, :4, :dh], w, 0, 1e-6, pos.expand(b, n), dh)
+    norm_close(ko, both[:, :, 4:, :dh], None, 0, 1e-6, pos.expand(b, n), dh)
+    assert torch.equal(d[:, :, 4:].cpu(), both[:, :, 4:]) and torch.equal(d[..., dh:].cpu(), both[..., dh:])
+    assert (longer[:, :5] == 7).all() and (longer[:, 14:] == 7).all()
+    # weights of each head of k alone; consecutive positions; one head read by all (stride 0)
+    x, one, kw = rand(7, 2, 5, 2, dh, dtype=dtype), rand(8, 2, 5, 1, dh, dtype=dtype), rand(9, 3, dh)
+    qo, ko = ops.norm_rope(dev(x), dev(one).expand(2, 5, 3, dh), k_weight=dev(kw), unit_offset=True)
+    at = torch.arange(5).expand(2, 5)
+    norm_close(qo, x, None, 0, 1e-6, at, dh)
+    norm_close(ko, one.expand(2, 5, 3, dh), kw, 1, 1e-6, at, dh)
+
+
+def test_norm_rope_zero_and_spoilt_heads(ops):
+    """A head of zeros stays zero; NaN and infinity spoil their own head only."""
+    x = rand(10, 1, 6, 2, 64)
+    x[0, 1, 0], x[0, 2, 1, 5], x[0, 3, 0, 7] = 0, float("nan"), INF
+    got = ops.norm_rope(dev(x))[0].cpu()
+    want, _ = norm64(x, None, 0, 1e-6, torch.arange(6)[None], 64)
+    assert torch.equal(got[0, 1, 0], torch.zeros(64)) and torch.isnan(got[0, 2, 1]).any() and torch.isnan(got[0, 3, 0]).any()
+    fine = torch.ones(1, 6, 2, dtype=torch.bool)
+    fine[0, 2, 1] = fine[0, 3, 0] = False
+    within(got[fine], want[fine], (32 + 16) * U * 8)
+
+
+# ---------------------------------------------------------------------------
+# append
+# ---------------------------------------------------------------------------
+def filled(seed, n_pages, kv, dh, page, code, scales=True):
+    """A pool of coded normal values as numpy: (k bytes, v bytes, k scales, v scales)."""
+    r = np.random.RandomState(seed)
+    out = []
+    for shape in ((dh // 16, page, 16), (page // 16, dh, 16)):
+        x = r.randn(n_pages, kv, *shape).astype(np.float32) * np.exp(0.7 * r.randn(n_pages, kv, 1, 1, 1)).astype(np.float32)
+        s = np.array([[ref.scale_for(float(np.abs(x[p, h]).max()), code) for h in range(kv)] for p in range(n_pages)], np.float32)
+        out.append((ref.encode(x / s[..., None, None, None], code), s))
+    return [out[0][0], out[1][0], out[0][1], out[1][1]]
+
+
+def on_gpu(ops, pool, code):
+    return ops.Pool(dev(pool[0]).view(CODES[code]), dev(pool[1]).view(CODES[code]), dev(pool[2]), dev(pool[3]))
+
+
+def same_pool(got, want):
+    for g, w, name in zip(got, want, ("k", "v", "k_scale", "v_scale")):
+        g = g.cpu()
+        g = g.numpy() if g.dtype == torch.float32 else g.view(torch.uint8).numpy()
+        if g.dtype == np.float32:
+            np.testing.assert_array_equal(g, w, err_msg=name)  # NaN equals NaN
+        else:
+            assert np.array_equal(g, w), "%s: %d of %d bytes differ" % (name, (g != w).sum(), g.size)
+
+
+def numbered(seed, counts, width, n_pages):
+    """A table whose rows take shuffled page numbers, garbage behind them."""
+    order = np.random.RandomState(seed).permutation(n_pages)
+    table, at = np.full((len(counts), width), -7, np.int32), 0
+    for s, c in enumerate(counts):
+        table[s, :c] = order[at:at + c]
+        at += c
+    assert at <= n_pages
+    return table
+
+
+def append_both(ops, pool, code, page, table, starts, k, v, n_new=None):
+    """Append on the GPU and in numpy, and compare; the pool in numpy changes."""
+    n = np.full(len(starts), k.shape[1]) if n_new is None else np.asarray(n_new)
+    d = on_gpu(ops, pool, code)
+    ops.append(d, dev(table), i32(starts), dev(k), dev(v), n_new=None if n_new is None else i32(n_new))
+    for i, x in ((0, k), (1, v)):
+        ref.append_one(pool[i], pool[2 + i], i == 0, code, page, table, starts, x.float().numpy(), n)
+    same_pool(d, pool)
+    return d
+
+
+APPEND = [
+    # sequences' slots before, tokens, tokens that are new (None: all), kv heads, dim, page
+    ([0], 1, None, 1, 64, 16),
+    ([0, 15, 16, 17, 31], 1, None, 2, 64, 16),
+    ([5, 0, 90, 63, 64], 70, [70, 0, 1, 33, 69], 2, 128, 64),
+    ([1, 127, 128, 300], 260, [260, 1, 129, 0], 1, 256, 128),
+    ([0, 3], 816, [816, 500], 1, 256, 32),
+    ([7, 8, 9], 3, None, 8, 128, 16),
+    ([40], 1000, [2000], 1, 64, 128),      # more than there are: all
+    ([-3, 2], 5, [-1, 5], 1, 64, 16),      # lengths and counts below 0: 0
+]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("code", CODES)
+@pytest.mark.parametrize("case", range(len(APPEND)))
+def test_append(ops, case, code, dtype):
+    starts, tokens, n_new, kv, dh, page = APPEND[case]
+    n = [tokens] * len(starts) if n_new is None else n_new
+    counts = [-(-(max(s, 0) + min(max(t, 0), tokens)) // page) for s, t in zip(starts, n)]
+    n_pages = sum(counts) + 2
+    pool = filled(case, n_pages, kv, dh, page, code)
+    table = numbered(case, counts, max(counts) + 1, n_pages)
+    k = rand(20 + case, len(starts), tokens, kv, dh) * torch.exp(0.8 * rand(30 + case, len(starts), tokens, 1, 1))
+    v = rand(40 + case, len(starts), tokens, kv, dh) * torch.exp(0.8 * rand(50 + case, len(starts), tokens, 1, 1))
+    append_both(ops, pool, code, page, table, starts, k.to(dtype), v.to(dtype), n_new)
+
+
+@pytest.mark.parametrize("code", CODES)
+def test_append_token_by_token(ops, code):
+    """Scales that grow again and again, and values that fall on ties and on the largest code."""
+    kv, dh, page = 1, 64, 16
+    pool = filled(3, 4, kv, dh, page, code)
+    table = numbered(3, [3], 3, 4)
+    top = ref.TOP[code]
+    for t in range(40):
+        x = rand(100 + t, 1, 1, kv, dh) * 1.3 ** t
+        if t % 4 == 1:
+            x = torch.round(x * 4) / 8  # halves: ties of int8
+        if t % 4 == 2:
+            x[..., 0] = top * 2.0 ** (t // 4)  # the largest code exactly
+        if t % 4 == 3:
+            x[..., 0] = top * 2.0 ** (t // 4) * (1 + 2.0 ** -22)  # just above it
+        append_both(ops, pool, code, page, table, [t], x, -x)
+
+
+@pytest.mark.parametrize("code", CODES)
+def test_append_odd_values(ops, code):
+    """Zeros, subnormals, the largest numbers, NaN and infinities, and scales that no append would have set."""
+    kv, dh, page = 2, 64, 16
+    pool = filled(4, 12, kv, dh, page, code)
+    table = numbered(4, [1] * 12, 2, 12)
+    pool[2][table[8, 0]], pool[2][table[9, 0]], pool[3][table[9, 0]] = 0.0, 0.3, 0.01
+    pool[2][table[10, 0], 0] = np.nan
+    k, v = rand(60, 12, 2, kv, dh), rand(61, 12, 2, kv, dh)
+    k[0], v[0] = 0, 0
+    k[1] *= 2.0 ** -130
+    v[1] *= 2.0 ** -148
+    k[2] *= 2.0 ** 124
+    k[3, 1, 0, 5], v[3, 0, 1, 6] = float("nan"), INF
+    k[4, 0, 1, 0], v[4, 0, 0, 0] = -INF, -float("nan")
+    k[5] = 3.3e38
+    k[6], v[7] = -3.4e38, 1.5e-45
+    k[8] = 0
+    starts = [0, 0, 0, 0, 3, 2, 3, 0, 4, 4, 4, 14]
+    append_both(ops, pool, code, page, table, starts, k, v)
+    # what was spoilt stays so, until the page is begun anew
+    append_both(ops, pool, code, page, table, [2, 2, 2, 2, 5, 4, 5, 2, 6, 6, 6, 15], rand(62, 12, 1, kv, dh), rand(63, 12, 1, kv, dh))
+    append_both(ops, pool, code, page, table, [0] * 12, rand(64, 12, 16, kv, dh), rand(65, 12, 16, kv, dh))
+    assert np.isfinite(pool[2]).all() and np.isfinite(pool[3]).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_append_strides_and_numbers_that_name_no_page(ops, dtype):
+    kv, dh, page, code = 2, 128, 32, "e4m3"
+    pool = filled(5, 9, kv, dh, page, code)
+    table = numbered(5, [3, 3, 3], 3, 9)
+    table[0, 1], table[1, 0], table[2, 2] = -1, 9, 1 << 30
+    qkv = rand(66, 3, 100, 4 * kv, dh + 1, dtype=dtype)  # rows off 16-byte boundaries
+    k, v = qkv[:, :, kv:2 * kv, :dh], qkv[:, :, 2 * kv:3 * kv, 1:]
+    before = [x.copy() for x in pool]
+    d = on_gpu(ops, pool, code)
+    g = dev(qkv)
+    ops.append(d, dev(np.hstack([table, table]))[:, :3], i32([0, 10, 20]), g[:, :, kv:2 * kv, :dh], g[:, :, 2 * kv:3 * kv, 1:])
+    for i, x in ((0, k), (1, v)):  # tokens past the table's three pages are dropped
+        ref.append_one(pool[i], pool[2 + i], i == 0, code, page, table, [0, 10, 20], x.float().numpy(), [100] * 3)
+    same_pool(d, pool)
+    assert sum((a != b).any() for a, b in zip(pool, before)) == 4
+    # a token of all sequences (stride 0 along them), aligned rows
+    one = rand(67, 1, 4, kv, dh, dtype=dtype)
+    d = on_gpu(ops, pool, code)
+    table = numbered(6, [3, 3, 3], 3, 9)
+    ops.append(d, dev(table), i32([30, 0, 64]), dev(one).expand(3, 4, kv, dh), dev(one).expand(3, 4, kv, dh))
+    for i in (0, 1):
+        ref.append_one(pool[i], pool[2 + i], i == 0, code, page, table, [30, 0, 64], one.float().expand(3, 4, kv, dh).numpy(), [4] * 3)
+    same_pool(d, pool)
+
+
+# ---------------------------------------------------------------------------
+# attention
+# ---------------------------------------------------------------------------
+def attn64(q, pool, code, page, table, lens, q_lens, causal, window, sinks, scale):
+    """out, lse; per element the sum of p |v|; per row the scale of its scores' errors; rows that exist."""
+    S, R, nh, D = q.shape
+    kv = pool[2].shape[1]
+    q = q.double().numpy()
+    out, mag = np.zeros((S, R, nh, D)), np.zeros((S, R, nh, D))
+    lse, err, there = np.full((S, R, nh), -INF), np.zeros((S, R, nh)), np.zeros((S, R), bool)
+    for s in range(S):
+        n, nq = min(max(lens[s], 0), table.shape[1] * page), min(max(q_lens[s], 0), R)
+        there[s, :nq] = True
+        K, V = (ref.slots(pool[i], pool[2 + i], i == 0, code, page, table[s], n) for i in (0, 1))
+        see = ref.seen(n, nq, causal, window, sinks)
+        for h in range(nh):
+            hk = h // (nh // kv)
+            for i in range(nq):
+                at = see[i]
+                if not at.any():
+                    continue
+                k, v = K[hk][at], V[hk][at]
+                x = scale * (k @ q[s, i, h])
+                m = x.max()
+                e = np.exp(x - m)
+                lse[s, i, h] = m + np.log(e.sum())
+                p = e / e.sum()
+                out[s, i, h], mag[s, i, h] = p @ v, p @ np.abs(v)
+                err[s, i, h] = scale * (np.abs(k) @ np.abs(q[s, i, h])).max()
+    return out, lse, mag, err, there
+
+
+def attn_tolerance(dtype, out, lse, mag, err, keys, D):
+    """Codes are exact.  Scores: products summed in fp32, D u of the sum of magnitudes (3 D in the parts of fp32 queries, whose
+    smaller ones add next to nothing), and 8 u for scale, page scale and reference; exp2, sums and joins (keys + 40) u; the
+    probability times the page's scale is rounded to bf16 or to 24 bits in parts; then the output's rounding."""
+    ds = ((1 if dtype == torch.bfloat16 else 3) * D + 8) * U * err + 8 * U * (np.nan_to_num(np.abs(lse), posinf=0) + 1)
+    soft = 2 * ds + (keys + 40) * U
+    p = H[dtype] if dtype == torch.bfloat16 else 4 * U
+    return H[dtype] * np.abs(out) + mag * (soft[..., None] + p) * 1.01 + 1e-30, np.where(lse == -INF, 0, soft + 1e-30)
+
+
+def attend_both(ops, q, pool, code, page, table, lens, q_lens=None, causal=True, window=0, sinks=0, scale=None):
+    S, R, nh, D = q.shape
+    ql = [R] * S if q_lens is None else q_lens
+    marker = -77.0
+    out = torch.full(q.shape, marker, dtype=q.dtype, device="cuda")
+    lse = torch.full(q.shape[:3], marker, device="cuda")
+    got = ops.attention(dev(q), on_gpu(ops, pool, code), dev(table), i32(lens), q_lens=None if q_lens is None else i32(q_lens),
+                        causal=causal, window=window, sinks=sinks, scale=scale, out=out, lse=lse)
+    assert got[0] is out and got[1] is lse
+    o, l, mag, err, there = attn64(q, pool, code, page, table, lens, ql, causal, window, sinks, D ** -0.5 if scale is None else scale)
+    tol_o, tol_l = attn_tolerance(q.dtype, o, l, mag, err, max([1] + list(lens)), D)
+    there = torch.from_numpy(there)
+    within(out.cpu()[there], o[there.numpy()], tol_o[there.numpy()])
+    within(lse.cpu()[there], l[there.numpy()], tol_l[there.numpy()])
+    assert (out.cpu()[~there] == marker).all() and (lse.cpu()[~there] == marker).all()
+    return out, lse
+
+
+ATTN = [
+    # rows, heads, kv heads, dim, page, lengths, rows of each (None: all), causal, window, sinks, pages in the table
+    (1, 1, 1, 64, 16, [1], None, True, 0, 0, 1),
+    (1, 8, 1, 256, 64, [817], None, True, 0, 0, 13),
+    (1, 8, 1, 256, 64, [817], None, True, 0, 0, 600),                       # a table for far more
+    (1, 32, 8, 128, 64, [300, 1, 0, 129, 64, 65], None, True, 0, 0, 8),
+    (5, 8, 1, 64, 16, [3, 5, 17, 100], None, True, 0, 0, 8),                # shorter than its rows
+    (7, 4, 2, 64, 16, [333, 113, 223], None, True, 100, 3, 21),
+    (7, 4, 2, 128, 32, [333, 0, 7, 223], [7, 3, 0, 1], True, 0, 0, 11),     # ragged rows
+    (50, 8, 1, 256, 32, [866, 50, 31], None, False, 0, 0, 28),
+    (33, 6, 6, 128, 128, [200, 40], None, True, 1, 0, 2),                   # a window of a row itself
+    (33, 6, 3, 64, 16, [200, 40], [20, 33], True, 5, 40, 13),               # more sinks than window
+    (65, 3, 1, 128, 64, [65, 300], None, True, 64, 64, 5),
+    (2, 16, 1, 64, 32, [5000, 4999, 31], None, True, 1000, 4, 157),
+    (1, 5, 5, 128, 16, [2049, 700], None, True, 37, 1, 129),
+    (3, 40, 1, 128, 16, [75, 64], None, True, 0, 0, 5),                     # 40 heads: rows of a token in two tiles
+    (300, 2, 2, 64, 128, [300], [299], True, 0, 0, 3),
+    (1, 4, 4, 256, 128, [9000], None, True, 0, 0, 71),
+]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("code", CODES)
+@pytest.mark.parametrize("case", range(len(ATTN)))
+def test_attention(ops, case, code, dtype):
+    rows, heads, kv, dh, page, lens, q_lens, causal, window, sinks, width = ATTN[case]
+    counts = [-(-n // page) for n in lens]
+    n_pages = sum(counts) + 1
+    pool = filled(case, n_pages, kv, dh, page, code)
+    table = numbered(case, counts, width, n_pages)
+    # what lies behind a length may be anything: NaN codes of e4m3 among it
+    for s, n in enumerate(lens):
+        if n % page:
+            for i in (0, 1):
+                x = ref.natural(pool[i][table[s, n // page]], i == 0).copy()
+                x[:, n % page:] = 0x7f
+                pool[i][table[s, n // page]] = ref.in_pieces(x, i == 0)
+    q = rand(70 + case, len(lens), rows, heads, dh, dtype=dtype)
+    attend_both(ops, q, pool, code, page, table, lens, q_lens, causal, window, sinks)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_attention_spoilt_pages(ops, dtype):
+    """A page that holds NaN, and a number that names none, spoil the rows that see them, and no others."""
+    kv, dh, page, code = 2, 64, 16, "e4m3"
+    lens = [200, 200, 200, 100]
+    pool = filled(7, 60, kv, dh, page, code)
+    table = numbered(7, [13, 13, 13, 7], 13, 60)
+    pool[2][table[0, 3], 1] = np.nan  # K of the second KV head
+    pool[3][table[1, 12], 0] = np.nan  # V of the last slots
+    table[2, 0] = 60
+    table[3, 5] = -1
+    q = rand(80, 4, 120, 4, dh, dtype=dtype)
+    out, lse = attend_both(ops, q, pool, code, page, table, lens, causal=True, window=20, sinks=2)
+    assert torch.isnan(out[0, :, 2:]).any() and not torch.isnan(out[0, :, :2]).any() and not torch.isnan(lse[1]).any()
+    assert torch.isnan(out[2]).all()
+    attend_both(ops, q[:, :1], pool, code, page, table, lens)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_attention_spoilt_queries_and_sizes_of_values(ops, dtype):
+    """NaN and infinity of a query stay in its row; scales of pages far apart; scores that differ by hundreds."""
+    kv, dh, page, code = 1, 128, 32, "int8"
+    pool = filled(8, 12, kv, dh, page, code)
+    table = numbered(8, [6, 6], 6, 12)
+    for i, p in enumerate(table[0]):
+        pool[3][p] = 2.0 ** (6 * i - 40)
+    for i, p in enumerate(table[1]):
+        pool[2][p] *= 2.0 ** (i - 2)
+    q = rand(81, 2, 9, 4, dh, dtype=dtype)
+    q[1] *= 8
+    attend_both(ops, q, pool, code, page, table, [190, 192])
+    bad = q.clone()
+    bad[0, 3, 1, 7], bad[1, 4, 2, 100] = float("nan"), INF
+    args = (on_gpu(ops, pool, code), dev(table), i32([190, 192]))
+    good, got = ops.attention(dev(q), *args), ops.attention(dev(bad), *args)
+    for g, w in zip(got, good):
+        keep = torch.ones(2, 9, 4, dtype=torch.bool)
+        keep[0, 3, 1] = keep[1, 4, 2] = False
+        assert torch.equal(g.cpu()[keep], w.cpu()[keep]) and torch.isnan(g.cpu()[~keep]).any(-1).all()
+
+
+def test_attention_strides_shared_pages_and_a_single_slot(ops):
+    """q as a part of a projection, out as heads of another tensor, a table with a longer row; sequences that share pages; all
+    probability on one slot gives its value."""
+    kv, dh, page, code = 2, 128, 64, "e4m3"
+    pool = filled(9, 5, kv, dh, page, code)
+    table = np.array([[3, 1, 0], [3, 1, 2], [4, 4, 4]], np.int32)
+    qkv = rand(82, 3, 6, 10, dh, dtype=torch.bfloat16)
+    g, wide = dev(qkv), torch.zeros(3, 4, 6, 16, dh, dtype=torch.bfloat16, device="cuda")
+    lens = [150, 180, 130]
+    d = on_gpu(ops, pool, code)
+    t = torch.full((3, 9), -1, dtype=torch.int32, device="cuda")
+    t[:, :3] = dev(table)
+    out, lse = ops.attention(g[:, 1:5, :6], d, t[:, :3], i32(lens), out=wide[:, :, :, 3])
+    o, l, mag, err, _ = attn64(qkv[:, 1:5, :6], pool, code, page, table, lens, [4] * 3, True, 0, 0, dh ** -0.5)
+    tol_o, tol_l = attn_tolerance(torch.bfloat16, o, l, mag, err, 180, dh)
+    within(out, o, tol_o)
+    within(lse, l, tol_l)
+    assert (wide[:, :, :, :3] == 0).all() and (wide[:, :, :, 4:] == 0).all()
+    q = rand(83, 3, 1, 2, dh)
+    one, lse = ops.attention(dev(q), d, dev(table), i32([1, 1, 1]))
+    for s in range(3):
+        v = ref.slots(pool[1], pool[3], False, code, page, table[s], 1)[:, 0]
+        assert torch.equal(one[s, 0].cpu().double(), torch.from_numpy(v))
+
+
+# ---------------------------------------------------------------------------
+# moves of pages
+# ---------------------------------------------------------------------------
+def scattered(seed, lens, page, width, n_pages, shared=0.0):
+    """Tables of sequences over a shuffled pool, some of whose pages are held twice, and the counts."""
+    r = np.random.RandomState(seed)
+    counts = [-(-n // page) for n in lens]
+    table = numbered(seed, counts, width, n_pages)
+    for s, c in enumerate(counts):
+        table[s, c:] = -1
+        if s and shared and r.rand() < shared:
+            m = min(c, counts[s - 1])
+            table[s, :m] = table[s - 1, :m]
+    refs = np.zeros(n_pages, np.int32)
+    for s, c in enumerate(counts):
+        for e in table[s, :c]:
+            refs[e] += 1
+    return table, np.array(lens, np.int32), refs
+
+
+def layered(seed, layers, n_pages, kv, dh, page):
+    r = np.random.RandomState(seed)
+    k = r.randint(0, 256, (layers, n_pages, kv, dh // 16, page, 16)).astype(np.uint8)
+    v = r.randint(0, 256, (layers, n_pages, kv, page // 16, dh, 16)).astype(np.uint8)
+    return [k, v, r.rand(layers, n_pages, kv).astype(np.float32), r.rand(layers, n_pages, kv).astype(np.float32)]
+
+
+def moved(pool, moves):
+    pool = [x.copy() for x in pool]
+    for a, b in moves:
+        for x in pool:
+            x[:, b] = x[:, a]
+    return pool
+
+
+def equal(got, want, name):
+    assert np.array_equal(got.cpu().numpy(), want), (name, got.cpu().numpy(), want)
+
+
+RESIZE = [
+    # lengths, new lengths, page, entries of a row, pages, how many share
+    ([0], [1], 16, 1, 1, 0),
+    ([5, 16, 0, 33], [6, 17, 40, 0], 16, 4, 12, 0),
+    ([5, 16, 0, 33], [60, -1, 64, 100], 16, 4, 12, 0),             # more than a row holds; more than there are
+    ([70, 70, 71, 70], [71, 75, -5, 128], 64, 2, 12, 1.0),         # copies
+    ([70, 70, 71, 70], [71, 75, 150, 128], 64, 3, 9, 1.0),         # some are not served
+    ([100] * 20, [101 + 7 * i for i in range(20)], 32, 9, 90, 0.7),
+    ([i % 50 for i in range(1500)], [(i * 7) % 60 for i in range(1500)], 16, 4, 6200, 0.5),
+    ([40] * 1030, [41] * 1030, 32, 2100, 9000, 0.9),               # rows of several workgroups
+    ([64, 64], [10, 65], 32, 4, 4, 1.0),                           # pages that a shorter one leaves serve from the next call on
+]
+
+
+@pytest.mark.parametrize("in_place", [True, False])
+@pytest.mark.parametrize("case", range(len(RESIZE)))
+def test_resize(ops, case, in_place):
+    lens, new, page, width, n_pages, share = RESIZE[case]
+    table, lens, refs = scattered(case, lens, page, width, n_pages, share)
+    layers, kv, dh = 3, 1, 64
+    pool = layered(case, layers, n_pages, kv, dh, page) if n_pages < 5000 else None
+    want_t, want_l, want_r, want_short, copies = ref.resize(table, lens, refs, new, page)
+    t, l, r = dev(table), dev(lens), dev(refs)
+    outs = {} if in_place else dict(table_out=torch.full_like(t, 9), lens_out=torch.full_like(l, 9), refs_out=torch.full_like(r, 9))
+    d = ops.Pool(dev(pool[0]).view(torch.int8), dev(pool[1]).view(torch.int8), dev(pool[2]), dev(pool[3])) if pool else None
+    got_l, short = ops.resize(t, l, r, i32(new), d, page=page, **outs)
+    equal(outs.get("table_out", t), want_t, "table")
+    equal(got_l, want_l, "lens")
+    equal(outs.get("refs_out", r), want_r, "refs")
+    assert short.item() == want_short
+    if pool:
+        same_pool(d, moved(pool, copies))
+    if not in_place:
+        equal(t, table, "table")
+        equal(l, lens, "lens")
+        equal(r, refs, "refs")
+
+
+REORDER = [
+    # lengths, parents, page, entries of a row
+    ([5], [0], 16, 1),
+    ([5], [-1], 16, 1),
+    ([40, 3, 0, 64], [0, 0, 0, 0], 16, 4),          # forks
+    ([40, 3, 0, 64], [1, 2, 3, 0], 16, 4),          # a turn
+    ([40, 3, 0, 64], [0, -1, 7, 3], 16, 4),         # freed
+    ([7 * i % 90 for i in range(300)], [(i * i + 3) % 310 for i in range(300)], 32, 3),
+    ([3000, 2000, 2999], [2, 2, 0], 16, 2500),
+]
+
+
+@pytest.mark.parametrize("in_place", [True, False])
+@pytest.mark.parametrize("case", range(len(REORDER)))
+def test_reorder(ops, case, in_place):
+    lens, parents, page, width = REORDER[case]
+    table, lens, refs = scattered(case, lens, page, width, sum(-(-n // page) for n in lens) + 3, 0.5)
+    want_t, want_l, want_r = ref.reorder(table, lens, refs, parents, page)
+    t, l, r = dev(table), dev(lens), dev(refs)
+    outs = {} if in_place else dict(table_out=torch.full_like(t, 9), lens_out=torch.full_like(l, 9), refs_out=torch.full_like(r, 9))
+    got_l = ops.reorder(t, l, r, i32(parents), page, **outs)
+    equal(outs.get("table_out", t), want_t, "table")
+    equal(got_l, want_l, "lens")
+    equal(outs.get("refs_out", r), want_r, "refs")
+
+
+COMPACT = [
+    # lengths, page, entries of a row, free pages, how many share
+    ([1], 16, 1, 0, 0),
+    ([1], 16, 3, 5, 0),
+    ([0, 0], 16, 3, 5, 0),                        # nothing in use
+    ([100, 50, 0, 64, 33], 16, 7, 40, 0.5),
+    ([16 * 7] * 9, 16, 7, 1, 0),                  # one hole
+    ([64 * (i % 5) + 1 for i in range(200)], 64, 5, 4200, 0.3),
+    ([500] * 100, 32, 1100, 9000, 0),
+]
+
+
+@pytest.mark.parametrize("in_place", [True, False])
+@pytest.mark.parametrize("case", range(len(COMPACT)))
+def test_compact(ops, case, in_place):
+    lens, page, width, spare, share = COMPACT[case]
+    n_pages = sum(-(-n // page) for n in lens) + spare
+    table, lens, refs = scattered(case, lens, page, width, n_pages, share)
+    if n_pages > 20:
+        refs[np.flatnonzero(refs == 0)[:2]] = -1  # free is free
+    pool = layered(case, 2, n_pages, 2, 64, page) if n_pages < 6000 else None
+    want_t, want_r, n_live, moves = ref.compact(table, refs)
+    t, r = dev(table), dev(refs)
+    outs = {} if in_place else dict(table_out=torch.full_like(t, 9), refs_out=torch.full_like(r, 9))
+    d = ops.Pool(dev(pool[0]).view(torch.int8), dev(pool[1]).view(torch.int8), dev(pool[2]), dev(pool[3])) if pool else None
+    assert ops.compact(t, r, d, **outs).item() == n_live
+    equal(outs.get("table_out", t), want_t, "table")
+    equal(outs.get("refs_out", r), want_r, "refs")
+    if pool:
+        same_pool(d, moved(pool, moves))
+
+
+def test_moves_pass_by_numbers_that_name_no_page(ops):
+    table = np.array([[0, -3, 5, -1], [99, 1, 2, -1], [3, 1 << 30, -1, -1]], np.int32)
+    lens, refs, page = np.array([40, 48, 20], np.int32), np.array([1, 1, 1, 1, 0, 1, 0, 0], np.int32), 16
+    for new in ([50, 10, 0], [16, 49, 21], [0, 0, 0]):
+        t, l, r = dev(table), dev(lens), dev(refs)
+        want = ref.resize(table, lens, refs, new, page)
+        _, short = ops.resize(t, l, r, i32(new), page=page)
+        for got, w in zip((t, l, r), want):
+            equal(got, w, "resize")
+        assert short.item() == want[3]
+    t, l, r = dev(table), dev(lens), dev(refs)
+    ops.reorder(t, l, r, i32([1, 1, -1]), page)
+    for got, w in zip((t, l, r), ref.reorder(table, lens, refs, [1, 1, -1], page)):
+        equal(got, w, "reorder")
+    t, r = dev(table), dev(refs)
+    assert ops.compact(t, r).item() == 5
+    for got, w in zip((t, r), ref.compact(table, refs)):
+        equal(got, w, "compact")
+
+
+# ---------------------------------------------------------------------------
+# together
+# ---------------------------------------------------------------------------
+@pytest.mark.parametrize("code,dtype", [("e4m3", torch.bfloat16), ("int8", torch.float32)])
+def test_a_run_of_them_together(ops, code, dtype):
+    """A prefix is read, forked into candidates, each grows by tokens of its own, the lighter ones are dropped for copies of
+    the others, and the pool is moved together; after each step everything is as the plain forms have it."""
+    layers, kv, heads, dh, page, S, width, n_pages = 2, 1, 4, 64, 16, 4, 6, 24
+    pool = [np.zeros_like(x) for x in layered(0, layers, n_pages, kv, dh, page)]
+    d = ops.Pool(dev(pool[0]).view(CODES[code]), dev(pool[1]).view(CODES[code]), dev(pool[2]), dev(pool[3]))
+    table, lens, refs = np.full((S, width), -1, np.int32), np.zeros(S, np.int32), np.zeros(n_pages, np.int32)
+    t, l, r = dev(table), dev(lens), dev(refs)
+    qw, kw = 1 + 0.2 * rand(1, dh), 1 + 0.2 * rand(2, dh)
+    seed = 100
+
+    def step(n_new, window):
+        nonlocal table, lens, refs, pool, seed
+        tokens = max(n_new)
+        starts, want = lens.copy(), lens + np.array(n_new, np.int32)
+        before = l.clone()
+        got_l, short = ops.resize(t, l, r, l + i32(n_new), d)
+        table, lens, refs, lack, copies = ref.resize(table, lens, refs, want, page)
+        pool = moved(pool, copies)
+        assert lack == 0 and short.item() == 0
+        pos = torch.from_numpy(starts)[:, None] + torch.arange(tokens)
+        for layer in range(layers):
+            seed += 3
+            q, k, v = (rand(seed + i, S, tokens, heads if i == 0 else kv, dh, dtype=dtype) for i in range(3))
+            qo, ko = ops.norm_rope(dev(q), dev(k), dev(pos.int()), q_weight=dev(qw), k_weight=dev(kw))
+            norm_close(qo, q, qw, 0, 1e-6, pos, dh)
+            norm_close(ko, k, kw, 0, 1e-6, pos, dh)
+            ops.append(d.layer(layer), t, before, ko, dev(v), n_new=i32(n_new))
+            mine = [x[layer] for x in pool]
+            for i, x in ((0, ko), (1, v)):
+                ref.append_one(mine[i], mine[2 + i], i == 0, code, page, table, starts, x.cpu().float().numpy(), n_new)
+            same_pool(d.layer(layer), mine)
+            out, lse = ops.attention(qo, d.layer(layer), t, l, q_lens=i32(n_new), window=window, sinks=2 if window else 0)
+            o, ls, mag, err, there = attn64(qo.cpu(), mine, code, page, table, lens, n_new, True, window, 2 if window else 0, dh ** -0.5)
+            tol_o, tol_l = attn_tolerance(dtype, o, ls, mag, err, lens.max(), dh)
+            within(out.cpu()[torch.from_numpy(there)], o[there], tol_o[there])
+            within(lse.cpu()[torch.from_numpy(there)], ls[there], tol_l[there])
+
+    def reordered(parents):
+        nonlocal table, lens, refs
+        ops.reorder(t, l, r, i32(parents), page)
+        table, lens, refs = ref.reorder(table, lens, refs, parents, page)
+
+    step([37, 0, 0, 0], 0)
+    reordered([0, 0, 0, 0])
+    step([1, 1, 1, 1], 0)
+    step([3, 1, 12, 0], 10)
+    reordered([2, 1, 2, -1])
+    table, refs, n_live, moves = ref.compact(table, refs)
+    pool = moved(pool, moves)
+    assert ops.compact(t, r, d).item() == n_live
+    step([1, 1, 1, 20], 10)
+    step([1, 1, 1, 1], 0)
+    for got, want, name in ((t, table, "table"), (l, lens, "lens"), (r, refs, "refs")):
+        equal(got, want, name)
+    reordered([-1] * 4)
+    assert (r.cpu() == 0).all()
