@@ -154,10 +154,11 @@ jpi_status jpi_cache_attention_workspace(const jpi_cache_attn* a, const jpi_cach
 jpi_status jpi_cache_attention(const jpi_cache_attn* a, const jpi_cache_pool* pool, const jpi_cache_seqs* seqs, void* workspace,
                                size_t workspace_bytes, void* stream);
 
-/* How a call with these sizes is cut, for tests that want a certain cut: waves of
- * a workgroup that share its rows' keys, row tiles of a (sequence, KV head), and
- * ranges of its keys.  Errors as the workspace query. */
-jpi_status jpi_debug_cache_plan(const jpi_cache_attn* a, const jpi_cache_pool* pool, const jpi_cache_seqs* seqs, int* waves,
+/* How a call with these sizes is cut, for tests that want a certain cut, for each
+ * (sequence, KV head): workgroups of 128 rows that pass the keys through a ring in
+ * LDS, or (groups 0) tiles of 16 rows and ranges of their keys.  Errors as the
+ * workspace query. */
+jpi_status jpi_debug_cache_plan(const jpi_cache_attn* a, const jpi_cache_pool* pool, const jpi_cache_seqs* seqs, int* groups,
                                 int* tiles, int* ranges);
 
 /* ---- moves of pages ---------------------------------------------------------

@@ -163,14 +163,14 @@ jpi_status jpi_cache_attention_workspace(const jpi_cache_attn* a, const jpi_cach
   return st;
 }
 
-jpi_status jpi_debug_cache_plan(const jpi_cache_attn* a, const jpi_cache_pool* pool, const jpi_cache_seqs* seqs, int* waves,
+jpi_status jpi_debug_cache_plan(const jpi_cache_attn* a, const jpi_cache_pool* pool, const jpi_cache_seqs* seqs, int* groups,
                                 int* tiles, int* ranges) {
   const char* call = "jpi_debug_cache_plan";
-  if (!waves || !tiles || !ranges) return fail(JPI_ERR_ARG, "%s: NULL argument", call);
+  if (!groups || !tiles || !ranges) return fail(JPI_ERR_ARG, "%s: NULL argument", call);
   const jpi_status st = check_attention(call, a, pool, seqs);
   if (st != JPI_OK) return st;
   const CachePlan p = cache_plan(*a, *pool, *seqs);
-  *waves = p.waves, *tiles = p.tiles, *ranges = p.splits;
+  *groups = p.groups, *tiles = p.tiles, *ranges = p.splits;
   return JPI_OK;
 }
 

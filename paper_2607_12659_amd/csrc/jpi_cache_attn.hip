@@ -30,7 +30,7 @@ namespace {
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
-constexpr int WAVES = 4, TILE = 32;
+constexpr int WAVES = 4;
 constexpr float LOG2E = 1.44269504088896341f, LN2 = 0.693147180559945309f;
 constexpr float HEADROOM = 16.f;  // log2 of the most that a probability may exceed its row's reference by
 
@@ -48,29 +48,33 @@ struct CacheArgs {
   int n_pages, lg_page, cap;
   int causal, window, sinks;
   float qscale;  // scale / ln 2
-  int splits, row_tiles;
-  float* part;     // [workgroup][32 rows][head_dim]
-  float2* stats;   // [workgroup][32 rows]: reference, sum
+  int splits;
+  float* part;    // [workgroup][rows of a tile][head_dim]
+  float2* stats;  // [workgroup][rows of a tile]: reference, sum
 };
 
-// What a row tile sees, in tiles of its keys: the first `sink_tiles` and those from lo_tile to hi_tile
+// What some rows see, in tiles of keys: the first `sink_tiles` and those from lo_tile on, `count` in all; but for the first
+// `sinks` slots those from lo up to hi
 struct Span {
-  int len, nq, rows, i0, i1, pos0, sink_tiles, lo_tile, count;
+  int len, nq, rows, i0, i1, pos0, lo, hi, sink_tiles, lo_tile, count;
   __device__ __forceinline__ int tile(int n) const { return n < sink_tiles ? n : n - sink_tiles + lo_tile; }
 };
 
-__device__ __forceinline__ Span span_of(const CacheArgs& a, int s, int rt) {
+// of rows nth * ROWS and the next ROWS - 1 of a (sequence, KV head)
+template <int ROWS, int KEYS>
+__device__ __forceinline__ Span span_of(const CacheArgs& a, int s, int nth) {
   Span x;
   x.len = clamp_len(a.len[s], a.cap);
   x.nq = a.q_len ? clamp_len(a.q_len[s], a.q_rows) : a.q_rows;
   x.rows = x.nq * a.group;
-  x.i0 = rt * TILE / a.group;
-  x.i1 = min(x.nq - 1, (rt * TILE + TILE - 1) / a.group);
+  x.i0 = nth * ROWS / a.group;
+  x.i1 = min(x.nq - 1, (nth * ROWS + ROWS - 1) / a.group);
   x.pos0 = x.len - x.nq;
-  const int hi = a.causal ? min(max(x.pos0 + x.i1 + 1, 0), x.len) : x.len;
-  const int hi_tile = (hi + TILE - 1) / TILE;
-  x.lo_tile = a.window ? min((int)(max((int64_t)x.pos0 + x.i0 - a.window + 1, (int64_t)0) / TILE), hi_tile) : 0;
-  x.sink_tiles = a.window ? min((min(a.sinks, hi) + TILE - 1) / TILE, x.lo_tile) : 0;
+  x.hi = a.causal ? min(max(x.pos0 + x.i1 + 1, 0), x.len) : x.len;
+  x.lo = a.window ? (int)max((int64_t)x.pos0 + x.i0 - a.window + 1, (int64_t)0) : 0;
+  const int hi_tile = (x.hi + KEYS - 1) / KEYS;
+  x.lo_tile = min(x.lo / KEYS, hi_tile);
+  x.sink_tiles = a.window ? min((min(a.sinks, x.hi) + KEYS - 1) / KEYS, x.lo_tile) : 0;
   x.count = x.sink_tiles + hi_tile - x.lo_tile;
   return x;
 }
@@ -79,7 +83,36 @@ __device__ __forceinline__ Span span_of(const CacheArgs& a, int s, int rt) {
 __device__ __forceinline__ int per_range(int count, int splits) { return max((count + splits - 1) / splits, WAVES); }
 __device__ __forceinline__ int ranges_of(int count, int per) { return max(1, (count + per - 1) / per); }
 
-__device__ __forceinline__ f32x16 mfma(bf16x8 a, bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+// One matrix instruction of R rows (queries) and R keys or dims
+template <int R>
+struct Tile;
+template <>
+struct Tile<32> {
+  typedef f32x16 acc;
+  static __device__ __forceinline__ acc mfma(bf16x8 a, bf16x8 b, acc c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+  // the tile's key that row i of a product takes, and the dim of register 4 quad of O^T in lane group g
+  static __device__ __forceinline__ int key(int i, int) { return ((i >> 2) & 1) * 16 + (i >> 3) * 4 + (i & 3); }
+  static __device__ __forceinline__ int dim(int quad, int g) { return 8 * quad + 4 * g; }
+};
+template <>
+struct Tile<16> {
+  typedef f32x4 acc;
+  static __device__ __forceinline__ acc mfma(bf16x8 a, bf16x8 b, acc c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+  static __device__ __forceinline__ int key(int i, int set) { return (i >> 2) * 16 + set * 4 + (i & 3); }
+  static __device__ __forceinline__ int dim(int quad, int g) { return 16 * quad + 4 * g; }
+};
+
+// over the lane groups of a row
+template <int R>
+__device__ __forceinline__ float groups_max(float v) {
+  v = halves_max(v);
+  return R == 32 ? v : fmaxf(v, __shfl_xor(v, 16, 64));
+}
+template <int R>
+__device__ __forceinline__ float groups_sum(float v) {
+  v = halves_sum(v);
+  return R == 32 ? v : v + __shfl_xor(v, 16, 64);
+}
 
 // x in PARTS parts of bf16: the largest first
 template <int PARTS>
@@ -95,263 +128,494 @@ __device__ __forceinline__ void split8(const float* x, bf16x8 (&part)[PARTS]) {
   }
 }
 
-// The raw pieces of a tile and its scales
-template <int DH>
-struct Raw {
-  u32x4 k[DH / 32], v[DH / 32];
-  float ks, vs;
-};
+// bits 0 .. n - 1 of 16
+__device__ __forceinline__ u32 below(int n) { return (1u << min(max(n, 0), 16)) - 1; }
 
-template <int DH, bool E4M3, typename T>
-__global__ __launch_bounds__(64 * WAVES) void k_cache_attn(CacheArgs a) {
+// A wave's row tile: the lane's row, its queries, and the running maximum, sum and O^T of its softmax.  A step takes NT times
+// 16 keys of each lane group, one page and one scale each.
+template <int DH, bool E4M3, typename T, int R, int NT>
+struct Rows {
   typedef Code<E4M3> C;
-  constexpr int PARTS = sizeof(T) == 2 ? 1 : 3, STEPS = DH / 16, DT = DH / 32;
-  constexpr int ROUND = DT < 4 ? DT : 4;  // 32-dim tiles that are joined at once
-  __shared__ __align__(16) f32x4 join[WAVES][ROUND][4][64];
-  __shared__ float2 wave_stats[WAVES][TILE];
+  typedef Tile<R> M;
+  static constexpr int PARTS = sizeof(T) == 2 ? 1 : 3;
+  static constexpr int G = 64 / R, KEYS = 16 * G * NT;             // lane groups, keys of a step
+  static constexpr int SETS = KEYS / R, REGS = R * R / 64;         // products of a step's keys, their registers
+  static constexpr int KK = DH / (16 * G), DT = DH / R;            // pieces of a lane's keys and values
+  static constexpr int QUADS = DH * R / 256;                       // groups of four dims of a lane
 
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int half = lane >> 5, col = lane & 31;
-  const int pairs = a.n_seqs * a.kv;
-  const int pair = blockIdx.x % pairs, rest = blockIdx.x / pairs;
-  const int split = rest % a.splits, rt = rest / a.splits;
-  const int s = pair / a.kv, h = pair - s * a.kv;
-  const Span x = span_of(a, s, rt);
-  if (rt * TILE >= x.rows) return;
-  const int per = per_range(x.count, a.splits), ranges = ranges_of(x.count, per);
-  if (split >= ranges) return;
-  const int last = min(x.count, (split + 1) * per);
+  int grp, token, head, see_lo, see_hi, full_lo, full_hi, len, sinks;
+  float qscale, m_ref, sum;
+  bf16x8 q[PARTS][KK][2];
+  typename M::acc o[DT];
 
-  // the lane's row, and the slots that it sees
-  const int r = min(rt * TILE + col, x.rows - 1), token = r / a.group, head = h * a.group + (r - token * a.group);
-  const int see_hi = a.causal ? min(x.pos0 + token + 1, x.len) : x.len;
-  const int64_t see_lo = a.window ? (int64_t)x.pos0 + token - a.window + 1 : 0;
-  // tiles from slot full_lo up to slot full_hi are seen whole by all rows
-  const int full_hi = a.causal ? min(x.pos0 + x.i0 + 1, x.len) : x.len;
-  const int64_t full_lo = a.window ? (int64_t)x.pos0 + x.i1 - a.window + 1 : 0;
-
-  bf16x8 q[PARTS][STEPS];
-  {
-    const T* p = reinterpret_cast<const T*>(a.q) + s * a.q_outer + token * a.q_row + head * a.q_head + 16 * half;
+  __device__ __forceinline__ void begin(const CacheArgs& a, const Span& x, int s, int h, int rt) {
+    const int lane = threadIdx.x & 63, col = lane % R;
+    grp = lane / R;
+    const int r = min(rt * R + col, x.rows - 1);
+    token = r / a.group, head = h * a.group + (r - token * a.group);
+    len = x.len, sinks = a.sinks, qscale = a.qscale;
+    see_hi = a.causal ? min(x.pos0 + token + 1, x.len) : x.len;
+    see_lo = a.window ? (int)max((int64_t)x.pos0 + token - a.window + 1, (int64_t)0) : 0;
+    // tiles from slot full_lo up to slot full_hi are seen whole by all rows
+    full_hi = a.causal ? min(x.pos0 + x.i0 + 1, x.len) : x.len;
+    full_lo = a.window ? (int)max((int64_t)x.pos0 + x.i1 - a.window + 1, (int64_t)0) : 0;
+    const T* p = reinterpret_cast<const T*>(a.q) + s * a.q_outer + token * a.q_row + head * a.q_head + 16 * grp;
 #pragma unroll
-    for (int kk = 0; kk < STEPS; ++kk) {
-      const T* at = p + (kk >> 1) * 32 + (kk & 1) * 8;
-      if constexpr (PARTS == 1) {
-        q[0][kk] = *reinterpret_cast<const bf16x8*>(at);
-      } else {
-        float f[8];
-        const f32x4 lo = *reinterpret_cast<const f32x4*>(at), hi = *reinterpret_cast<const f32x4*>(at + 4);
+    for (int kk = 0; kk < KK; ++kk)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) f[e] = lo[e], f[4 + e] = hi[e];
-        bf16x8 part[PARTS];
-        split8<PARTS>(f, part);
+      for (int m = 0; m < 2; ++m) {
+        const T* at = p + kk * 16 * G + 8 * m;
+        if constexpr (PARTS == 1) {
+          q[0][kk][m] = *reinterpret_cast<const bf16x8*>(at);
+        } else {
+          float f[8];
+          const f32x4 lo = *reinterpret_cast<const f32x4*>(at), hi = *reinterpret_cast<const f32x4*>(at + 4);
 #pragma unroll
-        for (int i = 0; i < PARTS; ++i) q[i][kk] = part[i];
+          for (int e = 0; e < 4; ++e) f[e] = lo[e], f[4 + e] = hi[e];
+          bf16x8 part[PARTS];
+          split8<PARTS>(f, part);
+#pragma unroll
+          for (int i = 0; i < PARTS; ++i) q[i][kk][m] = part[i];
+        }
       }
-    }
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int e = 0; e < REGS; ++e) o[d][e] = 0.f;
+    m_ref = -INFINITY, sum = 0.f;
   }
 
-  const int page = 1 << a.lg_page;
-  const int64_t page_bytes = (int64_t)page * DH;
-  const int32_t* table = a.table + s * a.table_stride;
-  const int key = ((col >> 2) & 1) * 16 + (col >> 3) * 4 + (col & 3);  // the tile's key that the lane loads for K
-
-  // pages of the two 16-key halves of a tile; -1 past the length, where nothing is read
-  auto pages = [&](int t, int (&id)[2]) {
+  // One step's keys from slot0 on, with the scales of the lane's pieces; keys(j, kk) and values(t, d) are those, and
+  // `between` is called when the keys have been used.
+  template <typename KF, typename VF, typename B>
+  __device__ __forceinline__ void step(int slot0, const float (&ks)[NT], const float (&vs)[NT], KF keys, VF values, B between) {
+    float sc[16 * NT];
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      const int slot = t * TILE + 16 * e;
-      id[e] = slot < x.len ? table[slot >> a.lg_page] : -2;
+    for (int j = 0; j < SETS; ++j) {
+      typename M::acc c;
+#pragma unroll
+      for (int e = 0; e < REGS; ++e) c[e] = 0.f;
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) {
+        const u32x4 w = keys(j, kk);
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+          const bf16x8 codes = C::widen8(w[2 * m], w[2 * m + 1]);
+#pragma unroll
+          for (int i = PARTS - 1; i >= 0; --i) c = M::mfma(codes, q[i][kk][m], c);
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < REGS; ++e) sc[j * REGS + e] = c[e];
     }
-  };
-  auto load = [&](int t, const int (&id)[2], Raw<DH>& raw) {
-    const int kid = (col >> 2) & 1 ? id[1] : id[0], vid = half ? id[1] : id[0];
-    const bool vok = (unsigned)vid < (unsigned)a.n_pages;
-    const int64_t kat = (int64_t)((unsigned)kid < (unsigned)a.n_pages ? kid : 0) * a.kv + h;
-    const int64_t vat = (int64_t)(vok ? vid : 0) * a.kv + h;
-    const uint8_t* kp = a.k + kat * page_bytes + (((half << a.lg_page) + ((t * TILE + key) & (page - 1))) << 4);
-    const uint8_t* vp = a.v + vat * page_bytes + ((((t * TILE + 16 * half) & (page - 1)) * DH) + (col << 4));
+    between();
+    __builtin_amdgcn_s_setprio(1);  // the other wave's products fill the time of these instructions, not the other way round
+    // The scores' share of the softmax, in powers of two, and of O.  One path, with masks aside: with one path for tiles that
+    // are seen whole and one for others, or tiles left out, O was copied from register to register for each tile.
+    const bool whole = slot0 + KEYS <= full_hi && (slot0 >= full_lo || slot0 + KEYS <= sinks);
+    u32 seen[NT];
 #pragma unroll
-    for (int kk = 0; kk < DT; ++kk) raw.k[kk] = *reinterpret_cast<const u32x4*>(kp + ((int64_t)kk << (a.lg_page + 5)));
-#pragma unroll
-    for (int d = 0; d < DT; ++d) raw.v[d] = *reinterpret_cast<const u32x4*>(vp + d * 512);
-    // a number that names no page: its slots are NaN; past the length nothing is seen
-    raw.ks = vok ? a.k_scale[vat] : vid == -2 ? 0.f : __builtin_nanf("");
-    raw.vs = vok ? a.v_scale[vat] : vid == -2 ? 0.f : __builtin_nanf("");
-  };
-
-  f32x16 o[DT];
-#pragma unroll
-  for (int d = 0; d < DT; ++d)
-#pragma unroll
-    for (int e = 0; e < 16; ++e) o[d][e] = 0.f;
-  float m_ref = -INFINITY, sum = 0.f;
-
-  int n = split * per + wave;
-  Raw<DH> raw;
-  int id[2];
-  if (n < last) {
-    pages(x.tile(n), id);
-    load(x.tile(n), id, raw);
-    if (n + WAVES < last) pages(x.tile(n + WAVES), id);
-  }
-  for (; n < last; n += WAVES) {
-    const int t = x.tile(n);
-    const Raw<DH> cur = raw;
-    if (n + WAVES < last) {
-      load(x.tile(n + WAVES), id, raw);
-      if (n + 2 * WAVES < last) pages(x.tile(n + 2 * WAVES), id);
-    }
-
-    f32x16 sc;
-#pragma unroll
-    for (int e = 0; e < 16; ++e) sc[e] = 0.f;
-#pragma unroll
-    for (int kk = 0; kk < STEPS; ++kk) {
-      const u32x4 w = cur.k[kk >> 1];
-      const bf16x8 codes = kk & 1 ? C::widen8(w[2], w[3]) : C::widen8(w[0], w[1]);
-#pragma unroll
-      for (int p = PARTS - 1; p >= 0; --p) sc = mfma(codes, q[p][kk], sc);
-    }
-
-    const int slot0 = t * TILE;
-    const bool whole = slot0 + TILE <= full_hi && (slot0 >= full_lo || slot0 + TILE <= a.sinks);
-    const float f = a.qscale * cur.ks;
-    u32 seen = 0xffffu;
+    for (int t = 0; t < NT; ++t) seen[t] = 0xffffu;
     if (!whole) {
-      seen = 0;
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const int j = slot0 + 16 * half + e;
-        seen |= (j < see_hi && (j >= see_lo || j < a.sinks) ? 1u : 0u) << e;
+      for (int t = 0; t < NT; ++t) {
+        const int slot = slot0 + 16 * (G * t + grp);
+        seen[t] = below(see_hi - slot) & (~below(see_lo - slot) | below(sinks - slot));
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sc[16 * t + e] = seen[t] >> e & 1 ? sc[16 * t + e] : -INFINITY;
       }
     }
     float top = -INFINITY;
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      sc[e] *= f;
-      if (!whole) sc[e] = seen >> e & 1 ? sc[e] : -INFINITY;
-      top = fmaxf(top, sc[e]);
+    for (int t = 0; t < NT; ++t) {
+      const float* x = sc + 16 * t;
+      float t0 = fmaxf(fmaxf(x[0], x[1]), x[2]), t1 = fmaxf(fmaxf(x[3], x[4]), x[5]);
+      t0 = fmaxf(fmaxf(t0, x[6]), x[7]), t1 = fmaxf(fmaxf(t1, x[8]), x[9]);
+      t0 = fmaxf(fmaxf(t0, x[10]), x[11]), t1 = fmaxf(fmaxf(t1, x[12]), x[13]);
+      t0 = fmaxf(fmaxf(t0, t1), fmaxf(x[14], x[15])) * (qscale * ks[t]);
+      top = seen[t] == 0 ? top : fmaxf(top, t0);  // -inf * 0
     }
-    top = halves_max(top);
+    top = groups_max<R>(top);
     if (__any(top > m_ref + HEADROOM || (m_ref == -INFINITY && top > -INFINITY))) {
-      const float now = fmaxf(m_ref, top);
-      const float g = m_ref == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_ref - now);
-      if (now > -INFINITY) {
-        sum *= g;
+      // a whole number: sums are brought to another reference by a power of two, and differences with it are exact
+      const float now = fmaxf(m_ref, ceilf(top));
+      const float g = m_ref == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_ref - now);  // with -inf O and the sum are 0
+      sum *= g;
 #pragma unroll
-        for (int d = 0; d < DT; ++d)
+      for (int d = 0; d < DT; ++d)
 #pragma unroll
-          for (int e = 0; e < 16; ++e) o[d][e] *= g;
-        m_ref = now;
+        for (int e = 0; e < REGS; ++e) o[d][e] *= g;
+      m_ref = now;
+    }
+    // Probabilities times V's scale: with a power of two, all that append writes, that is a whole number in the exponent and a
+    // factor of the lane's sum; others, and those that could take a probability out of fp32, are multiplied with
+    bool power[NT], fast = true;
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      const u32 bits = __builtin_bit_cast(u32, vs[t]);
+      power[t] = (bits & 0x807fffffu) == 0 && (bits >> 23) - (127 - 64) <= 128;
+      fast = fast && (power[t] || seen[t] == 0);
+    }
+    fast = __all(fast);
+    float p[16 * NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      const u32 bits = __builtin_bit_cast(u32, vs[t]);
+      const bool in = fast && power[t];
+      const float f = qscale * ks[t], ref = (m_ref == -INFINITY ? 0.f : m_ref) - (in ? (float)((int)(bits >> 23) - 127) : 0.f);
+#pragma unroll
+      for (int e = 0; e < 16; ++e) p[16 * t + e] = __builtin_amdgcn_exp2f(fmaf(sc[16 * t + e], f, -ref));
+      if (!whole) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) p[16 * t + e] = seen[t] >> e & 1 ? p[16 * t + e] : 0.f;
       }
-    }
-    const float ref = m_ref == -INFINITY ? 0.f : m_ref;
-    float p[16];
+      float part[4];
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      p[e] = __builtin_amdgcn_exp2f(sc[e] - ref);
-      sum += p[e];
-      p[e] *= cur.vs;
-      if (!whole) p[e] = seen >> e & 1 ? p[e] : 0.f;  // 0 * NaN
+      for (int e = 0; e < 4; ++e) part[e] = (p[16 * t + e] + p[16 * t + 4 + e]) + (p[16 * t + 8 + e] + p[16 * t + 12 + e]);
+      sum = fmaf((part[0] + part[1]) + (part[2] + part[3]), in ? __builtin_bit_cast(float, (254u << 23) - bits) : 1.f, sum);
     }
-    bf16x8 pp[2][PARTS];
-    split8<PARTS>(p, pp[0]);
-    split8<PARTS>(p + 8, pp[1]);
-
-    // codes past the length may be anything
-    const int valid = x.len - slot0 - 16 * half;
+    if (!fast) {
 #pragma unroll
-    for (int d = 0; d < DT; ++d) {
-      u32x4 w = cur.v[d];
-      if (slot0 + TILE > x.len) {
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) p[16 * t + e] = seen[t] >> e & 1 ? p[16 * t + e] * vs[t] : 0.f;  // 0 * NaN
+    }
+    __builtin_amdgcn_s_setprio(0);
+    bf16x8 pp[NT][2][PARTS];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) split8<PARTS>(p + 16 * t, pp[t][0]), split8<PARTS>(p + 16 * t + 8, pp[t][1]);
+    u32x4 w[NT][DT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int d = 0; d < DT; ++d) w[t][d] = values(t, d);
+    if (!whole) {  // codes past the length may be anything
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        u32x4 valid;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const int bytes = min(max(valid - 4 * e, 0), 4);
-          w[e] &= bytes == 4 ? ~0u : (1u << (8 * bytes)) - 1;
+          const int bytes = min(max(len - slot0 - 16 * (G * t + grp) - 4 * e, 0), 4);
+          valid[e] = bytes == 4 ? ~0u : (1u << (8 * bytes)) - 1;
         }
+#pragma unroll
+        for (int d = 0; d < DT; ++d) w[t][d] &= valid;
       }
-      const bf16x8 c0 = C::widen8(w[0], w[1]), c1 = C::widen8(w[2], w[3]);
-#pragma unroll
-      for (int i = PARTS - 1; i >= 0; --i) o[d] = mfma(c0, pp[0][i], o[d]);
-#pragma unroll
-      for (int i = PARTS - 1; i >= 0; --i) o[d] = mfma(c1, pp[1][i], o[d]);
     }
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+          const bf16x8 codes = C::widen8(w[t][d][2 * m], w[t][d][2 * m + 1]);
+#pragma unroll
+          for (int i = PARTS - 1; i >= 0; --i) o[d] = M::mfma(codes, pp[t][m][i], o[d]);
+        }
   }
-  sum = halves_sum(sum);
+
+  __device__ __forceinline__ f32x4 quad(int i) const {
+    f32x4 y;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] = o[i * 4 / REGS][i * 4 % REGS + e];
+    return y;
+  }
+};
+
+__device__ __forceinline__ float lse_of(float ref, float total) {
+  return total == 0.f ? -INFINITY : (ref + __builtin_amdgcn_logf(total)) * LN2;
+}
+
+template <typename T>
+__device__ __forceinline__ void put4(T* out, f32x4 y) {
+  if constexpr (sizeof(T) == 2) {
+    typedef bf16 b4 __attribute__((ext_vector_type(4)));
+    *reinterpret_cast<b4*>(out) = b4{(bf16)y[0], (bf16)y[1], (bf16)y[2], (bf16)y[3]};
+  } else {
+    *reinterpret_cast<f32x4*>(out) = y;
+  }
+}
+
+constexpr int NO_PAGE = -2;  // of slots past the length
+// a number that names no page: its slots are NaN; past the length nothing is seen
+__device__ __forceinline__ float scale_at(const CacheArgs& a, const float* scale, int id, int h) {
+  return (u32)id < (u32)a.n_pages ? scale[(int64_t)id * a.kv + h] : id == NO_PAGE ? 0.f : __builtin_nanf("");
+}
+__device__ __forceinline__ int64_t page_of(const CacheArgs& a, int id, int h) {
+  return (int64_t)((u32)id < (u32)a.n_pages ? id : 0) * a.kv + h;
+}
+
+// Few rows: the waves of a workgroup share out the keys of one row tile, each from memory to its own registers.
+// Two waves of a SIMD leave 256 registers each: with three and 168 the loads of a tile (64 registers of 128 dims) spilled.
+template <int DH, bool E4M3, typename T, int R>
+__global__ __launch_bounds__(64 * WAVES, DH == 256 ? 1 : 2) void k_cache_attn(CacheArgs a) {
+  typedef Rows<DH, E4M3, T, R, 1> W;
+  typedef typename W::M M;
+  constexpr int KEYS = W::KEYS, QUADS = W::QUADS;
+  constexpr int ROUND = QUADS < 8 ? QUADS : 8;  // quads that are joined at once
+  __shared__ __align__(16) f32x4 join[WAVES][ROUND][64];
+  __shared__ float2 wave_stats[WAVES][R];
+
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int grp = lane / R, col = lane % R;
+  const int pairs = a.n_seqs * a.kv;
+  const int pair = blockIdx.x % pairs, rest = blockIdx.x / pairs;
+  const int split = rest % a.splits, rt = rest / a.splits;
+  const int s = pair / a.kv, h = pair - s * a.kv;
+  const Span x = span_of<R, 1024 / R>(a, s, rt);
+  if (rt * R >= x.rows) return;
+  const int per = per_range(x.count, a.splits), ranges = ranges_of(x.count, per);
+  if (split >= ranges) return;
+  const int first = split * per + wave, last = min(x.count, (split + 1) * per);
+
+  W w;
+  w.begin(a, x, s, h, rt);
+
+  const int mask = (1 << a.lg_page) - 1;
+  const u32 page_bytes = (u32)DH << a.lg_page;
+  const int32_t* table = a.table + s * a.table_stride;
+  const int key0 = M::key(col, 0), kpiece = key0 & ~15;  // the keys of all sets lie in one piece
+  auto page_at = [&](int slot) { return slot < x.len ? table[slot >> a.lg_page] : NO_PAGE; };
+  u32x4 kraw[W::SETS][W::KK], vraw[W::DT];
+  auto load_k = [&](int t, int id) {
+    const uint8_t* p = a.k + page_of(a, id, h) * page_bytes + (((grp << a.lg_page) + ((t * KEYS + key0) & mask)) << 4);
+#pragma unroll
+    for (int kk = 0; kk < W::KK; ++kk)
+#pragma unroll
+      for (int j = 0; j < W::SETS; ++j) kraw[j][kk] = *reinterpret_cast<const u32x4*>(p + ((u32)(kk * W::G) << (a.lg_page + 4)) + j * 64);
+  };
+  auto load_v = [&](int t, int id) {
+    const uint8_t* p = a.v + page_of(a, id, h) * page_bytes + (u32)(((t * KEYS + 16 * grp) & mask) * DH + (col << 4));
+#pragma unroll
+    for (int d = 0; d < W::DT; ++d) vraw[d] = *reinterpret_cast<const u32x4*>(p + d * R * 16);
+  };
+
+  // pages of the lane's K and V pieces of the next tile, and the present one's scales
+  int kid = NO_PAGE, vid = NO_PAGE;
+  float ks[1] = {0.f}, vs[1] = {0.f};
+  if (first < last) {
+    const int t = x.tile(first);
+    const int k0 = page_at(t * KEYS + kpiece), v0 = page_at(t * KEYS + 16 * grp);
+    if (first + WAVES < last) {
+      const int t1 = x.tile(first + WAVES);
+      kid = page_at(t1 * KEYS + kpiece), vid = page_at(t1 * KEYS + 16 * grp);
+    }
+    ks[0] = scale_at(a, a.k_scale, v0, h), vs[0] = scale_at(a, a.v_scale, v0, h);
+    load_k(t, k0);
+    load_v(t, v0);
+  }
+  for (int n = first; n < last; n += WAVES) {
+    const int t = x.tile(n), next = x.tile(min(n + WAVES, last - 1));
+    const bool more = n + WAVES < last;
+    const int kid1 = kid, vid1 = vid;
+    // asked for before the next tile's loads, so that waiting for them does not wait for those
+    if (n + 2 * WAVES < last) {
+      const int t2 = x.tile(n + 2 * WAVES);
+      kid = page_at(t2 * KEYS + kpiece), vid = page_at(t2 * KEYS + 16 * grp);
+    }
+    float ks1 = 0.f, vs1 = 0.f;
+    w.step(
+        t * KEYS, ks, vs, [&](int j, int kk) { return kraw[j][kk]; }, [&](int, int d) { return vraw[d]; },
+        [&] {
+          if (!more) return;
+          ks1 = scale_at(a, a.k_scale, vid1, h), vs1 = scale_at(a, a.v_scale, vid1, h);
+          load_k(next, kid1);
+        });
+    if (more) load_v(next, vid1);
+    ks[0] = ks1, vs[0] = vs1;
+  }
 
   // the four waves' sums, brought to one reference and added in their order
-  if (half == 0) wave_stats[wave][col] = float2{m_ref, sum};
+  const float sum = groups_sum<R>(w.sum);
+  if (grp == 0) wave_stats[wave][col] = float2{w.m_ref, sum};
   __syncthreads();
   float ref = -INFINITY, total = 0.f;
 #pragma unroll
-  for (int w = 0; w < WAVES; ++w) ref = fmaxf(ref, wave_stats[w][col].x);
+  for (int i = 0; i < WAVES; ++i) ref = fmaxf(ref, wave_stats[i][col].x);
 #pragma unroll
-  for (int w = 0; w < WAVES; ++w) {
-    const float2 st = wave_stats[w][col];
+  for (int i = 0; i < WAVES; ++i) {
+    const float2 st = wave_stats[i][col];
     total += (st.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(st.x - ref)) * st.y;
   }
-  const float mine = m_ref == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_ref - ref);
-  const bool here = rt * TILE + col < x.rows, final = ranges == 1;
+  const float mine = w.m_ref == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(w.m_ref - ref);
+  const bool here = rt * R + col < x.rows, final = ranges == 1;
   const float norm = !final ? 1.f : total == 0.f ? 0.f : 1.f / total;
-  float* part = a.part + ((int64_t)blockIdx.x * TILE + col) * DH;
-  T* out = reinterpret_cast<T*>(a.out) + s * a.o_outer + token * a.o_row + head * a.o_head;
-  if (wave == 0 && half == 0 && here) {
-    if (!final) a.stats[(int64_t)blockIdx.x * TILE + col] = float2{ref, total};
-    else if (a.lse) a.lse[((int64_t)s * a.q_rows + token) * a.n_heads + head] = total == 0.f ? -INFINITY : (ref + __builtin_amdgcn_logf(total)) * LN2;
+  float* part = a.part + ((int64_t)blockIdx.x * R + col) * DH;
+  T* out = reinterpret_cast<T*>(a.out) + s * a.o_outer + w.token * a.o_row + w.head * a.o_head;
+  if (wave == 0 && grp == 0 && here) {
+    if (!final) a.stats[(int64_t)blockIdx.x * R + col] = float2{ref, total};
+    else if (a.lse) a.lse[((int64_t)s * a.q_rows + w.token) * a.n_heads + w.head] = lse_of(ref, total);
   }
 #pragma unroll
-  for (int d0 = 0; d0 < DT; d0 += ROUND) {
-    if (d0) __syncthreads();
+  for (int q0 = 0; q0 < QUADS; q0 += ROUND) {
+    if (q0) __syncthreads();
 #pragma unroll
-    for (int d = 0; d < ROUND; ++d)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        f32x4 y;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) y[e] = o[d0 + d][4 * j + e] * mine;
-        join[wave][d][j][lane] = y;
-      }
+    for (int i = 0; i < ROUND; ++i) join[wave][i][lane] = w.quad(q0 + i) * mine;
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < ROUND; ++i) {  // ROUND * 4 pieces over the four waves
-      const int piece = i * WAVES + wave, d = piece >> 2, j = piece & 3;
-      f32x4 y = join[0][d][j][lane];
+    for (int i = 0; i < ROUND; i += WAVES) {
+      f32x4 y = join[0][i + wave][lane];
 #pragma unroll
-      for (int w = 1; w < WAVES; ++w) y += join[w][d][j][lane];
+      for (int v = 1; v < WAVES; ++v) y += join[v][i + wave][lane];
       if (!here) continue;
-      const int at = (d0 + d) * 32 + 8 * j + 4 * half;
+      const int at = M::dim(q0 + i + wave, grp);
       y *= norm;
-      if (!final) {
-        *reinterpret_cast<f32x4*>(part + at) = y;
-      } else if constexpr (sizeof(T) == 2) {
-        typedef bf16 b4 __attribute__((ext_vector_type(4)));
-        *reinterpret_cast<b4*>(out + at) = b4{(bf16)y[0], (bf16)y[1], (bf16)y[2], (bf16)y[3]};
-      } else {
-        *reinterpret_cast<f32x4*>(out + at) = y;
-      }
+      if (!final) put4(part + at, y);
+      else put4(out + at, y);
     }
   }
 }
 
+// Many rows: each wave has a row tile of its own, and the workgroup's keys pass through a ring in LDS that direct-to-LDS
+// loads fill several steps of 64 keys ahead.
+template <int DH>
+struct Ring {
+  static constexpr int KEYS = 64, PIECES = DH / 8;  // KB of a step: K of 32 keys, of the next 32, then V so, in the order of a lane's reads
+  static constexpr int LOADS = PIECES / WAVES;      // of a wave for a step
+  static constexpr int STAGES = DH == 64 ? 4 : 3;
+};
+
+// 16 bytes of each lane to LDS at `to` + 16 * lane.  As assembly, which has no register outputs: loads to LDS that the
+// compiler knows of are waited for before any read of LDS.
+__device__ __forceinline__ void load_to_lds(const void* p, u32 to) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(p)
+               : "memory", "m0");
+}
+// the same from a base that all lanes share
+__device__ __forceinline__ void load_to_lds(const void* base, u32 offset, u32 to) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(offset), "s"(base)
+               : "memory", "m0");
+}
+
+// What a ring's steps are made of, in LDS: for each 16 keys of the next ones the page's place in the pool and its scales
+struct Piece16 {
+  u32 at;  // page * KV heads + head
+  float ks, vs;
+};
+constexpr int AHEAD = 16;  // steps of a block of these; two blocks are held
+
+template <int DH, bool E4M3>
+__global__ __launch_bounds__(64 * WAVES, DH == 256 ? 1 : 2) void k_cache_rows(CacheArgs a) {
+  typedef bf16 T;
+  typedef Rows<DH, E4M3, T, 32, 2> W;
+  typedef Ring<DH> RG;
+  constexpr int R = 32, KEYS = RG::KEYS, STAGE = RG::PIECES * 1024, HALF = RG::LOADS / 2;
+  static_assert(RG::PIECES == 2 * (W::KK + W::DT) && RG::LOADS % 2 == 0, "ring shape");
+  __shared__ __align__(1024) char ring[RG::STAGES * STAGE];
+  __shared__ Piece16 pieces[2][AHEAD][4];
+
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int grp = lane / R, col = lane % R;
+  const int pairs = a.n_seqs * a.kv;
+  const int pair = blockIdx.x % pairs, s = pair / a.kv, h = pair - s * a.kv;
+  // the last rows of causal ones see most: they come first
+  const int group = gridDim.x / pairs - 1 - blockIdx.x / pairs, rt = group * WAVES + wave;
+  const Span all = span_of<R * WAVES, KEYS>(a, s, group);
+  if (group * WAVES * R >= all.rows) return;
+  // a wave without rows computes others' again; steps left out would have O copied from register to register in each
+  const int own = min(rt, (all.rows - 1) / R);
+  const Span x = span_of<R, KEYS>(a, s, own);
+  W w;
+  w.begin(a, x, s, h, own);
+
+  const int32_t* table = a.table + s * a.table_stride;
+  auto look_up = [&](int block) {  // by one wave: the pieces of a block of steps
+    const int n = block * AHEAD + (lane >> 2);
+    if (n >= all.count) return;
+    const int slot = all.tile(n) * KEYS + 16 * (lane & 3);
+    const int id = slot < all.len ? table[slot >> a.lg_page] : NO_PAGE;
+    pieces[block & 1][lane >> 2][lane & 3] = Piece16{(u32)page_of(a, id, h), scale_at(a, a.k_scale, id, h), scale_at(a, a.v_scale, id, h)};
+  };
+  if (wave == 0) look_up(0);
+  if (wave == 1) look_up(1);
+  __syncthreads();
+  wait_vm<0>();  // the queries are there too: waited for in the loop, they would have it wait for the ring's loads
+
+  const int mask = (1 << a.lg_page) - 1;
+  const u32 page_bytes = (u32)DH << a.lg_page;
+  const int key0 = W::M::key(col, 0);
+  const u32 lds = (u32)(uintptr_t)(__attribute__((address_space(3))) char*)ring + wave * 1024;
+  // Load i of a wave is piece wave + 4 i of a step: of K, 32 keys after the other in units of 32 dims, then of V
+  u32 tile[RG::LOADS], unit[RG::LOADS];
+#pragma unroll
+  for (int i = 0; i < RG::LOADS; ++i) {
+    const int piece = wave + WAVES * (i % HALF);
+    tile[i] = piece / W::KK, unit[i] = piece % W::KK;  // as many units of K as of V
+  }
+  const bool one_page = a.lg_page >= 6;
+  auto issue = [&](int n, int stage) {
+    const int t0 = all.tile(n) * KEYS;
+    const Piece16* at = pieces[n / AHEAD & 1][n % AHEAD];
+    const u32 to = lds + stage * STAGE;
+    if (one_page) {  // of all 64 keys: its place is the same for all lanes
+      const uint64_t base = (uint64_t)(u32)__builtin_amdgcn_readfirstlane((int)at[0].at) * page_bytes;
+      const uint8_t *kp = a.k + base + (u32)(t0 & mask) * 16, *vp = a.v + base + (u32)(t0 & mask) * DH;
+#pragma unroll
+      for (int i = 0; i < RG::LOADS; ++i) {
+        if (i < HALF) load_to_lds(kp + ((unit[i] << (a.lg_page + 5)) + tile[i] * 512), (((u32)grp << a.lg_page) + key0) * 16, to + i * WAVES * 1024);
+        else load_to_lds(vp + (tile[i] * 32 * DH + unit[i] * 512), grp * 16 * DH + col * 16, to + i * WAVES * 1024);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < RG::LOADS; ++i) {
+        const int slot = t0 + tile[i] * 32 + (i < HALF ? key0 : 16 * grp);
+        const uint64_t base = (uint64_t)at[2 * tile[i] + (i < HALF ? key0 >> 4 : grp)].at * page_bytes;
+        const u32 in = i < HALF ? (((2 * unit[i] + grp) << a.lg_page) + (slot & mask)) * 16 : (slot & mask) * DH + unit[i] * 512 + col * 16;
+        load_to_lds((i < HALF ? a.k : a.v) + base + in, to + i * WAVES * 1024);
+      }
+    }
+  };
+
+  const int count = all.count;
+#pragma unroll
+  for (int n = 0; n < RG::STAGES - 1; ++n)
+    if (n < count) issue(n, n);
+  int stage = 0;
+  for (int n = 0; n < count; ++n) {
+    wait_later<RG::LOADS, RG::STAGES - 2>(min(RG::STAGES - 2, count - 1 - n));
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();  // the step's keys are there, and everybody is done with those before
+    asm volatile("" ::: "memory");
+    if (n % AHEAD == 0 && n > 0 && wave == 0) {  // the block before is done with; seen at the next barrier, used after it
+      look_up(n / AHEAD + 1);
+      __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt 0
+    }
+    if (n + RG::STAGES - 1 < count) issue(n + RG::STAGES - 1, stage == 0 ? RG::STAGES - 1 : stage - 1);
+    const Piece16 *mine = pieces[n / AHEAD & 1][n % AHEAD], p0 = mine[grp], p1 = mine[2 + grp];
+    const float ks[2] = {p0.ks, p1.ks}, vs[2] = {p0.vs, p1.vs};
+    const char* at = ring + stage * STAGE + lane * 16;
+    w.step(
+        all.tile(n) * KEYS, ks, vs, [&](int j, int kk) { return *reinterpret_cast<const u32x4*>(at + (j * W::KK + kk) * 1024); },
+        [&](int t, int d) { return *reinterpret_cast<const u32x4*>(at + (2 * W::KK + t * W::DT + d) * 1024); }, [] {});
+    stage = stage == RG::STAGES - 1 ? 0 : stage + 1;
+  }
+
+  const float total = groups_sum<R>(w.sum), norm = total == 0.f ? 0.f : 1.f / total;
+  if (rt * R + col >= x.rows) return;
+  T* out = reinterpret_cast<T*>(a.out) + s * a.o_outer + w.token * a.o_row + w.head * a.o_head;
+  if (grp == 0 && a.lse) a.lse[((int64_t)s * a.q_rows + w.token) * a.n_heads + w.head] = lse_of(w.m_ref, total);
+#pragma unroll
+  for (int i = 0; i < W::QUADS; ++i) put4(out + W::M::dim(i, grp), w.quad(i) * norm);
+}
+
 // One row of a row tile whose keys were cut into ranges: a workgroup adds up the ranges that have any.  Lanes take four dims
 // each, groups of DH / 4 of them one range after the other, and the groups' sums are added in their order.
-template <int DH, typename T>
+template <int DH, typename T, int R>
 __global__ __launch_bounds__(256) void k_cache_join(CacheArgs a) {
   constexpr int LANES = DH / 4, GROUPS = 256 / LANES;
   __shared__ __align__(16) f32x4 sums[GROUPS][LANES];
-  const int pairs = a.n_seqs * a.kv, per_tile = min(TILE, a.q_rows * a.group);
+  const int pairs = a.n_seqs * a.kv, per_tile = min(R, a.q_rows * a.group);
   const int pair = blockIdx.x % pairs, rest = blockIdx.x / pairs;
   const int col = rest % per_tile, rt = rest / per_tile;
   const int s = pair / a.kv, h = pair - s * a.kv;
-  const Span x = span_of(a, s, rt);
-  const int r = rt * TILE + col;
+  const Span x = span_of<R, 1024 / R>(a, s, rt);
+  const int r = rt * R + col;
   if (r >= x.rows) return;
   const int ranges = ranges_of(x.count, per_range(x.count, a.splits));
   if (ranges == 1) return;
   const int token = r / a.group, head = h * a.group + (r - token * a.group);
   // range i of the row tile is workgroup (rt * splits + i) * pairs + pair
-  const int64_t at = ((int64_t)rt * a.splits * pairs + pair) * TILE + col, step = (int64_t)pairs * TILE;
+  const int64_t at = ((int64_t)rt * a.splits * pairs + pair) * R + col, step = (int64_t)pairs * R;
 
   float ref = -INFINITY, total = 0.f;
   for (int i = threadIdx.x & 63; i < ranges; i += 64) ref = fmaxf(ref, a.stats[at + i * step].x);
@@ -388,48 +652,64 @@ __global__ __launch_bounds__(256) void k_cache_join(CacheArgs a) {
 }
 
 template <int DH, bool E4M3, typename T>
-void launch_typed(const CacheArgs& a, unsigned grid, unsigned rows, hipStream_t s) {
-  k_cache_attn<DH, E4M3, T><<<grid, 64 * WAVES, 0, s>>>(a);
-  if (a.splits > 1) k_cache_join<DH, T><<<rows, 256, 0, s>>>(a);
-}
-
-template <int DH, bool E4M3>
-void launch_code(const CacheArgs& a, bool f32, unsigned grid, unsigned rows, hipStream_t s) {
-  if (f32) launch_typed<DH, E4M3, float>(a, grid, rows, s);
-  else launch_typed<DH, E4M3, bf16>(a, grid, rows, s);
+void launch_typed(const CacheArgs& a, const CachePlan& plan, int pairs, hipStream_t s) {
+  if constexpr (sizeof(T) == 2) {
+    if (plan.groups) {
+      k_cache_rows<DH, E4M3><<<(unsigned)(pairs * plan.groups), 64 * WAVES, 0, s>>>(a);
+      return;
+    }
+  }
+  k_cache_attn<DH, E4M3, T, 16><<<(unsigned)(pairs * plan.tiles * plan.splits), 64 * WAVES, 0, s>>>(a);
+  if (plan.splits > 1)
+    k_cache_join<DH, T, 16><<<(unsigned)(pairs * plan.tiles * std::min(16, a.q_rows * a.group)), 256, 0, s>>>(a);
 }
 
 template <int DH>
-void launch_dim(const CacheArgs& a, int code, bool f32, unsigned grid, unsigned rows, hipStream_t s) {
-  if (code == JPI_E4M3) launch_code<DH, true>(a, f32, grid, rows, s);
-  else launch_code<DH, false>(a, f32, grid, rows, s);
+void launch_dim(const CacheArgs& a, int code, bool f32, const CachePlan& plan, int pairs, hipStream_t s) {
+  if (code == JPI_E4M3) {
+    if (f32) launch_typed<DH, true, float>(a, plan, pairs, s);
+    else launch_typed<DH, true, bf16>(a, plan, pairs, s);
+  } else {
+    if (f32) launch_typed<DH, false, float>(a, plan, pairs, s);
+    else launch_typed<DH, false, bf16>(a, plan, pairs, s);
+  }
 }
 
-int64_t workgroups(const CachePlan& plan, const jpi_cache_pool& p, const jpi_cache_seqs& q) {
-  return (int64_t)q.n_seqs * p.n_kv_heads * plan.tiles * plan.splits;
-}
+constexpr int GROUP_ROWS = 32 * WAVES;  // of a workgroup of the ring
 
 }  // namespace
 
 CachePlan cache_plan(const jpi_cache_attn& a, const jpi_cache_pool& p, const jpi_cache_seqs& q) {
   const int group = a.n_heads / p.n_kv_heads;
-  const int64_t tiles = ((int64_t)a.q_rows * group + TILE - 1) / TILE, units = (int64_t)q.n_seqs * p.n_kv_heads * tiles;
-  int64_t most = (int64_t)q.max_pages * p.page;
-  if (a.window) most = std::min<int64_t>(most, (int64_t)a.window + a.sinks + TILE / group + 2 * TILE);
-  const int64_t key_tiles = (most + TILE - 1) / TILE;
-  const int64_t splits = std::min<int64_t>({256, 512 / units, key_tiles / WAVES});
-  return {WAVES, (int)tiles, (int)std::max<int64_t>(1, splits)};
+  const int64_t all = (int64_t)a.q_rows * group, pairs = (int64_t)q.n_seqs * p.n_kv_heads;
+  int64_t keys = (int64_t)q.max_pages * p.page;
+  if (a.window) keys = std::min<int64_t>(keys, (int64_t)a.window + a.sinks + GROUP_ROWS / group + 2 * 64);
+  CachePlan plan{};
+  // The ring from a workgroup for each compute unit on (of 256 dims, which the other kernel holds in two rounds of registers,
+  // from less than half of that); fp32 has three times the products and none of its time in what the ring saves.  us, ring
+  // and other: 1024 rows of 32 heads on 8 of 128, 256 workgroups, 32 and 32; 2048 rows 60 and 90; 512 rows 19 and 14; 64, 32
+  // and 16 chunks of 50 rows, 8 heads of 256, 866 slots: 48, 47 and 46, 99, 56 and 28.
+  const int64_t groups = (all + GROUP_ROWS - 1) / GROUP_ROWS;
+  if (a.dtype == JPI_BF16 && all >= 64 && groups * pairs >= (p.head_dim == 256 ? 112 : 256)) {
+    plan.groups = (int)groups;
+    plan.splits = 1;
+    return plan;
+  }
+  plan.tiles = (int)((all + 15) / 16);
+  plan.splits = (int)std::max<int64_t>(1, std::min<int64_t>({256, 256 / (pairs * plan.tiles), (keys + 63) / 64 / WAVES}));
+  return plan;
 }
 
 bool cache_attention_fits(const jpi_cache_attn& a, const jpi_cache_pool& p, const jpi_cache_seqs& q) {
   const CachePlan plan = cache_plan(a, p, q);
-  return workgroups(plan, p, q) < 1 << 24 && (plan.splits == 1 || (int64_t)q.n_seqs * a.n_heads * a.q_rows < 1 << 24);
+  const int64_t pairs = (int64_t)q.n_seqs * p.n_kv_heads, most = 1 << 24;  // 2^32 threads
+  return pairs * plan.groups < most && pairs * plan.tiles * plan.splits < most && (plan.splits == 1 || pairs * plan.tiles * 16 < most);
 }
 
 size_t cache_attention_bytes(const jpi_cache_attn& a, const jpi_cache_pool& p, const jpi_cache_seqs& q) {
   const CachePlan plan = cache_plan(a, p, q);
   if (plan.splits == 1) return 0;
-  return (size_t)workgroups(plan, p, q) * TILE * (p.head_dim * sizeof(float) + sizeof(float2));
+  return (size_t)q.n_seqs * p.n_kv_heads * plan.tiles * plan.splits * 16 * (p.head_dim * sizeof(float) + sizeof(float2));
 }
 
 hipError_t launch_cache_attention(const jpi_cache_attn& c, const jpi_cache_pool& p, const jpi_cache_seqs& q, void* ws,
@@ -445,16 +725,15 @@ hipError_t launch_cache_attention(const jpi_cache_attn& c, const jpi_cache_pool&
   a.n_pages = p.n_pages, a.lg_page = __builtin_ctz(p.page), a.cap = q.max_pages * p.page;
   a.causal = c.causal != 0, a.window = c.window, a.sinks = c.sinks;
   a.qscale = c.scale * LOG2E;
-  a.splits = plan.splits, a.row_tiles = plan.tiles;
-  const int64_t wgs = workgroups(plan, p, q);
+  a.splits = plan.splits;
+  const int pairs = q.n_seqs * p.n_kv_heads;
   a.part = (float*)ws;
-  a.stats = (float2*)((char*)ws + (size_t)wgs * TILE * p.head_dim * sizeof(float));
-  const unsigned rows = (unsigned)((int64_t)q.n_seqs * p.n_kv_heads * plan.tiles * std::min(TILE, a.q_rows * a.group));
+  a.stats = (float2*)((char*)ws + (size_t)pairs * plan.tiles * plan.splits * 16 * p.head_dim * sizeof(float));
   const bool f32 = c.dtype == JPI_F32;
   switch (p.head_dim) {
-    case 64: launch_dim<64>(a, p.code, f32, (unsigned)wgs, rows, s); break;
-    case 128: launch_dim<128>(a, p.code, f32, (unsigned)wgs, rows, s); break;
-    default: launch_dim<256>(a, p.code, f32, (unsigned)wgs, rows, s);
+    case 64: launch_dim<64>(a, p.code, f32, plan, pairs, s); break;
+    case 128: launch_dim<128>(a, p.code, f32, plan, pairs, s); break;
+    default: launch_dim<256>(a, p.code, f32, plan, pairs, s);
   }
   return hipGetLastError();
 }

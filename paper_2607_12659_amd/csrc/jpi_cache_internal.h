@@ -17,9 +17,10 @@ bool append_fits(const jpi_cache_pool& p, const jpi_cache_seqs& q, int tokens);
 hipError_t launch_append(const jpi_cache_pool& p, const jpi_cache_seqs& q, jpi_dtype dt, int tokens, const jpi_view& k,
                          const jpi_view& v, const int32_t* n_new, hipStream_t s);
 
-// how a call is cut: waves that share a row tile's keys, row tiles of a (sequence, KV head), ranges of its keys
+// how a call is cut, for each (sequence, KV head): into workgroups of 128 rows that pass the keys through a ring, or (groups 0)
+// into tiles of 16 rows and ranges of their keys
 struct CachePlan {
-  int waves, tiles, splits;
+  int groups, tiles, splits;
 };
 CachePlan cache_plan(const jpi_cache_attn& a, const jpi_cache_pool& p, const jpi_cache_seqs& q);
 bool cache_attention_fits(const jpi_cache_attn& a, const jpi_cache_pool& p, const jpi_cache_seqs& q);

@@ -544,7 +544,7 @@ def jpi_cache_attention(args: jpi_cache_attn, pool: jpi_cache_pool, seqs: jpi_ca
 
 
 def jpi_debug_cache_plan(args: jpi_cache_attn, pool: jpi_cache_pool, seqs: jpi_cache_seqs):
-    """(status, waves, tiles, ranges)"""
+    """(status, groups, tiles, ranges)"""
     v = [ctypes.c_int() for _ in range(3)]
     st = _lib.jpi_debug_cache_plan(_ref(args), _ref(pool), _ref(seqs), *(ctypes.byref(x) for x in v))
     return (st, *(x.value for x in v))

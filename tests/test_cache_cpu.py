@@ -125,12 +125,13 @@ def test_attention_refuses_sequences(bad):
 def test_attention_refuses_types_sizes_and_workspaces():
     assert attend(attn(dtype=2)) == j.JPI_ERR_DTYPE and attend(p=pool(code=2)) == j.JPI_ERR_DTYPE
     assert attend(attn(q_rows=1 << 28)) == j.JPI_ERR_SHAPE
-    assert attend(attn(q_rows=1 << 22, n_heads=2), pool(), seqs(n_seqs=128)) == j.JPI_ERR_SHAPE  # a workgroup for each 32 rows
+    assert attend(attn(dtype=j.JPI_F32, q_rows=1 << 22, n_heads=2), pool(), seqs(n_seqs=128)) == j.JPI_ERR_SHAPE  # a workgroup for each 16 rows
     assert "workgroups" in j.jpi_cache_last_error()
     long = seqs(max_pages=1024, table_stride=1024)
     st, n = j.jpi_cache_attention_workspace(attn(), pool(), long)
-    st2, waves, tiles, ranges = j.jpi_debug_cache_plan(attn(), pool(), long)
-    assert st == st2 == j.JPI_OK and n > 0 and ranges > 1
+    st2, groups, tiles, ranges = j.jpi_debug_cache_plan(attn(), pool(), long)
+    assert st == st2 == j.JPI_OK and groups == 0 and tiles == 2 and ranges > 1
+    assert n == 3 * 2 * tiles * ranges * 16 * (128 * 4 + 8)  # a sum and two statistics of each row in each range
     assert attend(q=long, ws=None) == j.JPI_ERR_ARG and "workspace" in j.jpi_cache_last_error()
     assert attend(q=long, size=n - 1) == j.JPI_ERR_ARG and attend(q=long, ws=FAKE + 4, size=n) == j.JPI_ERR_ARG
     assert j.jpi_cache_attention_workspace(attn(scale=0.0), pool(), long) == (j.JPI_ERR_ARG, 0)
