@@ -15,6 +15,7 @@ namespace jpi {
 namespace {
 
 constexpr int PLAN_THREADS = 1024, THREADS = 256;
+constexpr int PER = 8;            // pages of a planning thread at a time
 constexpr int CHUNK = 16384;      // bytes of a page that a workgroup moves at a time
 constexpr int ROW_ENTRIES = 1024; // entries of a table row that a workgroup writes
 
@@ -95,7 +96,6 @@ __global__ __launch_bounds__(PLAN_THREADS) void k_resize_plan(Moves m, const int
   // free pages in ascending order, as many as are needed
   int found = 0;
   const bool other = m.refs_out != m.refs;
-  constexpr int PER = 4;
   for (int p0 = 0; p0 < m.n_pages && (other || found < needed); p0 += PLAN_THREADS * PER) {
     int r[PER], mine = 0;
 #pragma unroll
@@ -211,8 +211,8 @@ __global__ __launch_bounds__(THREADS) void k_reorder(Moves m, const int32_t* par
 // from n_live on; count[1]: n_live.
 __global__ __launch_bounds__(PLAN_THREADS) void k_compact_plan(Moves m, int32_t* n_live_out) {
   __shared__ int red[PLAN_THREADS / 64];
-  constexpr int PER = 4;
   int mine = 0, n_live;
+#pragma unroll 8
   for (int p = threadIdx.x; p < m.n_pages; p += PLAN_THREADS) mine += m.refs[p] > 0;
   scan_before(mine, n_live, red);
 
@@ -226,8 +226,10 @@ __global__ __launch_bounds__(PLAN_THREADS) void k_compact_plan(Moves m, int32_t*
       hole += p < n_live && r[e] <= 0;
       mover += p >= n_live && r[e] > 0;
     }
-    int all_holes, all_movers;
-    int at_hole = holes + scan_before(hole, all_holes, red), at_mover = movers + scan_before(mover, all_movers, red);
+    // both counts in one sum: there are 2^13 of either at most
+    int all;
+    const int before = scan_before(mover << 16 | hole, all, red), all_holes = all & 0xffff, all_movers = all >> 16;
+    int at_hole = holes + (before & 0xffff), at_mover = movers + (before >> 16);
 #pragma unroll
     for (int e = 0; e < PER; ++e) {
       const int p = p0 + (int)threadIdx.x * PER + e;

@@ -40,9 +40,20 @@ __device__ __forceinline__ void factors(float (&f)[N], const float* shared, cons
   }
 }
 
+// Sum over the neighbouring lanes of a head, a power of two of them, the same in each
+__device__ __forceinline__ float lanes_sum(float v, int lanes) {
+  if (lanes >= 16) {
+    v = group16_sum(v);
+    if (lanes >= 32) v += __shfl_xor(v, 16, 64);
+    return lanes == 64 ? halves_sum(v) : v;
+  }
+  for (int o = 1; o < lanes; o <<= 1) v += __shfl_xor(v, o, 64);
+  return v;
+}
+
 // A unit is N elements of a head, with JPI_ROPE_HALF and their N partners half a rotation further on; lane c of the
 // `lanes` (a power of two) of a head has units c, c + lanes ...: U at most.
-template <typename T, typename W, int N, bool VEC, bool INTER, int U>
+template <typename T, typename W, int N, bool VEC, bool INTER, int U, int B>
 __global__ __launch_bounds__(ROPE_THREADS) void k_norm_rope(RopeLaunch l, NormWeights nw, int first, int n_tok, int tile, int lanes) {
   __shared__ float2 table[ROPE_TABLE];
   __shared__ __align__(16) float shared_w[2][MAX_DIM];
@@ -63,79 +74,102 @@ __global__ __launch_bounds__(ROPE_THREADS) void k_norm_rope(RopeLaunch l, NormWe
   const unsigned heads = l.t[0].heads + l.t[1].heads, c0 = threadIdx.x & (lanes - 1);
   const unsigned step = ROPE_THREADS / lanes, rows = here * heads;
   const float inv_dim = 1.f / (float)l.head_dim;
-  for (unsigned r = threadIdx.x / lanes; r < rows; r += step) {  // a head's lanes leave together
-    const unsigned tt = r / heads, hh = r - tt * heads;
-    const bool key = hh >= (unsigned)l.t[0].heads;
-    const RopeTensor& x = l.t[key];
-    const unsigned h = key ? hh - l.t[0].heads : hh;
-    const unsigned n = tok0 + tt, b = n / (unsigned)l.tokens, t = n - b * l.tokens;
-    const T* src = reinterpret_cast<const T*>(x.src) + b * x.so + t * x.sr + h * x.sh;
-    T* dst = reinterpret_cast<T*>(x.dst) + b * x.d_o + t * x.dr + h * x.dh;
-    const void* own = per_head ? nw.w[key] : nullptr;
-    const float* w = shared_w[key];
-    const bool plain = per_head && !own;  // no weight of its own where the other tensor has one for each head
-
-    Piece<T, N, VEC> lo[U], hi[U];
-    float sum = 0.f;
+  const unsigned o0 = (unsigned)tok0 / (unsigned)l.tokens, t0 = tok0 - o0 * l.tokens;
+  const bool one = here == 1;
+  // B heads of a group of lanes at a time, whose loads are on their way together
+  for (unsigned r0 = threadIdx.x / lanes; r0 < rows; r0 += B * step) {  // a head's lanes leave together
+    Piece<T, N, VEC> lo[B][U], hi[B][U];
+    T* dst[B];
+    unsigned tt[B], h[B];
+    bool key[B];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const unsigned c = c0 + u * lanes;
-      if (c >= units) continue;
-      const bool turn = c < rot_units;
-      lo[u].load(src + (turn ? (int)c * N : l.rot_dim + (int)(c - rot_units) * N));
-      if (!INTER && turn) hi[u].load(src + pairs + (int)c * N);
+    for (int b = 0; b < B; ++b) {
+      const unsigned r = min(r0 + b * step, rows - 1);
+      tt[b] = one ? 0 : r / heads;
+      const unsigned hh = r - tt[b] * heads;
+      key[b] = hh >= (unsigned)l.t[0].heads;
+      const RopeTensor& x = l.t[key[b]];
+      h[b] = key[b] ? hh - l.t[0].heads : hh;
+      unsigned o = o0, t = t0 + tt[b];
+      if (t >= (unsigned)l.tokens) {
+        const unsigned by = here <= l.tokens ? 1 : t / (unsigned)l.tokens;
+        o += by, t -= by * l.tokens;
+      }
+      const T* src = reinterpret_cast<const T*>(x.src) + o * x.so + t * x.sr + h[b] * x.sh;
+      dst[b] = reinterpret_cast<T*>(x.dst) + o * x.d_o + t * x.dr + h[b] * x.dh;
+      if (r0 + b * step >= rows) continue;
 #pragma unroll
-      for (int e = 0; e < N; ++e) {
-        sum = fmaf((float)lo[u].v[e], (float)lo[u].v[e], sum);
-        if (!INTER && turn) sum = fmaf((float)hi[u].v[e], (float)hi[u].v[e], sum);
+      for (int u = 0; u < U; ++u) {
+        const unsigned c = c0 + u * lanes;
+        if (c >= units) continue;
+        lo[b][u].load(src + (c < rot_units ? (int)c * N : l.rot_dim + (int)(c - rot_units) * N));
+        if (!INTER && c < rot_units) hi[b][u].load(src + pairs + (int)c * N);
       }
     }
-    for (int o = 1; o < lanes; o <<= 1) sum += __shfl_xor(sum, o, 64);
-    const float f = 1.f / sqrtf(sum * inv_dim + nw.eps);
-
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const unsigned c = c0 + u * lanes;
-      if (c >= units) continue;
-      const bool turn = c < rot_units;
-      const int d = turn ? (int)c * N : l.rot_dim + (int)(c - rot_units) * N;
-      float wl[N];
-      if (plain) {
+    for (int b = 0; b < B; ++b) {
+      if (r0 + b * step >= rows) break;
+      float sum = 0.f;
 #pragma unroll
-        for (int e = 0; e < N; ++e) wl[e] = 1.f;
-      } else {
-        factors<N, VEC, W>(wl, w, own, h * nw.stride, d, nw.offset);
-      }
-      if (!turn) {
-#pragma unroll
-        for (int e = 0; e < N; ++e) lo[u].v[e] = from_f32<T>((float)lo[u].v[e] * f * wl[e]);
-        lo[u].store(dst + d);
-      } else if constexpr (INTER) {
-#pragma unroll
-        for (int e = 0; e < N; e += 2) {
-          const float2 cs = table[tt * pairs + (d + e) / 2];
-          const float a = (float)lo[u].v[e] * f * wl[e], z = (float)lo[u].v[e + 1] * f * wl[e + 1];
-          lo[u].v[e] = from_f32<T>(a * cs.x - z * cs.y);
-          lo[u].v[e + 1] = from_f32<T>(a * cs.y + z * cs.x);
-        }
-        lo[u].store(dst + d);
-      } else {
-        float wh[N];
-        if (plain) {
-#pragma unroll
-          for (int e = 0; e < N; ++e) wh[e] = 1.f;
-        } else {
-          factors<N, VEC, W>(wh, w, own, h * nw.stride, pairs + d, nw.offset);
-        }
+      for (int u = 0; u < U; ++u) {
+        const unsigned c = c0 + u * lanes;
+        if (c >= units) continue;
 #pragma unroll
         for (int e = 0; e < N; ++e) {
-          const float2 cs = table[tt * pairs + d + e];
-          const float a = (float)lo[u].v[e] * f * wl[e], z = (float)hi[u].v[e] * f * wh[e];
-          lo[u].v[e] = from_f32<T>(a * cs.x - z * cs.y);
-          hi[u].v[e] = from_f32<T>(a * cs.y + z * cs.x);
+          sum = fmaf((float)lo[b][u].v[e], (float)lo[b][u].v[e], sum);
+          if (!INTER && c < rot_units) sum = fmaf((float)hi[b][u].v[e], (float)hi[b][u].v[e], sum);
         }
-        lo[u].store(dst + d);
-        hi[u].store(dst + pairs + d);
+      }
+      sum = lanes_sum(sum, lanes);
+      const float f = rsqrtf(sum * inv_dim + nw.eps);
+      const void* own = per_head ? nw.w[key[b]] : nullptr;
+      const float* w = shared_w[key[b]];
+      const bool plain = per_head && !own;  // no weight of its own where the other tensor has one for each head
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const unsigned c = c0 + u * lanes;
+        if (c >= units) continue;
+        const bool turn = c < rot_units;
+        const int d = turn ? (int)c * N : l.rot_dim + (int)(c - rot_units) * N;
+        Piece<T, N, VEC>&x = lo[b][u], &y = hi[b][u];
+        float wl[N];
+        if (plain) {
+#pragma unroll
+          for (int e = 0; e < N; ++e) wl[e] = 1.f;
+        } else {
+          factors<N, VEC, W>(wl, w, own, h[b] * nw.stride, d, nw.offset);
+        }
+        if (!turn) {
+#pragma unroll
+          for (int e = 0; e < N; ++e) x.v[e] = from_f32<T>((float)x.v[e] * f * wl[e]);
+          x.store(dst[b] + d);
+        } else if constexpr (INTER) {
+#pragma unroll
+          for (int e = 0; e < N; e += 2) {
+            const float2 cs = table[tt[b] * pairs + (d + e) / 2];
+            const float p = (float)x.v[e] * f * wl[e], q = (float)x.v[e + 1] * f * wl[e + 1];
+            x.v[e] = from_f32<T>(p * cs.x - q * cs.y);
+            x.v[e + 1] = from_f32<T>(p * cs.y + q * cs.x);
+          }
+          x.store(dst[b] + d);
+        } else {
+          float wh[N];
+          if (plain) {
+#pragma unroll
+            for (int e = 0; e < N; ++e) wh[e] = 1.f;
+          } else {
+            factors<N, VEC, W>(wh, w, own, h[b] * nw.stride, pairs + d, nw.offset);
+          }
+#pragma unroll
+          for (int e = 0; e < N; ++e) {
+            const float2 cs = table[tt[b] * pairs + d + e];
+            const float p = (float)x.v[e] * f * wl[e], q = (float)y.v[e] * f * wh[e];
+            x.v[e] = from_f32<T>(p * cs.x - q * cs.y);
+            y.v[e] = from_f32<T>(p * cs.y + q * cs.x);
+          }
+          x.store(dst[b] + d);
+          y.store(dst[b] + pairs + d);
+        }
       }
     }
   }
@@ -161,10 +195,10 @@ void launch_units(const RopeLaunch& l, const NormWeights& nw, unsigned grid, int
   while (lanes < units && lanes < 64) lanes <<= 1;
   // units of a lane at most: 512 dims in pieces of 4 are two of 64 lanes, in single elements eight
   if constexpr (VEC) {
-    if (units <= lanes) k_norm_rope<T, W, N, VEC, INTER, 1><<<grid, ROPE_THREADS, 0, s>>>(l, nw, first, n, tile, lanes);
-    else k_norm_rope<T, W, N, VEC, INTER, 2><<<grid, ROPE_THREADS, 0, s>>>(l, nw, first, n, tile, lanes);
+    if (units <= lanes) k_norm_rope<T, W, N, VEC, INTER, 1, 2><<<grid, ROPE_THREADS, 0, s>>>(l, nw, first, n, tile, lanes);
+    else k_norm_rope<T, W, N, VEC, INTER, 2, 1><<<grid, ROPE_THREADS, 0, s>>>(l, nw, first, n, tile, lanes);
   } else {
-    k_norm_rope<T, W, N, VEC, INTER, 8><<<grid, ROPE_THREADS, 0, s>>>(l, nw, first, n, tile, lanes);
+    k_norm_rope<T, W, N, VEC, INTER, 8, 1><<<grid, ROPE_THREADS, 0, s>>>(l, nw, first, n, tile, lanes);
   }
 }
 
