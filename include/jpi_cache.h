@@ -64,7 +64,7 @@ typedef struct {
  * are not read.  An entry outside [0, n_pages) names no page: attention takes its
  * slots for NaN, append writes nothing there, and the page moves pass it by. */
 typedef struct {
-  int n_seqs, max_pages;    /* n_seqs 1 .. 65536; max_pages 1 .. 2^22, max_pages * page < 2^31 */
+  int n_seqs, max_pages;    /* n_seqs 1 .. 65536; max_pages 1 .. 2^22 */
   int64_t table_stride;     /* >= max_pages */
   const int32_t* table;     /* device */
   const int32_t* len;       /* device [n_seqs] */
@@ -74,7 +74,8 @@ typedef struct {
  * Each head of q and k is normed and then turned as by jpi_rope:
  *   y = x * (sum_d x_d^2 / head_dim + eps)^-1/2 * (weight + offset),
  * offset 1 with unit_offset != 0, else 0; a NULL weight counts as 1 - offset
- * (the norm alone).  All of it in fp32 (the angle as in jpi_rope), rounded once.
+ * (the norm alone).  All of it in fp32 (the angle as in jpi_rope), rounded once; a
+ * head whose squares sum past fp32 (elements of 2^60 and more) comes out 0.
  * q_weight, k_weight: device [head_dim] of type weight_dtype (JPI_BF16 or JPI_F32),
  * that of head h at + h * weight_stride elements (0: all heads share one).
  * eps > 0, also as a float.  Everything else, the errors too, as jpi_rope; a
@@ -168,9 +169,9 @@ jpi_status jpi_debug_cache_plan(const jpi_cache_attn* a, const jpi_cache_pool* p
  * refs_out whole: rows to their max_pages entries, -1 where the sequence holds
  * nothing.  Each of the three may be its input (same address and stride) or memory
  * that overlaps no input.  Where pages change their place their contents move in
- * all `layers` layers of the pool: layer l's k, v, k_scale and v_scale lie n_pages
- * pages behind layer l - 1's.  pool NULL: counts and tables alone, n_pages and page
- * as given.  workspace: as for jpi_cache_attention. */
+ * all `layers` layers of a pool: layer l's k, v, k_scale and v_scale lie n_pages
+ * pages behind layer l - 1's.  pool NULL: counts and tables alone.  workspace: as
+ * for jpi_cache_attention. */
 typedef struct {
   jpi_cache_seqs seqs;
   const int32_t* refs;
@@ -178,8 +179,6 @@ typedef struct {
   int64_t table_out_stride;
   int32_t *len_out, *refs_out; /* len_out is not used by jpi_cache_compact */
   int n_pages, page;           /* as the pool's, if there is one */
-  const jpi_cache_pool* pool;
-  int layers;                  /* >= 1 with a pool */
 } jpi_cache_moves;
 
 /* Bytes of workspace that any of the three calls below wants with these sizes. */
@@ -196,19 +195,20 @@ jpi_status jpi_cache_moves_workspace(const jpi_cache_moves* m, size_t* bytes);
  * (device int32 [1], or NULL): how many free pages all needs together lacked.
  * Pages that the call sets free serve from the next call on.  seqs->len and
  * new_len may not overlap len_out unless they are len_out itself. */
-jpi_status jpi_cache_resize(const jpi_cache_moves* m, const int32_t* new_len, int32_t* short_out, void* workspace,
-                            size_t workspace_bytes, void* stream);
+jpi_status jpi_cache_resize(const jpi_cache_moves* m, const jpi_cache_pool* pool, int layers, const int32_t* new_len,
+                            int32_t* short_out, void* workspace, size_t workspace_bytes, void* stream);
 
 /* Sequence s takes over what sequence parents[s] (device int32) holds before the
  * call; a parent outside [0, n_seqs) leaves it empty.  Nothing is copied: forks
- * share pages until they grow.  pool is not used. */
+ * share pages until they grow. */
 jpi_status jpi_cache_reorder(const jpi_cache_moves* m, const int32_t* parents, void* workspace, size_t workspace_bytes, void* stream);
 
 /* Pages in use get the numbers 0 .. n_live - 1: the i-th of them (ascending) whose
  * number is n_live or more moves to the i-th free one below n_live.  All entries of
  * the table that name pages are renumbered, behind a sequence's last slot too;
  * len is not read.  n_live_out: device int32 [1], or NULL. */
-jpi_status jpi_cache_compact(const jpi_cache_moves* m, int32_t* n_live_out, void* workspace, size_t workspace_bytes, void* stream);
+jpi_status jpi_cache_compact(const jpi_cache_moves* m, const jpi_cache_pool* pool, int layers, int32_t* n_live_out,
+                             void* workspace, size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

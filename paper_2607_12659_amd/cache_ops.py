@@ -43,7 +43,7 @@ _NORM = struct.Struct("@PP2iqd")
 _POOL = struct.Struct("@5iPPPP")
 _SEQS = struct.Struct("@2iqPP")
 _ATTN = struct.Struct("@6if" + _V + "P" + _V + "P")
-_MOVES = struct.Struct("@2iqPPPPqPP2iPi4x")
+_MOVES = struct.Struct("@2iqPPPPqPP2i")
 assert (_NORM.size, _POOL.size, _SEQS.size, _ATTN.size, _MOVES.size) == tuple(
     ctypes.sizeof(c) for c in (_j.jpi_head_norm, _j.jpi_cache_pool, _j.jpi_cache_seqs, _j.jpi_cache_attn, _j.jpi_cache_moves))
 
@@ -70,44 +70,60 @@ class Pool(NamedTuple):
         return Pool(self.k[i], self.v[i], self.k_scale[i], self.v_scale[i])
 
 
+# The checks below first ask in one expression whether all is well, and look for what is wrong only if not: a call's host time
+# is mostly its checks.
 def _pool(pool, layers):
     """The C structure, layers, pages, slots of a page, KV heads, head_dim and device of a pool, of one layer unless `layers`."""
     k, v, ks, vs = pool
-    shape = k.shape
-    if len(shape) != 5 and not (layers and len(shape) == 6):
+    shape, dtype, dev = k.shape, k.dtype, k.get_device()
+    if len(shape) == 5:
+        n_pages, kv, pieces, page, width = shape
+        n_layers, lead = 1, (n_pages, kv)
+    elif layers and len(shape) == 6:
+        n_layers, n_pages, kv, pieces, page, width = shape
+        lead = (n_layers, n_pages, kv)
+    else:
         raise ValueError("codes of K must be %s[pages][kv_heads][head_dim / 16][page][16]" % ("[layers]" if layers else ""))
-    lead, (pieces, page, width), dev = shape[:-3], shape[-3:], k.get_device()
-    code = _CODE.get(k.dtype)
-    if code is None:
-        raise TypeError("codes must be int8 or float8_e4m3fn, got %s" % k.dtype)
-    n_pages, kv = lead[-2:]
-    if width != 16 or page % 16 or max(n_pages, kv, pieces * 16, page) > _INT_MAX:
-        raise ValueError("codes of K must be [pages][kv_heads][head_dim / 16][page][16], got %s" % list(shape))
-    _want("codes of V", v, lead + (page // 16, pieces * 16, 16), k.dtype, dev)
-    _want("k_scale", ks, lead, _F32, dev)
-    _want("v_scale", vs, lead, _F32, dev)
-    packed = _POOL.pack(code, kv, pieces * 16, n_pages, page, _dense("codes of K", k), _dense("codes of V", v), _dense("k_scale", ks),
-                        _dense("v_scale", vs))
-    return packed, (lead[0] if len(lead) == 3 else 1), n_pages, page, kv, pieces * 16, dev
+    code, v_shape = _CODE.get(dtype), (*lead, page // 16, pieces * 16, 16)
+    if not (code is not None and width == 16 and page % 16 == 0 and v.shape == v_shape and v.dtype is dtype and v.get_device() == dev
+            and ks.shape == lead and ks.dtype is _F32 and ks.get_device() == dev and vs.shape == lead and vs.dtype is _F32
+            and vs.get_device() == dev and k.is_contiguous() and v.is_contiguous() and ks.is_contiguous() and vs.is_contiguous()
+            and n_pages <= _INT_MAX and kv <= _INT_MAX and pieces <= _INT_MAX >> 4 and page <= _INT_MAX):
+        if code is None:
+            raise TypeError("codes must be int8 or float8_e4m3fn, got %s" % dtype)
+        if width != 16 or page % 16 or max(n_pages, kv, pieces * 16, page) > _INT_MAX:
+            raise ValueError("codes of K must be [pages][kv_heads][head_dim / 16][page][16], got %s" % list(shape))
+        _want("codes of V", v, v_shape, dtype, dev)
+        _want("k_scale", ks, lead, _F32, dev)
+        _want("v_scale", vs, lead, _F32, dev)
+        for name, t in zip(("codes of K", "codes of V", "k_scale", "v_scale"), pool):
+            _dense(name, t)
+    packed = _POOL.pack(code, kv, pieces * 16, n_pages, page, k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr())
+    return packed, n_layers, n_pages, page, kv, pieces * 16, dev
 
 
 def _rows(name, table, n, dev):
-    """n_seqs, max_pages and the row stride of a table."""
-    if table.dim() != 2:
-        raise ValueError("%s must be [sequences][pages]" % name)
+    """n_seqs, max_pages and the row stride of a table of int32, with n rows unless that is None."""
     shape = table.shape
-    _want(name, table, shape if n is None else (n, shape[1]), _I32, dev)
-    if max(shape) > _INT_MAX:
-        raise ValueError("%s is larger than 2^31 - 1 in a dimension" % name)
-    if shape[1] > 1 and table.stride(1) != 1:
+    if len(shape) != 2:
+        raise ValueError("%s must be [sequences][pages]" % name)
+    rows, width = shape
+    stride, one = table.stride()
+    if not (table.dtype is _I32 and table.get_device() == dev and (n is None or rows == n) and rows <= _INT_MAX and width <= _INT_MAX
+            and (one == 1 or width <= 1)):
+        _want(name, table, shape if n is None else (n, width), _I32, dev)
+        if max(shape) > _INT_MAX:
+            raise ValueError("%s is larger than 2^31 - 1 in a dimension" % name)
         raise ValueError("the entries of a row of %s must be contiguous" % name)
-    return shape[0], shape[1], table.stride(0) if shape[0] > 1 else shape[1]
+    return rows, width, stride if rows > 1 else width
 
 
-def _seqs(table, lens, dev):
-    n, width, stride = _rows("table", table, None, dev)
-    _want("lens", lens, (n,), _I32, dev)
-    return n, width, stride, table.data_ptr(), _dense("lens", lens)
+def _ints(name, t, n, dev):
+    """The address of n int32."""
+    if not (t.shape == (n,) and t.dtype is _I32 and t.get_device() == dev and t.is_contiguous()):
+        _want(name, t, (n,), _I32, dev)
+        _dense(name, t)
+    return t.data_ptr()
 
 
 def _workspace(size_of, like, *args):
@@ -160,20 +176,17 @@ def append(pool, table, starts, k, v, *, n_new=None):
         raise ValueError("k must be [sequences][tokens][kv_heads][head_dim]")
     if _recording():
         _no_gradients(k, v, *pool)
-    n, width, stride, *at = _seqs(table, starts, dev)
+    n, width, stride = _rows("table", table, None, dev)
+    seqs = _SEQS.pack(n, width, stride, table.data_ptr(), _ints("starts", starts, n, dev))
     tokens = k.shape[1]
     if tokens > _INT_MAX:
         raise ValueError("k has more than 2^31 - 1 tokens")
-    dt = _dtype(k)
-    _want("k", k, (n, tokens, kv, dh), k.dtype, dev)
-    _want("v", v, k.shape, k.dtype, dev)
-    if n_new is not None:
-        _want("n_new", n_new, (n,), _I32, dev)
-        _dense("n_new", n_new)
-    _launch(dev, _lib.jpi_cache_append, packed, _SEQS.pack(n, width, stride, *at), dt, tokens, _VIEW.pack(*_view("k", k)),
-            _VIEW.pack(*_view("v", v)),
-            None if n_new is None else n_new.data_ptr())
-    _written(list(pool))
+    dt, shape = _dtype(k), (n, tokens, kv, dh)
+    _want("k", k, shape, k.dtype, dev)
+    _want("v", v, shape, k.dtype, dev)
+    _launch(dev, _lib.jpi_cache_append, packed, seqs, dt, tokens, _VIEW.pack(*_view("k", k)), _VIEW.pack(*_view("v", v)),
+            None if n_new is None else _ints("n_new", n_new, n, dev))
+    _written(pool)
 
 
 def attention(q, pool, table, lens, *, q_lens=None, causal=True, window=0, sinks=0, scale=None, out=None, lse=None):
@@ -190,16 +203,14 @@ def attention(q, pool, table, lens, *, q_lens=None, causal=True, window=0, sinks
     if _recording():
         _no_gradients(q, out, lse, *pool)
     given = [t for t in (out, lse) if t is not None]
-    n, width, stride, *at = _seqs(table, lens, dev)
+    n, width, stride = _rows("table", table, None, dev)
+    seqs = _SEQS.pack(n, width, stride, table.data_ptr(), _ints("lens", lens, n, dev))
     dt = _dtype(q)
     _, rows, heads, _ = q.shape
     _want("q", q, (n, rows, heads, dh), q.dtype, dev)
     if max(rows, heads) > _INT_MAX:
         raise ValueError("q is larger than 2^31 - 1 in a dimension")
-    ql = 0
-    if q_lens is not None:
-        _want("q_lens", q_lens, (n,), _I32, dev)
-        ql = _dense("q_lens", q_lens)
+    ql = 0 if q_lens is None else _ints("q_lens", q_lens, n, dev)
     if out is None:
         out = torch.empty_like(q, memory_format=torch.contiguous_format)
     else:
@@ -210,7 +221,6 @@ def attention(q, pool, table, lens, *, q_lens=None, causal=True, window=0, sinks
         _want("lse", lse, (n, rows, heads), _F32, dev)
     args = _pack(_ATTN, dt, rows, heads, int(bool(causal)), window, sinks, dh ** -0.5 if scale is None else scale, *_view("q", q), ql,
                  *_view("out", out), _dense("lse", lse))
-    seqs = _SEQS.pack(n, width, stride, *at)
     ws, size = _workspace(_lib.jpi_cache_attention_workspace, q, args, packed, seqs)
     _launch(dev, _lib.jpi_cache_attention, args, packed, seqs, ws.data_ptr() if size else None, size)
     if given:
@@ -219,7 +229,7 @@ def attention(q, pool, table, lens, *, q_lens=None, causal=True, window=0, sinks
 
 
 def _moves(table, lens, refs, pool, page, table_out, lens_out, refs_out):
-    """The C structure of a move, the workspace, the device, the outputs, and whether torch is told of them."""
+    """The C structures of a move and its pool, layers, the workspace, the device, the number of sequences, and what changes."""
     if pool is not None:
         packed, layers, n_pages, slots, _, _, dev = _pool(pool, True)
         if page not in (None, slots):
@@ -228,26 +238,24 @@ def _moves(table, lens, refs, pool, page, table_out, lens_out, refs_out):
         packed, layers, n_pages, slots, dev = None, 0, refs.shape[0] if refs.dim() == 1 else 0, page, refs.get_device()
         if n_pages > _INT_MAX:
             raise ValueError("refs has more than 2^31 - 1 pages")
-    _want("refs", refs, (n_pages,), _I32, dev)
     n, width, stride = _rows("table", table, None, dev)
-    table_out = table if table_out is None else table_out
-    _, _, out_stride = _rows("table_out", table_out, n, dev)
-    _want("table_out", table_out, table.shape, _I32, dev)
-    refs_out = refs if refs_out is None else refs_out
-    _want("refs_out", refs_out, (n_pages,), _I32, dev)
+    if table_out is None:
+        table_out, out_stride = table, stride
+    else:
+        _want("table_out", table_out, table.shape, _I32, dev)
+        out_stride = _rows("table_out", table_out, n, dev)[2]
     at = out = 0
+    changed = [table_out, refs if refs_out is None else refs_out]
     if lens is not None:
-        _want("lens", lens, (n,), _I32, dev)
-        at = _dense("lens", lens)
-        lens_out = lens if lens_out is None else lens_out
-        _want("lens_out", lens_out, (n,), _I32, dev)
-        out = _dense("lens_out", lens_out)
-    held = ctypes.create_string_buffer(packed, len(packed)) if packed else None
-    m = _pack(_MOVES, n, width, stride, table.data_ptr(), at, _dense("refs", refs), table_out.data_ptr(), out_stride, out,
-              _dense("refs_out", refs_out), n_pages, slots, ctypes.addressof(held) if packed else 0, layers)
+        at = out = _ints("lens", lens, n, dev)
+        if lens_out is not None:
+            out = _ints("lens_out", lens_out, n, dev)
+        changed.append(lens if lens_out is None else lens_out)
+    refs_at = _ints("refs", refs, n_pages, dev)
+    refs_to = refs_at if refs_out is None else _ints("refs_out", refs_out, n_pages, dev)
+    m = _pack(_MOVES, n, width, stride, table.data_ptr(), at, refs_at, table_out.data_ptr(), out_stride, out, refs_to, n_pages, slots)
     ws, size = _workspace(_lib.jpi_cache_moves_workspace, table, m)
-    changed = [table_out, refs_out] + ([] if lens is None else [lens_out])
-    return m, held, ws, size, dev, n, changed
+    return m, packed, layers, ws, size, dev, n, changed
 
 
 def _one(name, t, like, dev):
@@ -265,11 +273,11 @@ def resize(table, lens, refs, new_lens, pool=None, *, page=None, short=None, tab
     changed in place unless it has an output of its own.  pool: all layers whose pages are copied; None for tables alone,
     with `page` slots of a page.  Returns (lens_out, short), short int32 [1]: pages that were lacking.
     """
-    m, held, ws, size, dev, n, changed = _moves(table, lens, refs, pool, page, table_out, lens_out, refs_out)
-    _want("new_lens", new_lens, (n,), _I32, dev)
+    m, packed, layers, ws, size, dev, n, changed = _moves(table, lens, refs, pool, page, table_out, lens_out, refs_out)
+    new = _ints("new_lens", new_lens, n, dev)
     short = _one("short", short, table, dev)
-    _launch(dev, _lib.jpi_cache_resize, m, _dense("new_lens", new_lens), short.data_ptr(), ws.data_ptr(), size)
-    _written(changed + [short] + list(pool or ()))
+    _launch(dev, _lib.jpi_cache_resize, m, packed, layers, new, short.data_ptr(), ws.data_ptr(), size)
+    _written([*changed, short, *(pool or ())])
     return changed[2], short
 
 
@@ -277,9 +285,8 @@ def reorder(table, lens, refs, parents, page, *, table_out=None, lens_out=None, 
     """Sequence s takes over what sequence parents[s] holds, nothing where there is no such sequence: ``jpi_cache_reorder``.
     Forks share their pages until they grow.  Arguments as resize; returns lens_out.
     """
-    m, held, ws, size, dev, n, changed = _moves(table, lens, refs, None, page, table_out, lens_out, refs_out)
-    _want("parents", parents, (n,), _I32, dev)
-    _launch(dev, _lib.jpi_cache_reorder, m, _dense("parents", parents), ws.data_ptr(), size)
+    m, _, _, ws, size, dev, n, changed = _moves(table, lens, refs, None, page, table_out, lens_out, refs_out)
+    _launch(dev, _lib.jpi_cache_reorder, m, _ints("parents", parents, n, dev), ws.data_ptr(), size)
     _written(changed)
     return changed[2]
 
@@ -290,8 +297,8 @@ def compact(table, refs, pool=None, *, page=None, n_live=None, table_out=None, r
     """
     if pool is None and page is None:
         page = 16  # tables alone: of no consequence
-    m, held, ws, size, dev, _, changed = _moves(table, None, refs, pool, page, table_out, None, refs_out)
+    m, packed, layers, ws, size, dev, _, changed = _moves(table, None, refs, pool, page, table_out, None, refs_out)
     n_live = _one("n_live", n_live, table, dev)
-    _launch(dev, _lib.jpi_cache_compact, m, n_live.data_ptr(), ws.data_ptr(), size)
-    _written(changed + [n_live] + list(pool or ()))
+    _launch(dev, _lib.jpi_cache_compact, m, packed, layers, n_live.data_ptr(), ws.data_ptr(), size)
+    _written([*changed, n_live, *(pool or ())])
     return n_live

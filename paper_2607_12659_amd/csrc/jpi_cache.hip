@@ -30,11 +30,11 @@ jpi_status check_pool_data(const char* call, const jpi_cache_pool* p) {
   return JPI_OK;
 }
 
-jpi_status check_seqs(const char* call, const jpi_cache_seqs* q, int page) {
+jpi_status check_seqs(const char* call, const jpi_cache_seqs* q) {
   if (!q) return fail(JPI_ERR_ARG, "%s: NULL sequences", call);
   if (q->n_seqs < 1 || q->n_seqs > 65536) return fail(JPI_ERR_ARG, "%s: n_seqs must be 1 .. 65536", call);
-  if (q->max_pages < 1 || q->max_pages > 1 << 22 || (int64_t)q->max_pages * page > INT32_MAX)
-    return fail(JPI_ERR_ARG, "%s: max_pages must be 1 .. 2^22, max_pages * page below 2^31", call);
+  if (q->max_pages < 1 || q->max_pages > 1 << 22)  // 2^29 slots at most
+    return fail(JPI_ERR_ARG, "%s: max_pages must be 1 .. 2^22", call);
   if (q->table_stride < q->max_pages) return fail(JPI_ERR_ARG, "%s: table_stride below max_pages", call);
   return JPI_OK;
 }
@@ -57,7 +57,7 @@ jpi_status check_attention(const char* call, const jpi_cache_attn* a, const jpi_
   if (!a) return fail(JPI_ERR_ARG, "%s: NULL arguments", call);
   if (!known(a->dtype)) return fail(JPI_ERR_DTYPE, "%s: dtype must be JPI_BF16 or JPI_F32", call);
   jpi_status st;
-  if ((st = check_pool(call, p)) != JPI_OK || (st = check_seqs(call, q, p->page)) != JPI_OK) return st;
+  if ((st = check_pool(call, p)) != JPI_OK || (st = check_seqs(call, q)) != JPI_OK) return st;
   if (a->q_rows < 1) return fail(JPI_ERR_ARG, "%s: q_rows must be >= 1", call);
   if (a->n_heads < 1 || a->n_heads % p->n_kv_heads != 0)
     return fail(JPI_ERR_ARG, "%s: n_heads must be a multiple of n_kv_heads", call);
@@ -83,20 +83,15 @@ jpi_status check_moves_sizes(const char* call, const jpi_cache_moves* m) {
   if (!m) return fail(JPI_ERR_ARG, "%s: NULL arguments", call);
   if (!known_page(m->page)) return fail(JPI_ERR_ARG, "%s: page must be 16, 32, 64 or 128", call);
   if (m->n_pages < 1 || m->n_pages > 1 << 24) return fail(JPI_ERR_ARG, "%s: n_pages must be 1 .. 2^24", call);
-  jpi_status st = check_seqs(call, &m->seqs, m->page);
+  const jpi_status st = check_seqs(call, &m->seqs);
   if (st != JPI_OK) return st;
   if ((int64_t)m->seqs.n_seqs * (m->seqs.max_pages + 1) > INT32_MAX || !moves_fit(*m))
     return fail(JPI_ERR_SHAPE, "%s: tables of 2^31 entries or more", call);
-  if (m->pool) {
-    if ((st = check_pool(call, m->pool)) != JPI_OK) return st;
-    if (m->pool->n_pages != m->n_pages || m->pool->page != m->page)
-      return fail(JPI_ERR_ARG, "%s: n_pages or page is not the pool's", call);
-    if (m->layers < 1 || m->layers > 65536) return fail(JPI_ERR_ARG, "%s: layers must be 1 .. 65536", call);
-  }
   return JPI_OK;
 }
 
-jpi_status check_moves(const char* call, const jpi_cache_moves* m, bool lengths, const void* ws, size_t bytes) {
+jpi_status check_moves(const char* call, const jpi_cache_moves* m, const jpi_cache_pool* pool, int layers, bool lengths, const void* ws,
+                       size_t bytes) {
   jpi_status st = check_moves_sizes(call, m);
   if (st != JPI_OK) return st;
   const jpi_cache_seqs& q = m->seqs;
@@ -110,7 +105,12 @@ jpi_status check_moves(const char* call, const jpi_cache_moves* m, bool lengths,
     for (int j = 0; j < 3; ++j)
       if (out[i] && i != j && (out[i] == in[j] || out[i] == out[j]))
         return fail(JPI_ERR_ARG, "%s: an output is where another array is", call);
-  if (m->pool && (st = check_pool_data(call, m->pool)) != JPI_OK) return st;
+  if (pool) {
+    if ((st = check_pool(call, pool)) != JPI_OK || (st = check_pool_data(call, pool)) != JPI_OK) return st;
+    if (pool->n_pages != m->n_pages || pool->page != m->page)
+      return fail(JPI_ERR_ARG, "%s: n_pages or page is not the pool's", call);
+    if (layers < 1 || layers > 65536) return fail(JPI_ERR_ARG, "%s: layers must be 1 .. 65536", call);
+  }
   return check_workspace(call, moves_bytes(*m), ws, bytes);
 }
 
@@ -141,7 +141,7 @@ jpi_status jpi_cache_append(const jpi_cache_pool* pool, const jpi_cache_seqs* se
                             const jpi_view* v, const int32_t* n_new, void* stream) {
   const char* call = "jpi_cache_append";
   jpi_status st;
-  if ((st = check_pool(call, pool)) != JPI_OK || (st = check_seqs(call, seqs, pool->page)) != JPI_OK) return st;
+  if ((st = check_pool(call, pool)) != JPI_OK || (st = check_seqs(call, seqs)) != JPI_OK) return st;
   if (!known(dt)) return fail(JPI_ERR_DTYPE, "%s: dtype must be JPI_BF16 or JPI_F32", call);
   if (tokens < 0) return fail(JPI_ERR_ARG, "%s: negative tokens", call);
   if ((int64_t)seqs->n_seqs * tokens > INT32_MAX) return fail(JPI_ERR_SHAPE, "%s: more than 2^31 - 1 tokens", call);
@@ -197,29 +197,30 @@ jpi_status jpi_cache_moves_workspace(const jpi_cache_moves* m, size_t* bytes) {
   return st;
 }
 
-jpi_status jpi_cache_resize(const jpi_cache_moves* m, const int32_t* new_len, int32_t* short_out, void* workspace,
-                            size_t workspace_bytes, void* stream) {
+jpi_status jpi_cache_resize(const jpi_cache_moves* m, const jpi_cache_pool* pool, int layers, const int32_t* new_len,
+                            int32_t* short_out, void* workspace, size_t workspace_bytes, void* stream) {
   const char* call = "jpi_cache_resize";
-  const jpi_status st = check_moves(call, m, true, workspace, workspace_bytes);
+  const jpi_status st = check_moves(call, m, pool, layers, true, workspace, workspace_bytes);
   if (st != JPI_OK) return st;
   if (!new_len) return fail(JPI_ERR_ARG, "%s: NULL new_len", call);
-  return fail.launched(call, launch_resize(*m, new_len, short_out, workspace, (hipStream_t)stream));
+  return fail.launched(call, launch_resize(*m, pool, layers, new_len, short_out, workspace, (hipStream_t)stream));
 }
 
 jpi_status jpi_cache_reorder(const jpi_cache_moves* m, const int32_t* parents, void* workspace, size_t workspace_bytes, void* stream) {
   const char* call = "jpi_cache_reorder";
-  const jpi_status st = check_moves(call, m, true, workspace, workspace_bytes);
+  const jpi_status st = check_moves(call, m, nullptr, 0, true, workspace, workspace_bytes);
   if (st != JPI_OK) return st;
   if (!parents) return fail(JPI_ERR_ARG, "%s: NULL parents", call);
   if (parents == m->len_out) return fail(JPI_ERR_ARG, "%s: an output is where another array is", call);
   return fail.launched(call, launch_reorder(*m, parents, workspace, (hipStream_t)stream));
 }
 
-jpi_status jpi_cache_compact(const jpi_cache_moves* m, int32_t* n_live_out, void* workspace, size_t workspace_bytes, void* stream) {
+jpi_status jpi_cache_compact(const jpi_cache_moves* m, const jpi_cache_pool* pool, int layers, int32_t* n_live_out,
+                             void* workspace, size_t workspace_bytes, void* stream) {
   const char* call = "jpi_cache_compact";
-  const jpi_status st = check_moves(call, m, false, workspace, workspace_bytes);
+  const jpi_status st = check_moves(call, m, pool, layers, false, workspace, workspace_bytes);
   if (st != JPI_OK) return st;
-  return fail.launched(call, launch_compact(*m, n_live_out, workspace, (hipStream_t)stream));
+  return fail.launched(call, launch_compact(*m, pool, layers, n_live_out, workspace, (hipStream_t)stream));
 }
 
 }  // extern "C"

@@ -578,7 +578,7 @@ __global__ __launch_bounds__(64 * WAVES, DH == 256 ? 1 : 2) void k_cache_rows(Ca
     asm volatile("" ::: "memory");
     if (n % AHEAD == 0 && n > 0 && wave == 0) {  // the block before is done with; seen at the next barrier, used after it
       look_up(n / AHEAD + 1);
-      __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt 0
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     }
     if (n + RG::STAGES - 1 < count) issue(n + RG::STAGES - 1, stage == 0 ? RG::STAGES - 1 : stage - 1);
     const Piece16 *mine = pieces[n / AHEAD & 1][n % AHEAD], p0 = mine[grp], p1 = mine[2 + grp];

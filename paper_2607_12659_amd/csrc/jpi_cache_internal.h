@@ -30,8 +30,10 @@ hipError_t launch_cache_attention(const jpi_cache_attn& a, const jpi_cache_pool&
 
 bool moves_fit(const jpi_cache_moves& m);  // whether every launch holds its workgroups
 size_t moves_bytes(const jpi_cache_moves& m);
-hipError_t launch_resize(const jpi_cache_moves& m, const int32_t* new_len, int32_t* short_out, void* ws, hipStream_t s);
+hipError_t launch_resize(const jpi_cache_moves& m, const jpi_cache_pool* pool, int layers, const int32_t* new_len,
+                         int32_t* short_out, void* ws, hipStream_t s);
 hipError_t launch_reorder(const jpi_cache_moves& m, const int32_t* parents, void* ws, hipStream_t s);
-hipError_t launch_compact(const jpi_cache_moves& m, int32_t* n_live_out, void* ws, hipStream_t s);
+hipError_t launch_compact(const jpi_cache_moves& m, const jpi_cache_pool* pool, int layers, int32_t* n_live_out, void* ws,
+                          hipStream_t s);
 
 }  // namespace jpi

@@ -124,7 +124,7 @@ class jpi_cache_attn(ctypes.Structure):
 class jpi_cache_moves(ctypes.Structure):
     _fields_ = [("seqs", jpi_cache_seqs), ("refs", ctypes.c_void_p), ("table_out", ctypes.c_void_p),
                 ("table_out_stride", ctypes.c_int64), ("len_out", ctypes.c_void_p), ("refs_out", ctypes.c_void_p),
-                ("n_pages", ctypes.c_int), ("page", ctypes.c_int), ("pool", ctypes.c_void_p), ("layers", ctypes.c_int)]
+                ("n_pages", ctypes.c_int), ("page", ctypes.c_int)]
 
 
 # include/jpi_sched.h
@@ -234,9 +234,9 @@ _sig = {
     "jpi_cache_attention": (_i, [_vp, _vp, _vp, _vp, ctypes.c_size_t, _vp]),
     "jpi_debug_cache_plan": (_i, [_vp, _vp, _vp, _vp, _vp, _vp]),
     "jpi_cache_moves_workspace": (_i, [_vp, _vp]),
-    "jpi_cache_resize": (_i, [_vp, _vp, _vp, _vp, ctypes.c_size_t, _vp]),
+    "jpi_cache_resize": (_i, [_vp, _vp, _i, _vp, _vp, _vp, ctypes.c_size_t, _vp]),
     "jpi_cache_reorder": (_i, [_vp, _vp, _vp, ctypes.c_size_t, _vp]),
-    "jpi_cache_compact": (_i, [_vp, _vp, _vp, ctypes.c_size_t, _vp]),
+    "jpi_cache_compact": (_i, [_vp, _vp, _i, _vp, _vp, ctypes.c_size_t, _vp]),
 }
 for _name, (_res, _args) in _sig.items():
     _fn = getattr(_lib, _name)
@@ -556,16 +556,20 @@ def jpi_cache_moves_workspace(args: jpi_cache_moves):
     return st, n.value
 
 
-def jpi_cache_resize(args: jpi_cache_moves, new_len, short_out=None, workspace=None, workspace_bytes: int = 0, stream=None) -> int:
-    return _lib.jpi_cache_resize(_ref(args), addr(new_len), addr(short_out), addr(workspace), workspace_bytes, stream_handle(stream))
+def jpi_cache_resize(args: jpi_cache_moves, pool: jpi_cache_pool | None, layers: int, new_len, short_out=None, workspace=None,
+                     workspace_bytes: int = 0, stream=None) -> int:
+    return _lib.jpi_cache_resize(_ref(args), _ref(pool), layers, addr(new_len), addr(short_out), addr(workspace), workspace_bytes,
+                                 stream_handle(stream))
 
 
 def jpi_cache_reorder(args: jpi_cache_moves, parents, workspace=None, workspace_bytes: int = 0, stream=None) -> int:
     return _lib.jpi_cache_reorder(_ref(args), addr(parents), addr(workspace), workspace_bytes, stream_handle(stream))
 
 
-def jpi_cache_compact(args: jpi_cache_moves, n_live_out=None, workspace=None, workspace_bytes: int = 0, stream=None) -> int:
-    return _lib.jpi_cache_compact(_ref(args), addr(n_live_out), addr(workspace), workspace_bytes, stream_handle(stream))
+def jpi_cache_compact(args: jpi_cache_moves, pool: jpi_cache_pool | None, layers: int, n_live_out=None, workspace=None,
+                      workspace_bytes: int = 0, stream=None) -> int:
+    return _lib.jpi_cache_compact(_ref(args), _ref(pool), layers, addr(n_live_out), addr(workspace), workspace_bytes,
+                                  stream_handle(stream))
 
 
 class JpiError(RuntimeError):

@@ -724,3 +724,168 @@ def test_a_run_of_them_together(ops, code, dtype):
         equal(got, want, name)
     reordered([-1] * 4)
     assert (r.cpu() == 0).all()
+
+
+# ---------------------------------------------------------------------------
+# as programs call them
+# ---------------------------------------------------------------------------
+def decode_state(ops, code="e4m3", S=5, kv=2, heads=4, dh=64, page=16, width=8, n_pages=64, layers=1):
+    """Sequences of a few slots each, room for more, and everything on the GPU."""
+    pool = filled(1, n_pages, kv, dh, page, code)
+    lens = [37, 0, 16, 90, 5][:S]
+    table, lens, refs = scattered(1, lens, page, width, n_pages)
+    return dict(pool=on_gpu(ops, pool, code), table=dev(table), lens=dev(lens), refs=dev(refs), page=page,
+                qw=dev(1 + 0.1 * rand(1, dh)), kw=dev(1 + 0.1 * rand(2, dh)))
+
+
+def decode_step(ops, st, q, k, v, window=0):
+    """One token for each sequence, as a sampling program does it."""
+    starts = st["lens"].clone()
+    new = st["lens"] + 1
+    ops.resize(st["table"], st["lens"], st["refs"], new, st["pool"])
+    qo, ko = ops.norm_rope(q, k, starts[:, None], q_weight=st["qw"], k_weight=st["kw"])
+    ops.append(st["pool"], st["table"], starts, ko, v)
+    return ops.attention(qo, st["pool"], st["table"], st["lens"], window=window, sinks=2 if window else 0)
+
+
+def everything(st):
+    return [t.clone() for t in (*st["pool"], st["table"], st["lens"], st["refs"])]
+
+
+def same_bits(a, b):
+    for x, y in zip(a, b):
+        assert torch.equal(x.contiguous().view(torch.uint8), y.contiguous().view(torch.uint8))
+
+
+def copied(st):
+    return {k: type(v)(*(t.clone() for t in v)) if isinstance(v, tuple) else v.clone() if torch.is_tensor(v) else v for k, v in st.items()}
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_a_captured_step_replays_as_the_eager_one_runs(ops, dtype):
+    """The graph advances its own state; each replay is compared with an eager step on a copy, with eager work between."""
+    st = decode_state(ops)
+    inputs = [[rand(200 + 3 * i + j, 5, 1, 4 if j == 0 else 2, 64, dtype=dtype).cuda() for j in range(3)] for i in range(7)]
+    hold = [x.clone() for x in inputs[0]]
+    other = copied(st)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        want = decode_step(ops, other, *inputs[0], window=30)  # also the call before the capture
+        warm = copied(st)
+        decode_step(ops, warm, *hold, window=30)
+    torch.cuda.synchronize()
+    other = copied(st)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        got = decode_step(ops, st, *hold, window=30)
+    same_bits(everything(st), everything(other))  # capturing runs nothing
+    for i in range(7):
+        for h, x in zip(hold, inputs[i]):
+            h.copy_(x)
+        graph.replay()
+        want = decode_step(ops, other, *inputs[i], window=30)
+        torch.cuda.synchronize()
+        same_bits(got, want)
+        same_bits(everything(st), everything(other))
+        if i % 2:
+            rand(1, 100).cuda().sum().item()
+
+
+def test_two_graphs_in_turn(ops):
+    """Two captured calls that want workspaces, replayed one after the other, over and over."""
+    pool = on_gpu(ops, filled(2, 300, 1, 64, 16, "int8"), "int8")
+    table = dev(numbered(2, [140, 140], 140, 300))
+    lens = i32([2200, 1999])
+    q = [dev(rand(210 + i, 2, 1, 8, 64)) for i in range(2)]
+    want = [[t.clone() for t in ops.attention(x, pool, table, lens)] for x in q]
+    graphs, got = [], []
+    for x in q:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            got.append(ops.attention(x, pool, table, lens))
+        graphs.append(g)
+    for _ in range(4):
+        for g in graphs:
+            g.replay()
+        for t in (*got[0], *got[1]):
+            assert torch.isfinite(t).all()
+        for w, y in zip(want, got):
+            same_bits(w, y)
+        for y in got:
+            for t in y:
+                t.fill_(float("nan"))
+
+
+def test_streams(ops):
+    """On a stream of the caller's, whose earlier work makes the inputs; and two calls at once on two streams."""
+    pool = on_gpu(ops, filled(3, 300, 2, 128, 16, "e4m3"), "e4m3")
+    table, lens = dev(numbered(3, [140, 140], 140, 300)), i32([2200, 1500])
+    qs = [dev(rand(220 + i, 2, 3, 4, 128, dtype=torch.bfloat16)) for i in range(2)]
+    want = [[t.clone() for t in ops.attention(x, pool, table, lens)] for x in qs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(5):
+        got = []
+        for s, x in zip(streams, qs):
+            with torch.cuda.stream(s):
+                late = torch.zeros(1 << 24, device="cuda").add_(1).sum() * 0  # work before the input is there
+                got.append(ops.attention((x.float() + late).to(x.dtype), pool, table, lens))
+        torch.cuda.synchronize()
+        for w, y in zip(want, got):
+            same_bits(w, y)
+
+
+@pytest.mark.parametrize("code", CODES)
+def test_a_pool_past_4_gib(ops, code):
+    """Pages whose codes lie past 2^32 bytes, and past 2^31 elements, act as low ones do."""
+    kv, dh, page, n_pages = 8, 128, 128, 33500
+    pool = ops.Pool(*(torch.empty((n_pages, kv, *s), dtype=torch.uint8, device="cuda").view(CODES[code]) for s in ((dh // 16, page, 16), (page // 16, dh, 16))),
+                    *(torch.zeros((n_pages, kv), device="cuda") for _ in range(2)))
+    assert pool.k.numel() > 1 << 32
+    tables = [dev(np.array([[0, 1, 2], [3, 4, 5]], np.int32)), dev(np.array([[33499, 33000, 16500], [33498, 16384, 32768]], np.int32))]
+    k, v = dev(rand(230, 2, 300, kv, dh)), dev(rand(231, 2, 300, kv, dh))
+    got = []
+    for t in tables:
+        for start, n in ((0, 200), (200, 100)):
+            ops.append(pool, t, i32([start, start]), k[:, start:start + n], v[:, start:start + n])
+        few = ops.attention(dev(rand(232, 2, 1, 32, dh)), pool, t, i32([300, 299]))
+        many = ops.attention(dev(rand(233, 2, 600, 64, dh, dtype=torch.bfloat16)), pool, t, i32([300, 299]), causal=False)
+        got.append([*few, *many])
+    same_bits(*got)
+    # and moved: pages in use are the three highest
+    refs = torch.zeros(n_pages, dtype=torch.int32, device="cuda")
+    t = dev(np.array([[33499, 33000, 16500]], np.int32))
+    refs[t[0].long()] = 1
+    before = [x[t[0].long()].view(torch.uint8) for x in pool]
+    lead = ops.Pool(*(x[None] for x in pool))
+    assert ops.compact(t, refs, lead).item() == 3
+    assert sorted(t[0].tolist()) == [0, 1, 2]
+    same_bits(before, [x[t[0].long()] for x in pool])
+
+
+def test_equal_calls_give_equal_bits_and_writes_count(ops):
+    pool = on_gpu(ops, filled(4, 300, 2, 128, 16, "e4m3"), "e4m3")
+    table, lens = dev(numbered(4, [140, 140], 140, 300)), i32([2200, 1500])
+    q = dev(rand(240, 2, 3, 8, 128, dtype=torch.bfloat16))
+    first = [t.clone() for t in ops.attention(q, pool, table, lens)]
+    for _ in range(3):
+        same_bits(first, ops.attention(q, pool, table, lens))
+    out, lse = torch.empty_like(q), torch.empty(2, 3, 8, device="cuda")
+    refs = torch.ones(300, dtype=torch.int32, device="cuda")
+    k = dev(rand(241, 2, 1, 2, 128))
+
+    def moved_on(call, *tensors):
+        before = [t._version for t in tensors]
+        call()
+        assert all(t._version > b for t, b in zip(tensors, before))
+
+    moved_on(lambda: ops.attention(q, pool, table, lens, out=out, lse=lse), out, lse)
+    moved_on(lambda: ops.append(pool, table, lens, k, k), *pool)
+    moved_on(lambda: ops.resize(table, lens, refs, lens - 1, pool), table, lens, refs, *pool)
+    moved_on(lambda: ops.reorder(table, lens, refs, i32([1, 0]), 16), table, lens, refs)
+    moved_on(lambda: ops.compact(table, refs, pool), table, refs, *pool)
+    x = q.clone()
+    moved_on(lambda: ops.norm_rope(x, q_out=x), x)
+    with torch.inference_mode():
+        same_bits([ops.norm_rope(q)[0]], [ops.norm_rope(q.clone())[0]])
