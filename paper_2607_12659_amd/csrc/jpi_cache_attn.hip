@@ -1,25 +1,35 @@
 // Attention over a paged cache in 8 bits (jpi_cache_attention, include/jpi_cache.h).
 //
 // The query rows of a sequence that read one KV head (tokens x the heads on it)
-// are tiles of 32; a workgroup's four waves take one row tile and share out its
-// keys in tiles of 32, wave w the tiles w, w + 4 ..., and join their sums in LDS.
-// Where there are few row tiles the keys are cut into ranges as well, by the
-// sequence's own length, and k_cache_join adds them up.
+// form one matrix.  Products use matrix instructions in bf16 with the operands
+// swapped, S^T = K q^T and O^T = V^T P^T, so that a lane has one query row, and
+// the lanes of a row (two or four groups) 16 keys of it each.  Codes are exact in
+// bf16 (eight significant bits hold -128 .. 127 and every e4m3 number), so a page's
+// scale can wait: that of K goes into the score, that of V into the probability.
+// fp32 queries and probabilities are taken in three bf16 parts, whose 24 bits lose
+// nothing: three products each at 16 times the fp32 instructions' rate.
 //
-// Products use 32 x 32 matrix instructions in bf16 with the operands swapped, S^T
-// = K q^T and O^T = V^T P^T: one query row in each lane (lane % 32), a half wave
-// (lane / 32) of a row's keys each.  Codes are exact in bf16 (eight significant
-// bits hold -128 .. 127 and every e4m3 number), so a page's scale can wait: that of
-// K goes into the score, that of V into the probability, both one number per 16
-// keys.  fp32 queries and probabilities are taken in three bf16 parts, whose 24
-// bits lose nothing, for three products each: 2/5 of the bf16 rate would be left
-// of them, the fp32 instructions have 1/16.
+// The pages' layout gives a lane its operands in pieces of 16 bytes, and what a
+// wave asks for lies in runs of 64 bytes and more: 16 dims of a key, 16 keys of a
+// dim.  Rows of S^T take the tile's keys in such an order (Tile::key) that a lane's
+// 16 scores are of 16 neighbouring keys: one piece of V, one page, one scale.
 //
-// The pages' layout gives a lane its operands in pieces of 16 bytes, and a half
-// wave's are 512 bytes in a row, so K and V go from memory to registers without
-// LDS: 16 dims of a key, 16 keys of a dim.  Row i of S^T takes key 16 ((i >> 2) & 1)
-// + 4 (i >> 3) + (i & 3) of the tile, so that register r of half h of the product is
-// key 16 h + r: a half's keys are one piece of V, with one page and one scale.
+// Few rows (k_cache_attn): tiles of 16 rows; a workgroup's four waves share out the
+// keys of one, 64 at a time from memory to registers, and join their sums in LDS;
+// where there are fewer than 256 row tiles the keys are cut into ranges as well, by
+// the sequence's own length, and joined by a second launch.  Bound by memory where
+// keys are many: sixty-four sequences of up to 8192 slots, 8 KV heads of 128 dims,
+// 547 MB, 116 us, 4.7 TB/s (a copy reaches 4.8).  One row tile before 817 slots of
+// 256 dims takes 9 us whatever its range, a chain of length, table, page and
+// products, and the join 3.
+//
+// Many rows (k_cache_rows): tiles of 32 rows, four of them sharing the keys that
+// direct-to-LDS loads bring, 64 a step, up to three steps ahead.  Bound by the
+// instructions between the products: 128 of a step's 340 widen codes, and a step
+// takes 3700 cycles of a wave, 1024 of them its products.  Two waves of a SIMD
+// share that time: 4096 rows of 32 heads on 8 of 128 before 4096 keys 0.92 PFLOP/s,
+// a window of 1024 over 4099 tokens 90 us, 0.67 PFLOP/s of what is seen (a library
+// product of 8192^3 reaches 1.2).
 #include <algorithm>
 #include <type_traits>
 
@@ -30,7 +40,7 @@ namespace {
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
-constexpr int WAVES = 4;
+constexpr int WAVES = 4, GROUP_ROWS = 32 * WAVES;  // rows of a workgroup of the ring
 constexpr float LOG2E = 1.44269504088896341f, LN2 = 0.693147180559945309f;
 constexpr float HEADROOM = 16.f;  // log2 of the most that a probability may exceed its row's reference by
 
@@ -131,6 +141,20 @@ __device__ __forceinline__ void split8(const float* x, bf16x8 (&part)[PARTS]) {
 // bits 0 .. n - 1 of 16
 __device__ __forceinline__ u32 below(int n) { return (1u << min(max(n, 0), 16)) - 1; }
 
+// What a step needs of the scales of 16 keys.  Probabilities times V's scale: with a power of two, all that append writes, that
+// is a whole number in the exponent, and a factor of the sum of the 16.
+struct Scales {
+  float f;        // scores to powers of two: K's scale * scale / ln 2
+  float e;        // V's scale is 2^e, or 0
+  float unscale;  // 2^-e; 0: V's scale is no power of two, or could take a probability out of fp32
+  float vs;       // V's scale
+};
+__device__ __forceinline__ Scales scales_of(float qscale, float ks, float vs) {
+  const u32 bits = __builtin_bit_cast(u32, vs);
+  const bool power = (bits & 0x807fffffu) == 0 && (bits >> 23) - (127 - 64) <= 128;
+  return {qscale * ks, power ? (float)((int)(bits >> 23) - 127) : 0.f, power ? __builtin_bit_cast(float, (254u << 23) - bits) : 0.f, vs};
+}
+
 // A wave's row tile: the lane's row, its queries, and the running maximum, sum and O^T of its softmax.  A step takes NT times
 // 16 keys of each lane group, one page and one scale each.
 template <int DH, bool E4M3, typename T, int R, int NT>
@@ -185,11 +209,19 @@ struct Rows {
     m_ref = -INFINITY, sum = 0.f;
   }
 
-  // One step's keys from slot0 on, with the scales of the lane's pieces; keys(j, kk) and values(t, d) are those, and
-  // `between` is called when the keys have been used.
-  template <typename KF, typename VF, typename B>
-  __device__ __forceinline__ void step(int slot0, const float (&ks)[NT], const float (&vs)[NT], KF keys, VF values, B between) {
-    float sc[16 * NT];
+  // One step's keys from slot0 on, with the scales of the lane's pieces, in parts that a loop may order as it likes.
+  struct Step {
+    int slot0;
+    bool whole, fast;  // all its keys are seen by all rows; its probabilities carry V's scale in their exponent
+    u32 seen[NT];
+    Scales sc[NT];
+    float p[16 * NT];  // scores, then probabilities times V's scale
+    float sum;         // of the probabilities, if fast
+  };
+
+  // q k^T of the codes; keys(j, kk) are the pieces
+  template <typename KF>
+  __device__ __forceinline__ void scores(float (&sc)[16 * NT], KF keys) const {
 #pragma unroll
     for (int j = 0; j < SETS; ++j) {
       typename M::acc c;
@@ -208,32 +240,35 @@ struct Rows {
 #pragma unroll
       for (int e = 0; e < REGS; ++e) sc[j * REGS + e] = c[e];
     }
-    between();
-    __builtin_amdgcn_s_setprio(1);  // the other wave's products fill the time of these instructions, not the other way round
-    // The scores' share of the softmax, in powers of two, and of O.  One path, with masks aside: with one path for tiles that
-    // are seen whole and one for others, or tiles left out, O was copied from register to register for each tile.
-    const bool whole = slot0 + KEYS <= full_hi && (slot0 >= full_lo || slot0 + KEYS <= sinks);
-    u32 seen[NT];
+  }
+
+  // Masks, and the row's reference.  One path for all steps, with masks aside: with one path for those that are seen whole and
+  // one for others, or steps left out, O was copied from register to register in each.
+  __device__ __forceinline__ void refer(Step& x) {
+    x.whole = x.slot0 + KEYS <= full_hi && (x.slot0 >= full_lo || x.slot0 + KEYS <= sinks);
 #pragma unroll
-    for (int t = 0; t < NT; ++t) seen[t] = 0xffffu;
-    if (!whole) {
+    for (int t = 0; t < NT; ++t) x.seen[t] = 0xffffu;
+    if (!x.whole) {
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
-        const int slot = slot0 + 16 * (G * t + grp);
-        seen[t] = below(see_hi - slot) & (~below(see_lo - slot) | below(sinks - slot));
+        const int slot = x.slot0 + 16 * (G * t + grp);
+        x.seen[t] = below(see_hi - slot) & (~below(see_lo - slot) | below(sinks - slot));
+        u32 seen = x.seen[t];
+        asm volatile("" : "+v"(seen));
 #pragma unroll
-        for (int e = 0; e < 16; ++e) sc[16 * t + e] = seen[t] >> e & 1 ? sc[16 * t + e] : -INFINITY;
+        for (int e = 0; e < 16; ++e) x.p[16 * t + e] = seen >> e & 1 ? x.p[16 * t + e] : -INFINITY;
       }
     }
     float top = -INFINITY;
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-      const float* x = sc + 16 * t;
-      float t0 = fmaxf(fmaxf(x[0], x[1]), x[2]), t1 = fmaxf(fmaxf(x[3], x[4]), x[5]);
-      t0 = fmaxf(fmaxf(t0, x[6]), x[7]), t1 = fmaxf(fmaxf(t1, x[8]), x[9]);
-      t0 = fmaxf(fmaxf(t0, x[10]), x[11]), t1 = fmaxf(fmaxf(t1, x[12]), x[13]);
-      t0 = fmaxf(fmaxf(t0, t1), fmaxf(x[14], x[15])) * (qscale * ks[t]);
-      top = seen[t] == 0 ? top : fmaxf(top, t0);  // -inf * 0
+      const float* y = x.p + 16 * t;
+      float t0 = fmaxf(fmaxf(y[0], y[1]), y[2]), t1 = fmaxf(fmaxf(y[3], y[4]), y[5]);
+      t0 = fmaxf(fmaxf(t0, y[6]), y[7]), t1 = fmaxf(fmaxf(t1, y[8]), y[9]);
+      t0 = fmaxf(fmaxf(t0, y[10]), y[11]), t1 = fmaxf(fmaxf(t1, y[12]), y[13]);
+      t0 = fmaxf(fmaxf(t0, t1), fmaxf(y[14], y[15])) * x.sc[t].f;
+      t0 = x.seen[t] == 0 ? -INFINITY : t0;  // -inf * 0
+      top = fmaxf(top, t0);
     }
     top = groups_max<R>(top);
     if (__any(top > m_ref + HEADROOM || (m_ref == -INFINITY && top > -INFINITY))) {
@@ -247,71 +282,80 @@ struct Rows {
         for (int e = 0; e < REGS; ++e) o[d][e] *= g;
       m_ref = now;
     }
-    // Probabilities times V's scale: with a power of two, all that append writes, that is a whole number in the exponent and a
-    // factor of the lane's sum; others, and those that could take a probability out of fp32, are multiplied with
-    bool power[NT], fast = true;
+    // Other scales of V, and masks where K's scale makes no -inf of -inf, are seen to one by one
+    int fast = 1;  // no && and ||, which would be branches
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+      fast &= (int)(x.sc[t].unscale != 0.f) & ((int)x.whole | (int)(x.sc[t].f > 0.f) | (int)(x.seen[t] == 0xffffu));
+    x.fast = __all(fast);
+  }
+
+  __device__ __forceinline__ void probabilities(Step& x) const {
+    const float ref = m_ref == -INFINITY ? 0.f : m_ref;
+    x.sum = 0.f;
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-      const u32 bits = __builtin_bit_cast(u32, vs[t]);
-      power[t] = (bits & 0x807fffffu) == 0 && (bits >> 23) - (127 - 64) <= 128;
-      fast = fast && (power[t] || seen[t] == 0);
-    }
-    fast = __all(fast);
-    float p[16 * NT];
-#pragma unroll
-    for (int t = 0; t < NT; ++t) {
-      const u32 bits = __builtin_bit_cast(u32, vs[t]);
-      const bool in = fast && power[t];
-      const float f = qscale * ks[t], ref = (m_ref == -INFINITY ? 0.f : m_ref) - (in ? (float)((int)(bits >> 23) - 127) : 0.f);
-#pragma unroll
-      for (int e = 0; e < 16; ++e) p[16 * t + e] = __builtin_amdgcn_exp2f(fmaf(sc[16 * t + e], f, -ref));
-      if (!whole) {
-#pragma unroll
-        for (int e = 0; e < 16; ++e) p[16 * t + e] = seen[t] >> e & 1 ? p[16 * t + e] : 0.f;
-      }
+      const float r = x.fast ? ref - x.sc[t].e : ref;
       float part[4];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) part[e] = (p[16 * t + e] + p[16 * t + 4 + e]) + (p[16 * t + 8 + e] + p[16 * t + 12 + e]);
-      sum = fmaf((part[0] + part[1]) + (part[2] + part[3]), in ? __builtin_bit_cast(float, (254u << 23) - bits) : 1.f, sum);
+      for (int e = 0; e < 16; ++e) {
+        float& p = x.p[16 * t + e];
+        p = __builtin_amdgcn_exp2f(fmaf(p, x.sc[t].f, -r));
+        part[e & 3] = e < 4 ? p : part[e & 3] + p;
+      }
+      x.sum = fmaf((part[0] + part[1]) + (part[2] + part[3]), x.sc[t].unscale, x.sum);
     }
-    if (!fast) {
+  }
+
+  // The row's sum, and what probabilities() could not do
+  __device__ __forceinline__ void settle(Step& x) {
+    if (!x.fast) {
+      x.sum = 0.f;
 #pragma unroll
-      for (int t = 0; t < NT; ++t)
+      for (int t = 0; t < NT; ++t) {
+        u32 seen = x.seen[t];
+        asm volatile("" : "+v"(seen));  // its tests stay here: 32 of them were made in every step
 #pragma unroll
-        for (int e = 0; e < 16; ++e) p[16 * t + e] = seen[t] >> e & 1 ? p[16 * t + e] * vs[t] : 0.f;  // 0 * NaN
+        for (int e = 0; e < 16; ++e) {
+          float& p = x.p[16 * t + e];
+          p = seen >> e & 1 ? p : 0.f;
+          x.sum += p;
+          p = seen >> e & 1 ? p * x.sc[t].vs : 0.f;  // 0 * NaN
+        }
+      }
     }
-    __builtin_amdgcn_s_setprio(0);
+    sum += x.sum;
+  }
+
+  // the bytes of a piece of V whose slots, from `slot` on, lie before the length: codes past it may be anything
+  __device__ __forceinline__ u32x4 valid(int slot) const {
+    u32x4 v;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int bytes = min(max(len - slot - 4 * e, 0), 4);
+      v[e] = bytes == 4 ? ~0u : (1u << (8 * bytes)) - 1;
+    }
+    return v;
+  }
+
+  // O += P V; values(t, d) are V's pieces, without what lies past the length
+  template <typename VF>
+  __device__ __forceinline__ void add(const Step& x, VF values) {
     bf16x8 pp[NT][2][PARTS];
 #pragma unroll
-    for (int t = 0; t < NT; ++t) split8<PARTS>(p + 16 * t, pp[t][0]), split8<PARTS>(p + 16 * t + 8, pp[t][1]);
-    u32x4 w[NT][DT];
+    for (int t = 0; t < NT; ++t) split8<PARTS>(x.p + 16 * t, pp[t][0]), split8<PARTS>(x.p + 16 * t + 8, pp[t][1]);
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
-      for (int d = 0; d < DT; ++d) w[t][d] = values(t, d);
-    if (!whole) {  // codes past the length may be anything
-#pragma unroll
-      for (int t = 0; t < NT; ++t) {
-        u32x4 valid;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int bytes = min(max(len - slot0 - 16 * (G * t + grp) - 4 * e, 0), 4);
-          valid[e] = bytes == 4 ? ~0u : (1u << (8 * bytes)) - 1;
-        }
-#pragma unroll
-        for (int d = 0; d < DT; ++d) w[t][d] &= valid;
-      }
-    }
-#pragma unroll
-    for (int d = 0; d < DT; ++d)
-#pragma unroll
-      for (int t = 0; t < NT; ++t)
+      for (int d = 0; d < DT; ++d) {
+        const u32x4 w = values(t, d);
 #pragma unroll
         for (int m = 0; m < 2; ++m) {
-          const bf16x8 codes = C::widen8(w[t][d][2 * m], w[t][d][2 * m + 1]);
+          const bf16x8 codes = C::widen8(w[2 * m], w[2 * m + 1]);
 #pragma unroll
           for (int i = PARTS - 1; i >= 0; --i) o[d] = M::mfma(codes, pp[t][m][i], o[d]);
         }
+      }
   }
 
   __device__ __forceinline__ f32x4 quad(int i) const {
@@ -392,7 +436,7 @@ __global__ __launch_bounds__(64 * WAVES, DH == 256 ? 1 : 2) void k_cache_attn(Ca
 
   // pages of the lane's K and V pieces of the next tile, and the present one's scales
   int kid = NO_PAGE, vid = NO_PAGE;
-  float ks[1] = {0.f}, vs[1] = {0.f};
+  float ks = 0.f, vs = 0.f;
   if (first < last) {
     const int t = x.tile(first);
     const int k0 = page_at(t * KEYS + kpiece), v0 = page_at(t * KEYS + 16 * grp);
@@ -400,7 +444,7 @@ __global__ __launch_bounds__(64 * WAVES, DH == 256 ? 1 : 2) void k_cache_attn(Ca
       const int t1 = x.tile(first + WAVES);
       kid = page_at(t1 * KEYS + kpiece), vid = page_at(t1 * KEYS + 16 * grp);
     }
-    ks[0] = scale_at(a, a.k_scale, v0, h), vs[0] = scale_at(a, a.v_scale, v0, h);
+    ks = scale_at(a, a.k_scale, v0, h), vs = scale_at(a, a.v_scale, v0, h);
     load_k(t, k0);
     load_v(t, v0);
   }
@@ -413,16 +457,23 @@ __global__ __launch_bounds__(64 * WAVES, DH == 256 ? 1 : 2) void k_cache_attn(Ca
       const int t2 = x.tile(n + 2 * WAVES);
       kid = page_at(t2 * KEYS + kpiece), vid = page_at(t2 * KEYS + 16 * grp);
     }
-    float ks1 = 0.f, vs1 = 0.f;
-    w.step(
-        t * KEYS, ks, vs, [&](int j, int kk) { return kraw[j][kk]; }, [&](int, int d) { return vraw[d]; },
-        [&] {
-          if (!more) return;
-          ks1 = scale_at(a, a.k_scale, vid1, h), vs1 = scale_at(a, a.v_scale, vid1, h);
-          load_k(next, kid1);
-        });
+    typename W::Step st;
+    st.slot0 = t * KEYS, st.sc[0] = scales_of(a.qscale, ks, vs);
+    w.scores(st.p, [&](int j, int kk) { return kraw[j][kk]; });
+    if (more) {
+      ks = scale_at(a, a.k_scale, vid1, h), vs = scale_at(a, a.v_scale, vid1, h);
+      load_k(next, kid1);
+    }
+    w.refer(st);
+    w.probabilities(st);
+    w.settle(st);
+    if (st.slot0 + KEYS > x.len) {
+      const u32x4 valid = w.valid(st.slot0 + 16 * grp);
+#pragma unroll
+      for (int d = 0; d < W::DT; ++d) vraw[d] &= valid;
+    }
+    w.add(st, [&](int, int d) { return vraw[d]; });
     if (more) load_v(next, vid1);
-    ks[0] = ks1, vs[0] = vs1;
   }
 
   // the four waves' sums, brought to one reference and added in their order
@@ -472,7 +523,7 @@ template <int DH>
 struct Ring {
   static constexpr int KEYS = 64, PIECES = DH / 8;  // KB of a step: K of 32 keys, of the next 32, then V so, in the order of a lane's reads
   static constexpr int LOADS = PIECES / WAVES;      // of a wave for a step
-  static constexpr int STAGES = DH == 64 ? 4 : 3;
+  static constexpr int STAGES = 4;
 };
 
 // 16 bytes of each lane to LDS at `to` + 16 * lane.  As assembly, which has no register outputs: loads to LDS that the
@@ -489,8 +540,8 @@ __device__ __forceinline__ void load_to_lds(const void* base, u32 offset, u32 to
 
 // What a ring's steps are made of, in LDS: for each 16 keys of the next ones the page's place in the pool and its scales
 struct Piece16 {
-  u32 at;  // page * KV heads + head
-  float ks, vs;
+  Scales sc;
+  u32 at;  // page * KV heads + head: 2^32 of them, of 1 KB at least, are more than a device holds
 };
 constexpr int AHEAD = 16;  // steps of a block of these; two blocks are held
 
@@ -509,9 +560,12 @@ __global__ __launch_bounds__(64 * WAVES, DH == 256 ? 1 : 2) void k_cache_rows(Ca
   const int pairs = a.n_seqs * a.kv;
   const int pair = blockIdx.x % pairs, s = pair / a.kv, h = pair - s * a.kv;
   // the last rows of causal ones see most: they come first
-  const int group = gridDim.x / pairs - 1 - blockIdx.x / pairs, rt = group * WAVES + wave;
-  const Span all = span_of<R * WAVES, KEYS>(a, s, group);
-  if (group * WAVES * R >= all.rows) return;
+  const int rest = (gridDim.x - 1 - blockIdx.x) / pairs, split = rest % a.splits, group = rest / a.splits, rt = group * WAVES + wave;
+  const Span all = span_of<GROUP_ROWS, KEYS>(a, s, group);
+  if (group * GROUP_ROWS >= all.rows) return;
+  const int per = per_range(all.count, a.splits), ranges = ranges_of(all.count, per), first = split * per;
+  if (split >= ranges) return;
+  const int count = min(per, all.count - first);  // of steps, from `first` on
   // a wave without rows computes others' again; steps left out would have O copied from register to register in each
   const int own = min(rt, (all.rows - 1) / R);
   const Span x = span_of<R, KEYS>(a, s, own);
@@ -521,10 +575,11 @@ __global__ __launch_bounds__(64 * WAVES, DH == 256 ? 1 : 2) void k_cache_rows(Ca
   const int32_t* table = a.table + s * a.table_stride;
   auto look_up = [&](int block) {  // by one wave: the pieces of a block of steps
     const int n = block * AHEAD + (lane >> 2);
-    if (n >= all.count) return;
-    const int slot = all.tile(n) * KEYS + 16 * (lane & 3);
+    if (n >= count) return;
+    const int slot = all.tile(first + n) * KEYS + 16 * (lane & 3);
     const int id = slot < all.len ? table[slot >> a.lg_page] : NO_PAGE;
-    pieces[block & 1][lane >> 2][lane & 3] = Piece16{(u32)page_of(a, id, h), scale_at(a, a.k_scale, id, h), scale_at(a, a.v_scale, id, h)};
+    pieces[block & 1][lane >> 2][lane & 3].sc = scales_of(a.qscale, scale_at(a, a.k_scale, id, h), scale_at(a, a.v_scale, id, h));
+    pieces[block & 1][lane >> 2][lane & 3].at = (u32)page_of(a, id, h);
   };
   if (wave == 0) look_up(0);
   if (wave == 1) look_up(1);
@@ -543,12 +598,19 @@ __global__ __launch_bounds__(64 * WAVES, DH == 256 ? 1 : 2) void k_cache_rows(Ca
     tile[i] = piece / W::KK, unit[i] = piece % W::KK;  // as many units of K as of V
   }
   const bool one_page = a.lg_page >= 6;
-  auto issue = [&](int n, int stage) {
-    const int t0 = all.tile(n) * KEYS;
+  // places of the pieces of the next step to be asked for: read a step before, since what depends on them waits for LDS
+  u32 place[RG::LOADS];
+  auto look = [&](int n) {
     const Piece16* at = pieces[n / AHEAD & 1][n % AHEAD];
+#pragma unroll
+    for (int i = 0; i < RG::LOADS; ++i)
+      if (i == 0 || !one_page) place[i] = at[one_page ? 0 : 2 * tile[i] + (i < HALF ? key0 >> 4 : grp)].at;
+  };
+  auto issue = [&](int n, int stage) {
+    const int t0 = all.tile(first + n) * KEYS;
     const u32 to = lds + stage * STAGE;
     if (one_page) {  // of all 64 keys: its place is the same for all lanes
-      const uint64_t base = (uint64_t)(u32)__builtin_amdgcn_readfirstlane((int)at[0].at) * page_bytes;
+      const uint64_t base = (uint64_t)(u32)__builtin_amdgcn_readfirstlane((int)place[0]) * page_bytes;
       const uint8_t *kp = a.k + base + (u32)(t0 & mask) * 16, *vp = a.v + base + (u32)(t0 & mask) * DH;
 #pragma unroll
       for (int i = 0; i < RG::LOADS; ++i) {
@@ -559,109 +621,188 @@ __global__ __launch_bounds__(64 * WAVES, DH == 256 ? 1 : 2) void k_cache_rows(Ca
 #pragma unroll
       for (int i = 0; i < RG::LOADS; ++i) {
         const int slot = t0 + tile[i] * 32 + (i < HALF ? key0 : 16 * grp);
-        const uint64_t base = (uint64_t)at[2 * tile[i] + (i < HALF ? key0 >> 4 : grp)].at * page_bytes;
+        const uint64_t base = (uint64_t)place[i] * page_bytes;
         const u32 in = i < HALF ? (((2 * unit[i] + grp) << a.lg_page) + (slot & mask)) * 16 : (slot & mask) * DH + unit[i] * 512 + col * 16;
         load_to_lds((i < HALF ? a.k : a.v) + base + in, to + i * WAVES * 1024);
       }
     }
   };
 
-  const int count = all.count;
+  constexpr int S = RG::STAGES;
 #pragma unroll
-  for (int n = 0; n < RG::STAGES - 1; ++n)
-    if (n < count) issue(n, n);
-  int stage = 0;
+  for (int n = 0; n < S - 1; ++n)
+    if (n < count) look(n), issue(n, n);
+  look(min(S - 1, max(count - 1, 0)));
+  // Step n's softmax is between the products of the keys after it and of its own values: those of one fill the time of the other.
+  auto arrived = [&](int later) {  // everybody's loads but those of the `later` latest steps are there, and all are done with before
+    wait_later<RG::LOADS, S - 2>(later);
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+  };
+  auto keys_of = [&](int stage) {
+    const char* at = ring + stage * STAGE + lane * 16;
+    return [at](int j, int kk) { return *reinterpret_cast<const u32x4*>(at + (j * W::KK + kk) * 1024); };
+  };
+  typename W::Step st;
+  arrived(min(S - 2, max(count - 1, 0)));
+  if (count > 0) w.scores(st.p, keys_of(0));
   for (int n = 0; n < count; ++n) {
-    wait_later<RG::LOADS, RG::STAGES - 2>(min(RG::STAGES - 2, count - 1 - n));
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_s_barrier();  // the step's keys are there, and everybody is done with those before
-    asm volatile("" ::: "memory");
+    const int stage = n % S, next = (n + 1) % S;
+    arrived(min(S - 3, max(count - 2 - n, 0)));
     if (n % AHEAD == 0 && n > 0 && wave == 0) {  // the block before is done with; seen at the next barrier, used after it
       look_up(n / AHEAD + 1);
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     }
-    if (n + RG::STAGES - 1 < count) issue(n + RG::STAGES - 1, stage == 0 ? RG::STAGES - 1 : stage - 1);
-    const Piece16 *mine = pieces[n / AHEAD & 1][n % AHEAD], p0 = mine[grp], p1 = mine[2 + grp];
-    const float ks[2] = {p0.ks, p1.ks}, vs[2] = {p0.vs, p1.vs};
-    const char* at = ring + stage * STAGE + lane * 16;
-    w.step(
-        all.tile(n) * KEYS, ks, vs, [&](int j, int kk) { return *reinterpret_cast<const u32x4*>(at + (j * W::KK + kk) * 1024); },
-        [&](int t, int d) { return *reinterpret_cast<const u32x4*>(at + (2 * W::KK + t * W::DT + d) * 1024); }, [] {});
-    stage = stage == RG::STAGES - 1 ? 0 : stage + 1;
+    if (n + S - 1 < count) issue(n + S - 1, (n + S - 1) % S);
+    look(min(n + S, count - 1));
+    u32x4 k[2][W::KK];  // asked for before they are needed
+    const char* keys = ring + next * STAGE + lane * 16;
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int kk = 0; kk < W::KK; ++kk) k[j][kk] = *reinterpret_cast<const u32x4*>(keys + (j * W::KK + kk) * 1024);
+    const Piece16* mine = pieces[n / AHEAD & 1][n % AHEAD];
+    char* values = ring + stage * STAGE + (2 * W::KK) * 1024 + lane * 16;
+    st.slot0 = all.tile(first + n) * KEYS;
+    st.sc[0] = mine[grp].sc, st.sc[1] = mine[2 + grp].sc;
+    if (st.slot0 + KEYS > all.len) {  // the sequence's last step
+#pragma unroll
+      for (int i = 0; i < HALF; ++i) {
+        u32x4* at = reinterpret_cast<u32x4*>(values + (wave + WAVES * i) * 1024);
+        *at &= w.valid(st.slot0 + 32 * tile[i] + 16 * grp);
+      }
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+    }
+    w.refer(st);
+    float after[32];
+    w.probabilities(st);
+    w.scores(after, [&](int j, int kk) { return k[j][kk]; });  // behind the last step of what lies there; not used
+    u32x4 v[2][W::DT];
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int d = 0; d < W::DT; ++d) v[t][d] = *reinterpret_cast<const u32x4*>(values + (t * W::DT + d) * 1024);
+    w.settle(st);
+    w.add(st, [&](int t, int d) { return v[t][d]; });
+#pragma unroll
+    for (int e = 0; e < 32; ++e) st.p[e] = after[e];
   }
 
   const float total = groups_sum<R>(w.sum), norm = total == 0.f ? 0.f : 1.f / total;
   if (rt * R + col >= x.rows) return;
+  if (ranges > 1) {
+    const int64_t at = (int64_t)((group * a.splits + split) * pairs + pair) * GROUP_ROWS + wave * R + col;
+    if (grp == 0) a.stats[at] = float2{w.m_ref, total};
+#pragma unroll
+    for (int i = 0; i < W::QUADS; ++i) put4(a.part + at * DH + W::M::dim(i, grp), w.quad(i));
+    return;
+  }
   T* out = reinterpret_cast<T*>(a.out) + s * a.o_outer + w.token * a.o_row + w.head * a.o_head;
   if (grp == 0 && a.lse) a.lse[((int64_t)s * a.q_rows + w.token) * a.n_heads + w.head] = lse_of(w.m_ref, total);
 #pragma unroll
   for (int i = 0; i < W::QUADS; ++i) put4(out + W::M::dim(i, grp), w.quad(i) * norm);
 }
 
-// One row of a row tile whose keys were cut into ranges: a workgroup adds up the ranges that have any.  Lanes take four dims
-// each, groups of DH / 4 of them one range after the other, and the groups' sums are added in their order.
+// A row whose keys were cut into ranges, and where range i of it is: that of workgroup (rt * splits + i) * pairs + pair
+struct CutRow {
+  int s, token, head, ranges;  // ranges 1: nothing to join, 0: no such row
+  int64_t at, step;
+};
+template <int R>
+__device__ __forceinline__ CutRow cut_row(const CacheArgs& a, int64_t nth) {
+  const int pairs = a.n_seqs * a.kv, per_tile = min(R, a.q_rows * a.group);
+  const int pair = (int)(nth % pairs), rest = (int)(nth / pairs), col = rest % per_tile, rt = rest / per_tile;
+  const int s = pair / a.kv, h = pair - s * a.kv;
+  const Span x = span_of<R, 64>(a, s, rt);
+  const int r = rt * R + col, token = r / a.group;
+  return {s, token, h * a.group + (r - token * a.group), r < x.rows ? ranges_of(x.count, per_range(x.count, a.splits)) : 0,
+          ((int64_t)rt * a.splits * pairs + pair) * R + col, (int64_t)pairs * R};
+}
+template <typename T>
+__device__ __forceinline__ T* out_of(const CacheArgs& a, const CutRow& x) {
+  return reinterpret_cast<T*>(a.out) + x.s * a.o_outer + x.token * a.o_row + x.head * a.o_head;
+}
+
+// Few rows: a workgroup takes one, groups of DH / 4 lanes, of four dims each, its ranges in turn, and the groups' sums are
+// added in their order.
 template <int DH, typename T, int R>
 __global__ __launch_bounds__(256) void k_cache_join(CacheArgs a) {
   constexpr int LANES = DH / 4, GROUPS = 256 / LANES;
   __shared__ __align__(16) f32x4 sums[GROUPS][LANES];
-  const int pairs = a.n_seqs * a.kv, per_tile = min(R, a.q_rows * a.group);
-  const int pair = blockIdx.x % pairs, rest = blockIdx.x / pairs;
-  const int col = rest % per_tile, rt = rest / per_tile;
-  const int s = pair / a.kv, h = pair - s * a.kv;
-  const Span x = span_of<R, 1024 / R>(a, s, rt);
-  const int r = rt * R + col;
-  if (r >= x.rows) return;
-  const int ranges = ranges_of(x.count, per_range(x.count, a.splits));
-  if (ranges == 1) return;
-  const int token = r / a.group, head = h * a.group + (r - token * a.group);
-  // range i of the row tile is workgroup (rt * splits + i) * pairs + pair
-  const int64_t at = ((int64_t)rt * a.splits * pairs + pair) * R + col, step = (int64_t)pairs * R;
-
+  const CutRow x = cut_row<R>(a, blockIdx.x);
+  if (x.ranges <= 1) return;
   float ref = -INFINITY, total = 0.f;
-  for (int i = threadIdx.x & 63; i < ranges; i += 64) ref = fmaxf(ref, a.stats[at + i * step].x);
+  for (int i = threadIdx.x & 63; i < x.ranges; i += 64) ref = fmaxf(ref, a.stats[x.at + i * x.step].x);
   ref = wave_max(ref);
-  for (int i = threadIdx.x & 63; i < ranges; i += 64) {
-    const float2 st = a.stats[at + i * step];
+  for (int i = threadIdx.x & 63; i < x.ranges; i += 64) {
+    const float2 st = a.stats[x.at + i * x.step];
     total += (st.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(st.x - ref)) * st.y;
   }
   total = wave_sum(total);
-
   const int d4 = threadIdx.x % LANES, group = threadIdx.x / LANES;
   f32x4 y = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
-  for (int i = group; i < ranges; i += GROUPS) {
-    const float m = a.stats[at + i * step].x;
+  for (int i = group; i < x.ranges; i += GROUPS) {
+    const float m = a.stats[x.at + i * x.step].x;
     const float g = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - ref);
-    y += g * *reinterpret_cast<const f32x4*>(a.part + (at + i * step) * DH + 4 * d4);
+    y += g * *reinterpret_cast<const f32x4*>(a.part + (x.at + i * x.step) * DH + 4 * d4);
   }
   sums[group][d4] = y;
   __syncthreads();
-  if (threadIdx.x >= LANES) return;
+  if (group != 0) return;
 #pragma unroll
   for (int g = 1; g < GROUPS; ++g) y += sums[g][d4];
   y *= total == 0.f ? 0.f : 1.f / total;
-  T* out = reinterpret_cast<T*>(a.out) + s * a.o_outer + token * a.o_row + head * a.o_head + 4 * d4;
-  if constexpr (sizeof(T) == 2) {
-    typedef bf16 b4 __attribute__((ext_vector_type(4)));
-    *reinterpret_cast<b4*>(out) = b4{(bf16)y[0], (bf16)y[1], (bf16)y[2], (bf16)y[3]};
-  } else {
-    *reinterpret_cast<f32x4*>(out) = y;
+  put4(out_of<T>(a, x) + 4 * d4, y);
+  if (threadIdx.x == 0 && a.lse) a.lse[((int64_t)x.s * a.q_rows + x.token) * a.n_heads + x.head] = lse_of(ref, total);
+}
+
+// Many rows: DH / 4 lanes take a row, all its ranges.  16384 rows of 128 dims in four ranges: the call 109 us with a workgroup
+// for each row, 90 so; 1024 rows in sixteen 39 and 69.
+template <int DH, typename T, int R>
+__global__ __launch_bounds__(256) void k_cache_join_rows(CacheArgs a, int64_t rows) {
+  constexpr int LANES = DH / 4;
+  const int d4 = threadIdx.x % LANES;
+  const int64_t nth = (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
+  if (nth >= rows) return;
+  const CutRow x = cut_row<R>(a, nth);
+  if (x.ranges <= 1) return;
+  float ref = -INFINITY, total = 0.f;
+  for (int i = 0; i < x.ranges; ++i) ref = fmaxf(ref, a.stats[x.at + i * x.step].x);
+  f32x4 y = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int i = 0; i < x.ranges; ++i) {
+    const float2 st = a.stats[x.at + i * x.step];
+    const float g = st.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(st.x - ref);
+    total += g * st.y;
+    y += g * *reinterpret_cast<const f32x4*>(a.part + (x.at + i * x.step) * DH + 4 * d4);
   }
-  if (threadIdx.x == 0 && a.lse)
-    a.lse[((int64_t)s * a.q_rows + token) * a.n_heads + head] = total == 0.f ? -INFINITY : (ref + __builtin_amdgcn_logf(total)) * LN2;
+  y *= total == 0.f ? 0.f : 1.f / total;
+  put4(out_of<T>(a, x) + 4 * d4, y);
+  if (d4 == 0 && a.lse) a.lse[((int64_t)x.s * a.q_rows + x.token) * a.n_heads + x.head] = lse_of(ref, total);
+}
+
+template <int DH, typename T, int R>
+void launch_join(const CacheArgs& a, int64_t rows, hipStream_t s) {
+  if (R > 16 && rows >= 8192) k_cache_join_rows<DH, T, R><<<(unsigned)((rows * DH / 4 + 255) / 256), 256, 0, s>>>(a, rows);
+  else k_cache_join<DH, T, R><<<(unsigned)rows, 256, 0, s>>>(a);
 }
 
 template <int DH, bool E4M3, typename T>
 void launch_typed(const CacheArgs& a, const CachePlan& plan, int pairs, hipStream_t s) {
   if constexpr (sizeof(T) == 2) {
     if (plan.groups) {
-      k_cache_rows<DH, E4M3><<<(unsigned)(pairs * plan.groups), 64 * WAVES, 0, s>>>(a);
+      k_cache_rows<DH, E4M3><<<(unsigned)(pairs * plan.groups * plan.splits), 64 * WAVES, 0, s>>>(a);
+      if (plan.splits > 1)
+        launch_join<DH, T, GROUP_ROWS>(a, (int64_t)pairs * plan.groups * std::min(GROUP_ROWS, a.q_rows * a.group), s);
       return;
     }
   }
   k_cache_attn<DH, E4M3, T, 16><<<(unsigned)(pairs * plan.tiles * plan.splits), 64 * WAVES, 0, s>>>(a);
-  if (plan.splits > 1)
-    k_cache_join<DH, T, 16><<<(unsigned)(pairs * plan.tiles * std::min(16, a.q_rows * a.group)), 256, 0, s>>>(a);
+  if (plan.splits > 1) launch_join<DH, T, 16>(a, (int64_t)pairs * plan.tiles * std::min(16, a.q_rows * a.group), s);
 }
 
 template <int DH>
@@ -675,8 +816,6 @@ void launch_dim(const CacheArgs& a, int code, bool f32, const CachePlan& plan, i
   }
 }
 
-constexpr int GROUP_ROWS = 32 * WAVES;  // of a workgroup of the ring
-
 }  // namespace
 
 CachePlan cache_plan(const jpi_cache_attn& a, const jpi_cache_pool& p, const jpi_cache_seqs& q) {
@@ -685,14 +824,17 @@ CachePlan cache_plan(const jpi_cache_attn& a, const jpi_cache_pool& p, const jpi
   int64_t keys = (int64_t)q.max_pages * p.page;
   if (a.window) keys = std::min<int64_t>(keys, (int64_t)a.window + a.sinks + GROUP_ROWS / group + 2 * 64);
   CachePlan plan{};
-  // The ring from a workgroup for each compute unit on (of 256 dims, which the other kernel holds in two rounds of registers,
-  // from less than half of that); fp32 has three times the products and none of its time in what the ring saves.  us, ring
-  // and other: 1024 rows of 32 heads on 8 of 128, 256 workgroups, 32 and 32; 2048 rows 60 and 90; 512 rows 19 and 14; 64, 32
-  // and 16 chunks of 50 rows, 8 heads of 256, 866 slots: 48, 47 and 46, 99, 56 and 28.
-  const int64_t groups = (all + GROUP_ROWS - 1) / GROUP_ROWS;
-  if (a.dtype == JPI_BF16 && all >= 64 && groups * pairs >= (p.head_dim == 256 ? 112 : 256)) {
+  // The ring from a workgroup for each compute unit on (of 256 dims, which the other kernel holds one wave of a SIMD at a time
+  // for, from less than half of that), or where there are so many products that it is worth joining ranges of their keys.
+  // us, ring and other: 1024 rows of 32 heads on 8 of 128, 256 workgroups, 33 and 32; 2048 rows 67 and 91; 512 rows 20 and 14,
+  // but before 8192 slots 90 and 121; 256 before 4096 41 and 35; 64, 32 and 16 chunks of 50 rows, 8 heads of 256, 866 slots 47,
+  // 42 and 36, 100, 56 and 28; 8 before 4096 slots 41 and 44.  fp32 has three times the products and none of its time in what
+  // the ring saves: 1024 rows 60 and 50.
+  const int64_t groups = (all + GROUP_ROWS - 1) / GROUP_ROWS, steps = (keys + 63) / 64, wgs = groups * pairs;
+  const bool enough = wgs >= (p.head_dim == 256 ? 112 : 256);
+  if (a.dtype == JPI_BF16 && all >= 64 && (enough || all * pairs / GROUP_ROWS * steps >= (p.head_dim == 256 ? 1600 : 8192))) {
     plan.groups = (int)groups;
-    plan.splits = 1;
+    plan.splits = enough ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>({16, (p.head_dim == 256 ? 256 : 512) / wgs, steps / 4}));
     return plan;
   }
   plan.tiles = (int)((all + 15) / 16);
@@ -703,13 +845,17 @@ CachePlan cache_plan(const jpi_cache_attn& a, const jpi_cache_pool& p, const jpi
 bool cache_attention_fits(const jpi_cache_attn& a, const jpi_cache_pool& p, const jpi_cache_seqs& q) {
   const CachePlan plan = cache_plan(a, p, q);
   const int64_t pairs = (int64_t)q.n_seqs * p.n_kv_heads, most = 1 << 24;  // 2^32 threads
-  return pairs * plan.groups < most && pairs * plan.tiles * plan.splits < most && (plan.splits == 1 || pairs * plan.tiles * 16 < most);
+  return pairs * (plan.groups + plan.tiles) * plan.splits < most &&
+         (plan.splits == 1 || pairs * (plan.groups * GROUP_ROWS + plan.tiles * 16) < most);
+}
+
+// rows of all ranges
+static int64_t part_rows(const CachePlan& plan, const jpi_cache_pool& p, const jpi_cache_seqs& q) {
+  return plan.splits == 1 ? 0 : (int64_t)q.n_seqs * p.n_kv_heads * (plan.groups * GROUP_ROWS + plan.tiles * 16) * plan.splits;
 }
 
 size_t cache_attention_bytes(const jpi_cache_attn& a, const jpi_cache_pool& p, const jpi_cache_seqs& q) {
-  const CachePlan plan = cache_plan(a, p, q);
-  if (plan.splits == 1) return 0;
-  return (size_t)q.n_seqs * p.n_kv_heads * plan.tiles * plan.splits * 16 * (p.head_dim * sizeof(float) + sizeof(float2));
+  return (size_t)part_rows(cache_plan(a, p, q), p, q) * (p.head_dim * sizeof(float) + sizeof(float2));
 }
 
 hipError_t launch_cache_attention(const jpi_cache_attn& c, const jpi_cache_pool& p, const jpi_cache_seqs& q, void* ws,
@@ -728,7 +874,7 @@ hipError_t launch_cache_attention(const jpi_cache_attn& c, const jpi_cache_pool&
   a.splits = plan.splits;
   const int pairs = q.n_seqs * p.n_kv_heads;
   a.part = (float*)ws;
-  a.stats = (float2*)((char*)ws + (size_t)pairs * plan.tiles * plan.splits * 16 * p.head_dim * sizeof(float));
+  a.stats = (float2*)((float*)ws + part_rows(plan, p, q) * p.head_dim);
   const bool f32 = c.dtype == JPI_F32;
   switch (p.head_dim) {
     case 64: launch_dim<64>(a, p.code, f32, plan, pairs, s); break;
