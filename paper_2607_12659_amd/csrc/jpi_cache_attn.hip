@@ -161,7 +161,9 @@ template <int DH, bool E4M3, typename T, int R, int NT>
 struct Rows {
   typedef Code<E4M3> C;
   typedef Tile<R> M;
-  static constexpr int PARTS = sizeof(T) == 2 ? 1 : 3;
+  // bf16 parts of a query and of a probability.  One part of a probability doubles the error of a bf16 result's rounding
+  // (2.3e-3 instead of 1.6e-3 of it); two are taken where memory bounds the kernel, not where products do.
+  static constexpr int PARTS = sizeof(T) == 2 ? 1 : 3, P_PARTS = sizeof(T) == 4 ? 3 : R == 16 ? 2 : 1;
   static constexpr int G = 64 / R, KEYS = 16 * G * NT;             // lane groups, keys of a step
   static constexpr int SETS = KEYS / R, REGS = R * R / 64;         // products of a step's keys, their registers
   static constexpr int KK = DH / (16 * G), DT = DH / R;            // pieces of a lane's keys and values
@@ -272,8 +274,9 @@ struct Rows {
     }
     top = groups_max<R>(top);
     if (__any(top > m_ref + HEADROOM || (m_ref == -INFINITY && top > -INFINITY))) {
-      // a whole number: sums are brought to another reference by a power of two, and differences with it are exact
-      const float now = fmaxf(m_ref, ceilf(top));
+      // A whole number: sums are brought to another reference by a power of two, and differences with it are exact.  Not where
+      // probabilities are rounded to one part: the maximum itself makes that of a row's only key 1.
+      const float now = fmaxf(m_ref, P_PARTS == 1 ? top : ceilf(top));
       const float g = m_ref == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_ref - now);  // with -inf O and the sum are 0
       sum *= g;
 #pragma unroll
@@ -341,9 +344,9 @@ struct Rows {
   // O += P V; values(t, d) are V's pieces, without what lies past the length
   template <typename VF>
   __device__ __forceinline__ void add(const Step& x, VF values) {
-    bf16x8 pp[NT][2][PARTS];
+    bf16x8 pp[NT][2][P_PARTS];
 #pragma unroll
-    for (int t = 0; t < NT; ++t) split8<PARTS>(x.p + 16 * t, pp[t][0]), split8<PARTS>(x.p + 16 * t + 8, pp[t][1]);
+    for (int t = 0; t < NT; ++t) split8<P_PARTS>(x.p + 16 * t, pp[t][0]), split8<P_PARTS>(x.p + 16 * t + 8, pp[t][1]);
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -353,7 +356,7 @@ struct Rows {
         for (int m = 0; m < 2; ++m) {
           const bf16x8 codes = C::widen8(w[2 * m], w[2 * m + 1]);
 #pragma unroll
-          for (int i = PARTS - 1; i >= 0; --i) o[d] = M::mfma(codes, pp[t][m][i], o[d]);
+          for (int i = P_PARTS - 1; i >= 0; --i) o[d] = M::mfma(codes, pp[t][m][i], o[d]);
         }
       }
   }

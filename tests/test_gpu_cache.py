@@ -435,6 +435,37 @@ def test_attention(ops, case, code, dtype):
     attend_both(ops, q, pool, code, page, table, lens, q_lens, causal, window, sinks)
 
 
+# many rows whose keys are cut into ranges: mostly tables for far more slots than there are; the last entry: 8192 rows and more
+RANGES = [
+    (100, 4, 1, 64, 128, [1500, 100, 0, 257, 256], None, True, 0, 0, 1400, False),
+    (64, 2, 2, 128, 64, [1025, 64, 1, 640], [64, 1, 64, 63], False, 0, 0, 5000, False),
+    (200, 16, 16, 128, 16, [2700, 200, 515, 199, 0], [200, 200, 131, 7, 3], True, 0, 0, 550, True),
+    (70, 64, 8, 64, 64, [9300, 70], None, True, 9000, 70, 10000, True),           # ranges of a window's keys
+    (50, 8, 1, 256, 32, [866, 50, 31, 116, 1100, 0, 600, 64], None, False, 0, 0, 128, False),
+    (50, 16, 2, 256, 64, [300, 50, 49, 1] * 3, [50, 49, 50, 0] * 3, True, 0, 0, 64, True),
+]
+
+
+@pytest.mark.parametrize("code", CODES)
+@pytest.mark.parametrize("case", range(len(RANGES)))
+def test_attention_ranges_of_many_rows(ops, case, code):
+    rows, heads, kv, dh, page, lens, q_lens, causal, window, sinks, width, large = RANGES[case]
+    groups, _, ranges = plan_of(len(lens), rows, heads, kv, dh, page, causal, window, sinks, width, code)
+    assert groups > 0 and ranges > 1
+    assert large == (len(lens) * kv * groups * 128 >= 8192)
+    counts = [-(-n // page) for n in lens]
+    pool = filled(40 + case, sum(counts) + 1, kv, dh, page, code)
+    table = numbered(40 + case, counts, width, sum(counts) + 1)
+    if page > 16 and lens[0] % page:  # codes behind a length
+        for i in (0, 1):
+            x = ref.natural(pool[i][table[0, lens[0] // page]], i == 0).copy()
+            x[:, lens[0] % page:] = 0x7f
+            pool[i][table[0, lens[0] // page]] = ref.in_pieces(x, i == 0)
+    q = rand(140 + case, len(lens), rows, heads, dh, dtype=torch.bfloat16)
+    first = attend_both(ops, q, pool, code, page, table, lens, q_lens, causal, window, sinks)
+    same_bits(first, attend_both(ops, q, pool, code, page, table, lens, q_lens, causal, window, sinks))
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 def test_attention_spoilt_pages(ops, dtype):
     """A page that holds NaN, and a number that names none, spoil the rows that see them, and no others."""
