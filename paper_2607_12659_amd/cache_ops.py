@@ -61,6 +61,8 @@ class Pool(NamedTuple):
         """A new pool; without `layers` of one layer."""
         if code not in _CODE:
             raise TypeError("codes must be int8 or float8_e4m3fn, got %s" % code)
+        if head_dim % 16 or page % 16:
+            raise ValueError("head_dim and page must be multiples of 16")
         lead = (n_pages, kv_heads) if layers is None else (layers, n_pages, kv_heads)
         shapes = ((head_dim // 16, page, 16), (page // 16, head_dim, 16))
         return cls(*(torch.zeros(lead + s, dtype=torch.uint8, device=device).view(code) for s in shapes),

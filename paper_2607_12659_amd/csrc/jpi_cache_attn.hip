@@ -273,10 +273,12 @@ struct Rows {
       top = fmaxf(top, t0);
     }
     top = groups_max<R>(top);
-    if (__any(top > m_ref + HEADROOM || (m_ref == -INFINITY && top > -INFINITY))) {
+    const bool low = top > m_ref + HEADROOM || (m_ref == -INFINITY && top > -INFINITY);
+    if (__any(low)) {
       // A whole number: sums are brought to another reference by a power of two, and differences with it are exact.  Not where
       // probabilities are rounded to one part: the maximum itself makes that of a row's only key 1.
-      const float now = fmaxf(m_ref, P_PARTS == 1 ? top : ceilf(top));
+      // Rows whose own is not too low keep it: what is in a row changes no other's bits.
+      const float now = !low ? m_ref : P_PARTS == 1 ? top : ceilf(top);
       const float g = m_ref == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_ref - now);  // with -inf O and the sum are 0
       sum *= g;
 #pragma unroll

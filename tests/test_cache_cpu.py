@@ -237,7 +237,8 @@ def test_tensors_of_other_shapes_and_types_are_refused(ops):
              lambda: ops.resize(table, lens, refs[:3], lens, p), lambda: ops.resize(table, lens, refs, refs, p),
              lambda: ops.resize(table, lens, refs, lens, p, page=64), lambda: ops.resize(table, lens, refs, lens, p, short=refs),
              lambda: ops.reorder(table, lens, refs, refs, 32), lambda: ops.reorder(table, lens, refs, lens, 32, table_out=table[:1]),
-             lambda: ops.compact(table, refs, p, n_live=lens), lambda: ops.compact(table, refs, p, refs_out=lens)]
+             lambda: ops.compact(table, refs, p, n_live=lens), lambda: ops.compact(table, refs, p, refs_out=lens),
+             lambda: ops.Pool.zeros(3, 1, 72, 16, device="cpu"), lambda: ops.Pool.zeros(3, 1, 64, 24, device="cpu")]
     for i, call in enumerate(shape):
         with pytest.raises(ValueError):
             call()

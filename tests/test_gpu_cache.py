@@ -512,6 +512,60 @@ def test_attention_spoilt_queries_and_sizes_of_values(ops, dtype):
         assert torch.equal(g.cpu()[keep], w.cpu()[keep]) and torch.isnan(g.cpu()[~keep]).any(-1).all()
 
 
+MANY = [(9, 4, 1, 64), (70, 64, 32, 64), (70, 32, 4, 256)]  # rows, heads, KV heads, dim: few rows, and many
+
+
+@pytest.mark.parametrize("case", MANY)
+def test_attention_counts_out_of_range_and_a_broadcast_query(ops, case):
+    """Lengths and counts of rows outside their ranges count as the nearer end; a query of all heads has a stride of 0."""
+    rows, heads, kv, dh = case
+    page, width, code = 16, 10, "e4m3"
+    lens, q_lens = [-5, 1 << 30, 161, 100, 160, 7, 90, -(1 << 31)], [rows, 1 << 30, rows, -1, rows - 1, 1 << 30, -(1 << 31), 3]
+    assert (plan_of(8, rows, heads, kv, dh, page, True, 0, 0, width, code)[0] > 0) == (rows == 70)
+    pool = filled(60, 81, kv, dh, page, code)
+    table = numbered(60, [10] * 8, width, 81)
+    q = rand(160, 8, rows, 1, dh, dtype=torch.bfloat16).expand(8, rows, heads, dh)
+    out, lse = torch.full((2, 8, rows, heads, dh), -77.0, dtype=q.dtype, device="cuda"), torch.full((8, rows, heads), -77.0, device="cuda")
+    g = dev(q[:, :, :1]).expand(8, rows, heads, dh)
+    ops.attention(g, on_gpu(ops, pool, code), dev(table), i32(lens), q_lens=i32(q_lens), out=out[1], lse=lse)
+    o, l, mag, err, there = attn64(q, pool, code, page, table, lens, q_lens, True, 0, 0, dh ** -0.5)
+    tol_o, tol_l = attn_tolerance(q.dtype, o, l, mag, err, 160, dh)
+    within(out[1].cpu()[torch.from_numpy(there)], o[there], tol_o[there])
+    within(lse.cpu()[torch.from_numpy(there)], l[there], tol_l[there])
+    assert (out[1].cpu()[torch.from_numpy(~there)] == -77).all() and (out[0] == -77).all()
+    assert (lse.cpu()[torch.from_numpy(~there)] == -77).all()
+
+
+@pytest.mark.parametrize("case", MANY[1:])
+@pytest.mark.parametrize("code", CODES)
+def test_attention_many_rows_spoilt_queries_and_sizes_of_values(ops, case, code):
+    """As for few rows: NaN and infinity stay in their rows; scales of pages far apart, and none of a power of two; scores that
+    differ by hundreds; scales of 0."""
+    rows, heads, kv, dh = case
+    page = 32
+    pool = filled(61, 50, kv, dh, page, code)
+    table = numbered(61, [6] * 8, 6, 50)
+    for i in range(6):
+        pool[3][table[0, i]] = 2.0 ** (6 * i - 20)
+        pool[3][table[1, i]] = 1.3 * 2.0 ** (i - 3)
+        pool[2][table[2, i]] *= 2.0 ** (i - 2)
+        pool[3][table[4, i]] = 2.0 ** (90 * (i % 2) - 45 + i)
+    pool[2][table[3, 2]], pool[3][table[3, 3]], pool[2][table[3, 5]], pool[3][table[3, 5]] = 0, 0, 0, 0
+    q = rand(161, 8, rows, heads, dh, dtype=torch.bfloat16)
+    q[2] *= 8
+    lens = [190, 192, 180, 192, 150, 70, 64, 33]
+    assert plan_of(8, rows, heads, kv, dh, page, True, 0, 0, 6, code)[0] > 0
+    attend_both(ops, q, pool, code, page, table, lens)
+    bad = q.clone()
+    bad[0, 3, 1, 7], bad[1, 4, 2, 60] = float("nan"), INF
+    args = (on_gpu(ops, pool, code), dev(table), i32(lens))
+    good, got = ops.attention(dev(q), *args), ops.attention(dev(bad), *args)
+    keep = torch.ones(8, rows, heads, dtype=torch.bool)
+    keep[0, 3, 1] = keep[1, 4, 2] = False
+    for g, w in zip(got, good):
+        assert torch.equal(g.cpu()[keep], w.cpu()[keep]) and torch.isnan(g.cpu()[~keep].reshape(2, -1)).any(-1).all()
+
+
 def test_attention_strides_shared_pages_and_a_single_slot(ops):
     """q as a part of a projection, out as heads of another tensor, a table with a longer row; sequences that share pages; all
     probability on one slot gives its value."""
