@@ -168,6 +168,7 @@ struct Rows {
   static constexpr int SETS = KEYS / R, REGS = R * R / 64;         // products of a step's keys, their registers
   static constexpr int KK = DH / (16 * G), DT = DH / R;            // pieces of a lane's keys and values
   static constexpr int QUADS = DH * R / 256;                       // groups of four dims of a lane
+  static constexpr int CHAINS = R == 16 ? 4 : 1;                   // sums whose products take turns: one after the other they wait
 
   int grp, token, head, see_lo, see_hi, full_lo, full_hi, len, sinks;
   float qscale, m_ref, sum;
@@ -224,24 +225,33 @@ struct Rows {
   // q k^T of the codes; keys(j, kk) are the pieces
   template <typename KF>
   __device__ __forceinline__ void scores(float (&sc)[16 * NT], KF keys) const {
+    typename M::acc c[SETS];
 #pragma unroll
-    for (int j = 0; j < SETS; ++j) {
-      typename M::acc c;
+    for (int j = 0; j < SETS; ++j)
 #pragma unroll
-      for (int e = 0; e < REGS; ++e) c[e] = 0.f;
+      for (int e = 0; e < REGS; ++e) c[j][e] = 0.f;
+    // all sets take a piece before the next: products of one sum have to wait for each other
 #pragma unroll
-      for (int kk = 0; kk < KK; ++kk) {
-        const u32x4 w = keys(j, kk);
+    for (int kk = 0; kk < KK; ++kk)
 #pragma unroll
-        for (int m = 0; m < 2; ++m) {
-          const bf16x8 codes = C::widen8(w[2 * m], w[2 * m + 1]);
+      for (int m = 0; m < 2; ++m)
 #pragma unroll
-          for (int i = PARTS - 1; i >= 0; --i) c = M::mfma(codes, q[i][kk][m], c);
+        for (int j0 = 0; j0 < SETS; j0 += CHAINS) {
+          bf16x8 codes[CHAINS];
+#pragma unroll
+          for (int j = 0; j < CHAINS; ++j) {
+            const u32x4 w = keys(j0 + j, kk);
+            codes[j] = C::widen8(w[2 * m], w[2 * m + 1]);
+          }
+#pragma unroll
+          for (int i = PARTS - 1; i >= 0; --i)
+#pragma unroll
+            for (int j = 0; j < CHAINS; ++j) c[j0 + j] = M::mfma(codes[j], q[i][kk][m], c[j0 + j]);
         }
-      }
 #pragma unroll
-      for (int e = 0; e < REGS; ++e) sc[j * REGS + e] = c[e];
-    }
+    for (int j = 0; j < SETS; ++j)
+#pragma unroll
+      for (int e = 0; e < REGS; ++e) sc[j * REGS + e] = c[j][e];
   }
 
   // Masks, and the row's reference.  One path for all steps, with masks aside: with one path for those that are seen whole and
@@ -352,15 +362,20 @@ struct Rows {
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
-      for (int d = 0; d < DT; ++d) {
-        const u32x4 w = values(t, d);
+      for (int d0 = 0; d0 < DT; d0 += CHAINS)
 #pragma unroll
         for (int m = 0; m < 2; ++m) {
-          const bf16x8 codes = C::widen8(w[2 * m], w[2 * m + 1]);
+          bf16x8 codes[CHAINS];
 #pragma unroll
-          for (int i = P_PARTS - 1; i >= 0; --i) o[d] = M::mfma(codes, pp[t][m][i], o[d]);
+          for (int d = 0; d < CHAINS; ++d) {
+            const u32x4 w = values(t, d0 + d);
+            codes[d] = C::widen8(w[2 * m], w[2 * m + 1]);
+          }
+#pragma unroll
+          for (int i = P_PARTS - 1; i >= 0; --i)
+#pragma unroll
+            for (int d = 0; d < CHAINS; ++d) o[d0 + d] = M::mfma(codes[d], pp[t][m][i], o[d0 + d]);
         }
-      }
   }
 
   __device__ __forceinline__ f32x4 quad(int i) const {
@@ -401,8 +416,7 @@ __global__ __launch_bounds__(64 * WAVES, DH == 256 ? 1 : 2) void k_cache_attn(Ca
   typedef Rows<DH, E4M3, T, R, 1> W;
   typedef typename W::M M;
   constexpr int KEYS = W::KEYS, QUADS = W::QUADS;
-  constexpr int ROUND = QUADS < 8 ? QUADS : 8;  // quads that are joined at once
-  __shared__ __align__(16) f32x4 join[WAVES][ROUND][64];
+  __shared__ __align__(16) f32x4 join[WAVES][QUADS][64];
   __shared__ float2 wave_stats[WAVES][R];
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -481,44 +495,39 @@ __global__ __launch_bounds__(64 * WAVES, DH == 256 ? 1 : 2) void k_cache_attn(Ca
     if (more) load_v(next, vid1);
   }
 
-  // the four waves' sums, brought to one reference and added in their order
+  // the four waves' sums, brought to one reference and added in their order; a wave adds and writes a quarter of the dims
   const float sum = groups_sum<R>(w.sum);
   if (grp == 0) wave_stats[wave][col] = float2{w.m_ref, sum};
-  __syncthreads();
-  float ref = -INFINITY, total = 0.f;
 #pragma unroll
-  for (int i = 0; i < WAVES; ++i) ref = fmaxf(ref, wave_stats[i][col].x);
+  for (int i = 0; i < QUADS; ++i) join[wave][i][lane] = w.quad(i);
+  __syncthreads();
+  float ref = -INFINITY, total = 0.f, g[WAVES];
+  float2 st[WAVES];
+#pragma unroll
+  for (int i = 0; i < WAVES; ++i) st[i] = wave_stats[i][col], ref = fmaxf(ref, st[i].x);
 #pragma unroll
   for (int i = 0; i < WAVES; ++i) {
-    const float2 st = wave_stats[i][col];
-    total += (st.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(st.x - ref)) * st.y;
+    g[i] = st[i].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(st[i].x - ref);
+    total += g[i] * st[i].y;
   }
-  const float mine = w.m_ref == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(w.m_ref - ref);
-  const bool here = rt * R + col < x.rows, final = ranges == 1;
-  const float norm = !final ? 1.f : total == 0.f ? 0.f : 1.f / total;
-  float* part = a.part + ((int64_t)blockIdx.x * R + col) * DH;
-  T* out = reinterpret_cast<T*>(a.out) + s * a.o_outer + w.token * a.o_row + w.head * a.o_head;
-  if (wave == 0 && grp == 0 && here) {
+  if (rt * R + col >= x.rows) return;
+  const bool final = ranges == 1;
+  if (wave == 0 && grp == 0) {
     if (!final) a.stats[(int64_t)blockIdx.x * R + col] = float2{ref, total};
     else if (a.lse) a.lse[((int64_t)s * a.q_rows + w.token) * a.n_heads + w.head] = lse_of(ref, total);
   }
+  const float norm = !final ? 1.f : total == 0.f ? 0.f : 1.f / total;
+  float* part = a.part + ((int64_t)blockIdx.x * R + col) * DH;
+  T* out = reinterpret_cast<T*>(a.out) + s * a.o_outer + w.token * a.o_row + w.head * a.o_head;
 #pragma unroll
-  for (int q0 = 0; q0 < QUADS; q0 += ROUND) {
-    if (q0) __syncthreads();
+  for (int i = 0; i < QUADS; i += WAVES) {
+    f32x4 y = join[0][i + wave][lane] * g[0];
 #pragma unroll
-    for (int i = 0; i < ROUND; ++i) join[wave][i][lane] = w.quad(q0 + i) * mine;
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < ROUND; i += WAVES) {
-      f32x4 y = join[0][i + wave][lane];
-#pragma unroll
-      for (int v = 1; v < WAVES; ++v) y += join[v][i + wave][lane];
-      if (!here) continue;
-      const int at = M::dim(q0 + i + wave, grp);
-      y *= norm;
-      if (!final) put4(part + at, y);
-      else put4(out + at, y);
-    }
+    for (int v = 1; v < WAVES; ++v) y += join[v][i + wave][lane] * g[v];
+    y *= norm;
+    const int at = M::dim(i + wave, grp);
+    if (!final) put4(part + at, y);
+    else put4(out + at, y);
   }
 }
 
