@@ -112,16 +112,28 @@ struct Tile<16> {
   static __device__ __forceinline__ int dim(int quad, int g) { return 16 * quad + 4 * g; }
 };
 
+// this lane's value and that of the lane 16 away
+__device__ __forceinline__ void quarters(float v, float& a, float& b) {
+  const auto p = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(u32, v), __builtin_bit_cast(u32, v), false, false);
+  const u32 x = p[0], y = p[1];
+  a = __builtin_bit_cast(float, x), b = __builtin_bit_cast(float, y);
+}
 // over the lane groups of a row
 template <int R>
 __device__ __forceinline__ float groups_max(float v) {
   v = halves_max(v);
-  return R == 32 ? v : fmaxf(v, __shfl_xor(v, 16, 64));
+  if (R == 32) return v;
+  float a, b;
+  quarters(v, a, b);
+  return fmaxf(a, b);
 }
 template <int R>
 __device__ __forceinline__ float groups_sum(float v) {
   v = halves_sum(v);
-  return R == 32 ? v : v + __shfl_xor(v, 16, 64);
+  if (R == 32) return v;
+  float a, b;
+  quarters(v, a, b);
+  return a + b;
 }
 
 // x in PARTS parts of bf16: the largest first
@@ -212,6 +224,15 @@ struct Rows {
     m_ref = -INFINITY, sum = 0.f;
   }
 
+  // O of 256 dims is in the accumulation registers, which the products take as they are.  Left to itself the compiler had it in
+  // the others around the branch that brings it to another reference, and copied it there and back in each step.
+  __device__ __forceinline__ void hold() {
+    if constexpr (DH == 256) {
+#pragma unroll
+      for (int d = 0; d < DT; ++d) asm volatile("" : "+a"(o[d]));
+    }
+  }
+
   // One step's keys from slot0 on, with the scales of the lane's pieces, in parts that a loop may order as it likes.
   struct Step {
     int slot0;
@@ -284,6 +305,7 @@ struct Rows {
     }
     top = groups_max<R>(top);
     const bool low = top > m_ref + HEADROOM || (m_ref == -INFINITY && top > -INFINITY);
+    hold();
     if (__any(low)) {
       // A whole number: sums are brought to another reference by a power of two, and differences with it are exact.  Not where
       // probabilities are rounded to one part: the maximum itself makes that of a row's only key 1.
@@ -295,6 +317,7 @@ struct Rows {
       for (int d = 0; d < DT; ++d)
 #pragma unroll
         for (int e = 0; e < REGS; ++e) o[d][e] *= g;
+      hold();
       m_ref = now;
     }
     // Other scales of V, and masks where K's scale makes no -inf of -inf, are seen to one by one
@@ -376,6 +399,7 @@ struct Rows {
 #pragma unroll
             for (int d = 0; d < CHAINS; ++d) o[d0 + d] = M::mfma(codes[d], pp[t][m][i], o[d0 + d]);
         }
+    hold();
   }
 
   __device__ __forceinline__ f32x4 quad(int i) const {
