@@ -44,6 +44,19 @@ constexpr int WAVES = 4, GROUP_ROWS = 32 * WAVES;  // rows of a workgroup of the
 constexpr float LOG2E = 1.44269504088896341f, LN2 = 0.693147180559945309f;
 constexpr float HEADROOM = 16.f;  // log2 of the most that a probability may exceed its row's reference by
 
+// n / by for 0 <= n < 2^31, by a product with 2^(31 + l) / by rounded up, 2^l >= by: a chain of thirty instructions is ahead of
+// a kernel's first load for each division that it makes itself
+struct Divisor {
+  u32 mul;
+  int shift;
+};
+__host__ __device__ __forceinline__ int operator/(int n, Divisor d) { return (int)(((uint64_t)(u32)n * d.mul) >> d.shift); }
+Divisor divisor(int64_t by) {
+  int l = 0;
+  while ((int64_t)1 << l < by) ++l;
+  return {(u32)((((uint64_t)1 << (31 + l)) + by - 1) / by), 31 + l};
+}
+
 struct CacheArgs {
   const void* q;
   int64_t q_outer, q_row, q_head;
@@ -58,7 +71,8 @@ struct CacheArgs {
   int n_pages, lg_page, cap;
   int causal, window, sinks;
   float qscale;  // scale / ln 2
-  int splits;
+  int splits, pairs, per_tile;  // pairs: sequences times KV heads; per_tile: rows of a tile, as far as there are
+  Divisor by_splits, by_pairs, by_kv, by_group, by_per_tile;
   float* part;    // [workgroup][rows of a tile][head_dim]
   float2* stats;  // [workgroup][rows of a tile]: reference, sum
 };
@@ -77,8 +91,8 @@ __device__ __forceinline__ Span span_of(const CacheArgs& a, int s, int nth) {
   x.len = clamp_len(a.len[s], a.cap);
   x.nq = a.q_len ? clamp_len(a.q_len[s], a.q_rows) : a.q_rows;
   x.rows = x.nq * a.group;
-  x.i0 = nth * ROWS / a.group;
-  x.i1 = min(x.nq - 1, (nth * ROWS + ROWS - 1) / a.group);
+  x.i0 = nth * ROWS / a.by_group;
+  x.i1 = min(x.nq - 1, (nth * ROWS + ROWS - 1) / a.by_group);
   x.pos0 = x.len - x.nq;
   x.hi = a.causal ? min(max(x.pos0 + x.i1 + 1, 0), x.len) : x.len;
   x.lo = a.window ? (int)max((int64_t)x.pos0 + x.i0 - a.window + 1, (int64_t)0) : 0;
@@ -90,7 +104,7 @@ __device__ __forceinline__ Span span_of(const CacheArgs& a, int s, int nth) {
 }
 
 // Tiles of a range, and how many ranges have any (one at least): a wave gets a tile each where there are as many
-__device__ __forceinline__ int per_range(int count, int splits) { return max((count + splits - 1) / splits, WAVES); }
+__device__ __forceinline__ int per_range(const CacheArgs& a, int count) { return max((count + a.splits - 1) / a.by_splits, WAVES); }
 __device__ __forceinline__ int ranges_of(int count, int per) { return max(1, (count + per - 1) / per); }
 
 // One matrix instruction of R rows (queries) and R keys or dims
@@ -187,17 +201,12 @@ struct Rows {
   bf16x8 q[PARTS][KK][2];
   typename M::acc o[DT];
 
-  __device__ __forceinline__ void begin(const CacheArgs& a, const Span& x, int s, int h, int rt) {
+  // Asks for the queries, before the sequence's counts are there: lanes past its rows have others of the array, or the last
+  __device__ __forceinline__ void ask(const CacheArgs& a, int s, int h, int rt) {
     const int lane = threadIdx.x & 63, col = lane % R;
     grp = lane / R;
-    const int r = min(rt * R + col, x.rows - 1);
-    token = r / a.group, head = h * a.group + (r - token * a.group);
-    len = x.len, sinks = a.sinks, qscale = a.qscale;
-    see_hi = a.causal ? min(x.pos0 + token + 1, x.len) : x.len;
-    see_lo = a.window ? (int)max((int64_t)x.pos0 + token - a.window + 1, (int64_t)0) : 0;
-    // tiles from slot full_lo up to slot full_hi are seen whole by all rows
-    full_hi = a.causal ? min(x.pos0 + x.i0 + 1, x.len) : x.len;
-    full_lo = a.window ? (int)max((int64_t)x.pos0 + x.i1 - a.window + 1, (int64_t)0) : 0;
+    const int r = min(rt * R + col, a.q_rows * a.group - 1);
+    token = r / a.by_group, head = h * a.group + (r - token * a.group);
     const T* p = reinterpret_cast<const T*>(a.q) + s * a.q_outer + token * a.q_row + head * a.q_head + 16 * grp;
 #pragma unroll
     for (int kk = 0; kk < KK; ++kk)
@@ -217,6 +226,15 @@ struct Rows {
           for (int i = 0; i < PARTS; ++i) q[i][kk][m] = part[i];
         }
       }
+  }
+
+  __device__ __forceinline__ void begin(const CacheArgs& a, const Span& x) {
+    len = x.len, sinks = a.sinks, qscale = a.qscale;
+    see_hi = a.causal ? min(x.pos0 + token + 1, x.len) : x.len;
+    see_lo = a.window ? (int)max((int64_t)x.pos0 + token - a.window + 1, (int64_t)0) : 0;
+    // tiles from slot full_lo up to slot full_hi are seen whole by all rows
+    full_hi = a.causal ? min(x.pos0 + x.i0 + 1, x.len) : x.len;
+    full_lo = a.window ? (int)max((int64_t)x.pos0 + x.i1 - a.window + 1, (int64_t)0) : 0;
 #pragma unroll
     for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -445,18 +463,17 @@ __global__ __launch_bounds__(64 * WAVES, DH == 256 ? 1 : 2) void k_cache_attn(Ca
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int grp = lane / R, col = lane % R;
-  const int pairs = a.n_seqs * a.kv;
-  const int pair = blockIdx.x % pairs, rest = blockIdx.x / pairs;
-  const int split = rest % a.splits, rt = rest / a.splits;
-  const int s = pair / a.kv, h = pair - s * a.kv;
+  const int rest = (int)blockIdx.x / a.by_pairs, pair = blockIdx.x - rest * a.pairs;
+  const int rt = rest / a.by_splits, split = rest - rt * a.splits;
+  const int s = pair / a.by_kv, h = pair - s * a.kv;
+  W w;
+  w.ask(a, s, h, rt);
   const Span x = span_of<R, 1024 / R>(a, s, rt);
   if (rt * R >= x.rows) return;
-  const int per = per_range(x.count, a.splits), ranges = ranges_of(x.count, per);
-  if (split >= ranges) return;
+  const int per = per_range(a, x.count);
+  if (split > 0 && split * per >= x.count) return;
   const int first = split * per + wave, last = min(x.count, (split + 1) * per);
-
-  W w;
-  w.begin(a, x, s, h, rt);
+  w.begin(a, x);
 
   const int mask = (1 << a.lg_page) - 1;
   const u32 page_bytes = (u32)DH << a.lg_page;
@@ -535,7 +552,7 @@ __global__ __launch_bounds__(64 * WAVES, DH == 256 ? 1 : 2) void k_cache_attn(Ca
     total += g[i] * st[i].y;
   }
   if (rt * R + col >= x.rows) return;
-  const bool final = ranges == 1;
+  const bool final = x.count <= per;
   if (wave == 0 && grp == 0) {
     if (!final) a.stats[(int64_t)blockIdx.x * R + col] = float2{ref, total};
     else if (a.lse) a.lse[((int64_t)s * a.q_rows + w.token) * a.n_heads + w.head] = lse_of(ref, total);
@@ -595,20 +612,20 @@ __global__ __launch_bounds__(64 * WAVES, DH == 256 ? 1 : 2) void k_cache_rows(Ca
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int grp = lane / R, col = lane % R;
-  const int pairs = a.n_seqs * a.kv;
-  const int pair = blockIdx.x % pairs, s = pair / a.kv, h = pair - s * a.kv;
   // the last rows of causal ones see most: they come first
-  const int rest = (gridDim.x - 1 - blockIdx.x) / pairs, split = rest % a.splits, group = rest / a.splits, rt = group * WAVES + wave;
+  const int nth = gridDim.x - 1 - blockIdx.x, rest = nth / a.by_pairs, pair = nth - rest * a.pairs, s = pair / a.by_kv, h = pair - s * a.kv;
+  const int group = rest / a.by_splits, split = rest - group * a.splits, rt = group * WAVES + wave;
   const Span all = span_of<GROUP_ROWS, KEYS>(a, s, group);
   if (group * GROUP_ROWS >= all.rows) return;
-  const int per = per_range(all.count, a.splits), ranges = ranges_of(all.count, per), first = split * per;
-  if (split >= ranges) return;
+  const int per = per_range(a, all.count), first = split * per;
+  if (split > 0 && first >= all.count) return;
   const int count = min(per, all.count - first);  // of steps, from `first` on
   // a wave without rows computes others' again; steps left out would have O copied from register to register in each
   const int own = min(rt, (all.rows - 1) / R);
   const Span x = span_of<R, KEYS>(a, s, own);
   W w;
-  w.begin(a, x, s, h, own);
+  w.ask(a, s, h, own);
+  w.begin(a, x);
 
   const int32_t* table = a.table + s * a.table_stride;
   auto look_up = [&](int block) {  // by one wave: the pieces of a block of steps
@@ -731,8 +748,8 @@ __global__ __launch_bounds__(64 * WAVES, DH == 256 ? 1 : 2) void k_cache_rows(Ca
 
   const float total = groups_sum<R>(w.sum), norm = total == 0.f ? 0.f : 1.f / total;
   if (rt * R + col >= x.rows) return;
-  if (ranges > 1) {
-    const int64_t at = (int64_t)((group * a.splits + split) * pairs + pair) * GROUP_ROWS + wave * R + col;
+  if (all.count > per) {
+    const int64_t at = (int64_t)((group * a.splits + split) * a.pairs + pair) * GROUP_ROWS + wave * R + col;
     if (grp == 0) a.stats[at] = float2{w.m_ref, total};
 #pragma unroll
     for (int i = 0; i < W::QUADS; ++i) put4(a.part + at * DH + W::M::dim(i, grp), w.quad(i));
@@ -750,14 +767,13 @@ struct CutRow {
   int64_t at, step;
 };
 template <int R>
-__device__ __forceinline__ CutRow cut_row(const CacheArgs& a, int64_t nth) {
-  const int pairs = a.n_seqs * a.kv, per_tile = min(R, a.q_rows * a.group);
-  const int pair = (int)(nth % pairs), rest = (int)(nth / pairs), col = rest % per_tile, rt = rest / per_tile;
-  const int s = pair / a.kv, h = pair - s * a.kv;
+__device__ __forceinline__ CutRow cut_row(const CacheArgs& a, int nth) {
+  const int rest = nth / a.by_pairs, pair = nth - rest * a.pairs, rt = rest / a.by_per_tile, col = rest - rt * a.per_tile;
+  const int s = pair / a.by_kv, h = pair - s * a.kv;
   const Span x = span_of<R, 64>(a, s, rt);
-  const int r = rt * R + col, token = r / a.group;
-  return {s, token, h * a.group + (r - token * a.group), r < x.rows ? ranges_of(x.count, per_range(x.count, a.splits)) : 0,
-          ((int64_t)rt * a.splits * pairs + pair) * R + col, (int64_t)pairs * R};
+  const int r = rt * R + col, token = r / a.by_group;
+  return {s, token, h * a.group + (r - token * a.group), r < x.rows ? ranges_of(x.count, per_range(a, x.count)) : 0,
+          ((int64_t)rt * a.splits * a.pairs + pair) * R + col, (int64_t)a.pairs * R};
 }
 template <typename T>
 __device__ __forceinline__ T* out_of(const CacheArgs& a, const CutRow& x) {
@@ -801,10 +817,10 @@ __global__ __launch_bounds__(256) void k_cache_join(CacheArgs a) {
 // Many rows: DH / 4 lanes take a row, all its ranges.  16384 rows of 128 dims in four ranges: the call 109 us with a workgroup
 // for each row, 90 so; 1024 rows in sixteen 39 and 69.
 template <int DH, typename T, int R>
-__global__ __launch_bounds__(256) void k_cache_join_rows(CacheArgs a, int64_t rows) {
+__global__ __launch_bounds__(256) void k_cache_join_rows(CacheArgs a, int rows) {
   constexpr int LANES = DH / 4;
   const int d4 = threadIdx.x % LANES;
-  const int64_t nth = (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
+  const int nth = blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
   if (nth >= rows) return;
   const CutRow x = cut_row<R>(a, nth);
   if (x.ranges <= 1) return;
@@ -823,34 +839,36 @@ __global__ __launch_bounds__(256) void k_cache_join_rows(CacheArgs a, int64_t ro
   if (d4 == 0 && a.lse) a.lse[((int64_t)x.s * a.q_rows + x.token) * a.n_heads + x.head] = lse_of(ref, total);
 }
 
+// the row tiles' R rows in ranges
 template <int DH, typename T, int R>
-void launch_join(const CacheArgs& a, int64_t rows, hipStream_t s) {
-  if (R > 16 && rows >= 8192) k_cache_join_rows<DH, T, R><<<(unsigned)((rows * DH / 4 + 255) / 256), 256, 0, s>>>(a, rows);
+void launch_join(CacheArgs& a, int tiles, hipStream_t s) {
+  a.per_tile = std::min(R, a.q_rows * a.group), a.by_per_tile = divisor(a.per_tile);
+  const int rows = a.pairs * tiles * a.per_tile;  // below 2^24: cache_attention_fits
+  if (R > 16 && rows >= 8192) k_cache_join_rows<DH, T, R><<<(unsigned)(((int64_t)rows * DH / 4 + 255) / 256), 256, 0, s>>>(a, rows);
   else k_cache_join<DH, T, R><<<(unsigned)rows, 256, 0, s>>>(a);
 }
 
 template <int DH, bool E4M3, typename T>
-void launch_typed(const CacheArgs& a, const CachePlan& plan, int pairs, hipStream_t s) {
+void launch_typed(CacheArgs& a, const CachePlan& plan, hipStream_t s) {
   if constexpr (sizeof(T) == 2) {
     if (plan.groups) {
-      k_cache_rows<DH, E4M3><<<(unsigned)(pairs * plan.groups * plan.splits), 64 * WAVES, 0, s>>>(a);
-      if (plan.splits > 1)
-        launch_join<DH, T, GROUP_ROWS>(a, (int64_t)pairs * plan.groups * std::min(GROUP_ROWS, a.q_rows * a.group), s);
+      k_cache_rows<DH, E4M3><<<(unsigned)(a.pairs * plan.groups * plan.splits), 64 * WAVES, 0, s>>>(a);
+      if (plan.splits > 1) launch_join<DH, T, GROUP_ROWS>(a, plan.groups, s);
       return;
     }
   }
-  k_cache_attn<DH, E4M3, T, 16><<<(unsigned)(pairs * plan.tiles * plan.splits), 64 * WAVES, 0, s>>>(a);
-  if (plan.splits > 1) launch_join<DH, T, 16>(a, (int64_t)pairs * plan.tiles * std::min(16, a.q_rows * a.group), s);
+  k_cache_attn<DH, E4M3, T, 16><<<(unsigned)(a.pairs * plan.tiles * plan.splits), 64 * WAVES, 0, s>>>(a);
+  if (plan.splits > 1) launch_join<DH, T, 16>(a, plan.tiles, s);
 }
 
 template <int DH>
-void launch_dim(const CacheArgs& a, int code, bool f32, const CachePlan& plan, int pairs, hipStream_t s) {
+void launch_dim(CacheArgs& a, int code, bool f32, const CachePlan& plan, hipStream_t s) {
   if (code == JPI_E4M3) {
-    if (f32) launch_typed<DH, true, float>(a, plan, pairs, s);
-    else launch_typed<DH, true, bf16>(a, plan, pairs, s);
+    if (f32) launch_typed<DH, true, float>(a, plan, s);
+    else launch_typed<DH, true, bf16>(a, plan, s);
   } else {
-    if (f32) launch_typed<DH, false, float>(a, plan, pairs, s);
-    else launch_typed<DH, false, bf16>(a, plan, pairs, s);
+    if (f32) launch_typed<DH, false, float>(a, plan, s);
+    else launch_typed<DH, false, bf16>(a, plan, s);
   }
 }
 
@@ -909,15 +927,15 @@ hipError_t launch_cache_attention(const jpi_cache_attn& c, const jpi_cache_pool&
   a.n_pages = p.n_pages, a.lg_page = __builtin_ctz(p.page), a.cap = q.max_pages * p.page;
   a.causal = c.causal != 0, a.window = c.window, a.sinks = c.sinks;
   a.qscale = c.scale * LOG2E;
-  a.splits = plan.splits;
-  const int pairs = q.n_seqs * p.n_kv_heads;
+  a.splits = plan.splits, a.pairs = q.n_seqs * p.n_kv_heads;
+  a.by_splits = divisor(a.splits), a.by_pairs = divisor(a.pairs), a.by_kv = divisor(a.kv), a.by_group = divisor(a.group);
   a.part = (float*)ws;
   a.stats = (float2*)((float*)ws + part_rows(plan, p, q) * p.head_dim);
   const bool f32 = c.dtype == JPI_F32;
   switch (p.head_dim) {
-    case 64: launch_dim<64>(a, p.code, f32, plan, pairs, s); break;
-    case 128: launch_dim<128>(a, p.code, f32, plan, pairs, s); break;
-    default: launch_dim<256>(a, p.code, f32, plan, pairs, s);
+    case 64: launch_dim<64>(a, p.code, f32, plan, s); break;
+    case 128: launch_dim<128>(a, p.code, f32, plan, s); break;
+    default: launch_dim<256>(a, p.code, f32, plan, s);
   }
   return hipGetLastError();
 }
