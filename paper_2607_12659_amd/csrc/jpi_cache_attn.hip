@@ -154,12 +154,14 @@ __device__ __forceinline__ float groups_sum(float v) {
 template <int PARTS>
 __device__ __forceinline__ void split8(const float* x, bf16x8 (&part)[PARTS]) {
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    float rest = x[e];
+  for (int e = 0; e < 8; e += 2) {
+    float a = x[e], b = x[e + 1];
 #pragma unroll
     for (int p = 0; p < PARTS; ++p) {
-      part[p][e] = (__bf16)rest;
-      if (p + 1 < PARTS) rest -= (float)part[p][e];
+      const bf16x2 both = {(__bf16)a, (__bf16)b};  // one instruction, whose halves are taken as bits
+      part[p][e] = both[0], part[p][e + 1] = both[1];
+      const u32 bits = __builtin_bit_cast(u32, both);
+      a -= __builtin_bit_cast(float, bits << 16), b -= __builtin_bit_cast(float, bits & 0xffff0000u);
     }
   }
 }
