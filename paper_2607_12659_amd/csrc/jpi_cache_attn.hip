@@ -883,20 +883,24 @@ CachePlan cache_plan(const jpi_cache_attn& a, const jpi_cache_pool& p, const jpi
   if (a.window) keys = std::min<int64_t>(keys, (int64_t)a.window + a.sinks + GROUP_ROWS / group + 2 * 64);
   CachePlan plan{};
   // The ring from a workgroup for each compute unit on (of 256 dims, which the other kernel holds one wave of a SIMD at a time
-  // for, from less than half of that), or where there are so many products that it is worth joining ranges of their keys.
-  // us, ring and other: 1024 rows of 32 heads on 8 of 128, 256 workgroups, 33 and 32; 2048 rows 67 and 91; 512 rows 20 and 14,
-  // but before 8192 slots 90 and 121; 256 before 4096 41 and 35; 64, 32 and 16 chunks of 50 rows, 8 heads of 256, 866 slots 47,
-  // 42 and 36, 100, 56 and 28; 8 before 4096 slots 41 and 44.  fp32 has three times the products and none of its time in what
-  // the ring saves: 1024 rows 60 and 50.
+  // for, from half of that), or where there are so many products that it is worth joining ranges of their keys.  us, ring and
+  // other: 1024 rows of 32 heads on 8 of 128, 256 workgroups, 27 and 30; 2048 rows 54 and 86; 512 rows 20 and 13, but before
+  // 8192 slots 87 and 130; 256 before 4096 41 and 38; 32, 28 and 16 chunks of 50 rows, 8 heads of 256, 866 slots 42, 42 and 33,
+  // 52, 41 and 27; 16 and 8 before 4096 slots 54 and 41, 77 and 42.  fp32 has three times the products and none of its time in
+  // what the ring saves: 1024 rows 60 and 43.
   const int64_t groups = (all + GROUP_ROWS - 1) / GROUP_ROWS, steps = (keys + 63) / 64, wgs = groups * pairs;
-  const bool enough = wgs >= (p.head_dim == 256 ? 112 : 256);
+  const bool enough = wgs >= (p.head_dim == 256 ? 128 : 256);
   if (a.dtype == JPI_BF16 && all >= 64 && (enough || all * pairs / GROUP_ROWS * steps >= (p.head_dim == 256 ? 1600 : 8192))) {
     plan.groups = (int)groups;
     plan.splits = enough ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>({16, (p.head_dim == 256 ? 256 : 512) / wgs, steps / 4}));
     return plan;
   }
+  // Ranges until there is a workgroup for each unit; two, if they are resident together, where there is enough for both to
+  // compute.  us, one and two: 64 rows of 32 heads on 8 of 128 before 8192 slots 32 and 27, 128 rows before 2048 15 and 20; one
+  // row of 32 sequences, memory alone, before 4096 51 and 55.
+  const int64_t slots = p.head_dim < 256 && all >= 64 && steps >= 64 ? 512 : 256;
   plan.tiles = (int)((all + 15) / 16);
-  plan.splits = (int)std::max<int64_t>(1, std::min<int64_t>({256, 256 / (pairs * plan.tiles), (keys + 63) / 64 / WAVES}));
+  plan.splits = (int)std::max<int64_t>(1, std::min<int64_t>({256, slots / (pairs * plan.tiles), steps / WAVES}));
   return plan;
 }
 
