@@ -133,7 +133,10 @@ __global__ __launch_bounds__(PLAN_THREADS) void k_resize_plan(Moves m, const int
   if (threadIdx.x == 0) m.count[0] = copies;
 }
 
-// Chunk c of a moving page: K and V of each layer in pieces, the scales with each layer's first
+// Chunk c of a moving page: K and V of each layer in pieces, the scales with each layer's first.  PASSING: through no cache, for
+// many pages whose old places nobody reads again: 227 MB of them 104 us, through the caches 115; the few copies of growing forks,
+// whose sources and copies are read next, took 16 us instead of 15 so.
+template <bool PASSING>
 __device__ __forceinline__ void move_chunk(const Contents& x, int src, int dst, int item) {
   const int per_layer = 2 * x.chunks, layer = item / per_layer, c = item - layer * per_layer;
   const bool values = c >= x.chunks;
@@ -143,23 +146,27 @@ __device__ __forceinline__ void move_chunk(const Contents& x, int src, int dst, 
   u32x4* to = reinterpret_cast<u32x4*>(data + (base + dst) * x.page_bytes + at);
   const int pieces = (int)(min((int64_t)CHUNK, x.page_bytes - at) / 16);
 #pragma unroll 4
-  for (int i = threadIdx.x; i < pieces; i += THREADS) to[i] = from[i];
+  for (int i = threadIdx.x; i < pieces; i += THREADS) {
+    if constexpr (PASSING) __builtin_nontemporal_store(__builtin_nontemporal_load(from + i), to + i);
+    else to[i] = from[i];
+  }
   if (at == 0) {
     float* scale = values ? x.v_scale : x.k_scale;
     for (int i = threadIdx.x; i < x.kv; i += THREADS) scale[(base + dst) * x.kv + i] = scale[(base + src) * x.kv + i];
   }
 }
 
+template <bool PASSING>
 __device__ __forceinline__ void move_pages(const Moves& m, const Contents& x, int first, int workgroups) {
   const int moves = m.count[0], items = x.layers * 2 * x.chunks;
   for (int64_t i = first; i < (int64_t)moves * items; i += workgroups) {
     const int n = (int)(i / items);
-    move_chunk(x, m.src[2 * n], m.src[2 * n + 1], (int)(i - (int64_t)n * items));
+    move_chunk<PASSING>(x, m.src[2 * n], m.src[2 * n + 1], (int)(i - (int64_t)n * items));
   }
 }
 
 __global__ __launch_bounds__(THREADS) void k_resize(Moves m, Contents x, int row_groups, int per_row) {
-  if ((int)blockIdx.x >= row_groups) return move_pages(m, x, blockIdx.x - row_groups, gridDim.x - row_groups);
+  if ((int)blockIdx.x >= row_groups) return move_pages<false>(m, x, blockIdx.x - row_groups, gridDim.x - row_groups);
   const int s = blockIdx.x / per_row, e0 = (blockIdx.x - s * per_row) * ROW_ENTRIES;
   const int old = m.b[s], now = m.len_out[s], first = m.a[s], copied = first >= 0 ? m.c[s] : -1;
   const int had = pages_of(old, m.lg_page), has = pages_of(now, m.lg_page);
@@ -298,7 +305,7 @@ __global__ __launch_bounds__(PLAN_THREADS) void k_compact_plan(Moves m, int32_t*
 }
 
 __global__ __launch_bounds__(THREADS) void k_compact(Moves m, Contents x, int row_groups, int per_row) {
-  if ((int)blockIdx.x >= row_groups) return move_pages(m, x, blockIdx.x - row_groups, gridDim.x - row_groups);
+  if ((int)blockIdx.x >= row_groups) return move_pages<true>(m, x, blockIdx.x - row_groups, gridDim.x - row_groups);
   const int s = blockIdx.x / per_row, e0 = (blockIdx.x - s * per_row) * ROW_ENTRIES, n_live = m.count[1];
   for (int e = e0 + threadIdx.x; e < min(e0 + ROW_ENTRIES, m.max_pages); e += THREADS) {
     const int32_t was = m.table[s * m.table_stride + e];
