@@ -16,20 +16,22 @@
 //
 // Few rows (k_cache_attn): tiles of 16 rows; a workgroup's four waves share out the
 // keys of one, 64 at a time from memory to registers, and join their sums in LDS;
-// where there are fewer than 256 row tiles the keys are cut into ranges as well, by
-// the sequence's own length, and joined by a second launch.  Bound by memory where
-// keys are many: sixty-four sequences of up to 8192 slots, 8 KV heads of 128 dims,
-// 547 MB, 116 us, 4.7 TB/s (a copy reaches 4.8).  One row tile before 817 slots of
-// 256 dims takes 9 us whatever its range, a chain of length, table, page and
-// products, and the join 3.
+// where there are few row tiles the keys are cut into ranges as well, by the
+// sequence's own length, and joined by a second launch.  Bound by memory where keys
+// are many: sixty-four sequences of up to 8192 slots, 8 KV heads of 128 dims, 547 MB,
+// 115 us, 4.7 TB/s (a copy reaches 4.8).  Where rows are more, by a wave's own
+// instructions, of 256 dims the only wave of its SIMD: a tile takes 5000 cycles of it,
+// 1500 of them products.  One row tile before 817 slots of 256 dims takes 8 us whatever
+// its range, a chain of counts, table, pages and products, and the join 3.
 //
 // Many rows (k_cache_rows): tiles of 32 rows, four of them sharing the keys that
 // direct-to-LDS loads bring, 64 a step, up to three steps ahead.  Bound by the
-// instructions between the products: 128 of a step's 340 widen codes, and a step
-// takes 3700 cycles of a wave, 1024 of them its products.  Two waves of a SIMD
-// share that time: 4096 rows of 32 heads on 8 of 128 before 4096 keys 0.92 PFLOP/s,
-// a window of 1024 over 4099 tokens 90 us, 0.67 PFLOP/s of what is seen (a library
-// product of 8192^3 reaches 1.2).
+// instructions between the products: of a step's 310, 1740 cycles of a wave and as
+// many of the SIMD's other one in 3700, 128 widen codes, 33 scale, 32 are powers at a
+// quarter of the rate, 30 add up and 28 look for the maximum; products take 1024.
+// 4096 rows of 32 heads on 8 of 128 before 4096 keys 0.92 PFLOP/s, a window of 1024
+// over 4099 tokens 89 us, 0.68 PFLOP/s of what is seen (a library product of 8192^3
+// reaches 1.2).
 #include <algorithm>
 #include <type_traits>
 
