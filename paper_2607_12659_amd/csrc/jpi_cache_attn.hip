@@ -29,7 +29,7 @@
 // instructions between the products: of a step's 310, 1740 cycles of a wave and as
 // many of the SIMD's other one in 3700, 128 widen codes, 33 scale, 32 are powers at a
 // quarter of the rate, 30 add up and 28 look for the maximum; products take 1024.
-// 4096 rows of 32 heads on 8 of 128 before 4096 keys 0.92 PFLOP/s, a window of 1024
+// 4096 rows of 32 heads on 8 of 128 before 4096 keys 0.97 PFLOP/s, a window of 1024
 // over 4099 tokens 89 us, 0.68 PFLOP/s of what is seen (a library product of 8192^3
 // reaches 1.2).
 #include <algorithm>
