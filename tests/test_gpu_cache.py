@@ -949,6 +949,80 @@ def test_a_pool_past_4_gib(ops, code):
     same_bits(before, [x[t[0].long()] for x in pool])
 
 
+@pytest.mark.parametrize("rows,heads,dh,dtype", [(1, 4, 128, torch.float32), (3, 4, 64, torch.bfloat16), (150, 256, 64, torch.bfloat16),
+                                                 (100, 128, 256, torch.bfloat16)])
+def test_the_longest_sequence(ops, rows, heads, dh, dtype):
+    """2^29 slots in 2^22 pages, most of them the same few: a window at its end sees what the end of a short sequence does."""
+    kv, page, code, window, sinks, width = heads // 4, 128, "int8", 700, 5, 1 << 22
+    assert (plan_of(1, rows, heads, kv, dh, page, True, window, sinks, width, code)[0] > 0) == (rows >= 100)
+    pool = filled(70, 12, kv, dh, page, code)
+    behind = 37  # slots of the last page that are not there
+    few = np.array([[3, 7, 0, 9, 4, 1, 5, 8]], np.int32)  # the first page, and the last ones
+    table = torch.full((1, width), 11, dtype=torch.int32)
+    table[0, 0], table[0, -7:] = 3, torch.from_numpy(few[0, 1:])
+    q = rand(250, 1, rows, heads, dh, dtype=dtype)
+    o, l, mag, err, _ = attn64(q, pool, code, page, few, [8 * page - behind], [rows], True, window, sinks, dh ** -0.5)
+    tol_o, tol_l = attn_tolerance(dtype, o, l, mag, err, window + sinks, dh)
+    d = on_gpu(ops, pool, code)
+    out, lse = ops.attention(dev(q), d, dev(table), i32([(1 << 29) - behind]), window=window, sinks=sinks)
+    within(out, o, tol_o)
+    within(lse, l, tol_l)
+    # tokens at its end; those past it are dropped
+    k, v = rand(251, 1, 41, kv, dh), rand(252, 1, 41, kv, dh)
+    ops.append(d, dev(table), i32([(1 << 29) - behind]), dev(k), dev(v))
+    for i, x in ((0, k), (1, v)):
+        ref.append_one(pool[i], pool[2 + i], i == 0, code, page, few, [8 * page - behind], x.numpy(), [41])
+    same_pool(d, pool)
+
+
+def test_moves_of_the_longest_sequence(ops):
+    width, n_pages, page = 1 << 22, (1 << 22) + 3, 128
+    table, lens = torch.full((1, width), -1, dtype=torch.int32, device="cuda"), i32([0])
+    refs = torch.zeros(n_pages, dtype=torch.int32, device="cuda")
+    refs[1::1 << 21] = 1  # three pages of others
+    others = refs.clone()
+    free = (others == 0).nonzero()[:width, 0].int()
+    _, short = ops.resize(table, lens, refs, i32([1 << 29]), page=page)
+    assert short.item() == 0 and lens.item() == 1 << 29 and torch.equal(table[0], free)
+    assert (refs == 1).all()
+    ops.resize(table, lens, refs, i32([(1 << 28) + 1]), page=page)
+    has = (1 << 21) + 1
+    assert torch.equal(table[0, :has], free[:has]) and (table[0, has:] == -1).all()
+    assert torch.equal((refs == 0).nonzero()[:, 0], free[has:].long())
+    both = torch.cat([table, table])
+    other = torch.tensor([(1 << 28) + 1, 0], dtype=torch.int32, device="cuda")
+    ops.reorder(both, other, refs, i32([1, 0]), page)
+    assert (both[0] == -1).all() and torch.equal(both[1], table[0]) and other.tolist() == [0, (1 << 28) + 1]
+    ops.reorder(both, other, refs, i32([-1, 1]), page)
+    assert torch.equal((refs != 0).nonzero()[:, 0], torch.cat([free[:has].long(), (others != 0).nonzero()[:, 0]]).sort().values)
+    n_live = ops.compact(both, refs)
+    assert n_live.item() == has + 3 and (refs[:has + 3] == 1).all() and (refs[has + 3:] == 0).all()
+
+
+@pytest.mark.parametrize("rows,heads", [(3, 8), (3, 160)])
+def test_strides_past_2_to_the_31(ops, rows, heads):
+    """Rows 2^31 elements apart give what neighbouring ones give."""
+    kv, dh, page, code = heads // 4, 128, 32, "e4m3"
+    far = torch.empty((2 << 31) + heads * dh, dtype=torch.bfloat16, device="cuda")
+    wide = far.as_strided((1, rows, heads, dh), (far.numel(), 1 << 31, dh, 1))
+    q = dev(rand(260, 1, rows, heads, dh, dtype=torch.bfloat16))
+    w = dev(rand(261, dh))
+    wide.copy_(q)
+    near, _ = ops.norm_rope(q, q_weight=w)
+    ops.norm_rope(wide, q_weight=w, q_out=wide)
+    same_bits([wide], [near])
+    d, other = (on_gpu(ops, filled(71, 4, kv, dh, page, code), code) for _ in range(2))
+    table = dev(np.array([[2, 0, 3]], np.int32))
+    ops.append(d, table, i32([60]), near[:, :, :kv], near[:, :, kv:2 * kv])
+    ops.append(other, table, i32([60]), wide[:, :, :kv], wide[:, :, kv:2 * kv])
+    same_bits(d, other)
+    want, lse = ops.attention(near, d, table, i32([63]))
+    got, lse_far = ops.attention(wide, d, table, i32([63]))
+    same_bits([want, lse], [got, lse_far])
+    ops.attention(near, d, table, i32([63]), out=wide)
+    same_bits([want], [wide])
+
+
 def test_equal_calls_give_equal_bits_and_writes_count(ops):
     pool = on_gpu(ops, filled(4, 300, 2, 128, 16, "e4m3"), "e4m3")
     table, lens = dev(numbered(4, [140, 140], 140, 300)), i32([2200, 1500])
