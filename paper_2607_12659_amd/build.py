@@ -4,6 +4,7 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
@@ -29,13 +30,11 @@ def _run(cmd):
 def build_libjpi(verbose: bool = False) -> str:
     bdir = os.path.join(ROOT, "_build")
     os.makedirs(bdir, exist_ok=True)
-    objs = []
-    for src in SOURCES:
-        obj = os.path.join(bdir, os.path.splitext(src)[0] + ".o")
-        out = _run([HIPCC, *FLAGS, "-c", os.path.join(CSRC, src), "-o", obj])
-        if verbose and out.strip():
-            print(out)
-        objs.append(obj)
+    objs = [os.path.join(bdir, os.path.splitext(src)[0] + ".o") for src in SOURCES]
+    with ThreadPoolExecutor(4) as pool:  # compilers at once: 200 s one after the other
+        for out in pool.map(lambda src, obj: _run([HIPCC, *FLAGS, "-c", os.path.join(CSRC, src), "-o", obj]), SOURCES, objs):
+            if verbose and out.strip():
+                print(out)
     tmp = LIB + ".tmp%d" % os.getpid()
     _run([HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", *objs, "-o", tmp])
     os.replace(tmp, LIB)
