@@ -42,7 +42,7 @@ namespace {
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
-constexpr int WAVES = 4, GROUP_ROWS = 32 * WAVES;  // rows of a workgroup of the ring
+constexpr int RING_WAVES = 4, GROUP_ROWS = 32 * RING_WAVES;  // rows of a workgroup of the ring
 constexpr float LOG2E = 1.44269504088896341f, LN2 = 0.693147180559945309f;
 constexpr float HEADROOM = 16.f;  // log2 of the most that a probability may exceed its row's reference by
 
@@ -73,7 +73,7 @@ struct CacheArgs {
   int n_pages, lg_page, cap;
   int causal, window, sinks;
   float qscale;  // scale / ln 2
-  int splits, pairs, per_tile;  // pairs: sequences times KV heads; per_tile: rows of a tile, as far as there are
+  int splits, waves, pairs, per_tile;  // pairs: sequences times KV heads; per_tile: rows of a tile, as far as there are
   Divisor by_splits, by_pairs, by_kv, by_group, by_per_tile;
   float* part;    // [workgroup][rows of a tile][head_dim]
   float2* stats;  // [workgroup][rows of a tile]: reference, sum
@@ -106,7 +106,7 @@ __device__ __forceinline__ Span span_of(const CacheArgs& a, int s, int nth) {
 }
 
 // Tiles of a range, and how many ranges have any (one at least): a wave gets a tile each where there are as many
-__device__ __forceinline__ int per_range(const CacheArgs& a, int count) { return max((count + a.splits - 1) / a.by_splits, WAVES); }
+__device__ __forceinline__ int per_range(const CacheArgs& a, int count) { return max((count + a.splits - 1) / a.by_splits, a.waves); }
 __device__ __forceinline__ int ranges_of(int count, int per) { return max(1, (count + per - 1) / per); }
 
 // One matrix instruction of R rows (queries) and R keys or dims
@@ -186,8 +186,9 @@ __device__ __forceinline__ Scales scales_of(float qscale, float ks, float vs) {
 }
 
 // A wave's row tile: the lane's row, its queries, and the running maximum, sum and O^T of its softmax.  A step takes NT times
-// 16 keys of each lane group, one page and one scale each.
-template <int DH, bool E4M3, typename T, int R, int NT>
+// 16 keys of each lane group, one page and one scale each.  Q_LDS: the queries are in LDS, where all waves of a workgroup have the
+// same row tile.
+template <int DH, bool E4M3, typename T, int R, int NT, bool Q_LDS = false>
 struct Rows {
   typedef Code<E4M3> C;
   typedef Tile<R> M;
@@ -202,18 +203,27 @@ struct Rows {
 
   int grp, token, head, see_lo, see_hi, full_lo, full_hi, len, sinks;
   float qscale, m_ref, sum;
-  bf16x8 q[PARTS][KK][2];
+  bf16x8 q[PARTS][Q_LDS ? 1 : KK][2];
+  const bf16x8* q_lds;  // the lane's first piece
   typename M::acc o[DT];
 
-  // Asks for the queries, before the sequence's counts are there: lanes past its rows have others of the array, or the last
-  __device__ __forceinline__ void ask(const CacheArgs& a, int s, int h, int rt) {
+  // Asks for the queries, before the sequence's counts are there: lanes past its rows have others of the array, or the last.
+  // Q_LDS: each of eight waves brings a piece to `lds`, and all may read them after a barrier.
+  __device__ __forceinline__ void ask(const CacheArgs& a, int s, int h, int rt, bf16x8* lds = nullptr) {
     const int lane = threadIdx.x & 63, col = lane % R;
     grp = lane / R;
     const int r = min(rt * R + col, a.q_rows * a.group - 1);
     token = r / a.by_group, head = h * a.group + (r - token * a.group);
     const T* p = reinterpret_cast<const T*>(a.q) + s * a.q_outer + token * a.q_row + head * a.q_head + 16 * grp;
+    if constexpr (Q_LDS) {
+      static_assert(2 * KK == 8 && PARTS == 1, "a wave's piece");
+      const int wave = threadIdx.x >> 6;
+      lds[wave * 64 + lane] = *reinterpret_cast<const bf16x8*>(p + (wave >> 1) * 16 * G + 8 * (wave & 1));
+      q_lds = lds + lane;
+      return;
+    }
 #pragma unroll
-    for (int kk = 0; kk < KK; ++kk)
+    for (int kk = 0; kk < (Q_LDS ? 0 : KK); ++kk)
 #pragma unroll
       for (int m = 0; m < 2; ++m) {
         const T* at = p + kk * 16 * G + 8 * m;
@@ -249,7 +259,7 @@ struct Rows {
   // O of 256 dims is in the accumulation registers, which the products take as they are.  Left to itself the compiler had it in
   // the others around the branch that brings it to another reference, and copied it there and back in each step.
   __device__ __forceinline__ void hold() {
-    if constexpr (DH == 256) {
+    if constexpr (DH == 256 && !Q_LDS) {
 #pragma unroll
       for (int d = 0; d < DT; ++d) asm volatile("" : "+a"(o[d]));
     }
@@ -289,7 +299,7 @@ struct Rows {
 #pragma unroll
           for (int i = PARTS - 1; i >= 0; --i)
 #pragma unroll
-            for (int j = 0; j < CHAINS; ++j) c[j0 + j] = M::mfma(codes[j], q[i][kk][m], c[j0 + j]);
+            for (int j = 0; j < CHAINS; ++j) c[j0 + j] = M::mfma(codes[j], Q_LDS ? q_lds[(2 * kk + m) * 64] : q[i][Q_LDS ? 0 : kk][m], c[j0 + j]);
         }
 #pragma unroll
     for (int j = 0; j < SETS; ++j)
@@ -456,10 +466,14 @@ __device__ __forceinline__ int64_t page_of(const CacheArgs& a, int id, int h) {
 }
 
 // Few rows: the waves of a workgroup share out the keys of one row tile, each from memory to its own registers.
-// Two waves of a SIMD leave 256 registers each: with three and 168 the loads of a tile (64 registers of 128 dims) spilled.
-template <int DH, bool E4M3, typename T, int R>
-__global__ __launch_bounds__(64 * WAVES, DH == 256 ? 1 : 2) void k_cache_attn(CacheArgs a) {
-  typedef Rows<DH, E4M3, T, R, 1> W;
+// Two waves of a SIMD leave 256 registers each: with three and 168 the loads of a tile (64 registers of 128 dims) spilled.  Of 256
+// dims one wave has 330, or two of them, in a workgroup of eight, 256 each: the queries are then in LDS, and values and half of the
+// next keys are asked for when what came before is done with.
+template <int DH, bool E4M3, typename T, int R, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, DH == 256 && WAVES == 4 ? 1 : 2) void k_cache_attn(CacheArgs a) {
+  constexpr bool LATE = WAVES == 8;
+  typedef Rows<DH, E4M3, T, R, 1, LATE> W;
+  constexpr int EARLY = LATE ? W::KK / 2 : W::KK;
   typedef typename W::M M;
   constexpr int KEYS = W::KEYS, QUADS = W::QUADS;
   __shared__ __align__(16) f32x4 join[WAVES][QUADS][64];
@@ -471,13 +485,14 @@ __global__ __launch_bounds__(64 * WAVES, DH == 256 ? 1 : 2) void k_cache_attn(Ca
   const int rt = rest / a.by_splits, split = rest - rt * a.splits;
   const int s = pair / a.by_kv, h = pair - s * a.kv;
   W w;
-  w.ask(a, s, h, rt);
+  w.ask(a, s, h, rt, reinterpret_cast<bf16x8*>(join));
   const Span x = span_of<R, 1024 / R>(a, s, rt);
   if (rt * R >= x.rows) return;
   const int per = per_range(a, x.count);
   if (split > 0 && split * per >= x.count) return;
   const int first = split * per + wave, last = min(x.count, (split + 1) * per);
   w.begin(a, x);
+  if (LATE) __syncthreads();  // the queries
 
   const int mask = (1 << a.lg_page) - 1;
   const u32 page_bytes = (u32)DH << a.lg_page;
@@ -485,10 +500,10 @@ __global__ __launch_bounds__(64 * WAVES, DH == 256 ? 1 : 2) void k_cache_attn(Ca
   const int key0 = M::key(col, 0), kpiece = key0 & ~15;  // the keys of all sets lie in one piece
   auto page_at = [&](int slot) { return slot < x.len ? table[slot >> a.lg_page] : NO_PAGE; };
   u32x4 kraw[W::SETS][W::KK], vraw[W::DT];
-  auto load_k = [&](int t, int id) {
+  auto load_k = [&](int t, int id, int from, int to) {
     const uint8_t* p = a.k + page_of(a, id, h) * page_bytes + (((grp << a.lg_page) + ((t * KEYS + key0) & mask)) << 4);
 #pragma unroll
-    for (int kk = 0; kk < W::KK; ++kk)
+    for (int kk = from; kk < to; ++kk)
 #pragma unroll
       for (int j = 0; j < W::SETS; ++j) kraw[j][kk] = *reinterpret_cast<const u32x4*>(p + ((u32)(kk * W::G) << (a.lg_page + 4)) + j * 64);
   };
@@ -498,8 +513,8 @@ __global__ __launch_bounds__(64 * WAVES, DH == 256 ? 1 : 2) void k_cache_attn(Ca
     for (int d = 0; d < W::DT; ++d) vraw[d] = *reinterpret_cast<const u32x4*>(p + d * R * 16);
   };
 
-  // pages of the lane's K and V pieces of the next tile, and the present one's scales
-  int kid = NO_PAGE, vid = NO_PAGE;
+  // pages of the lane's K and V pieces of the next tile, of V's of the present one, and the present one's scales
+  int kid = NO_PAGE, vid = NO_PAGE, vid0 = NO_PAGE;
   float ks = 0.f, vs = 0.f;
   if (first < last) {
     const int t = x.tile(first);
@@ -509,8 +524,9 @@ __global__ __launch_bounds__(64 * WAVES, DH == 256 ? 1 : 2) void k_cache_attn(Ca
       kid = page_at(t1 * KEYS + kpiece), vid = page_at(t1 * KEYS + 16 * grp);
     }
     ks = scale_at(a, a.k_scale, v0, h), vs = scale_at(a, a.v_scale, v0, h);
-    load_k(t, k0);
-    load_v(t, v0);
+    load_k(t, k0, 0, W::KK);
+    if (!LATE) load_v(t, v0);
+    vid0 = v0;
   }
   for (int n = first; n < last; n += WAVES) {
     const int t = x.tile(n), next = x.tile(min(n + WAVES, last - 1));
@@ -523,24 +539,32 @@ __global__ __launch_bounds__(64 * WAVES, DH == 256 ? 1 : 2) void k_cache_attn(Ca
     }
     typename W::Step st;
     st.slot0 = t * KEYS, st.sc[0] = scales_of(a.qscale, ks, vs);
+    if (LATE) asm volatile("" ::: "memory");  // the queries stay in LDS
     w.scores(st.p, [&](int j, int kk) { return kraw[j][kk]; });
+    if (LATE) load_v(t, vid0);
+    vid0 = vid1;
     if (more) {
       ks = scale_at(a, a.k_scale, vid1, h), vs = scale_at(a, a.v_scale, vid1, h);
-      load_k(next, kid1);
+      if (!LATE) load_k(next, kid1, 0, W::KK);
     }
     w.refer(st);
     w.probabilities(st);
     w.settle(st);
+    if (LATE && more) load_k(next, kid1, 0, EARLY);
     if (st.slot0 + KEYS > x.len) {
       const u32x4 valid = w.valid(st.slot0 + 16 * grp);
 #pragma unroll
       for (int d = 0; d < W::DT; ++d) vraw[d] &= valid;
     }
     w.add(st, [&](int, int d) { return vraw[d]; });
-    if (more) load_v(next, vid1);
+    if (more) {
+      if (LATE) load_k(next, kid1, EARLY, W::KK);
+      else load_v(next, vid1);
+    }
   }
 
-  // the four waves' sums, brought to one reference and added in their order; a wave adds and writes a quarter of the dims
+  if (LATE) __syncthreads();  // the queries are done with
+  // the waves' sums, brought to one reference and added in their order; each adds and writes its part of the dims
   const float sum = groups_sum<R>(w.sum);
   if (grp == 0) wave_stats[wave][col] = float2{w.m_ref, sum};
 #pragma unroll
@@ -581,7 +605,7 @@ __global__ __launch_bounds__(64 * WAVES, DH == 256 ? 1 : 2) void k_cache_attn(Ca
 template <int DH>
 struct Ring {
   static constexpr int KEYS = 64, PIECES = DH / 8;  // KB of a step: K of 32 keys, of the next 32, then V so, in the order of a lane's reads
-  static constexpr int LOADS = PIECES / WAVES;      // of a wave for a step
+  static constexpr int LOADS = PIECES / RING_WAVES;      // of a wave for a step
   static constexpr int STAGES = 4;
 };
 
@@ -605,7 +629,7 @@ struct Piece16 {
 constexpr int AHEAD = 16;  // steps of a block of these; two blocks are held
 
 template <int DH, bool E4M3>
-__global__ __launch_bounds__(64 * WAVES, DH == 256 ? 1 : 2) void k_cache_rows(CacheArgs a) {
+__global__ __launch_bounds__(64 * RING_WAVES, DH == 256 ? 1 : 2) void k_cache_rows(CacheArgs a) {
   typedef bf16 T;
   typedef Rows<DH, E4M3, T, 32, 2> W;
   typedef Ring<DH> RG;
@@ -618,7 +642,7 @@ __global__ __launch_bounds__(64 * WAVES, DH == 256 ? 1 : 2) void k_cache_rows(Ca
   const int grp = lane / R, col = lane % R;
   // the last rows of causal ones see most: they come first
   const int nth = gridDim.x - 1 - blockIdx.x, rest = nth / a.by_pairs, pair = nth - rest * a.pairs, s = pair / a.by_kv, h = pair - s * a.kv;
-  const int group = rest / a.by_splits, split = rest - group * a.splits, rt = group * WAVES + wave;
+  const int group = rest / a.by_splits, split = rest - group * a.splits, rt = group * RING_WAVES + wave;
   const Span all = span_of<GROUP_ROWS, KEYS>(a, s, group);
   if (group * GROUP_ROWS >= all.rows) return;
   const int per = per_range(a, all.count), first = split * per;
@@ -653,7 +677,7 @@ __global__ __launch_bounds__(64 * WAVES, DH == 256 ? 1 : 2) void k_cache_rows(Ca
   u32 tile[RG::LOADS], unit[RG::LOADS];
 #pragma unroll
   for (int i = 0; i < RG::LOADS; ++i) {
-    const int piece = wave + WAVES * (i % HALF);
+    const int piece = wave + RING_WAVES * (i % HALF);
     tile[i] = piece / W::KK, unit[i] = piece % W::KK;  // as many units of K as of V
   }
   const bool one_page = a.lg_page >= 6;
@@ -673,8 +697,8 @@ __global__ __launch_bounds__(64 * WAVES, DH == 256 ? 1 : 2) void k_cache_rows(Ca
       const uint8_t *kp = a.k + base + (u32)(t0 & mask) * 16, *vp = a.v + base + (u32)(t0 & mask) * DH;
 #pragma unroll
       for (int i = 0; i < RG::LOADS; ++i) {
-        if (i < HALF) load_to_lds(kp + ((unit[i] << (a.lg_page + 5)) + tile[i] * 512), (((u32)grp << a.lg_page) + key0) * 16, to + i * WAVES * 1024);
-        else load_to_lds(vp + (tile[i] * 32 * DH + unit[i] * 512), grp * 16 * DH + col * 16, to + i * WAVES * 1024);
+        if (i < HALF) load_to_lds(kp + ((unit[i] << (a.lg_page + 5)) + tile[i] * 512), (((u32)grp << a.lg_page) + key0) * 16, to + i * RING_WAVES * 1024);
+        else load_to_lds(vp + (tile[i] * 32 * DH + unit[i] * 512), grp * 16 * DH + col * 16, to + i * RING_WAVES * 1024);
       }
     } else {
 #pragma unroll
@@ -682,7 +706,7 @@ __global__ __launch_bounds__(64 * WAVES, DH == 256 ? 1 : 2) void k_cache_rows(Ca
         const int slot = t0 + tile[i] * 32 + (i < HALF ? key0 : 16 * grp);
         const uint64_t base = (uint64_t)place[i] * page_bytes;
         const u32 in = i < HALF ? (((2 * unit[i] + grp) << a.lg_page) + (slot & mask)) * 16 : (slot & mask) * DH + unit[i] * 512 + col * 16;
-        load_to_lds((i < HALF ? a.k : a.v) + base + in, to + i * WAVES * 1024);
+        load_to_lds((i < HALF ? a.k : a.v) + base + in, to + i * RING_WAVES * 1024);
       }
     }
   };
@@ -728,7 +752,7 @@ __global__ __launch_bounds__(64 * WAVES, DH == 256 ? 1 : 2) void k_cache_rows(Ca
     if (st.slot0 + KEYS > all.len) {  // the sequence's last step
 #pragma unroll
       for (int i = 0; i < HALF; ++i) {
-        u32x4* at = reinterpret_cast<u32x4*>(values + (wave + WAVES * i) * 1024);
+        u32x4* at = reinterpret_cast<u32x4*>(values + (wave + RING_WAVES * i) * 1024);
         *at &= w.valid(st.slot0 + 32 * tile[i] + 16 * grp);
       }
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -856,12 +880,16 @@ template <int DH, bool E4M3, typename T>
 void launch_typed(CacheArgs& a, const CachePlan& plan, hipStream_t s) {
   if constexpr (sizeof(T) == 2) {
     if (plan.groups) {
-      k_cache_rows<DH, E4M3><<<(unsigned)(a.pairs * plan.groups * plan.splits), 64 * WAVES, 0, s>>>(a);
+      k_cache_rows<DH, E4M3><<<(unsigned)(a.pairs * plan.groups * plan.splits), 64 * RING_WAVES, 0, s>>>(a);
       if (plan.splits > 1) launch_join<DH, T, GROUP_ROWS>(a, plan.groups, s);
       return;
     }
   }
-  k_cache_attn<DH, E4M3, T, 16><<<(unsigned)(a.pairs * plan.tiles * plan.splits), 64 * WAVES, 0, s>>>(a);
+  const unsigned grid = (unsigned)(a.pairs * plan.tiles * plan.splits);
+  if constexpr (DH == 256 && sizeof(T) == 2) {
+    if (plan.waves == 8) k_cache_attn<DH, E4M3, T, 16, 8><<<grid, 512, 0, s>>>(a);
+  }
+  if (plan.waves == 4) k_cache_attn<DH, E4M3, T, 16, 4><<<grid, 256, 0, s>>>(a);
   if (plan.splits > 1) launch_join<DH, T, 16>(a, plan.tiles, s);
 }
 
@@ -883,7 +911,7 @@ CachePlan cache_plan(const jpi_cache_attn& a, const jpi_cache_pool& p, const jpi
   const int64_t all = (int64_t)a.q_rows * group, pairs = (int64_t)q.n_seqs * p.n_kv_heads;
   int64_t keys = (int64_t)q.max_pages * p.page;
   if (a.window) keys = std::min<int64_t>(keys, (int64_t)a.window + a.sinks + GROUP_ROWS / group + 2 * 64);
-  CachePlan plan{};
+  CachePlan plan{0, 0, 1, 4};
   // The ring from a workgroup for each compute unit on (of 256 dims, which the other kernel holds one wave of a SIMD at a time
   // for, from half of that), or where there are so many products that it is worth joining ranges of their keys.  us, ring and
   // other: 1024 rows of 32 heads on 8 of 128, 256 workgroups, 27 and 30; 2048 rows 54 and 86; 512 rows 20 and 13, but before
@@ -902,7 +930,10 @@ CachePlan cache_plan(const jpi_cache_attn& a, const jpi_cache_pool& p, const jpi
   // row of 32 sequences, memory alone, before 4096 51 and 55.
   const int64_t slots = p.head_dim < 256 && all >= 64 && steps >= 64 ? 512 : 256;
   plan.tiles = (int)((all + 15) / 16);
-  plan.splits = (int)std::max<int64_t>(1, std::min<int64_t>({256, slots / (pairs * plan.tiles), steps / WAVES}));
+  // Eight waves where rows have them compute and there are tiles for half of the units at least.  us, four and eight: 8 and 16
+  // chunks of 50 rows of 8 heads 14.6 and 27, 12.8 and 24; four of 10 rows 11.9 and 12.4; decoding 32 sequences of 4096 96 and 101.
+  if (p.head_dim == 256 && a.dtype == JPI_BF16 && all >= 64 && pairs * plan.tiles >= 128) plan.waves = 8;
+  plan.splits = (int)std::max<int64_t>(1, std::min<int64_t>({256, slots / (pairs * plan.tiles), steps / plan.waves}));
   return plan;
 }
 
@@ -935,7 +966,7 @@ hipError_t launch_cache_attention(const jpi_cache_attn& c, const jpi_cache_pool&
   a.n_pages = p.n_pages, a.lg_page = __builtin_ctz(p.page), a.cap = q.max_pages * p.page;
   a.causal = c.causal != 0, a.window = c.window, a.sinks = c.sinks;
   a.qscale = c.scale * LOG2E;
-  a.splits = plan.splits, a.pairs = q.n_seqs * p.n_kv_heads;
+  a.splits = plan.splits, a.waves = plan.waves, a.pairs = q.n_seqs * p.n_kv_heads;
   a.by_splits = divisor(a.splits), a.by_pairs = divisor(a.pairs), a.by_kv = divisor(a.kv), a.by_group = divisor(a.group);
   a.part = (float*)ws;
   a.stats = (float2*)((float*)ws + part_rows(plan, p, q) * p.head_dim);

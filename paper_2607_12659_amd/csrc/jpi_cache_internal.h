@@ -18,9 +18,9 @@ hipError_t launch_append(const jpi_cache_pool& p, const jpi_cache_seqs& q, jpi_d
                          const jpi_view& v, const int32_t* n_new, hipStream_t s);
 
 // how a call is cut, for each (sequence, KV head): into workgroups of 128 rows that pass the keys through a ring, or (groups 0)
-// into tiles of 16 rows and ranges of their keys
+// into tiles of 16 rows and ranges of their keys, shared out among 4 or 8 waves
 struct CachePlan {
-  int groups, tiles, splits;
+  int groups, tiles, splits, waves;
 };
 CachePlan cache_plan(const jpi_cache_attn& a, const jpi_cache_pool& p, const jpi_cache_seqs& q);
 bool cache_attention_fits(const jpi_cache_attn& a, const jpi_cache_pool& p, const jpi_cache_seqs& q);

@@ -398,6 +398,10 @@ ATTN = [
     (3, 40, 1, 128, 16, [75, 64], None, True, 0, 0, 5),                     # 40 heads: rows of a token in two tiles
     (300, 2, 2, 64, 128, [300], [299], True, 0, 0, 3),
     (1, 4, 4, 256, 128, [9000], None, True, 0, 0, 71),
+    # 256 dims, tiles for half of the card: eight waves share out a tile's keys
+    (50, 8, 1, 256, 32, [866, 50, 31, 0, 513, 70], [50, 50, 31, 7, 49, 1], False, 0, 0, 28),
+    (816, 8, 1, 256, 64, [816], None, True, 0, 0, 13),
+    (35, 16, 4, 256, 16, [700, 36, 513, 1], [35, 35, 0, 1], True, 300, 3, 44),
 ]
 
 
