@@ -912,15 +912,15 @@ CachePlan cache_plan(const jpi_cache_attn& a, const jpi_cache_pool& p, const jpi
   int64_t keys = (int64_t)q.max_pages * p.page;
   if (a.window) keys = std::min<int64_t>(keys, (int64_t)a.window + a.sinks + GROUP_ROWS / group + 2 * 64);
   CachePlan plan{0, 0, 1, 4};
-  // The ring from a workgroup for each compute unit on (of 256 dims, which the other kernel holds one wave of a SIMD at a time
-  // for, from half of that), or where there are so many products that it is worth joining ranges of their keys.  us, ring and
-  // other: 1024 rows of 32 heads on 8 of 128, 256 workgroups, 27 and 30; 2048 rows 54 and 86; 512 rows 20 and 13, but before
-  // 8192 slots 87 and 130; 256 before 4096 41 and 38; 32, 28 and 16 chunks of 50 rows, 8 heads of 256, 866 slots 42, 42 and 33,
-  // 52, 41 and 27; 16 and 8 before 4096 slots 54 and 41, 77 and 42.  fp32 has three times the products and none of its time in
-  // what the ring saves: 1024 rows 60 and 43.
+  // The ring from a workgroup for each compute unit on (of 256 dims, which it holds one wave of a SIMD at a time for, from half
+  // of that), or where there are so many products that it is worth joining ranges of their keys.  us, ring and other: 1024 rows
+  // of 32 heads on 8 of 128, 256 workgroups, 27 and 30; 2048 rows 54 and 86; 512 rows 20 and 13, but before 8192 slots 87 and
+  // 130; 256 before 4096 41 and 38; 48, 32 and 16 chunks of 50 rows, 8 heads of 256, 866 slots 43, 42 and 33, 57, 45 and 24; 12,
+  // 10 and 4 before 4096, 4096 and 8192 slots 50, 45 and 40, 66, 37 and 39.  fp32 has three times the products and none of its
+  // time in what the ring saves: 1024 rows 60 and 43.
   const int64_t groups = (all + GROUP_ROWS - 1) / GROUP_ROWS, steps = (keys + 63) / 64, wgs = groups * pairs;
   const bool enough = wgs >= (p.head_dim == 256 ? 128 : 256);
-  if (a.dtype == JPI_BF16 && all >= 64 && (enough || all * pairs / GROUP_ROWS * steps >= (p.head_dim == 256 ? 1600 : 8192))) {
+  if (a.dtype == JPI_BF16 && all >= 64 && (enough || all * pairs / GROUP_ROWS * steps >= (p.head_dim == 256 ? 2400 : 8192))) {
     plan.groups = (int)groups;
     plan.splits = enough ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>({16, (p.head_dim == 256 ? 256 : 512) / wgs, steps / 4}));
     return plan;
@@ -930,9 +930,9 @@ CachePlan cache_plan(const jpi_cache_attn& a, const jpi_cache_pool& p, const jpi
   // row of 32 sequences, memory alone, before 4096 51 and 55.
   const int64_t slots = p.head_dim < 256 && all >= 64 && steps >= 64 ? 512 : 256;
   plan.tiles = (int)((all + 15) / 16);
-  // Eight waves where rows have them compute and there are tiles for half of the units at least.  us, four and eight: 8 and 16
-  // chunks of 50 rows of 8 heads 14.6 and 27, 12.8 and 24; four of 10 rows 11.9 and 12.4; decoding 32 sequences of 4096 96 and 101.
-  if (p.head_dim == 256 && a.dtype == JPI_BF16 && all >= 64 && pairs * plan.tiles >= 128) plan.waves = 8;
+  // Eight waves where a sequence's rows have them compute.  us, four and eight: 16, 8, 5 and one chunk of 50 rows of 8 heads 27,
+  // 14.6, 16.6 and 12.7, 24, 12.8, 13.7 and 12.3; one of 8 rows 11.7 and 12.1; decoding 32 sequences of 4096 slots 96 and 101.
+  if (p.head_dim == 256 && a.dtype == JPI_BF16 && all >= 128) plan.waves = 8;
   plan.splits = (int)std::max<int64_t>(1, std::min<int64_t>({256, slots / (pairs * plan.tiles), steps / plan.waves}));
   return plan;
 }

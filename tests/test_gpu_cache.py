@@ -445,7 +445,7 @@ RANGES = [
     (64, 2, 2, 128, 64, [1025, 64, 1, 640], [64, 1, 64, 63], False, 0, 0, 5000, False),
     (200, 16, 16, 128, 16, [2700, 200, 515, 199, 0], [200, 200, 131, 7, 3], True, 0, 0, 550, True),
     (70, 64, 8, 64, 64, [9300, 70], None, True, 9000, 70, 10000, True),           # ranges of a window's keys
-    (50, 8, 1, 256, 32, [866, 50, 31, 116, 1100, 0, 600, 64], None, False, 0, 0, 128, False),
+    (50, 8, 1, 256, 32, [866, 50, 31, 116, 1100, 0, 600, 64], None, False, 0, 0, 200, False),
     (50, 16, 2, 256, 64, [300, 50, 49, 1] * 3, [50, 49, 50, 0] * 3, True, 0, 0, 64, True),
 ]
 
