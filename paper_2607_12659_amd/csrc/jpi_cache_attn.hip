@@ -14,15 +14,16 @@
 // dim.  Rows of S^T take the tile's keys in such an order (Tile::key) that a lane's
 // 16 scores are of 16 neighbouring keys: one piece of V, one page, one scale.
 //
-// Few rows (k_cache_attn): tiles of 16 rows; a workgroup's four waves share out the
-// keys of one, 64 at a time from memory to registers, and join their sums in LDS;
-// where there are few row tiles the keys are cut into ranges as well, by the
+// Few rows (k_cache_attn): tiles of 16 rows; a workgroup's four or eight waves share
+// out the keys of one, 64 at a time from memory to registers, and join their sums in
+// LDS; where there are few row tiles the keys are cut into ranges as well, by the
 // sequence's own length, and joined by a second launch.  Bound by memory where keys
 // are many: sixty-four sequences of up to 8192 slots, 8 KV heads of 128 dims, 547 MB,
-// 115 us, 4.7 TB/s (a copy reaches 4.8).  Where rows are more, by a wave's own
-// instructions, of 256 dims the only wave of its SIMD: a tile takes 5000 cycles of it,
-// 1500 of them products.  One row tile before 817 slots of 256 dims takes 8 us whatever
-// its range, a chain of counts, table, pages and products, and the join 3.
+// 115 us, 4.7 TB/s (a copy reaches 4.8).  Where rows are more, by a SIMD's
+// instructions, 4000 cycles a tile of 256 dims, 1500 of them products: eight chunks of
+// 50 rows of 8 heads before 866 slots 12.8 us, 2.5 of them before the first tile is
+// there and 1.5 for the join.  One row tile before 817 slots of 256 dims takes 8 us
+// whatever its range, a chain of counts, table, pages and products, and the join 3.
 //
 // Many rows (k_cache_rows): tiles of 32 rows, four of them sharing the keys that
 // direct-to-LDS loads bring, 64 a step, up to three steps ahead.  Bound by the
