@@ -873,8 +873,13 @@ template <int DH, typename T, int R>
 void launch_join(CacheArgs& a, int tiles, hipStream_t s) {
   a.per_tile = std::min(R, a.q_rows * a.group), a.by_per_tile = divisor(a.per_tile);
   const int rows = a.pairs * tiles * a.per_tile;  // below 2^24: cache_attention_fits
-  if (R > 16 && rows >= 8192) k_cache_join_rows<DH, T, R><<<(unsigned)(((int64_t)rows * DH / 4 + 255) / 256), 256, 0, s>>>(a, rows);
-  else k_cache_join<DH, T, R><<<(unsigned)rows, 256, 0, s>>>(a);
+  if constexpr (R == GROUP_ROWS) {
+    if (rows >= 8192) {
+      k_cache_join_rows<DH, T, R><<<(unsigned)(((int64_t)rows * DH / 4 + 255) / 256), 256, 0, s>>>(a, rows);
+      return;
+    }
+  }
+  k_cache_join<DH, T, R><<<(unsigned)rows, 256, 0, s>>>(a);
 }
 
 template <int DH, bool E4M3, typename T>
