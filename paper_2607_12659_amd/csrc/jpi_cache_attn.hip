@@ -938,7 +938,10 @@ CachePlan cache_plan(const jpi_cache_attn& a, const jpi_cache_pool& p, const jpi
   plan.tiles = (int)((all + 15) / 16);
   // Eight waves where a sequence's rows have them compute.  us, four and eight: 16, 8, 5 and one chunk of 50 rows of 8 heads 27,
   // 14.6, 16.6 and 12.7, 24, 12.8, 13.7 and 12.3; one of 8 rows 11.7 and 12.1; decoding 32 sequences of 4096 slots 96 and 101.
-  if (p.head_dim == 256 && a.dtype == JPI_BF16 && all >= 128) plan.waves = 8;
+  // And where they spare the launch that joins ranges, with two tiles a wave at most: a row of 8 heads before 817 slots 11.2 and
+  // 11.5 of the GPU, but one launch of the host instead of two (int8, whose codes take three times as much to widen, 12.7 and 15.2).
+  const bool spares = p.code == JPI_E4M3 && steps >= 8 && steps <= 16 && pairs * plan.tiles <= slots / 2;
+  if (p.head_dim == 256 && a.dtype == JPI_BF16 && (all >= 128 || spares)) plan.waves = 8;
   plan.splits = (int)std::max<int64_t>(1, std::min<int64_t>({256, slots / (pairs * plan.tiles), steps / plan.waves}));
   return plan;
 }
