@@ -472,11 +472,12 @@ __device__ __forceinline__ int64_t page_of(const CacheArgs& a, int id, int h) {
 // next keys are asked for when what came before is done with.
 template <int DH, bool E4M3, typename T, int R, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, DH == 256 && WAVES == 4 ? 1 : 2) void k_cache_attn(CacheArgs a) {
-  constexpr bool LATE = WAVES == 8;
+  constexpr bool LATE = DH == 256 && WAVES == 8;
   typedef Rows<DH, E4M3, T, R, 1, LATE> W;
   constexpr int EARLY = LATE ? W::KK / 2 : W::KK;
   typedef typename W::M M;
   constexpr int KEYS = W::KEYS, QUADS = W::QUADS;
+  static_assert(QUADS % WAVES == 0 || QUADS < WAVES, "quads of a wave");
   __shared__ __align__(16) f32x4 join[WAVES][QUADS][64];
   __shared__ float2 wave_stats[WAVES][R];
 
@@ -591,6 +592,7 @@ __global__ __launch_bounds__(64 * WAVES, DH == 256 && WAVES == 4 ? 1 : 2) void k
   T* out = reinterpret_cast<T*>(a.out) + s * a.o_outer + w.token * a.o_row + w.head * a.o_head;
 #pragma unroll
   for (int i = 0; i < QUADS; i += WAVES) {
+    if (QUADS < WAVES && wave >= QUADS) break;  // 64 dims are four quads
     f32x4 y = join[0][i + wave][lane] * g[0];
 #pragma unroll
     for (int v = 1; v < WAVES; ++v) y += join[v][i + wave][lane] * g[v];
@@ -892,7 +894,7 @@ void launch_typed(CacheArgs& a, const CachePlan& plan, hipStream_t s) {
     }
   }
   const unsigned grid = (unsigned)(a.pairs * plan.tiles * plan.splits);
-  if constexpr (DH == 256 && sizeof(T) == 2) {
+  if constexpr (sizeof(T) == 2) {
     if (plan.waves == 8) k_cache_attn<DH, E4M3, T, 16, 8><<<grid, 512, 0, s>>>(a);
   }
   if (plan.waves == 4) k_cache_attn<DH, E4M3, T, 16, 4><<<grid, 256, 0, s>>>(a);
@@ -936,13 +938,15 @@ CachePlan cache_plan(const jpi_cache_attn& a, const jpi_cache_pool& p, const jpi
   // row of 32 sequences, memory alone, before 4096 51 and 55.
   const int64_t slots = p.head_dim < 256 && all >= 64 && steps >= 64 ? 512 : 256;
   plan.tiles = (int)((all + 15) / 16);
-  // Eight waves where a sequence's rows have them compute.  us, four and eight: 16, 8, 5 and one chunk of 50 rows of 8 heads 27,
-  // 14.6, 16.6 and 12.7, 24, 12.8, 13.7 and 12.3; one of 8 rows 11.7 and 12.1; decoding 32 sequences of 4096 slots 96 and 101.
-  // And where they spare the launch that joins ranges, with two tiles a wave at most: a row of 8 heads before 817 slots 11.2 and
-  // 11.5 of the GPU, but one launch of the host instead of two (int8, whose codes take three times as much to widen, 12.7 and 15.2).
-  const bool spares = p.code == JPI_E4M3 && steps >= 8 && steps <= 16 && pairs * plan.tiles <= slots / 2;
-  if (p.head_dim == 256 && a.dtype == JPI_BF16 && (all >= 128 || spares)) plan.waves = 8;
-  plan.splits = (int)std::max<int64_t>(1, std::min<int64_t>({256, slots / (pairs * plan.tiles), steps / plan.waves}));
+  // Eight waves of 256 dims where a sequence's rows have them compute.  us, four and eight: 16, 8, 5 and one chunk of 50 rows of 8
+  // heads 27, 14.6, 16.6 and 12.7, 24, 12.8, 13.7 and 12.3; one of 8 rows 11.7 and 12.1; decoding 32 sequences of 4096 slots 96
+  // and 101.  And of all dims where they spare the launch that joins ranges, with two tiles a wave at most: a row before 817 slots
+  // of 256 dims 11.2 and 11.5 of the GPU, before 600 and 1024 of 128 8.9 and 7.6, 6.7 and 7.9, 50 rows before 1024 10.6 and 8.5,
+  // and 11 us of the host instead of 15.  Not int8 of 256 dims, 12.7 and 15.2 of the GPU, nor fp32, of 128 dims 8.3 and 9.9.
+  const bool bf = a.dtype == JPI_BF16, wide = p.head_dim == 256;
+  const bool spares = bf && (!wide || p.code == JPI_E4M3) && steps >= 8 && steps <= 16 && pairs * plan.tiles <= slots / 2;
+  if (spares || (bf && wide && all >= 128)) plan.waves = 8;
+  plan.splits = spares ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>({256, slots / (pairs * plan.tiles), steps / plan.waves}));
   return plan;
 }
 

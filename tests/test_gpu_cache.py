@@ -402,6 +402,10 @@ ATTN = [
     (50, 8, 1, 256, 32, [866, 50, 31, 0, 513, 70], [50, 50, 31, 7, 49, 1], False, 0, 0, 28),
     (816, 8, 1, 256, 64, [816], None, True, 0, 0, 13),
     (35, 16, 4, 256, 16, [700, 36, 513, 1], [35, 35, 0, 1], True, 300, 3, 44),
+    # tables for so few slots that eight waves need no ranges
+    (2, 8, 2, 64, 64, [1024, 513, 1], None, True, 0, 0, 16),
+    (9, 4, 4, 128, 32, [500, 0, 31, 544], [9, 9, 3, 0], False, 0, 0, 17),
+    (1, 8, 1, 256, 16, [1000, 64, 129], None, True, 500, 2, 64),
 ]
 
 
