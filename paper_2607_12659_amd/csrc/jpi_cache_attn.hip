@@ -22,8 +22,9 @@
 // 115 us, 4.7 TB/s (a copy reaches 4.8).  Where rows are more, by a SIMD's
 // instructions, 4000 cycles a tile of 256 dims, 1500 of them products: eight chunks of
 // 50 rows of 8 heads before 866 slots 12.8 us, 2.5 of them before the first tile is
-// there and 1.5 for the join.  One row tile before 817 slots of 256 dims takes 8 us
-// whatever its range, a chain of counts, table, pages and products, and the join 3.
+// there and 1.5 for the join.  One row tile before 817 slots of 256 dims takes 11 us in
+// eight waves of two tiles each, a chain of counts, table, pages and products (in four
+// waves and three ranges 8, and their join 3 more in a launch of its own).
 //
 // Many rows (k_cache_rows): tiles of 32 rows, four of them sharing the keys that
 // direct-to-LDS loads bring, 64 a step, up to three steps ahead.  Bound by the
