@@ -458,10 +458,10 @@ __device__ __forceinline__ void put4(T* out, f32x4 y) {
   }
 }
 
-constexpr int NO_PAGE = -2;  // of slots past the length
-// a number that names no page: its slots are NaN; past the length nothing is seen
-__device__ __forceinline__ float scale_at(const CacheArgs& a, const float* scale, int id, int h) {
-  return (u32)id < (u32)a.n_pages ? scale[(int64_t)id * a.kv + h] : id == NO_PAGE ? 0.f : __builtin_nanf("");
+constexpr int NO_PAGE = -1;  // of slots past the length
+// A number that names no page, of slots that are there: they are NaN.  Past the length nothing is seen.
+__device__ __forceinline__ float scale_at(const CacheArgs& a, const float* scale, int id, int h, bool there) {
+  return (u32)id < (u32)a.n_pages ? scale[(int64_t)id * a.kv + h] : there ? __builtin_nanf("") : 0.f;
 }
 __device__ __forceinline__ int64_t page_of(const CacheArgs& a, int id, int h) {
   return (int64_t)((u32)id < (u32)a.n_pages ? id : 0) * a.kv + h;
@@ -526,7 +526,8 @@ __global__ __launch_bounds__(64 * WAVES, DH == 256 && WAVES == 4 ? 1 : 2) void k
       const int t1 = x.tile(first + WAVES);
       kid = page_at(t1 * KEYS + kpiece), vid = page_at(t1 * KEYS + 16 * grp);
     }
-    ks = scale_at(a, a.k_scale, v0, h), vs = scale_at(a, a.v_scale, v0, h);
+    const bool there = t * KEYS + 16 * grp < x.len;
+    ks = scale_at(a, a.k_scale, v0, h, there), vs = scale_at(a, a.v_scale, v0, h, there);
     load_k(t, k0, 0, W::KK);
     if (!LATE) load_v(t, v0);
     vid0 = v0;
@@ -547,7 +548,8 @@ __global__ __launch_bounds__(64 * WAVES, DH == 256 && WAVES == 4 ? 1 : 2) void k
     if (LATE) load_v(t, vid0);
     vid0 = vid1;
     if (more) {
-      ks = scale_at(a, a.k_scale, vid1, h), vs = scale_at(a, a.v_scale, vid1, h);
+      const bool there = next * KEYS + 16 * grp < x.len;
+      ks = scale_at(a, a.k_scale, vid1, h, there), vs = scale_at(a, a.v_scale, vid1, h, there);
       if (!LATE) load_k(next, kid1, 0, W::KK);
     }
     w.refer(st);
@@ -664,8 +666,10 @@ __global__ __launch_bounds__(64 * RING_WAVES, DH == 256 ? 1 : 2) void k_cache_ro
     const int n = block * AHEAD + (lane >> 2);
     if (n >= count) return;
     const int slot = all.tile(first + n) * KEYS + 16 * (lane & 3);
-    const int id = slot < all.len ? table[slot >> a.lg_page] : NO_PAGE;
-    pieces[block & 1][lane >> 2][lane & 3].sc = scales_of(a.qscale, scale_at(a, a.k_scale, id, h), scale_at(a, a.v_scale, id, h));
+    const bool there = slot < all.len;
+    const int id = there ? table[slot >> a.lg_page] : NO_PAGE;
+    pieces[block & 1][lane >> 2][lane & 3].sc =
+        scales_of(a.qscale, scale_at(a, a.k_scale, id, h, there), scale_at(a, a.v_scale, id, h, there));
     pieces[block & 1][lane >> 2][lane & 3].at = (u32)page_of(a, id, h);
   };
   if (wave == 0) look_up(0);

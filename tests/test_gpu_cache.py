@@ -497,6 +497,25 @@ def test_attention_spoilt_pages(ops, dtype):
     assert torch.isnan(out[2]).all() and not torch.isnan(out[0, :, :32]).any()
 
 
+NO_PAGE_CALLS = [(5, 4, 64, torch.float32), (5, 4, 64, torch.bfloat16), (5, 4, 256, torch.bfloat16), (200, 256, 64, torch.bfloat16),
+                 (200, 128, 256, torch.bfloat16)]  # rows, heads, dim, type: few rows of four and eight waves, and many
+
+
+@pytest.mark.parametrize("number", [-1, -2, -3, -(1 << 31), (1 << 31) - 1, 40])
+@pytest.mark.parametrize("case", range(len(NO_PAGE_CALLS)))
+def test_attention_takes_any_number_that_names_no_page_for_nan(ops, case, number):
+    """Each number outside [0, n_pages), in the middle of what all rows see and in the last page."""
+    rows, heads, dh, dtype = NO_PAGE_CALLS[case]
+    kv, page, code, lens = heads // 4, 16, "e4m3", [300, 296, 300]
+    pool = filled(11, 40, kv, dh, page, code)
+    table = numbered(11, [13] * 3, 19, 40)
+    table[:, 13:] = table[:, :6]
+    table[0, 4], table[1, 18] = number, number
+    q = rand(85 + case, 3, rows, heads, dh, dtype=dtype)
+    out, _ = attend_both(ops, q, pool, code, page, table, lens)
+    assert torch.isnan(out[0]).all() and torch.isnan(out[1, -1]).all() and not torch.isnan(out[2]).any()
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 def test_attention_spoilt_queries_and_sizes_of_values(ops, dtype):
     """NaN and infinity of a query stay in its row; scales of pages far apart; scores that differ by hundreds."""
