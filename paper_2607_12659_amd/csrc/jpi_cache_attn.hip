@@ -410,6 +410,10 @@ struct Rows {
     return v;
   }
 
+  // All bits of a piece of V that is there, none where its scale is NaN: in place of a number that names no page another one is
+  // read, whose codes may be NaN, and rows that do not see it have probabilities of 0.
+  static __device__ __forceinline__ u32 known(const Scales& x) { return x.vs == x.vs ? ~0u : 0u; }
+
   // O += P V; values(t, d) are V's pieces, without what lies past the length
   template <typename VF>
   __device__ __forceinline__ void add(const Step& x, VF values) {
@@ -560,6 +564,11 @@ __global__ __launch_bounds__(64 * WAVES, DH == 256 && WAVES == 4 ? 1 : 2) void k
       const u32x4 valid = w.valid(st.slot0 + 16 * grp);
 #pragma unroll
       for (int d = 0; d < W::DT; ++d) vraw[d] &= valid;
+    }
+    if (!st.fast) {
+      const u32 known = W::known(st.sc[0]);
+#pragma unroll
+      for (int d = 0; d < W::DT; ++d) vraw[d] &= known;
     }
     w.add(st, [&](int, int d) { return vraw[d]; });
     if (more) {
@@ -777,6 +786,14 @@ __global__ __launch_bounds__(64 * RING_WAVES, DH == 256 ? 1 : 2) void k_cache_ro
 #pragma unroll
       for (int d = 0; d < W::DT; ++d) v[t][d] = *reinterpret_cast<const u32x4*>(values + (t * W::DT + d) * 1024);
     w.settle(st);
+    if (!st.fast) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const u32 known = W::known(st.sc[t]);
+#pragma unroll
+        for (int d = 0; d < W::DT; ++d) v[t][d] &= known;
+      }
+    }
     w.add(st, [&](int t, int d) { return v[t][d]; });
 #pragma unroll
     for (int e = 0; e < 32; ++e) st.p[e] = after[e];

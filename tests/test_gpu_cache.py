@@ -516,6 +516,34 @@ def test_attention_takes_any_number_that_names_no_page_for_nan(ops, case, number
     assert torch.isnan(out[0]).all() and torch.isnan(out[1, -1]).all() and not torch.isnan(out[2]).any()
 
 
+@pytest.mark.parametrize("case", range(len(NO_PAGE_CALLS)))
+def test_attention_reads_nothing_out_of_pages_that_are_none(ops, case):
+    """Entries that name no page, behind a window: rows that do not see them are as without them, whatever free pages hold."""
+    rows, heads, dh, dtype = NO_PAGE_CALLS[case]
+    kv, page, code, lens, window = heads // 4, 16, "e4m3", [300, 296, 301], 53
+    pool = filled(12, 40, kv, dh, page, code)
+    table = numbered(12, [13] * 3, 19, 40)
+    table[:, 13:] = table[:, :6]
+    used = set(table.ravel().tolist())
+    free = [p for p in range(40) if p not in used]
+    pool[0][free], pool[1][free] = 0x7f, 0x7f  # NaN codes
+    order = np.arange(40)  # page 0 is free
+    order[[0, free[0]]] = free[0], 0
+    pool, table = [x[order] for x in pool], np.argsort(order)[table].astype(np.int32)
+    q = rand(86 + case, 3, rows, heads, dh, dtype=dtype)
+    attend_both(ops, q, pool, code, page, table, lens, causal=True, window=window)
+    # pages that lie before all windows go, those of their tiles of 64 slots among them
+    for s, n in enumerate(lens):
+        gone = max(0, n - rows - window + 1) // page
+        assert gone * page % 64 != 0
+        table[s, :gone] = -1
+    out, _ = attend_both(ops, q, pool, code, page, table, lens, causal=True, window=window)
+    assert torch.isfinite(out).all()
+    table[1, 17] = 1 << 20  # among what some rows see
+    out, _ = attend_both(ops, q, pool, code, page, table, lens, causal=True, window=window)
+    assert torch.isfinite(out[0]).all() and torch.isnan(out[1, -1]).all() and torch.isfinite(out[2]).all()
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 def test_attention_spoilt_queries_and_sizes_of_values(ops, dtype):
     """NaN and infinity of a query stay in its row; scales of pages far apart; scores that differ by hundreds."""
