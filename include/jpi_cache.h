@@ -8,9 +8,11 @@
  * slots lie in pages that a table names, pages may belong to several sequences
  * at once, and a code of 8 bits stands for each element.  A step of such a
  * program is jpi_cache_resize (room for the new tokens), then for each layer
- * jpi_norm_rope (or jpi_rope), jpi_cache_append and jpi_cache_attention;
- * jpi_cache_reorder forks, frees and reorders sequences between steps, and
- * jpi_cache_compact moves the pages in use together.
+ * jpi_norm_rope (or jpi_rope), jpi_cache_append and jpi_cache_attention, these two
+ * with n_new and q_len the lengths after the resize less those before it: 0 for a
+ * sequence that the pool had no pages for; jpi_cache_reorder forks, frees and
+ * reorders sequences between steps, and jpi_cache_compact moves the pages in use
+ * together.
  *
  * Conventions as include/jpi_prefix.h: no handle and no state, the caller's
  * memory and stream, nothing allocated, only kernels enqueued (so a call may be
@@ -107,13 +109,14 @@ jpi_status jpi_norm_rope(const jpi_head_norm* norm, const jpi_rope_config* cfg, 
  * halving an e4m3 code loses nothing.  Slots that are neither new nor rescaled
  * are left as they were; tokens past max_pages * page slots, and those of pages
  * that are none, are dropped.  A page that the call writes to may belong to one
- * sequence only (jpi_cache_resize sees to it).  k, v: [n_seqs][tokens][n_kv_heads]
- * [head_dim] of type dt; n_new: device [n_seqs], or NULL for `tokens` each; values
- * outside [0, tokens] count as the nearer end.  Any alignment and strides; 16-byte
- * aligned rows are fastest.  tokens 0: nothing is done.  Errors: JPI_ERR_ARG (NULL,
- * values out of the ranges above, alignment, negative strides), JPI_ERR_SHAPE (more
- * than 2^31 - 1 tokens, or workgroups of 256 threads for pages x KV heads that no
- * launch holds), JPI_ERR_DTYPE, JPI_ERR_HIP. */
+ * sequence only: jpi_cache_resize sees to it for as many tokens as it lengthened
+ * the sequence by, and not for one that it left as it was.  k, v: [n_seqs][tokens]
+ * [n_kv_heads][head_dim] of type dt; n_new: device [n_seqs], or NULL for `tokens`
+ * each; values outside [0, tokens] count as the nearer end.  Any alignment and
+ * strides; 16-byte aligned rows are fastest.  tokens 0: nothing is done.  Errors:
+ * JPI_ERR_ARG (NULL, values out of the ranges above, alignment, negative strides),
+ * JPI_ERR_SHAPE (more than 2^31 - 1 tokens, or workgroups of 256 threads for pages x
+ * KV heads that no launch holds), JPI_ERR_DTYPE, JPI_ERR_HIP. */
 jpi_status jpi_cache_append(const jpi_cache_pool* pool, const jpi_cache_seqs* seqs, jpi_dtype dt, int tokens, const jpi_view* k,
                             const jpi_view* v, const int32_t* n_new, void* stream);
 
@@ -192,8 +195,9 @@ jpi_status jpi_cache_moves_workspace(const jpi_cache_moves* m, size_t* bytes);
  * in a page that others hold.  Free pages (those with a count <= 0 before the call)
  * are taken in ascending order, by the sequences in their order, the copy before
  * the new ones.  A sequence that needs pages is served if the needs up to and with
- * its own are no more than the free pages; otherwise it stays as it was.  short_out
- * (device int32 [1], or NULL): how many free pages all needs together lacked.
+ * its own are no more than the free pages; otherwise it stays as it was, its last
+ * page shared as before: nothing may be appended to it.  short_out (device int32 [1],
+ * or NULL): how many free pages all needs together lacked.
  * Pages that the call sets free serve from the next call on.  seqs->len and
  * new_len may not overlap len_out unless they are len_out itself. */
 jpi_status jpi_cache_resize(const jpi_cache_moves* m, const jpi_cache_pool* pool, int layers, const int32_t* new_len,

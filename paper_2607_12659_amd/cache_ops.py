@@ -13,14 +13,17 @@ devices and types).
 
 Sequence s holds slots 0 .. lens[s] - 1, slot j in the page that table[s][j //
 page] names; refs counts the sequences that hold each page, and a page that none
-holds is free.  A step of a program that samples texts::
+holds is free.  Where pages are lacking, sequences keep the length that they had,
+and their last page may still be another's too: what resize gave is the growth of
+lens, and that is what a step may write.  A step of a program that samples texts::
 
     starts = lens.clone()
     resize(table, lens, refs, lens + n, pool)         # room, in all layers
+    n_new = lens - starts                             # 0 for who was not served: nothing of it is written or attends
     for each layer:
         q, k = norm_rope(q, k, positions, q_weight=..., k_weight=...)
-        append(pool.layer(i), table, starts, k, v)
-        out, lse = attention(q, pool.layer(i), table, lens)
+        append(pool.layer(i), table, starts, k, v, n_new=n_new)
+        out, lse = attention(q, pool.layer(i), table, lens, q_lens=n_new)
     reorder(table, lens, refs, parents, page)         # fork, free, reorder
 """
 from __future__ import annotations
@@ -171,7 +174,8 @@ def norm_rope(q, k=None, positions=None, *, q_weight=None, k_weight=None, eps=1e
 
 def append(pool, table, starts, k, v, *, n_new=None):
     """Write token t of k and v [sequences][tokens][kv_heads][head_dim] as slot starts[s] + t of sequence s into the pages of
-    its row of table: ``jpi_cache_append``.  n_new: int32 [sequences], how many of its tokens are new, None for all.
+    its row of table: ``jpi_cache_append``.  n_new: int32 [sequences], how many of its tokens are new, None for all; no more
+    than resize gave room for, since a page that is written to may be no other sequence's as well.
     """
     packed, _, _, _, kv, dh, dev = _pool(pool, False)
     if k.dim() != 4:

@@ -272,3 +272,65 @@ def test_tensors_that_want_gradients_are_refused(ops):
             call()
         with torch.no_grad(), pytest.raises(ValueError, match="GPU"):
             call()
+
+
+# ---- the step that the module describes, in a pool that runs out -------------------------------------------------------------
+def test_the_described_step_leaves_alone_who_was_not_served(ops):
+    """The step of the module's docstring, run over the plain forms: two forks that share their last page want to grow, and the
+    pool has a page for neither or for one; a third one has room in its own page."""
+    import re
+    import textwrap
+
+    import numpy as np
+
+    import cache_reference as ref
+
+    text = re.search(r"::\n\n(.*?)\n\n?\Z", ops.__doc__ + "\n", re.S).group(1)
+    code = textwrap.dedent(text).replace("for each layer:", "for i in range(layers):")
+    page, layers, kv, dh = 16, 2, 1, 64
+
+    class Layers(list):
+        layer = list.__getitem__
+
+    for free in (0, 1):
+        n_pages = 3 + free
+        r = np.random.RandomState(free)
+        pool = Layers([[r.randint(0, 64, (n_pages, kv, dh // 16, page, 16)).astype(np.uint8),
+                        r.randint(0, 64, (n_pages, kv, page // 16, dh, 16)).astype(np.uint8),
+                        np.ones((n_pages, kv), np.float32), np.ones((n_pages, kv), np.float32)] for _ in range(layers)])
+        table, lens = np.array([[1, -1], [1, -1], [2, -1]], np.int32), np.array([5, 5, 7], np.int32)
+        refs = np.array([1, 2, 1] + [0] * free, np.int32)
+        shared = [[x[1].copy() for x in p] for p in pool]
+        rows = []
+
+        class Lens(np.ndarray):
+            clone = np.ndarray.copy
+
+        def resize(table, lens, refs, new, pool):
+            *state, short, copies = ref.resize(table, np.asarray(lens), refs, np.asarray(new), page)
+            for x, y in zip((table, lens, refs), state):
+                x[...] = y
+            for p in pool:
+                for x in p:
+                    for a, b in copies:
+                        x[b] = x[a]
+            return lens, short
+
+        def append(p, table, starts, k, v, n_new=None):
+            n = np.full(3, k.shape[1]) if n_new is None else np.asarray(n_new)
+            for x, of in ((0, k), (1, v)):
+                ref.append_one(p[x], p[2 + x], x == 0, "int8", page, table, starts, of, n)
+
+        def attention(q, p, table, lens, q_lens=None, **kw):
+            rows.append(np.full(3, q.shape[1]) if q_lens is None else np.asarray(q_lens))
+            return q, None
+
+        x = r.randn(3, 1, kv, dh).astype(np.float32)
+        exec(code, dict(resize=resize, append=append, attention=attention, norm_rope=lambda q, k, *a, **kw: (q, k),
+                        reorder=lambda *a: None, table=table, lens=lens.view(Lens), refs=refs, pool=pool, layers=layers, page=page,
+                        n=1, q=x, k=x, v=x, positions=None, parents=None))
+        assert lens.tolist() == [5 + free, 5, 8]
+        assert [n.tolist() for n in rows] == [[free, 0, 1]] * layers
+        for p, before in zip(pool, shared):
+            for y, b in zip(p, before):
+                assert np.array_equal(y[1], b), "a shared page changed"

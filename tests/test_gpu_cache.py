@@ -866,6 +866,51 @@ def test_a_run_of_them_together(ops, code, dtype):
     assert (r.cpu() == 0).all()
 
 
+@pytest.mark.parametrize("code,dtype", [("e4m3", torch.bfloat16), ("int8", torch.float32)])
+def test_a_step_in_a_pool_that_runs_out(ops, code, dtype):
+    """Three forks of 21 slots and a sequence of 26 want three tokens each, and there is one page: it goes to the first fork;
+    the two others' shared page, their rows of the outputs and their lengths stay as they were, until pages are free again."""
+    kv, heads, dh, page, S, tokens = 2, 4, 64, 16, 4, 3
+    pool = filled(13, 6, kv, dh, page, code)
+    d = on_gpu(ops, pool, code)
+    table = np.array([[0, 1, -1], [0, 1, -1], [0, 1, -1], [2, 3, -1]], np.int32)
+    lens, refs = np.array([21, 21, 21, 26], np.int32), np.array([3, 3, 1, 1, 1, 0], np.int32)  # page 4 is somebody else's
+    t, l, r = dev(table), dev(lens), dev(refs)
+    for step, given in enumerate(([3, 0, 0, 3], [0, 0, 3, 3])):
+        if step:  # the first two forks give their pages back; the third has its last page for itself
+            ops.reorder(t, l, r, i32([-1, -1, 2, 3]), page)
+            table, lens, refs = ref.reorder(table, lens, refs, [-1, -1, 2, 3], page)
+            want = np.array([0, 0, 24, 32], np.int32)
+        else:
+            want = lens + 3
+        starts, before = l.clone(), [x.copy() for x in pool]
+        _, short = ops.resize(t, l, r, i32(want), ops.Pool(*(x[None] for x in d)))
+        table, lens, refs, lack, copies = ref.resize(table, lens, refs, want, page)
+        assert short.item() == lack == (0 if step else 2)
+        pool = [x.copy() for x in pool]
+        for a, b in copies:
+            for x in pool:
+                x[b] = x[a]
+        n_new = l - starts
+        assert n_new.tolist() == given
+        q, k, v = (dev(rand(270 + 3 * step + i, S, tokens, heads if i == 0 else kv, dh, dtype=dtype)) for i in range(3))
+        ops.append(d, t, starts, k, v, n_new=n_new)
+        for i, x in ((0, k), (1, v)):
+            ref.append_one(pool[i], pool[2 + i], i == 0, code, page, table, starts.tolist(), x.cpu().float().numpy(), given)
+        same_pool(d, pool)
+        if not step:
+            assert all(np.array_equal(x[1], b[1]) for x, b in zip(pool, before))  # the shared page
+        out = torch.full(q.shape, -77.0, dtype=dtype, device="cuda")
+        lse = torch.full(q.shape[:3], -77.0, device="cuda")
+        ops.attention(q, d, t, l, q_lens=n_new, out=out, lse=lse)
+        o, ls, mag, err, there = attn64(q.cpu(), pool, code, page, table, lens, given, True, 0, 0, dh ** -0.5)
+        tol_o, tol_l = attn_tolerance(dtype, o, ls, mag, err, 32, dh)
+        there = torch.from_numpy(there)
+        within(out.cpu()[there], o[there.numpy()], tol_o[there.numpy()])
+        within(lse.cpu()[there], ls[there.numpy()], tol_l[there.numpy()])
+        assert (out.cpu()[~there] == -77).all() and (lse.cpu()[~there] == -77).all()
+
+
 # ---------------------------------------------------------------------------
 # as programs call them
 # ---------------------------------------------------------------------------
