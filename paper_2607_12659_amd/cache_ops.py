@@ -237,6 +237,8 @@ def attention(q, pool, table, lens, *, q_lens=None, causal=True, window=0, sinks
 def _moves(table, lens, refs, pool, page, table_out, lens_out, refs_out):
     """The C structures of a move and its pool, layers, the workspace, the device, the number of sequences, and what changes."""
     if pool is not None:
+        if _recording():
+            _no_gradients(*pool)
         packed, layers, n_pages, slots, _, _, dev = _pool(pool, True)
         if page not in (None, slots):
             raise ValueError("page is %s, that of the pool %d" % (page, slots))

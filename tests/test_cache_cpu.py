@@ -274,6 +274,18 @@ def test_tensors_that_want_gradients_are_refused(ops):
             call()
 
 
+def test_pools_that_want_gradients_are_refused_by_moves(ops):
+    import torch
+    p, table, lens, refs, _, _ = tensors(ops)
+    for i in (2, 3):
+        leaf = p._replace(**{p._fields[i]: p[i].clone().requires_grad_()})
+        for call in (lambda: ops.resize(table, lens, refs, lens.clone(), leaf), lambda: ops.compact(table, refs, leaf)):
+            with pytest.raises(ValueError, match="gradients"):
+                call()
+            with torch.no_grad(), pytest.raises(ValueError, match="GPU"):
+                call()
+
+
 # ---- the step that the module describes, in a pool that runs out -------------------------------------------------------------
 def test_the_described_step_leaves_alone_who_was_not_served(ops):
     """The step of the module's docstring, run over the plain forms: two forks that share their last page want to grow, and the
