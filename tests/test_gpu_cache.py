@@ -621,6 +621,82 @@ def test_attention_many_rows_spoilt_queries_and_sizes_of_values(ops, case, code)
         assert torch.equal(g.cpu()[keep], w.cpu()[keep]) and torch.isnan(g.cpu()[~keep].reshape(2, -1)).any(-1).all()
 
 
+# rows, heads, KV heads, dim of eight sequences: few rows in four and in eight waves, and many
+PRECISE = [(9, 4, 1, 64), (1, 8, 2, 128), (20, 8, 1, 256), (70, 64, 32, 64), (70, 64, 16, 128), (70, 32, 4, 256)]
+
+
+@pytest.mark.parametrize("case", range(len(PRECISE)))
+@pytest.mark.parametrize("code", CODES)
+def test_attention_of_few_slots_is_as_good_as_its_parts(ops, case, code):
+    """Two bf16 parts of a probability leave 2^-16 of it (half a step, 2^-8, of the remainder, itself 2^-8 at most), one part
+    2^-8.  The output's own half step shrinks with values that cancel, and slots are few, so that one part where there should be
+    two shows.  Scores and sums as in attn_tolerance."""
+    rows, heads, kv, dh = PRECISE[case]
+    page, width, many = 16, 10, rows == 70
+    assert (plan_of(8, rows, heads, kv, dh, page, False, 0, 0, width, code)[0] > 0) == many
+    lens = [1, 2, 3, 4, 5, 7, 17, 40]
+    pool = filled(62, 12, kv, dh, page, code)
+    table = numbered(62, [-(-n // page) for n in lens], width, 12)
+    q = (0.5 * rand(162 + case, 8, rows, heads, dh)).to(torch.bfloat16)
+    out, lse = ops.attention(dev(q), on_gpu(ops, pool, code), dev(table), i32(lens), causal=False)
+    o, l, mag, err, _ = attn64(q, pool, code, page, table, lens, [rows] * 8, False, 0, 0, dh ** -0.5)
+    ds = (dh + 8) * U * err + 8 * U * (np.abs(l) + 1)
+    soft = 2 * ds + (40 + 40) * U
+    within(lse, l, soft)
+    within(out, o, 2.0 ** -8 * np.abs(o) + mag * (soft[..., None] + (2.0 ** -8 if many else 2.0 ** -16)) * 1.01)
+    # all of a row on one slot: its value, which bf16 holds
+    out, _ = ops.attention(dev(q), on_gpu(ops, pool, code), dev(table), i32([1] * 8), causal=False)
+    for s in range(8):
+        v = torch.from_numpy(ref.slots(pool[1], pool[3], False, code, page, table[s], 1)[:, 0])
+        assert torch.equal(out[s].cpu().double(), v.repeat_interleave(heads // kv, 0).expand(rows, heads, dh))
+
+
+@pytest.mark.parametrize("code", CODES)
+def test_attention_takes_fp32_queries_whole(ops, code):
+    """Slots with one element that is not 0: a row's score is the product of two numbers, 24 bits of them the query's.  fp32
+    rounds the sum of the three parts' products, the scale, the product with it, the reference, the power and the logarithm,
+    once each or twice: 8 u of the score, and 8 u of a number below 2.  Without the third part 128 u of it would be missing."""
+    kv, dh, page = 1, 64, 16
+    codes = np.zeros((1, kv, page, dh), np.uint8)
+    pool = filled(63, 1, kv, dh, page, code)
+    codes[0, 0, 0, 37] = ref.encode(96.0, code)
+    pool[0] = ref.in_pieces(codes, True)
+    pool[2][:] = 0.25
+    q = rand(163, 1, 500, 2, dh)
+    _, lse = ops.attention(dev(q), on_gpu(ops, pool, code), dev(np.zeros((1, 1), np.int32)), i32([1]), causal=False)
+    want = q[..., 37].double() * 24 / 8
+    within(lse, want, 8 * U * (want.abs() + 1))
+
+
+@pytest.mark.parametrize("case", range(len(PRECISE)))
+@pytest.mark.parametrize("code", CODES)
+def test_attention_scales_of_values_from_end_to_end(ops, case, code):
+    """Pages of zeros as append writes them (a scale of 2^-126), scales from 2^-90 to 2^100, 0 and odd ones, one of them in a
+    sequence and several: out and lse as ever, in the scale of what a row sees."""
+    rows, heads, kv, dh = PRECISE[case]
+    page, width = 16, 10
+    pool = filled(64, 60, kv, dh, page, code)
+    scales = [[2.0 ** -126] * 6, [2.0 ** -126, 1, 2.0 ** -126, 0.5, 1, 1], [2.0 ** 100] * 6, [2.0 ** -90] * 6,
+              [2.0 ** -60, 2.0 ** -70, 2.0 ** -80, 2.0 ** -79, 2.0 ** -62, 2.0 ** -66], [2.0 ** 60, 2.0 ** 66, 2.0 ** 64, 2.0 ** 65, 2.0 ** 63, 2.0 ** 70],
+              [0, 0, 2.0 ** -6, 0, 2.0 ** -6, 0], [1.7 * 2.0 ** 30, 1.999 * 2.0 ** -3, 2.0 ** -3, 1.2 * 2.0 ** 30, 2.0 ** 29, 1]]
+    table = numbered(64, [6] * 8, width, 60)
+    for s in range(8):
+        for i in range(6):
+            pool[3][table[s, i]] = scales[s][i]
+            if scales[s][i] == 2.0 ** -126:
+                pool[1][table[s, i]] = 0
+    lens = [96, 95, 80, 96, 90, 96, 33, 96]
+    q = rand(164 + case, 8, rows, heads, dh).to(torch.bfloat16)
+    q[1] *= 4
+    out, lse = ops.attention(dev(q), on_gpu(ops, pool, code), dev(table), i32(lens))
+    o, l, mag, err, _ = attn64(q, pool, code, page, table, lens, [rows] * 8, True, 0, 0, dh ** -0.5)
+    tol_o, tol_l = attn_tolerance(q.dtype, o, l, mag, err, 96, dh)
+    # instead of 1e-30: nothing below 2^-126, fp32's and bf16's least normal number, need be held
+    tol_o = np.where(mag > 0, tol_o - 1e-30 + 2.0 ** -126, 0)
+    within(lse, l, tol_l)
+    within(out, o, tol_o)
+
+
 def test_attention_strides_shared_pages_and_a_single_slot(ops):
     """q as a part of a projection, out as heads of another tensor, a table with a longer row; sequences that share pages; all
     probability on one slot gives its value."""
