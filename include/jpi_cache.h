@@ -165,6 +165,8 @@ jpi_status jpi_cache_attention(const jpi_cache_attn* a, const jpi_cache_pool* po
  * workspace query. */
 jpi_status jpi_debug_cache_plan(const jpi_cache_attn* a, const jpi_cache_pool* pool, const jpi_cache_seqs* seqs, int* groups,
                                 int* tiles, int* ranges);
+/* And how many waves a workgroup has: 4 or 8. */
+jpi_status jpi_debug_cache_waves(const jpi_cache_attn* a, const jpi_cache_pool* pool, const jpi_cache_seqs* seqs, int* waves);
 
 /* ---- moves of pages ---------------------------------------------------------
  * refs: device int32 [n_pages], the number of sequences that hold each page; a

@@ -174,6 +174,14 @@ jpi_status jpi_debug_cache_plan(const jpi_cache_attn* a, const jpi_cache_pool* p
   return JPI_OK;
 }
 
+jpi_status jpi_debug_cache_waves(const jpi_cache_attn* a, const jpi_cache_pool* pool, const jpi_cache_seqs* seqs, int* waves) {
+  const char* call = "jpi_debug_cache_waves";
+  if (!waves) return fail(JPI_ERR_ARG, "%s: NULL argument", call);
+  const jpi_status st = check_attention(call, a, pool, seqs);
+  if (st == JPI_OK) *waves = cache_plan(*a, *pool, *seqs).waves;
+  return st;
+}
+
 jpi_status jpi_cache_attention(const jpi_cache_attn* a, const jpi_cache_pool* pool, const jpi_cache_seqs* seqs, void* workspace,
                                size_t workspace_bytes, void* stream) {
   const char* call = "jpi_cache_attention";

@@ -33,7 +33,7 @@ EXPORTED = ["jpi_abi_version", "jpi_status_str", "jpi_last_error", "jpi_create",
             "jpi_corr_predict", "jpi_corr_last_error", "jpi_prefix_last_error", "jpi_rope",
             "jpi_shared_attention_workspace", "jpi_prefix_weight_workspace", "jpi_shared_attention", "jpi_prefix_weight",
             "jpi_evict", "jpi_debug_prefix_plan", "jpi_cache_last_error", "jpi_norm_rope", "jpi_cache_append",
-            "jpi_cache_attention_workspace", "jpi_cache_attention", "jpi_debug_cache_plan", "jpi_cache_moves_workspace",
+            "jpi_cache_attention_workspace", "jpi_cache_attention", "jpi_debug_cache_plan", "jpi_debug_cache_waves", "jpi_cache_moves_workspace",
             "jpi_cache_resize", "jpi_cache_reorder", "jpi_cache_compact"]
 JPI_ROPE_HALF, JPI_ROPE_INTERLEAVED = 0, 1
 JPI_ROPE_PLAIN, JPI_ROPE_LINEAR, JPI_ROPE_BASE, JPI_ROPE_PARTS = range(4)
@@ -233,6 +233,7 @@ _sig = {
     "jpi_cache_attention_workspace": (_i, [_vp, _vp, _vp, _vp]),
     "jpi_cache_attention": (_i, [_vp, _vp, _vp, _vp, ctypes.c_size_t, _vp]),
     "jpi_debug_cache_plan": (_i, [_vp, _vp, _vp, _vp, _vp, _vp]),
+    "jpi_debug_cache_waves": (_i, [_vp, _vp, _vp, _vp]),
     "jpi_cache_moves_workspace": (_i, [_vp, _vp]),
     "jpi_cache_resize": (_i, [_vp, _vp, _i, _vp, _vp, _vp, ctypes.c_size_t, _vp]),
     "jpi_cache_reorder": (_i, [_vp, _vp, _vp, ctypes.c_size_t, _vp]),
@@ -548,6 +549,13 @@ def jpi_debug_cache_plan(args: jpi_cache_attn, pool: jpi_cache_pool, seqs: jpi_c
     v = [ctypes.c_int() for _ in range(3)]
     st = _lib.jpi_debug_cache_plan(_ref(args), _ref(pool), _ref(seqs), *(ctypes.byref(x) for x in v))
     return (st, *(x.value for x in v))
+
+
+def jpi_debug_cache_waves(args: jpi_cache_attn, pool: jpi_cache_pool, seqs: jpi_cache_seqs):
+    """(status, waves)"""
+    v = ctypes.c_int()
+    st = _lib.jpi_debug_cache_waves(_ref(args), _ref(pool), _ref(seqs), ctypes.byref(v))
+    return st, v.value
 
 
 def jpi_cache_moves_workspace(args: jpi_cache_moves):

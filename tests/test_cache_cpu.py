@@ -140,6 +140,23 @@ def test_attention_refuses_types_sizes_and_workspaces():
     assert j._lib.jpi_debug_cache_plan(None, None, None, None, None, None) == j.JPI_ERR_ARG
 
 
+def test_how_a_call_is_cut():
+    """Waves, groups and ranges by sizes: a row before a short table, a chunk, a long table, many rows, and fp32."""
+    def plan(rows, heads, kv, dim, width, n=1, **kw):
+        a, p, q = attn(q_rows=rows, n_heads=heads, **kw), pool(n_kv_heads=kv, head_dim=dim), seqs(n_seqs=n, max_pages=width, table_stride=width)
+        (st, groups, _, ranges), (st2, waves) = j.jpi_debug_cache_plan(a, p, q), j.jpi_debug_cache_waves(a, p, q)
+        assert st == st2 == j.JPI_OK
+        return waves, groups > 0, ranges > 1
+    assert plan(1, 8, 1, 256, 13) == (8, False, False) and plan(1, 8, 1, 256, 13, dtype=j.JPI_F32) == (4, False, True)
+    assert plan(50, 8, 1, 256, 14, n=8) == (8, False, False) and plan(50, 8, 1, 256, 64) == (8, False, True)
+    assert plan(1, 32, 8, 128, 64) == (4, False, True) and plan(1, 32, 8, 128, 7) == (4, False, False)
+    assert plan(1, 32, 8, 128, 128, n=64) == (4, False, False) and plan(4096, 32, 8, 128, 64)[1:] == (True, False)
+    assert plan(512, 32, 8, 128, 128)[1:] == (True, True)
+    assert j.jpi_debug_cache_waves(attn(q_rows=0), pool(), seqs()) == (j.JPI_ERR_ARG, 0)
+    assert j.jpi_cache_last_error().startswith("jpi_debug_cache_waves: ")
+    assert j._lib.jpi_debug_cache_waves(None, None, None, None) == j.JPI_ERR_ARG
+
+
 # ---- moves of pages ------------------------------------------------------------------------------------------------------
 def moves(**kw):
     m = j.jpi_cache_moves(seqs(table=FAKE, len=2 * FAKE), 3 * FAKE, 4 * FAKE, 8, 5 * FAKE, 6 * FAKE, 100, 64)

@@ -443,6 +443,62 @@ def test_attention(ops, case, code, dtype):
     attend_both(ops, q, pool, code, page, table, lens, q_lens, causal, window, sinks)
 
 
+# few rows whose keys are cut into ranges; the last two entries: waves of a workgroup, and whether they are cut
+SPLIT = [
+    (1, 32, 8, 128, 64, [4000, 70], None, True, 0, 0, 64, 4, True),
+    (5, 16, 2, 128, 16, [1700, 3, 900], [5, 3, 0], True, 1200, 7, 300, 4, True),
+    (3, 4, 4, 64, 32, [3000, 64, 1], None, False, 0, 0, 100, 4, True),
+    (1, 8, 1, 256, 64, [5000, 817], None, True, 0, 0, 80, 4, True),
+    (50, 8, 1, 256, 64, [4000, 50], None, True, 0, 0, 64, 8, True),
+    (40, 16, 2, 256, 32, [2000, 700], [40, 33], True, 1500, 3, 64, 8, True),
+    (33, 4, 1, 256, 16, [1500, 33, 0, 64], [33, 1, 33, 30], False, 0, 0, 128, 8, True),
+    (130, 1, 1, 256, 128, [3000], [129], True, 0, 0, 30, 8, True),
+    (2, 8, 1, 256, 64, [300, 65], None, True, 0, 0, 5, 4, False),
+]
+
+
+def waves_of(n, rows, heads, kv, dh, page, causal, window, sinks, width, code, dtype=torch.bfloat16):
+    from paper_2607_12659_amd import jpi as j
+    a = j.jpi_cache_attn(j.JPI_BF16 if dtype == torch.bfloat16 else j.JPI_F32, rows, heads, int(causal), window, sinks, dh ** -0.5)
+    st, waves = j.jpi_debug_cache_waves(a, j.jpi_cache_pool(getattr(j, "JPI_" + code.upper()), kv, dh, 1, page), j.jpi_cache_seqs(n, width, width))
+    assert st == j.JPI_OK
+    return waves
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("code", CODES)
+@pytest.mark.parametrize("case", range(len(SPLIT)))
+def test_attention_ranges_of_few_rows(ops, case, code, dtype):
+    rows, heads, kv, dh, page, lens, q_lens, causal, window, sinks, width, waves, cut = SPLIT[case]
+    sizes = (len(lens), rows, heads, kv, dh, page, causal, window, sinks, width, code)
+    if dtype == torch.bfloat16:
+        groups, _, ranges = plan_of(*sizes)
+        assert groups == 0 and (ranges > 1) == cut and waves_of(*sizes) == waves
+    counts = [-(-n // page) for n in lens]
+    pool = filled(30 + case, sum(counts) + 1, kv, dh, page, code)
+    table = numbered(30 + case, counts, width, sum(counts) + 1)
+    q = rand(130 + case, len(lens), rows, heads, dh, dtype=dtype)
+    first = attend_both(ops, q, pool, code, page, table, lens, q_lens, causal, window, sinks)
+    same_bits(first, attend_both(ops, q, pool, code, page, table, lens, q_lens, causal, window, sinks))
+
+
+@pytest.mark.parametrize("code", CODES)
+def test_every_form_of_few_rows_is_compared(ops, code):
+    """The entries above reach each number of waves of each dim, with ranges and without, that a rule sends calls to: if a limit
+    between them moves, their sizes have to move too."""
+    reached = set()
+    for entry in ATTN + SPLIT:
+        rows, heads, kv, dh, page, lens, _, causal, window, sinks, width = entry[:11]
+        for dtype in TYPES:
+            sizes = (len(lens), rows, heads, kv, dh, page, causal, window, sinks, width, code)
+            groups, _, ranges = plan_of(*sizes)
+            if dtype == torch.bfloat16 and groups == 0:
+                reached.add((dh, waves_of(*sizes), ranges > 1))
+            assert dtype == torch.bfloat16 or waves_of(*sizes, dtype) == 4
+    assert reached == {(64, 4, False), (64, 4, True), (64, 8, False), (128, 4, False), (128, 4, True), (128, 8, False), (256, 4, False),
+                       (256, 4, True), (256, 8, False), (256, 8, True)}
+
+
 # many rows whose keys are cut into ranges: mostly tables for far more slots than there are; the last entry: 8192 rows and more
 RANGES = [
     (100, 4, 1, 64, 128, [1500, 100, 0, 257, 256], None, True, 0, 0, 1400, False),
