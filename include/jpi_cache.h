@@ -128,10 +128,12 @@ jpi_status jpi_cache_append(const jpi_cache_pool* pool, const jpi_cache_seqs* se
  *   s_ij = scale * q_i . k_j,  lse_i = log sum_j exp(s_ij),
  *   out_i = sum_j exp(s_ij - lse_i) v_j.
  * A row that sees nothing has out 0 and lse -inf.  Rows i >= q_len[s] of out and
- * lse are left as they were.  In bf16 probabilities are taken in two bf16 parts for
- * the product with V, and rounded to one where a call has many rows; fp32 queries
- * and probabilities are taken in three, which lose nothing (codes are exact in
- * bf16).  Sums are fp32. */
+ * lse are left as they were.  NaN in slots that a row does not see does not reach it.
+ * In bf16 probabilities are taken in two bf16 parts for the product with V, 2^-16 of
+ * each at most lost, and rounded to one, 2^-8, where a call has many rows; calls of
+ * fewer than 64 rows on a KV head (q_rows * n_heads / n_kv_heads) take two always.
+ * fp32 queries and probabilities are taken in three, which lose nothing (codes are
+ * exact in bf16).  Sums are fp32. */
 typedef struct {
   jpi_dtype dtype;         /* JPI_BF16 or JPI_F32: q and out */
   int q_rows, n_heads;     /* q_rows >= 1; n_heads a multiple of the pool's n_kv_heads */

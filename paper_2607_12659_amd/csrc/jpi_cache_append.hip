@@ -6,8 +6,9 @@
 // the token's row, V in pieces of 16 slots of a dim, which a lane collects from 16
 // rows that a wave reads along the dims.  Pieces of which only some slots are new
 // are read, changed and written back.  Bound by the chain of dependent reads
-// (length, table, tokens and scale): a token of 64 sequences takes 6.0 us, 816 of
-// eight sequences, 10 MB in all, 7.5.
+// (length, table, tokens and scale) where tokens are few: one of 64 sequences takes
+// 6.0 us, 816 of eight sequences, 10 MB in all, 7.5; by memory where they are many:
+// 4096 of eight sequences in 8 heads of 128 dims, 201 MB, 45 us, 4.4 TB/s.
 #include <algorithm>
 
 #include "jpi_cache_device.h"

@@ -194,8 +194,12 @@ template <int DH, bool E4M3, typename T, int R, int NT, bool Q_LDS = false>
 struct Rows {
   typedef Code<E4M3> C;
   typedef Tile<R> M;
-  // bf16 parts of a query and of a probability.  One part of a probability doubles the error of a bf16 result's rounding
-  // (2.3e-3 instead of 1.6e-3 of it); two are taken where memory bounds the kernel, not where products do.
+  // bf16 parts of a query and of a probability.  One part of a probability adds 1.5e-3 to the 1.6e-3 of a bf16 result's own
+  // rounding (2.2e-3 of both); two, which add nothing that shows, are taken where memory bounds the kernel, not where products
+  // do.  us of the ring, one part and two: a window of 1024 over 4099 tokens 88 and 114, 4096 rows before 4096 keys 281 and 370,
+  // 816 rows of 256 dims for eight sequences 46 and 51: a remainder is two instructions of 310 for each of 32 probabilities, and
+  // its product half as many matrix instructions again.  fp16 in place of bf16, 93, 288 and 47, holds codes and 11 bits (1.7e-3
+  // of both), but no probability below 2^-32 of a row's largest: elements where larger ones meet codes of 0 came out wrong.
   static constexpr int PARTS = sizeof(T) == 2 ? 1 : 3, P_PARTS = sizeof(T) == 4 ? 3 : R == 16 ? 2 : 1;
   static constexpr int G = 64 / R, KEYS = 16 * G * NT;             // lane groups, keys of a step
   static constexpr int SETS = KEYS / R, REGS = R * R / 64;         // products of a step's keys, their registers
@@ -963,8 +967,12 @@ CachePlan cache_plan(const jpi_cache_attn& a, const jpi_cache_pool& p, const jpi
   // Eight waves of 256 dims where a sequence's rows have them compute.  us, four and eight: 16, 8, 5 and one chunk of 50 rows of 8
   // heads 27, 14.6, 16.6 and 12.7, 24, 12.8, 13.7 and 12.3; one of 8 rows 11.7 and 12.1; decoding 32 sequences of 4096 slots 96
   // and 101.  And of all dims where they spare the launch that joins ranges, with two tiles a wave at most: a row before 817 slots
-  // of 256 dims 11.2 and 11.5 of the GPU, before 600 and 1024 of 128 8.9 and 7.6, 6.7 and 7.9, 50 rows before 1024 10.6 and 8.5,
-  // and 11 us of the host instead of 15.  Not int8 of 256 dims, 12.7 and 15.2 of the GPU, nor fp32, of 128 dims 8.3 and 9.9.
+  // of 256 dims 11.3 and 11.5 of the GPU, before 600 and 1024 of 128 8.9 and 7.6, 6.7 and 7.9, in int8 8.0 and 9.5 before 1024,
+  // 50 rows before 1024 10.6 and 8.5, and 11 us of the host instead of 15, which a captured graph has no use for.  Not int8 of
+  // 256 dims, 12.7 and 15.2 of the GPU, nor fp32, of 128 dims 8.3 and 9.9.
+  // All of this goes by the slots that the table has room for: the lengths are on the device.  The row before 817 slots in a table
+  // for 1088 and more: four ranges, 9.6 of the GPU and 16 with the host.  Eight chunks of 50 rows of 8 heads before 866 slots: 12.9
+  // in tables for up to 6080, 32 in wider ones, which go to the ring.
   const bool bf = a.dtype == JPI_BF16, wide = p.head_dim == 256;
   const bool spares = bf && (!wide || p.code == JPI_E4M3) && steps >= 8 && steps <= 16 && pairs * plan.tiles <= slots / 2;
   if (spares || (bf && wide && all >= 128)) plan.waves = 8;

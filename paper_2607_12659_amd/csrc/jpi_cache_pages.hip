@@ -8,7 +8,11 @@
 // out the list of pages that move, in chunks.  Bound by the memory that moved pages
 // are (compaction of 227 MB 104 us, 4.4 TB/s, 9 of them the plan), for few of them by
 // the chain of reads of the two launches: eight forks of a prefix and their growth
-// 11 us, 64 that are reordered and grow 15.
+// 11 us, 64 that are reordered and grow 15.  In large pools by the plan, whose one
+// workgroup walks the counts, 8192 pages a step: to the last free page that a growth
+// needs, through all of them for a compaction or where counts go elsewhere.  One free
+// page at the end of 4096, 131072 and 2^20 pages: growth and its way back 13, 78 and
+// 552 us, a compaction that moves nothing 8, 99 and 891; 5 where nobody needs a page.
 #include <algorithm>
 
 #include "jpi_cache_device.h"

@@ -7,7 +7,9 @@
 // whose table of (cos, sin), and the weights that all heads share, it keeps in LDS.
 // The norm costs a pass through the lanes for each head and no memory.  336 MB in
 // and out of fp32, 67 us, 5.0 TB/s (half of it from the last cache); a token alone
-// 4.1 us, a launch and its chain of reads.
+// 4.1 us, a launch and its chain of reads.  Heads off 16-byte boundaries go element by
+// element: 8000 tokens of 9 heads of 256 take 19 us in bf16 and 25 in fp32, 39 and 42
+// so; with weights of each head 20 and 27.
 #include <algorithm>
 
 #include "jpi_cache_internal.h"
