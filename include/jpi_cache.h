@@ -106,7 +106,7 @@ jpi_status jpi_norm_rope(const jpi_head_norm* norm, const jpi_rope_config* cfg, 
  *   - Where A is not finite, or the old scale is NaN, the scale becomes NaN and the
  *     new codes 0: the page holds NaN until it is free again.
  * Scales that are powers of two make every step but the rounding exact, and
- * halving an e4m3 code loses nothing.  Slots that are neither new nor rescaled
+ * halving an e4m3 code of 2^-5 or more loses nothing.  Slots that are neither new nor rescaled
  * are left as they were; tokens past max_pages * page slots, and those of pages
  * that are none, are dropped.  A page that the call writes to may belong to one
  * sequence only: jpi_cache_resize sees to it for as many tokens as it lengthened
@@ -133,7 +133,8 @@ jpi_status jpi_cache_append(const jpi_cache_pool* pool, const jpi_cache_seqs* se
  * each at most lost, and rounded to one, 2^-8, where a call has many rows; calls of
  * fewer than 64 rows on a KV head (q_rows * n_heads / n_kv_heads) take two always.
  * fp32 queries and probabilities are taken in three, which lose nothing (codes are
- * exact in bf16).  Sums are fp32. */
+ * exact in bf16).  Sums are fp32, and the one over V is divided at the end: elements
+ * of q past 2^100, or of V past 2^80, may take them out of its range. */
 typedef struct {
   jpi_dtype dtype;         /* JPI_BF16 or JPI_F32: q and out */
   int q_rows, n_heads;     /* q_rows >= 1; n_heads a multiple of the pool's n_kv_heads */
